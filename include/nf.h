@@ -327,6 +327,89 @@ int32_t nf_block_evaluate(const nf_block *blk, int32_t exit_layer, int32_t B, in
                           int32_t *pred_out, int32_t *n_correct, void *ws, size_t ws_bytes, void *stream);
 int32_t nf_select_exit(int32_t n_exits, const int64_t *n_correct, const int64_t *n_params, int32_t *exit_out);
 
+/* ---- pointwise layers: linear with a fused epilogue, group norm, dropout, a quantised cache --------------
+ * The operators around a 1x1 layer of channels-last activations, forward and backward, in three types: a
+ * dtype of NF_F32, NF_BF16 or NF_F16 is that of the activations and of the weights W; biases, gamma, beta,
+ * statistics and the gradients of parameters are fp32.  Products, sums, statistics and activations are formed
+ * in fp32 and each result is rounded once.  Rows are dense.  Every pointer is 16-byte aligned at its base; rows
+ * need no alignment (any K, N, C, cols, n).  A workspace of 0 bytes may be NULL.  Outputs must not overlap
+ * inputs, but for dropout's y, which may be x or r (and dx, which may be dy).  Results do not depend on the order
+ * in which workgroups run. */
+enum { NF_F32 = 0, NF_BF16 = 1, NF_F16 = 2 };
+/* relu: max(v, 0), its slope at 0 is 0; silu: v / (1 + e^-v); gelu: v Phi(v), Phi the normal distribution's. */
+enum { NF_ACT_NONE = 0, NF_ACT_RELU = 1, NF_ACT_SILU = 2, NF_ACT_GELU = 3 };
+
+/* D: an element of a row-major matrix is dropped (0) where u < T = rint(65536 p), else scaled by
+ * 65536 / (65536 - T).  u(row, col) is the (col % 8)-th half word (low halves first) of Philox4x32-10 (Salmon et
+ * al., SC'11) at counter (row * ceil(cols / 8) + col / 8, step), two 64-bit words, with the 64-bit key seed.  The
+ * mask is formed again wherever it is needed and never stored; another step gives another mask.  0 <= p, T < 65536. */
+typedef struct {
+  double p;
+  uint64_t seed, step;
+} nf_dropout_desc;
+/* y = r + D(x) (r may be NULL); backward: dx = D(dy).  rows, cols >= 1, cols < 2^31 - 8, rows * cols < 2^62. */
+int32_t nf_dropout_fwd(const nf_dropout_desc *drop, int32_t dtype, int64_t rows, int64_t cols, const void *x,
+                       const void *r, void *y, void *stream);
+int32_t nf_dropout_bwd(const nf_dropout_desc *drop, int32_t dtype, int64_t rows, int64_t cols, const void *dy,
+                       void *dx, void *stream);
+
+/* A layer of N filters on rows of K channels: x [M][K], W [N][K], y [M][N].  1 <= M, N, K, M < 2^31 - 512, K, N <= 2^20. */
+typedef struct {
+  int32_t dtype, K, N, act;
+} nf_linear_desc;
+/* Bytes of workspace that the three calls below want at M rows. */
+int32_t nf_linear_workspace_bytes(const nf_linear_desc *d, int64_t M, size_t *out);
+/* z = x W^T + b, y = r + D(act(z)).  b (fp32), r and drop may be NULL; z may be NULL (else it receives the sums before
+ * the activation, rounded to the type, which the backward epilogue reads). */
+int32_t nf_linear_fwd(const nf_linear_desc *d, int64_t M, const void *x, const void *W, const float *b, const void *r,
+                      const nf_dropout_desc *drop, void *y, void *z, void *ws, size_t ws_bytes, void *stream);
+/* dz = act'(z) D(dy) and db[n] = sum over the rows of dz before its rounding.  z may be NULL where act is
+ * NF_ACT_NONE; drop and db may be NULL. */
+int32_t nf_linear_bwd_epilogue(const nf_linear_desc *d, int64_t M, const void *dy, const void *z,
+                               const nf_dropout_desc *drop, void *dz, float *db, void *ws, size_t ws_bytes,
+                               void *stream);
+/* dx = dz W [M][K] in the type, dW = dz^T x [N][K] in fp32.  Either may be NULL (a first layer has no dx; x is not read
+ * without dW, nor W without dx), not both. */
+int32_t nf_linear_bwd(const nf_linear_desc *d, int64_t M, const void *dz, const void *x, const void *W, void *dx,
+                      float *dW, void *ws, size_t ws_bytes, void *stream);
+
+/* Group norm over x [B][HW][C]: C / G neighbouring channels of an image share a mean and a variance.
+ * 1 <= B <= 65535, G divides C, C <= 2^16, C / G <= 2048, HW < 2^24, eps >= 0. */
+typedef struct {
+  int32_t dtype, C, G, act, HW;
+  float eps;
+} nf_groupnorm_desc;
+int32_t nf_groupnorm_workspace_bytes(const nf_groupnorm_desc *d, int32_t B, size_t *out);
+/* y = act((x - mean) rstd gamma + beta), rstd = (var + eps)^-1/2, var the mean square about the mean; mean and rstd
+ * [B][G] are written too. */
+int32_t nf_groupnorm_fwd(const nf_groupnorm_desc *d, int32_t B, const void *x, const float *gamma, const float *beta,
+                         void *y, float *mean, float *rstd, void *ws, size_t ws_bytes, void *stream);
+/* With xh = (x - mean) rstd and g = dy act'(xh gamma + beta): dx = rstd (g gamma - avg(g gamma) - xh avg(g gamma xh)),
+ * averages over the group; dgamma = sum g xh, dbeta = sum g over images and pixels.  mean and rstd are what the
+ * forward wrote. */
+int32_t nf_groupnorm_bwd(const nf_groupnorm_desc *d, int32_t B, const void *dy, const void *x, const float *gamma,
+                         const float *beta, const float *mean, const float *rstd, void *dx, float *dgamma,
+                         float *dbeta, void *ws, size_t ws_bytes, void *stream);
+
+/* The activation cache in 8 or 4 bits an element.  A row of n elements is cut into groups of 32 (the last may be
+ * shorter); group j has the exponent byte scales[row][j] = E + 127 and its elements are code * 2^E:
+ *   NF_Q_INT8  signed bytes -127 ... 127
+ *   NF_Q_E4M3  8-bit floats, 4 exponent bits, largest 448
+ *   NF_Q_E2M1  4-bit floats 0, .5, 1, 1.5, 2, 3, 4, 6 with a sign, two to a byte, the earlier element in the low half
+ * E is the least (>= -127) with which the group's largest magnitude is at most the largest code; codes are rounded to
+ * nearest, ties to even (next to the largest fp32 number that may be an infinity).  A group that holds an infinity or a NaN gets the exponent byte 255 and reads back as NaN.
+ * Row strides are nf_qcache_row_bytes: the codes' bytes and the exponents' bytes, both rounded up to 16.
+ * Write stores batch rows at [first, first+B); read gathers as nf_cache_read does (an index outside [0, capacity)
+ * is clamped).  Labels as there. */
+enum { NF_Q_INT8 = 0, NF_Q_E4M3 = 1, NF_Q_E2M1 = 2 };
+int32_t nf_qcache_row_bytes(int32_t format, int64_t n, size_t *code_bytes, size_t *scale_bytes);
+int32_t nf_qcache_write(int32_t format, int32_t dtype, uint8_t *codes, uint8_t *scales, int32_t *cache_labels,
+                        int64_t capacity, int64_t n, int64_t first, int32_t B, const void *x, const int32_t *labels,
+                        void *stream);
+int32_t nf_qcache_read(int32_t format, int32_t dtype, const uint8_t *codes, const uint8_t *scales,
+                       const int32_t *cache_labels, int64_t capacity, int64_t n, int64_t first, const int64_t *idx,
+                       int32_t B, void *x_out, int32_t *labels_out, void *stream);
+
 /* ---- Profiler and Partitioner ("Modules", Algorithm 1): host functions, no device work ---------
  * The Profiler's measured memory is replaced by the exact device bytes of one local step with
  * this library: parameters + gradients (+ momentum buffers) of the layer and its head, the input,

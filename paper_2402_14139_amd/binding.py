@@ -26,11 +26,17 @@ EXPORTS = ("nf_strerror", "nf_layer_out_dims", "nf_workspace_bytes", "nf_layer_f
            "nf_block_train_epoch", "nf_block_fill_cache", "nf_layer_step_bytes", "nf_fit_linear",
            "nf_profile_layer", "nf_partition", "nf_aux_predict", "nf_block_evaluate", "nf_select_exit",
            "nf_device_info", "nf_local_step_static", "nf_contraction", "nf_block_graph_create",
-           "nf_block_graph_launch", "nf_block_graph_destroy")
+           "nf_block_graph_launch", "nf_block_graph_destroy", "nf_dropout_fwd", "nf_dropout_bwd",
+           "nf_linear_workspace_bytes", "nf_linear_fwd", "nf_linear_bwd_epilogue", "nf_linear_bwd",
+           "nf_groupnorm_workspace_bytes", "nf_groupnorm_fwd", "nf_groupnorm_bwd", "nf_qcache_row_bytes",
+           "nf_qcache_write", "nf_qcache_read")
 
 NF_WS_AUX_ACT, NF_WS_POOL_ARG, NF_WS_HEAD_ARG = 0, 1, 2
 NF_HEAD_POOL_AVG, NF_HEAD_POOL_MAX = 0, 1
 NF_LOSS_CE, NF_LOSS_MSE = 0, 1
+NF_F32, NF_BF16, NF_F16 = 0, 1, 2
+NF_ACT_NONE, NF_ACT_RELU, NF_ACT_SILU, NF_ACT_GELU = 0, 1, 2, 3
+NF_Q_INT8, NF_Q_E4M3, NF_Q_E2M1 = 0, 1, 2
 
 
 class NfError(RuntimeError):
@@ -67,6 +73,18 @@ class ProfRecord(C.Structure):
 
 class AuxParams(C.Structure):
     _fields_ = [("Wa", C.c_void_p), ("ba", C.c_void_p), ("Wf", C.c_void_p), ("bf", C.c_void_p)]
+
+
+class DropoutDesc(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("step", C.c_uint64)]
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "K", "N", "act")]
+
+
+class GroupNormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "C", "G", "act", "HW")] + [("eps", C.c_float)]
 
 
 class LinearModel(C.Structure):
@@ -152,6 +170,19 @@ def lib():
         L.nf_partition.argtypes = [C.c_int32, C.POINTER(LinearModel), C.c_double, C.c_int32, C.c_double,
                                    C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32),
                                    C.POINTER(C.c_int32)]
+        i32, i64, ptr, size = C.c_int32, C.c_int64, C.c_void_p, C.c_size_t
+        L.nf_dropout_fwd.argtypes = [C.POINTER(DropoutDesc), i32, i64, i64, ptr, ptr, ptr, ptr]
+        L.nf_dropout_bwd.argtypes = [C.POINTER(DropoutDesc), i32, i64, i64, ptr, ptr, ptr]
+        L.nf_linear_workspace_bytes.argtypes = [C.POINTER(LinearDesc), i64, C.POINTER(size)]
+        L.nf_linear_fwd.argtypes = [C.POINTER(LinearDesc), i64, ptr, ptr, ptr, ptr, C.POINTER(DropoutDesc), ptr, ptr, ptr, size, ptr]
+        L.nf_linear_bwd_epilogue.argtypes = [C.POINTER(LinearDesc), i64, ptr, ptr, C.POINTER(DropoutDesc), ptr, ptr, ptr, size, ptr]
+        L.nf_linear_bwd.argtypes = [C.POINTER(LinearDesc), i64, ptr, ptr, ptr, ptr, ptr, ptr, size, ptr]
+        L.nf_groupnorm_workspace_bytes.argtypes = [C.POINTER(GroupNormDesc), i32, C.POINTER(size)]
+        L.nf_groupnorm_fwd.argtypes = [C.POINTER(GroupNormDesc), i32, ptr, ptr, ptr, ptr, ptr, ptr, ptr, size, ptr]
+        L.nf_groupnorm_bwd.argtypes = [C.POINTER(GroupNormDesc), i32] + [ptr] * 10 + [size, ptr]
+        L.nf_qcache_row_bytes.argtypes = [i32, i64, C.POINTER(size), C.POINTER(size)]
+        L.nf_qcache_write.argtypes = [i32, i32, ptr, ptr, ptr, i64, i64, i64, i32, ptr, ptr, ptr]
+        L.nf_qcache_read.argtypes = [i32, i32, ptr, ptr, ptr, i64, i64, i64, ptr, i32, ptr, ptr, ptr]
         _lib = L
     return _lib
 
@@ -429,3 +460,77 @@ def nf_device_info():
     cu, khz = C.c_int32(), C.c_int32()
     _check(lib().nf_device_info(C.byref(cu), C.byref(khz)), "nf_device_info")
     return int(cu.value), int(khz.value)
+
+
+# ---- pointwise layers and the quantised cache ----
+
+def _ref(d):
+    return None if d is None else C.byref(d)
+
+
+def nf_dropout_fwd(drop: DropoutDesc, dtype, rows, cols, x, r, y, stream=None):
+    _check(lib().nf_dropout_fwd(_ref(drop), dtype, rows, cols, _ptr(x), _ptr(r), _ptr(y), _stream(stream)),
+           "nf_dropout_fwd")
+
+
+def nf_dropout_bwd(drop: DropoutDesc, dtype, rows, cols, dy, dx, stream=None):
+    _check(lib().nf_dropout_bwd(_ref(drop), dtype, rows, cols, _ptr(dy), _ptr(dx), _stream(stream)), "nf_dropout_bwd")
+
+
+def nf_linear_workspace_bytes(d: LinearDesc, M: int) -> int:
+    out = C.c_size_t()
+    _check(lib().nf_linear_workspace_bytes(_ref(d), M, C.byref(out)), "nf_linear_workspace_bytes")
+    return int(out.value)
+
+
+def nf_linear_fwd(d: LinearDesc, M, x, W, b, r, drop, y, z, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check(lib().nf_linear_fwd(_ref(d), M, _ptr(x), _ptr(W), _ptr(b), _ptr(r), _ref(drop), _ptr(y), _ptr(z), wp, wn,
+                               _stream(stream)), "nf_linear_fwd")
+
+
+def nf_linear_bwd_epilogue(d: LinearDesc, M, dy, z, drop, dz, db, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check(lib().nf_linear_bwd_epilogue(_ref(d), M, _ptr(dy), _ptr(z), _ref(drop), _ptr(dz), _ptr(db), wp, wn,
+                                        _stream(stream)), "nf_linear_bwd_epilogue")
+
+
+def nf_linear_bwd(d: LinearDesc, M, dz, x, W, dx, dW, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check(lib().nf_linear_bwd(_ref(d), M, _ptr(dz), _ptr(x), _ptr(W), _ptr(dx), _ptr(dW), wp, wn, _stream(stream)),
+           "nf_linear_bwd")
+
+
+def nf_groupnorm_workspace_bytes(d: GroupNormDesc, B: int) -> int:
+    out = C.c_size_t()
+    _check(lib().nf_groupnorm_workspace_bytes(_ref(d), B, C.byref(out)), "nf_groupnorm_workspace_bytes")
+    return int(out.value)
+
+
+def nf_groupnorm_fwd(d: GroupNormDesc, B, x, gamma, beta, y, mean, rstd, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check(lib().nf_groupnorm_fwd(_ref(d), B, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd), wp, wn,
+                                  _stream(stream)), "nf_groupnorm_fwd")
+
+
+def nf_groupnorm_bwd(d: GroupNormDesc, B, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check(lib().nf_groupnorm_bwd(_ref(d), B, _ptr(dy), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd),
+                                  _ptr(dx), _ptr(dgamma), _ptr(dbeta), wp, wn, _stream(stream)), "nf_groupnorm_bwd")
+
+
+def nf_qcache_row_bytes(fmt: int, n: int):
+    """(bytes of a row's codes, bytes of its exponents): the strides of the two arrays."""
+    c, s = C.c_size_t(), C.c_size_t()
+    _check(lib().nf_qcache_row_bytes(fmt, n, C.byref(c), C.byref(s)), "nf_qcache_row_bytes")
+    return int(c.value), int(s.value)
+
+
+def nf_qcache_write(fmt, dtype, codes, scales, cache_labels, capacity, n, first, B, x, labels, stream=None):
+    _check(lib().nf_qcache_write(fmt, dtype, _ptr(codes), _ptr(scales), _ptr(cache_labels), capacity, n, first, B,
+                                 _ptr(x), _ptr(labels), _stream(stream)), "nf_qcache_write")
+
+
+def nf_qcache_read(fmt, dtype, codes, scales, cache_labels, capacity, n, first, idx, B, x_out, labels_out, stream=None):
+    _check(lib().nf_qcache_read(fmt, dtype, _ptr(codes), _ptr(scales), _ptr(cache_labels), capacity, n, first,
+                                _ptr(idx), B, _ptr(x_out), _ptr(labels_out), _stream(stream)), "nf_qcache_read")

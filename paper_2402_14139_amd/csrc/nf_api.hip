@@ -9,6 +9,7 @@
 #include <mutex>
 #include <vector>
 
+#include "nf_enqueue.h"
 #include "nf_internal.h"
 
 // Scratch of nf_local_step_static: one copy per GPU the library runs on, held until the process
@@ -18,6 +19,7 @@ static __device__ __align__(256) unsigned char scratch[NF_STATIC_SCRATCH_BYTES];
 namespace nf {
 
 std::atomic<int> g_contraction{NF_CONTRACT_F32};
+ProfState g_prof;
 int contraction_mode() { return g_contraction.load(std::memory_order_relaxed); }
 namespace {
 
@@ -337,56 +339,7 @@ int32_t check_ws(const void *ws, size_t have, size_t need) {
 
 inline float *wsf(void *ws, size_t off) { return reinterpret_cast<float *>(static_cast<char *>(ws) + off); }
 
-// A HIP error while enqueueing is reported on stderr with the failing expression (the status code
-// alone cannot say which launch it was), then returned as NF_ERR_DEVICE.
-#define NF_HIP(expr)                                                                     \
-  do {                                                                                   \
-    const hipError_t e_ = (expr);                                                        \
-    if (e_ != hipSuccess) {                                                              \
-      std::fprintf(stderr, "libnf: %s: %s\n", hipGetErrorString(e_), #expr);             \
-      return NF_ERR_DEVICE;                                                              \
-    }                                                                                    \
-  } while (0)
-
-// ---- optional kernel timing (nf_prof_begin / nf_prof_end): one HIP-event pair per launch ----
-struct ProfEvent {
-  const char *name;
-  hipEvent_t a, b;
-  double flops, bytes;
-};
-struct ProfState {
-  bool on = false;
-  bool apart = false;  // kernels that share a launch are launched one by one
-  std::vector<ProfEvent> ev;
-  std::mutex mu;  // guards ev: launches from several host threads may record while profiling is on
-};
-ProfState g_prof;
-
-struct ProfScope {
-  hipStream_t st;
-  hipEvent_t a = nullptr, b = nullptr;
-  bool on;
-  explicit ProfScope(hipStream_t s) : st(s), on(g_prof.on) {
-    if (on) {
-      on = hipEventCreate(&a) == hipSuccess && hipEventCreate(&b) == hipSuccess && hipEventRecord(a, st) == hipSuccess;
-    }
-  }
-  void done(const char *name, double flops, double bytes) {
-    if (on && hipEventRecord(b, st) == hipSuccess) {
-      std::lock_guard<std::mutex> lk(g_prof.mu);
-      g_prof.ev.push_back({name, a, b, flops, bytes});
-    }
-  }
-};
-
 // ---- enqueue helpers (arguments already validated) ----
-
-#define NF_RUN(st, name, flops, bytes, call) \
-  do {                                       \
-    ProfScope sc_(st);                       \
-    NF_HIP(call);                            \
-    sc_.done(name, flops, bytes);            \
-  } while (0)
 
 // algorithmic work of the two contractions (dense formula: padding taps counted, tile padding not)
 int32_t enqueue_fwd(const FwdProblem &f, hipStream_t st) {

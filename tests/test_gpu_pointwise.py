@@ -1,0 +1,359 @@
+"""Pointwise layers on the GPU against their definitions in 64 bits: products with an epilogue, its gradient, group norm,
+dropout.  Tolerances count roundings: half a step of the result's type, one step of fp32 per term of a sum relative to the
+sum of the terms' magnitudes, and what the activations' evaluation adds."""
+import pytest
+import torch
+
+from paper_2402_14139_amd import binding as nf
+from tests import pointwise_ref as ref
+from tests.pointwise_ref import ACTS, DT, FUNC, HALF, SUM, TINY, TYPES
+
+pytestmark = pytest.mark.gpu
+CANARY = -77.25
+
+
+class Out:
+    """A device tensor between two bands that no call may write."""
+
+    def __init__(self, *shape, dtype=torch.float32):
+        n = 1
+        for s in shape:
+            n *= s
+        self.band, self.n = 64, n
+        self.all = torch.full((n + 2 * self.band,), CANARY, dtype=dtype, device="cuda")
+        self.t = self.all[self.band:self.band + n].view(*shape)
+        self.t.fill_(float("nan"))
+
+    def cpu(self):
+        torch.cuda.synchronize()
+        assert (self.all[:self.band] == CANARY).all() and (self.all[self.band + self.n:] == CANARY).all(), "written outside"
+        return self.t.double().cpu()
+
+
+def randn(g, *shape, T=torch.float32, scale=1.0):
+    return (torch.randn(*shape, generator=g) * scale).to(T).cuda()
+
+
+def workspace(n):
+    return torch.full((max(n, 1),), 255, dtype=torch.uint8, device="cuda")[:n]  # NaN as fp32
+
+
+def close(name, got, want, tol):
+    if not got.numel():
+        return
+    assert torch.isfinite(got).all(), f"{name}: not finite"
+    off = (got - want).abs() - tol
+    assert off.max() <= 0, f"{name}: {int((off > 0).sum())} of {off.numel()} off, worst {(got - want).abs().max():.3e} where {tol.reshape(-1)[off.argmax()]:.3e} is allowed"
+
+
+def linear_case(t, M, K, N, act, p, res, z, seed=3):
+    g = torch.Generator().manual_seed(seed + M * 31 + K * 7 + N)
+    T = TYPES[t]
+    x, W, b = randn(g, M, K, T=T), randn(g, N, K, T=T, scale=K ** -0.5), randn(g, N, scale=0.1)
+    r = randn(g, M, N, T=T) if res else None
+    drop = nf.DropoutDesc(p, 0xABCDEF0123456789, 77) if p else None
+    d = nf.LinearDesc(dtype=DT[t], K=K, N=N, act=ACTS.index(act))
+    ws = workspace(nf.nf_linear_workspace_bytes(d, M))
+    y, zz = Out(M, N, dtype=T), Out(M, N, dtype=T) if z else None
+    nf.nf_linear_fwd(d, M, x, W, b, r, drop, y.t, zz.t if z else None, ws)
+    X, w, B = x.double().cpu(), W.double().cpu(), b.double().cpu()
+    Z = X @ w.t() + B
+    err = (K + 2) * SUM * (X.abs() @ w.abs().t() + B.abs())
+    if z:
+        close("z", zz.cpu(), Z, err + HALF[t] * Z.abs() + TINY[t])
+    keep = ref.keep_scale(M, N, p, 0xABCDEF0123456789, 77)
+    v = ref.act(act, Z) * keep
+    tol = (1.13 * err + FUNC * Z.abs()) * keep
+    Y = v + r.double().cpu() if res else v
+    got = y.cpu()
+    close("y", got, Y, tol + (HALF[t] + 2 * SUM) * (Y.abs() + tol) + SUM * v.abs() + TINY[t])
+    if p and not res:
+        assert (got[keep == 0] == 0).all()
+
+
+SHAPES = [(1, 1, 1), (1, 2048, 40), (3, 5, 7), (2, 16, 129), (17, 33, 100), (65, 64, 72), (64, 2048, 64), (129, 100, 130), (300, 24, 8),
+          (200, 136, 264), (257, 1000, 65), (2100, 72, 1600)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("M,K,N", SHAPES)
+def test_linear_forward(t, M, K, N):
+    linear_case(t, M, K, N, "none", 0.0, False, False)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("act,p,res,z", [("relu", 0.0, True, False), ("silu", 0.3, True, True), ("gelu", 0.1, False, True),
+                                         ("none", 0.5, False, False), ("gelu", 0.0, True, True)])
+@pytest.mark.parametrize("M,K,N", [(1, 40, 24), (70, 88, 61), (300, 520, 256), (1, 1030, 515), (33, 4096, 16)])
+def test_linear_epilogue_forward(t, act, p, res, z, M, K, N):
+    linear_case(t, M, K, N, act, p, res, z)
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_linear_forward_without_bias(t):
+    g = torch.Generator().manual_seed(1)
+    x, W = randn(g, 5, 24, T=TYPES[t]), randn(g, 9, 24, T=TYPES[t])
+    d = nf.LinearDesc(dtype=DT[t], K=24, N=9, act=0)
+    y = Out(5, 9, dtype=TYPES[t])
+    nf.nf_linear_fwd(d, 5, x, W, None, None, None, y.t, None, workspace(nf.nf_linear_workspace_bytes(d, 5)))
+    X, w = x.double().cpu(), W.double().cpu()
+    close("y", y.cpu(), X @ w.t(), 26 * SUM * (X.abs() @ w.abs().t()) + HALF[t] * (X @ w.t()).abs() + TINY[t])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("M,N", [(1, 1), (3, 7), (129, 130), (1000, 24), (70, 2056), (4096, 8)])
+@pytest.mark.parametrize("act,p", [("none", 0.25), ("relu", 0.0), ("silu", 0.5), ("gelu", 0.1), ("none", 0.0)])
+def test_linear_epilogue_gradient(t, M, N, act, p):
+    g = torch.Generator().manual_seed(M + N)
+    T = TYPES[t]
+    dy, z = randn(g, M, N, T=T), randn(g, M, N, T=T, scale=2.0)
+    d = nf.LinearDesc(dtype=DT[t], K=8, N=N, act=ACTS.index(act))
+    drop = nf.DropoutDesc(p, 5, 1 << 40) if p else None
+    dz, db = Out(M, N, dtype=T), Out(N)
+    ws = workspace(nf.nf_linear_workspace_bytes(d, M))
+    nf.nf_linear_bwd_epilogue(d, M, dy, z if act != "none" else None, drop, dz.t, db.t, ws)
+    D, Z = dy.double().cpu() * ref.keep_scale(M, N, p, 5, 1 << 40), z.double().cpu()
+    want = D * ref.slope(act, Z)
+    err = FUNC * D.abs() * (1 + Z.abs()) + 2 * SUM * want.abs()
+    close("dz", dz.cpu(), want, err + HALF[t] * want.abs() + TINY[t])
+    close("db", db.cpu(), want.sum(0), err.sum(0) + M * SUM * want.abs().sum(0))
+    dz2 = Out(M, N, dtype=T)
+    nf.nf_linear_bwd_epilogue(d, M, dy, z if act != "none" else None, drop, dz2.t, None, ws)
+    assert torch.equal(dz2.cpu(), dz.cpu())
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("M,K,N", SHAPES + [(5000, 64, 48), (3000, 130, 257), (12, 1024, 1024)])
+def test_linear_gradients(t, M, K, N):
+    g = torch.Generator().manual_seed(M + 3 * K + 5 * N)
+    T = TYPES[t]
+    dz, x, W = randn(g, M, N, T=T, scale=N ** -0.5), randn(g, M, K, T=T), randn(g, N, K, T=T)
+    d = nf.LinearDesc(dtype=DT[t], K=K, N=N, act=0)
+    ws = workspace(nf.nf_linear_workspace_bytes(d, M))
+    dx, dW = Out(M, K, dtype=T), Out(N, K)
+    nf.nf_linear_bwd(d, M, dz, x, W, dx.t, dW.t, ws)
+    D, X, w = dz.double().cpu(), x.double().cpu(), W.double().cpu()
+    want = D @ w
+    close("dx", dx.cpu(), want, (N + 2) * SUM * (D.abs() @ w.abs()) + HALF[t] * want.abs() + TINY[t])
+    want = D.t() @ X
+    close("dW", dW.cpu(), want, (M + 2) * SUM * (D.abs().t() @ X.abs()))
+    only_x, only_w = Out(M, K, dtype=T), Out(N, K)
+    nf.nf_linear_bwd(d, M, dz, None, W, only_x.t, None, ws)
+    nf.nf_linear_bwd(d, M, dz, x, None, None, only_w.t, ws)
+    assert torch.equal(only_x.cpu(), dx.cpu()) and torch.equal(only_w.cpu(), dW.cpu())
+
+
+def test_linear_gradient_against_differences():
+    """The whole layer's loss sum(y * w) in fp32 moved along random directions."""
+    g = torch.Generator().manual_seed(9)
+    M, K, N, p = 40, 24, 36, 0.25
+    x, W, b, w = (randn(g, *s) for s in ((M, K), (N, K), (N,), (M, N)))
+    d, drop = nf.LinearDesc(dtype=nf.NF_F32, K=K, N=N, act=nf.NF_ACT_SILU), nf.DropoutDesc(p, 11, 12)
+    ws = workspace(nf.nf_linear_workspace_bytes(d, M))
+    y, z, dz, db, dx, dW = (torch.empty(s, device="cuda") for s in ((M, N), (M, N), (M, N), (N,), (M, K), (N, K)))
+
+    def loss(x, W, b):
+        nf.nf_linear_fwd(d, M, x, W, b, None, drop, y, z, ws)
+        return (y.double() * w.double()).sum().item()
+
+    loss(x, W, b)
+    nf.nf_linear_bwd_epilogue(d, M, w, z, drop, dz, db, ws)
+    nf.nf_linear_bwd(d, M, dz, x, W, dx, dW, ws)
+    for k, grad in enumerate((dx, dW, db)):
+        v = randn(g, *grad.shape)
+        h = 2e-3
+        up, down = [x, W, b], [x, W, b]
+        up[k], down[k] = up[k] + h * v, down[k] - h * v
+        got = (loss(*up) - loss(*down)) / (2 * h)
+        want = (grad.double() * v.double()).sum().item()
+        # the differences' own error: h^2 of third derivatives, and fp32 losses of 1440 terms over 2h
+        assert abs(got - want) <= 5e-3 * abs(want) + 0.05, (k, got, want)
+
+
+NORMS = [(1, 1, 1, 1), (1, 1, 8, 1), (2, 7, 3, 3), (3, 25, 12, 4), (8, 64, 16, 4), (2, 675, 72, 12), (5, 49, 100, 1), (1, 4096, 64, 32),
+         (2, 130, 1024, 32), (3, 33, 37, 37), (2, 1024, 130, 5), (1, 3000, 256, 1), (40, 4, 2056, 8), (2, 300, 515, 1)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("B,HW,C,G", NORMS)
+def test_group_norm(t, B, HW, C, G):
+    g = torch.Generator().manual_seed(B + HW + C + G)
+    T = TYPES[t]
+    act = ACTS[(B + C + G) % 4]
+    x = (torch.randn(B, HW, C, generator=g) * (0.5 + torch.rand(C, generator=g)) + torch.randn(C, generator=g)).to(T).cuda()
+    gamma, beta = (1 + 0.2 * torch.randn(C, generator=g)).cuda(), (0.2 * torch.randn(C, generator=g)).cuda()
+    dy = randn(g, B, HW, C, T=T)
+    d = nf.GroupNormDesc(dtype=DT[t], C=C, G=G, act=ACTS.index(act), HW=HW, eps=1e-5)
+    ws = workspace(nf.nf_groupnorm_workspace_bytes(d, B))
+    y, mean, rstd = Out(B, HW, C, dtype=T), Out(B, G), Out(B, G)
+    nf.nf_groupnorm_fwd(d, B, x, gamma, beta, y.t, mean.t, rstd.t, ws)
+    X, ga, be = x.double().cpu(), gamma.double().cpu(), beta.double().cpu()
+    n = HW * (C // G)
+    terms = 64 + n ** 0.5  # the sums are cut over threads and added in trees: far fewer roundings than terms
+    Y, mu, rs = ref.group_norm(X, ga, be, G, d.eps, act)
+    v = X.reshape(B, HW, G, -1)
+    mag = v.abs().mean((1, 3))
+    close("mean", mean.cpu(), mu, terms * SUM * mag + 1e-37)
+    # the squares' sum is off by terms roundings and by 2 |x - mean| times the mean's error (whose first order vanishes)
+    rel = terms * SUM + (terms * SUM * mag * rs) ** 2
+    close("rstd", rstd.cpu(), rs, (rel + 4 * SUM) * rs)
+    per = lambda s: s[:, None, :, None].expand(B, HW, G, C // G).reshape(X.shape)  # noqa: E731
+    xh = (X - per(mu)) * per(rs)
+    ez = ga.abs() * (per(terms * SUM * mag * rs) + 4 * SUM * X.abs() * per(rs) + per(rel + 4 * SUM) * xh.abs()) + 4 * SUM * be.abs()
+    z = (xh * ga + be).abs()
+    close("y", y.cpu(), Y, 1.13 * ez + FUNC * z + HALF[t] * (Y.abs() + ez) + TINY[t])
+
+    dx, dg, db = Out(B, HW, C, dtype=T), Out(C), Out(C)
+    nf.nf_groupnorm_bwd(d, B, dy, x, gamma, beta, mean.t, rstd.t, dx.t, dg.t, db.t, ws)
+    D = dy.double().cpu()
+    dX, dG, dB, gg, xh = ref.group_norm_grad(D, X, ga, be, mean.cpu(), rstd.cpu(), act)
+    exh = 4 * SUM * (X.abs() + per(mean.cpu()).abs()) * per(rstd.cpu())
+    eg = D.abs() * ((0 if act == "relu" else 1) * (0.8 * (exh * ga.abs() + 4 * SUM * z) + FUNC * (1 + z)) + 2 * SUM)
+    many = 64 + (B * HW) ** 0.5
+    close("dbeta", db.cpu(), dB, eg.sum((0, 1)) + many * SUM * gg.abs().sum((0, 1)) + 1e-37)
+    ep = eg * xh.abs() + gg.abs() * exh
+    close("dgamma", dg.cpu(), dG, ep.sum((0, 1)) + many * SUM * (gg * xh).abs().sum((0, 1)) + 1e-37)
+    m = lambda s: per(s.reshape(B, HW, G, -1).mean((1, 3)))  # noqa: E731
+    a = ga.abs()
+    inner = eg * a + m(eg * a + terms * SUM * (gg * ga).abs()) + xh.abs() * m(ep * a + terms * SUM * (gg * ga * xh).abs()) + exh * m((gg * ga * xh).abs()) \
+        + 4 * SUM * ((gg * ga).abs() + xh.abs() * m((gg * ga * xh).abs()))
+    close("dx", dx.cpu(), dX, per(rstd.cpu()) * inner + HALF[t] * dX.abs() + TINY[t])
+
+
+def test_group_norm_of_constant_and_far_inputs():
+    """Zero variance: rstd is eps^-1/2 and y the activation of beta; a mean of 1000 deviations keeps its digits."""
+    d = nf.GroupNormDesc(dtype=nf.NF_F32, C=16, G=4, act=0, HW=64, eps=1e-5)
+    ws = workspace(nf.nf_groupnorm_workspace_bytes(d, 2))
+    x = torch.full((2, 64, 16), 3.0, device="cuda")
+    gamma, beta = torch.ones(16, device="cuda"), torch.arange(16, device="cuda") * 0.5
+    y, mean, rstd = Out(2, 64, 16), Out(2, 4), Out(2, 4)
+    nf.nf_groupnorm_fwd(d, 2, x, gamma, beta, y.t, mean.t, rstd.t, ws)
+    assert torch.equal(y.cpu(), beta.double().cpu().expand(2, 64, 16)) and (mean.cpu() == 3).all()
+    close("rstd", rstd.cpu(), torch.full((2, 4), float(d.eps) ** -0.5, dtype=torch.float64), torch.tensor(1e-4))
+    x = torch.randn(2, 64, 16, device="cuda") + 1000
+    nf.nf_groupnorm_fwd(d, 2, x, gamma, beta, y.t, mean.t, rstd.t, ws)
+    Y = ref.group_norm(x.double().cpu(), gamma.double().cpu(), beta.double().cpu(), 4, d.eps, "none")[0]
+    close("y", y.cpu(), Y, torch.tensor(1000 * 16 * SUM))
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 8), (3, 7), (100, 100), (33, 72), (5, 1031), (70, 520)])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.3, 0.999])
+def test_dropout(t, rows, cols, p):
+    g = torch.Generator().manual_seed(rows + cols)
+    T = TYPES[t]
+    x, r = randn(g, rows, cols, T=T), randn(g, rows, cols, T=T)
+    x[0, 0] = float("nan")
+    d = nf.DropoutDesc(p, (1 << 63) + 12345, (1 << 35) + 3)
+    keep = ref.keep_scale(rows, cols, p, d.seed, d.step)
+    X = torch.where(keep == 0, torch.zeros(()).double(), x.double().cpu() * keep)
+    for res in (r, None):
+        y = Out(rows, cols, dtype=T)
+        nf.nf_dropout_fwd(d, DT[t], rows, cols, x, res, y.t)
+        want = X + r.double().cpu() if res is not None else X
+        got = y.cpu()
+        nan = torch.isnan(want)
+        assert torch.equal(nan, torch.isnan(got))
+        tol = HALF[t] * want.abs() + 2 * SUM * X.abs() + TINY[t]
+        close("y", got[~nan], want[~nan], tol[~nan])
+    dx = Out(rows, cols, dtype=T)
+    nf.nf_dropout_bwd(d, DT[t], rows, cols, x, dx.t)
+    assert torch.equal(dx.cpu().nan_to_num(5e5), y.cpu().nan_to_num(5e5))
+    nf.nf_dropout_bwd(d, DT[t], rows, cols, x, x)  # in place
+    assert torch.equal(x.double().cpu().nan_to_num(5e5), y.cpu().nan_to_num(5e5))
+
+
+def test_dropout_of_another_step_and_far_rows():
+    """Counters past 32 bits: 2^33 + 40 columns' groups, the last rows of a matrix of 2.2e9 elements."""
+    cols, rows = 1 << 16, (1 << 15) + 1000
+    x = torch.ones(rows, cols, dtype=torch.float16, device="cuda")
+    d = nf.DropoutDesc(0.5, 3, 9)
+    nf.nf_dropout_bwd(d, nf.NF_F16, rows, cols, x, x)
+    torch.cuda.synchronize()
+    for first in (0, (1 << 15) - 1, rows - 2):
+        assert torch.equal(x[first:first + 2].double().cpu(), ref.keep_scale(2, cols, 0.5, 3, 9, first))
+    y = torch.ones(4, cols, dtype=torch.float16, device="cuda")
+    nf.nf_dropout_bwd(nf.DropoutDesc(0.5, 3, 10), nf.NF_F16, 4, cols, y, y)
+    assert not torch.equal(x[:4], y)
+
+
+def test_linear_rows_past_32_bits():
+    M, K, N = (1 << 21) + 3000, 1024, 16
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator().manual_seed(4)
+    tail = randn(g, 5, K, T=torch.bfloat16)
+    x[-5:] = tail
+    W = randn(g, N, K, T=torch.bfloat16)
+    d = nf.LinearDesc(dtype=nf.NF_BF16, K=K, N=N, act=0)
+    ws = workspace(nf.nf_linear_workspace_bytes(d, M))
+    y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    nf.nf_linear_fwd(d, M, x, W, None, None, None, y, None, ws)
+    X, w = tail.double().cpu(), W.double().cpu()
+    close("y", y[-5:].double().cpu(), X @ w.t(), K * SUM * (X.abs() @ w.abs().t()) + HALF["bf16"] * (X @ w.t()).abs())
+    assert (y[:-5] == 0).all()
+    dz = torch.zeros(M, N, dtype=torch.bfloat16, device="cuda")
+    dz[-5:] = y[-5:]
+    dW = Out(N, K)
+    nf.nf_linear_bwd(d, M, dz, x, None, None, dW.t, ws)
+    D = dz[-5:].double().cpu()
+    close("dW", dW.cpu(), D.t() @ X, 64 * SUM * (D.abs().t() @ X.abs()))
+
+
+def test_infinities_reach_the_results_that_hold_them():
+    d = nf.LinearDesc(dtype=nf.NF_BF16, K=72, N=40, act=0)
+    x, W = torch.ones(70, 72, dtype=torch.bfloat16, device="cuda"), torch.ones(40, 72, dtype=torch.bfloat16, device="cuda")
+    x[3, 71], W[7, 0], x[69, 5] = float("inf"), float("nan"), float("-inf")
+    y = torch.empty(70, 40, dtype=torch.bfloat16, device="cuda")
+    nf.nf_linear_fwd(d, 70, x, W, None, None, None, y, None, workspace(nf.nf_linear_workspace_bytes(d, 70)))
+    want = x.float().cpu() @ W.float().cpu().t()
+    assert torch.equal(y.float().cpu().nan_to_num(9.0), want.nan_to_num(9.0))
+
+
+def test_calls_on_another_stream_and_in_a_graph():
+    """The calls follow the stream that they are given; a captured layer replays to the eager results, with eager calls of
+    the same buffers between."""
+    g = torch.Generator().manual_seed(2)
+    M, K, N = 200, 520, 72
+    T = torch.bfloat16
+    x, W, b, dy = randn(g, M, K, T=T), randn(g, N, K, T=T, scale=K ** -0.5), randn(g, N), randn(g, M, N, T=T)
+    gamma, beta = torch.ones(K, device="cuda"), torch.zeros(K, device="cuda")
+    d, drop = nf.LinearDesc(dtype=nf.NF_BF16, K=K, N=N, act=nf.NF_ACT_GELU), nf.DropoutDesc(0.2, 1, 2)
+    n = nf.GroupNormDesc(dtype=nf.NF_BF16, C=K, G=8, act=nf.NF_ACT_RELU, HW=50, eps=1e-5)
+    ws = workspace(max(nf.nf_linear_workspace_bytes(d, M), nf.nf_groupnorm_workspace_bytes(n, 4)))
+    h, dh, dx = (torch.empty(M, K, dtype=T, device="cuda") for _ in range(3))
+    y, z, dz = (torch.empty(M, N, dtype=T, device="cuda") for _ in range(3))
+    mean, rstd, dg, db, dW, dbias = (torch.empty(s, device="cuda") for s in ((4, 8), (4, 8), (K,), (K,), (N, K), (N,)))
+
+    def layer(stream):
+        nf.nf_groupnorm_fwd(n, 4, x, gamma, beta, h, mean, rstd, ws, stream)
+        nf.nf_linear_fwd(d, M, h, W, b, None, drop, y, z, ws, stream)
+        nf.nf_linear_bwd_epilogue(d, M, dy, z, drop, dz, dbias, ws, stream)
+        nf.nf_linear_bwd(d, M, dz, h, W, dh, dW, ws, stream)
+        nf.nf_groupnorm_bwd(n, 4, dh, x, gamma, beta, mean, rstd, dx, dg, db, ws, stream)
+
+    outs = (y, z, dz, dbias, dh, dW, dx, dg, db)
+    layer(None)
+    torch.cuda.synchronize()
+    want = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for o in outs:
+        o.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    layer(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer(torch.cuda.current_stream())
+    for turn in range(4):
+        for o in outs:
+            o.zero_()
+        if turn & 1:
+            layer(None)
+            torch.cuda.synchronize()
+            for o in outs:
+                o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), turn
