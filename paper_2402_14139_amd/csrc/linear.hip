@@ -48,7 +48,7 @@ struct GemmArgs {
 
 // 8 neighbouring results of a row through the forward's epilogue
 template <typename T>
-__device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int C, const float bias[8], float v[8]) {
+__device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int C, const float bias[8], float (&v)[8]) {
   const int n = C - col;
   const long long at = row * C + col;
   float s[8];
@@ -56,8 +56,7 @@ __device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] += bias[i];
   if (e.z) store8((T *)e.z + at, v, n);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = act_of<T>(e.act, v[i]);
+  act_of<T>(e.act, v);
   drop8(e.drop, (unsigned long long)row * (unsigned)((C + 7) >> 3) + (unsigned)(col >> 3), v);
   if (e.res) {
 #pragma unroll
@@ -375,10 +374,7 @@ __global__ __launch_bounds__(LT) void linear_epilogue_kernel(long long M, int N,
       load8(dy + m * N + col, v, n);
       if (e.act != NF_ACT_NONE) load8(z + m * N + col, zv, n);
       drop8(e.drop, (unsigned long long)m * (unsigned)groups + (unsigned)g8, v);
-      if (e.act != NF_ACT_NONE) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= act_slope<T>(e.act, zv[k]);
-      }
+      if (e.act != NF_ACT_NONE) times_slope<T>(e.act, zv, v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) s[k] += v[k];
       store8((T *)e.out + m * N + col, v, n);

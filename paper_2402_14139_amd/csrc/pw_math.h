@@ -76,31 +76,45 @@ __device__ inline float normal_tail(float z, float &bell) {
   return 0.5f * t * bell * P;
 }
 
-template <typename T>
-__device__ inline float act_of(int act, float v) {
-  if (act == NF_ACT_RELU) return v < 0.f ? 0.f : v;  // a NaN stays one
-  if (act == NF_ACT_SILU) return v * recip<T>(1.f + exp_of<T>(-v));
-  if (act == NF_ACT_GELU) {
-    float bell;
-    const float q = normal_tail<T>(v, bell);
-    return v * (v > 0.f ? 1.f - q : q);
+// The activation of N values, and its slope at them (times what s holds).  The activation is the same for a whole launch: one
+// branch to a vector, not to an element.
+template <typename T, int N>
+__device__ inline void act_of(int act, float (&v)[N]) {
+  if (act == NF_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];  // a NaN stays one
+  } else if (act == NF_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] *= recip<T>(1.f + exp_of<T>(-v[e]));
+  } else if (act == NF_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      float bell;
+      const float q = normal_tail<T>(v[e], bell);
+      v[e] *= v[e] > 0.f ? 1.f - q : q;
+    }
   }
-  return v;
 }
 
-template <typename T>
-__device__ inline float act_slope(int act, float v) {
-  if (act == NF_ACT_RELU) return v > 0.f ? 1.f : 0.f;
-  if (act == NF_ACT_SILU) {
-    const float q = recip<T>(1.f + exp_of<T>(-v));
-    return q * (1.f + v * (1.f - q));
+template <typename T, int N>
+__device__ inline void times_slope(int act, const float (&z)[N], float (&s)[N]) {
+  if (act == NF_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) s[e] = z[e] > 0.f ? s[e] : 0.f;
+  } else if (act == NF_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float q = recip<T>(1.f + exp_of<T>(-z[e]));
+      s[e] *= q * (1.f + z[e] * (1.f - q));
+    }
+  } else if (act == NF_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      float bell;
+      const float q = normal_tail<T>(z[e], bell);
+      s[e] *= (z[e] > 0.f ? 1.f - q : q) + z[e] * bell * 0.39894228040143268f;
+    }
   }
-  if (act == NF_ACT_GELU) {
-    float bell;
-    const float q = normal_tail<T>(v, bell);
-    return (v > 0.f ? 1.f - q : q) + v * bell * 0.39894228040143268f;
-  }
-  return 1.f;
 }
 
 // Dropout as the kernels take it: T = 0 means none.
