@@ -205,10 +205,19 @@ def _ptr(t):
     return t.data_ptr()
 
 
+_current_stream = None
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        global _current_stream
+        if _current_stream is None:
+            import torch
+            get, dev = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+            torch.cuda.current_stream()   # initialises the device, or raises where there is none
+            # the handle itself, without a Stream object around it (a third of a short call's host time)
+            _current_stream = (lambda: get(dev())) if get and dev else (lambda: torch.cuda.current_stream().cuda_stream)
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -13,29 +13,19 @@ __global__ __launch_bounds__(DT) void dropout_kernel(DropArgs d, long long total
                                                      const T *x, const T *r, T *y) {
   const long long i = (long long)blockIdx.x * DT + threadIdx.x;
   if (i >= total) return;
-  float v[8], s[8];
-  if constexpr (WHOLE) {  // rows of whole groups: the group's number is its place
-    const long long at = i * 8;
-    load8(x + at, v);
-    if (r) load8(r + at, s);
-    drop8(d, (unsigned long long)i, v);
-    if (r) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += s[e];
-    }
-    store8(y + at, v);
-  } else {
-    const long long row = i / groups, g = i - row * groups, at = row * cols + g * 8;
-    const int n = (int)min(8ll, cols - g * 8);
-    load8(x + at, v, n);
-    if (r) load8(r + at, s, n);
-    drop8(d, (unsigned long long)i, v);
-    if (r) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += s[e];
-    }
-    store8(y + at, v, n);
+  long long at = i * 8;
+  int n = 8;
+  if constexpr (!WHOLE) {  // rows that end inside a group
+    const long long row = i / groups, g = i - row * groups;
+    at = row * cols + g * 8, n = (int)min(8ll, cols - g * 8);
   }
+  float v[8], s[8];
+  load8(x + at, v, n);
+  if (r) load8(r + at, s, n);
+  drop8(d, (unsigned long long)i, v);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = r ? fmaf(v[e], d.scale, s[e]) : v[e] * d.scale;
+  store8(y + at, v, n);
 }
 
 template <typename T>
@@ -53,7 +43,7 @@ hipError_t launch(const DropArgs &d, long long rows, long long cols, const void 
 }  // namespace
 
 DropArgs drop_args(const nf_dropout_desc *d) {
-  DropArgs a = {};
+  DropArgs a = {0, 1.f, 0, 0, 0, 0};
   if (!d) return a;
   a.T = (uint32_t)__builtin_rint(65536.0 * d->p);
   a.scale = (float)(65536.0 / (65536.0 - a.T));

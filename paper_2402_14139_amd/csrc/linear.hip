@@ -11,8 +11,9 @@
 //               fragment lie in 16 different bank groups; terms apart: see turned_swizzle
 //   copies      memory to LDS without registers (buffer loads with LDS as their target, zeros for what lies outside) where rows
 //               are whole 16 bytes, else through registers
-//   order       the MFMA takes B's fragment first, so that a lane ends with 4 neighbouring columns of one row
+//   order       the MFMA takes B's fragment first, so that a lane ends with 4 neighbouring columns of one row (write_sums)
 #include <algorithm>
+#include <type_traits>
 
 #include "pw_math.h"
 
@@ -46,23 +47,28 @@ struct GemmArgs {
   Epilogue e;
 };
 
-// 8 neighbouring results of a row through the forward's epilogue
+// 8 neighbouring results of a row through the forward's epilogue; s holds the residual
 template <typename T>
-__device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int C, const float bias[8], float (&v)[8]) {
+__device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int C, const float (&bias)[8], const float (&s)[8], float (&v)[8]) {
   const int n = C - col;
   const long long at = row * C + col;
-  float s[8];
-  if (e.res) load8((const T *)e.res + at, s, n);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] += bias[i];
   if (e.z) store8((T *)e.z + at, v, n);
   act_of<T>(e.act, v);
   drop8(e.drop, (unsigned long long)row * (unsigned)((C + 7) >> 3) + (unsigned)(col >> 3), v);
-  if (e.res) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += s[i];
-  }
+  for (int i = 0; i < 8; ++i) v[i] = e.res ? fmaf(v[i], e.drop.scale, s[i]) : v[i] * e.drop.scale;
   store8((T *)e.out + at, v, n);
+}
+template <typename T>
+__device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int C, float (&v)[8]) {
+  float s[8], bias[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) bias[i] = s[i] = 0.f;
+  if (e.res) load8((const T *)e.res + row * C + col, s, C - col);
+  if (e.bias) load8(e.bias + col, bias, C - col);
+  finish_fwd<T>(e, row, col, C, bias, s, v);
 }
 
 // Where the terms lie apart an LDS row is one term's BR elements, and a fragment's read takes 32 bytes (16 bits) or 64 bytes
@@ -157,21 +163,105 @@ __device__ inline void wait_copies() {
 }
 __device__ inline void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
+__device__ inline void barrier() {  // no LDS access moves across it
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // workgroups go round the 8 XCDs: each XCD gets a run of neighbouring tiles, which share operands in its L2
 __device__ inline int xcd_run(int id, int n) {
   const int x = id & 7, q = n >> 3, r = n & 7;
   return x * q + min(x, r) + (id >> 3);
 }
 
+// bytes of LDS of a tile: two stages
+template <int BM, int BN>
+constexpr int tile_lds() {
+  return 2 * (BM + BN) * 128;
+}
+
+// A wave's sums, MT x NT fragments from row r0 and column c0 on, to where they go, straight from the registers.  A lane ends with 4
+// neighbouring columns of a row; it gives those of every second fragment to the lane 16 further and takes its for the
+// others, and then has 8: one 16-byte access of a 16-bit type and one Philox call.  KEPT: sums stay in the accumulator registers
+// until their turn (mfma_in_place).
+template <typename T, int EPI, bool KEPT, int MT, int NT>
+__device__ inline void write_sums(const GemmArgs &g, int split, long long r0, int c0, int lane, floatx4 (&acc)[MT][NT]) {
+  const int i16 = lane & 15, q = lane >> 4;
+#pragma unroll
+  for (int p = 0; p < NT / 2; ++p) {
+    const int col = c0 + 32 * p + 16 * (q & 1) + 8 * (q >> 1), n = g.C - col;
+    float bias[8];
+    if (EPI == EPI_FWD) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bias[e] = 0.f;
+      if (g.e.bias && n > 0) load8(g.e.bias + col, bias, n);
+    }
+    struct Eight {
+      T v[8];
+    };
+    static_assert(MT % 4 == 0 || MT == 2, "");
+    constexpr int AHEAD = MT < 4 ? MT : 4;
+    uintx4 res[AHEAD][sizeof(T) / 2];  // of four rows, as they lie in memory: their reads are in flight together
+    const bool with = EPI == EPI_FWD && g.e.res && !g.part;
+    auto fetch = [&](int first) {
+      if (!with) return;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const long long row = r0 + 16 * (first + i) + i16;
+        if (row < g.R && n > 0) {
+          const T *src = (const T *)g.e.res + row * g.C + col;
+          if (n >= 8) {
+            __builtin_memcpy(res[i], src, sizeof(Eight));
+          } else {
+            Eight t;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t.v[e] = e < n ? src[e] : (T)0.f;
+            __builtin_memcpy(res[i], &t, sizeof(Eight));
+          }
+        }
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      if (i % 4 == 0) fetch(i);
+      if constexpr (KEPT) asm volatile("" : "+a"(acc[i][2 * p]), "+a"(acc[i][2 * p + 1]));
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const auto t = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, (float)acc[i][2 * p][e]),
+                                                        __builtin_bit_cast(uint32_t, (float)acc[i][2 * p + 1][e]), false, false);
+        const uint32_t own = t[0], got = t[1];
+        v[e] = __builtin_bit_cast(float, own), v[e + 4] = __builtin_bit_cast(float, got);
+      }
+      const long long row = r0 + 16 * i + i16;
+      if (row >= g.R || n <= 0) continue;
+      if (EPI == EPI_F32 || g.part) {
+        store8(g.part + (split * g.R + row) * g.part_ld + col, v, (int)min(g.part_ld - col, 8ll));
+      } else if constexpr (EPI == EPI_FWD) {
+        float s[8];
+        if (with) {
+          Eight t;
+#pragma unroll
+          for (int w = 0; w < (int)sizeof(T) / 2; ++w) asm volatile("" : "+v"(res[i % AHEAD][w]));  // unpacked here, not before
+          __builtin_memcpy(&t, res[i % AHEAD], sizeof(Eight));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[e] = (float)t.v[e];
+        }
+        finish_fwd<T>(g.e, row, col, g.C, bias, s, v);
+      } else {
+        store8((T *)g.e.out + row * g.C + col, v, n);
+      }
+    }
+  }
+}
+
 template <typename T, int BM, int BN, bool AT, bool BT, int EPI, bool COPY>
-__global__ __launch_bounds__(LT) void gemm_kernel(GemmArgs g) {
+__device__ inline void gemm_tile(const GemmArgs &g, int id, char *lds) {
   using A = Staged<T, BM, AT>;
   using B = Staged<T, BN, BT>;
   constexpr int STEP = A::STEP, MT = BM / 32, NT = BN / 32, STAGE = A::BYTES + B::BYTES;
-  __shared__ __align__(1024) char lds[2 * STAGE];  // holds the tile's fp32 results, BM * BN * 4, at the end
-  static_assert(BM * BN * 4 <= 2 * STAGE, "");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int id = xcd_run(blockIdx.x, g.tiles * g.splits);
   const int split = id / g.tiles, tile = id - split * g.tiles, tr = tile / g.tiles_c;
   const long long r0 = (long long)tr * BM;
   const int c0 = (tile - tr * g.tiles_c) * BN;
@@ -273,7 +363,7 @@ __global__ __launch_bounds__(LT) void gemm_kernel(GemmArgs g) {
       if constexpr (COPY) wait_copies<0>();
     }
     wait_lds();
-    __builtin_amdgcn_s_barrier();
+    barrier();
     const char *la = lds + cur * STAGE, *lb = la + A::BYTES;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
@@ -290,69 +380,331 @@ __global__ __launch_bounds__(LT) void gemm_kernel(GemmArgs g) {
     if constexpr (!COPY)
       if (s + 1 < steps) put(cur ^ 1);  // read last a step ago, behind the barrier above
     wait_lds();
-    __builtin_amdgcn_s_barrier();
+    barrier();
   }
 
-  // the tile's results through LDS: row-wise 8 neighbours per thread, 16-byte stores and one Philox call each
-  float *const res = reinterpret_cast<float *>(lds);
-  constexpr int CH = BN / 4;  // 16-byte chunks of a row; chunk c of row r lies at c ^ (r & 15)
+  write_sums<T, EPI, false>(g, split, r0 + wm, c0 + wn, lane, acc);
+}
+
+template <typename T, int BLOCK, bool AT, bool BT, int EPI, bool COPY>
+__global__ __launch_bounds__(LT) void gemm_kernel(GemmArgs g) {
+  __shared__ __align__(1024) char lds[tile_lds<BLOCK, BLOCK>()];
+  gemm_tile<T, BLOCK, BLOCK, AT, BT, EPI, COPY>(g, xcd_run(blockIdx.x, gridDim.x), lds);
+}
+
+// ---- 256 x 256 tiles, 16 bits ----
+// Eight waves of 128 x 64, two to a SIMD: one's MFMAs run while the other issues its copies (32 of the pipe's cycles each, measured)
+// and address arithmetic.  A step is 32 terms; four stages of 32 KB.  While a step's MFMAs run, the next step's fragments are read
+// and the copies of the third next are issued, between the MFMAs: one barrier a step, behind which a stage is whole and the one before
+// it free.  128 accumulators and two sets of fragments take the 256 registers that two waves leave each other.
+constexpr int WIDE = 256, WT = 512;
+
+template <typename T, bool APART>
+struct StagedWide {
+  static constexpr int ROWB = APART ? WIDE * 2 : 64, CPR = ROWB / 16, BYTES = WIDE * 64, PIECES = BYTES / 8192;
+  static __device__ inline void place(int q, int wave, int lane, int &row, int &chunk) {
+    const int at = (q * 8 + wave) * 64 + lane;
+    row = at / CPR;
+    const int c = at % CPR;
+    chunk = APART ? c ^ (turned_swizzle<T, WIDE>(row) << 1) : c ^ swizzle(row);
+  }
+  // terms together: the LDS serves 16 lanes of a 16-byte read at a time, lanes 0-3, 12-15, 20-23 and 24-27 together, and so on:
+  // rows 0-3 and 12-15 of one quarter, 4-11 of the next.  0, 2, 3, 1 by the row's fourth of 16 keeps those apart
+  static __device__ inline int swizzle(int row) { return ((row >> 2 ^ row >> 3) & 1) << 1 | (row >> 3 & 1); }
+  // this lane's part of a fragment's address; fragment t of the wave's at rows w + 16 t
+  static __device__ inline uint32_t lane_address(int w, int lane) {
+    const int i = lane & 15, q = lane >> 4;
+    if (!APART) return (uint32_t)((w + i) * 64 + ((q ^ swizzle(i)) << 4));
+    const int row = q * 8 + (i >> 2);
+    return (uint32_t)(row * ROWB + (((w >> 4) ^ turned_swizzle<T, WIDE>(row)) << 5) + (i & 3) * 8);
+  }
+  static __device__ inline uintx4 fragment(const char *lds, uint32_t at, int t) {
+    if constexpr (!APART) {
+      return *reinterpret_cast<const uintx4 *>(lds + at + t * 1024);
+    } else {
+      uintx4 f;
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int r = wm + i * 16 + (lane & 15), c = (wn + j * 16) / 4 + (lane >> 4);
-      reinterpret_cast<floatx4 *>(res)[r * CH + (c ^ (r & 15))] = acc[i][j];
+      for (int h = 0; h < 2; ++h) {  // the swizzle is the same for both halves: rows 4 apart
+        const uint2 v = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                      (__attribute__((address_space(3))) shortx4 *)(lds + (at ^ (t << 5)) + h * 4 * ROWB)));
+        f[2 * h] = v.x, f[2 * h + 1] = v.y;
+      }
+      return f;
     }
-  __syncthreads();
-  const int c8 = tid % (BN / 8), col = c0 + c8 * 8;
-  if (col >= g.C) return;
-  float bias[8];
+  }
+};
+
+// c += the MFMA of a and b, in place in the accumulator registers: left to itself the compiler gives sums new registers, and
+// with most of them taken moves them about.  What it does not see: a result may be read 18 cycles after its MFMA at the earliest, by another
+// instruction than an MFMA that adds to it (settle_sums).
+template <typename T>
+__device__ inline void mfma_in_place(floatx4 &c, const uintx4 &a, const uintx4 &b) {
+  if constexpr (__is_same(T, __bf16))
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  else
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+template <int N>
+__device__ inline void settle_sums(floatx4 (&c)[8][N]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) bias[e] = 0.f;
-  if (EPI == EPI_FWD && g.e.bias) load8(g.e.bias + col, bias, g.C - col);
-#pragma unroll 2
-  for (int r = tid / (BN / 8); r < BM; r += LT / (BN / 8)) {
-    if (r0 + r >= g.R) break;
-    float v[8];
-    const floatx4 lo = reinterpret_cast<const floatx4 *>(res)[r * CH + ((2 * c8) ^ (r & 15))];
-    const floatx4 hi = reinterpret_cast<const floatx4 *>(res)[r * CH + ((2 * c8 + 1) ^ (r & 15))];
+  for (int i = 0; i < 8 * N; ++i) asm volatile("" : "+a"(c[i / N][i % N]));
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = lo[e], v[e + 4] = hi[e];
-    if (EPI == EPI_F32 || g.part)
-      store8(g.part + (split * g.R + r0 + r) * g.part_ld + col, v, (int)min(g.part_ld - col, 8ll));
-    else if (EPI == EPI_FWD)
-      finish_fwd<T>(g.e, r0 + r, col, g.C, bias, v);
-    else
-      store8((T *)g.e.out + (r0 + r) * g.C + col, v, g.C - col);
+  for (int i = 0; i < 8 * N; ++i) asm volatile("" : "+a"(c[i / N][i % N]));
+}
+
+template <typename T, bool AT, bool BT, int EPI>
+__global__ __launch_bounds__(WT, 2) void gemm_wide_kernel(GemmArgs g) {
+  using A = StagedWide<T, AT>;
+  using B = StagedWide<T, BT>;
+  constexpr int STEP = 32, STAGE = A::BYTES + B::BYTES, STAGES = 4;
+  __shared__ __align__(1024) char lds[STAGES * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int id = xcd_run(blockIdx.x, gridDim.x);
+  const int split = id / g.tiles, tile = id - split * g.tiles, tr = tile / g.tiles_c;
+  const long long r0 = (long long)tr * WIDE;
+  const int c0 = (tile - tr * g.tiles_c) * WIDE;
+  const long long l0 = split * g.per, l1 = min(g.L, l0 + g.per);
+  const int steps = (int)((l1 - l0 + STEP - 1) / STEP), rest = (int)(l1 - l0 - (long long)(steps - 1) * STEP);
+  uint32_t av[A::PIECES], bv[B::PIECES];
+  uint32_t last = 0;  // bits of the pieces that lie inside the last step, too
+#pragma unroll
+  for (int q = 0; q < A::PIECES; ++q) {
+    int row, chunk;
+    A::place(q, wave, lane, row, chunk);
+    av[q] = (uint32_t)(row * g.lda + chunk * 16);
+    if (AT ? (long long)chunk * 8 >= g.R - r0 : row >= g.R - r0) av[q] = OUTSIDE;
+    last |= (uint32_t)((AT ? row : chunk * 8) < rest) << q;
+  }
+#pragma unroll
+  for (int q = 0; q < B::PIECES; ++q) {
+    int row, chunk;
+    B::place(q, wave, lane, row, chunk);
+    bv[q] = (uint32_t)(row * g.ldb + chunk * 16);
+    if (BT ? chunk * 8 >= g.C - c0 : row >= g.C - c0) bv[q] = OUTSIDE;
+    last |= (uint32_t)((BT ? row : chunk * 8) < rest) << (A::PIECES + q);
+  }
+  const char *pa = g.a + (AT ? l0 * g.lda + r0 * 2 : r0 * g.lda + l0 * 2);
+  const char *pb = g.b + (BT ? l0 * g.ldb + (long long)c0 * 2 : c0 * g.ldb + l0 * 2);
+  const long long sa = AT ? STEP * g.lda : 64, sb = BT ? STEP * g.ldb : 64;
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
+  // piece q of step s, which lies `stage` stages into LDS; beyond the last step zeros, so that the counts of copies stay
+  auto copy_piece = [&](int s, int stage, int q, const uintx4 &ba, const uintx4 &bb) {
+    uint32_t off = q < A::PIECES ? av[q % A::PIECES] : bv[q % B::PIECES];
+    if (s >= steps - 1) off = s == steps - 1 && (last >> q & 1) ? off : OUTSIDE;
+    copy16(q < A::PIECES ? ba : bb, off, base + stage * STAGE + (q < A::PIECES ? q * 8192 : A::BYTES + (q - A::PIECES) * 8192));
+  };
+  constexpr int PIECES = A::PIECES + B::PIECES;
+  const int wm = (wave >> 2) * 128, wn = (wave & 3) * 64;
+  const uint32_t at_a = A::lane_address(wm, lane), at_b = B::lane_address(wn, lane) + A::BYTES;
+  floatx4 acc[8][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) {
+    const uintx4 ba = buffer_of(pa), bb = buffer_of(pb);
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) copy_piece(s, s, q, ba, bb);
+    pa += sa, pb += sb;
+  }
+  wait_copies<2 * PIECES>();
+  barrier();
+  settle_sums(acc);  // the zeros, too, are there before the first MFMA reads them
+  uintx4 fa[2][8], fb[2][4];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) fa[0][t] = A::fragment(lds, at_a, t);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) fb[0][t] = B::fragment(lds, at_b, t);
+  for (int s0 = 0; s0 < steps; s0 += STAGES) {
+#pragma unroll
+    for (int u = 0; u < STAGES; ++u) {
+      const int s = s0 + u, cur = u & 1;
+      if (u > 0 && s >= steps) break;
+      wait_copies<PIECES>();  // of step s + 1: this wave's
+      barrier();              // everyone's; and step s - 1's fragments have been read
+      const uintx4 ba = buffer_of(pa), bb = buffer_of(pb);
+      pa += sa, pb += sb;
+      const char *const next = lds + ((u + 1) & 3) * STAGE;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (i % 2 == 0) copy_piece(s + 3, (u + 3) & 3, i / 2, ba, bb);
+        fa[cur ^ 1][i] = A::fragment(next, at_a, i);
+        if (i % 2 == 1) fb[cur ^ 1][i / 2] = B::fragment(next, at_b, i / 2);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mfma_in_place<T>(acc[i][j], fb[cur][j], fa[cur][i]);
+      }
+    }
+  }
+  wait_copies<0>();
+  settle_sums(acc);
+  write_sums<T, EPI, true>(g, split, r0 + wm, c0 + wn, lane, acc);
+}
+
+// Both gradients in one launch: the first workgroups take dx's tiles, the others dW's.  Neither waits for the other, so the tail
+// of one is filled by the other, and small layers pay one launch.
+template <typename T, int BX, int BW, bool COPY>
+__global__ __launch_bounds__(LT) void gemm_gradients_kernel(GemmArgs x, GemmArgs w) {
+  constexpr int BIG = BX > BW ? BX : BW;
+  __shared__ __align__(1024) char lds[tile_lds<BIG, BIG>()];
+  const int nx = x.tiles * x.splits, nx8 = (nx + 7) & ~7;  // dW starts at a multiple of the XCDs' number
+  if ((int)blockIdx.x < nx8) {
+    const int id = xcd_run(blockIdx.x, nx);
+    if ((int)blockIdx.x < nx) gemm_tile<T, BX, BX, false, true, EPI_STORE, COPY>(x, id, lds);
+  } else {
+    gemm_tile<T, BW, BW, true, true, EPI_F32, COPY>(w, xcd_run(blockIdx.x - nx8, w.tiles * w.splits), lds);
   }
 }
 
-// Sums of the splits in order, and what follows them.  OUT is the results' type; FWD: the forward's epilogue.
+// The forward of few rows: 16 columns and up to 64 rows to a workgroup, whose waves share the sum's axis.  Weights and rows go
+// from memory into the fragments, without LDS: nothing is used twice, and a wave's loads are in flight together.  A lane's 16 bytes
+// need not follow the MFMA's term order (any order that x and W share will do): the four lanes of a row take 128 neighbouring bytes.
+// Up to 8 rows (HALVES): the MFMA's 16 x 16 results hold 8 columns of W's first half of terms by x's, and 8 of the second by the
+// second, so that twice as many workgroups share W.  Latency-bound; reads of W bound it from some MB on.
+template <typename T, int MT, int NW, bool HALVES, bool ALIGNED>
+__global__ __launch_bounds__(64 * NW) void linear_few_rows_kernel(GemmArgs g) {
+  constexpr int EPC = 16 / sizeof(T), ROWS = HALVES ? 8 : 16 * MT, COLS = HALVES ? 8 : 16;
+  __shared__ floatx4 lds[NW * MT * 64];  // [wave][row of 16][4 chunks of 4 columns], chunk c at c ^ (row & 3)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
+  const int c0 = blockIdx.x * COLS;
+  const long long r0 = (long long)blockIdx.y * ROWS;
+  const int K = (int)g.L, all = (K * (int)sizeof(T) + 127) / 128, steps = HALVES ? (all + 1) / 2 : all;
+  const int own = HALVES ? i & 7 : i, first = HALVES && i >= 8 ? steps * 8 : 0;  // first chunk
+  const char *const w = g.b + min(c0 + own, g.C - 1) * g.ldb;  // rows beyond the last read it again; their results are not used
+  const char *x[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) x[m] = g.a + min(r0 + 16 * m + own, g.R - 1) * g.lda;
+  floatx4 acc[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) acc[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+  auto load = [&](const char *row, int term) -> uintx4 {
+    uintx4 v;
+    const int inside = K - term;
+    if (ALIGNED) {  // whole chunks lie inside or outside: no branch, what lies outside is the last chunk, replaced by zeros
+      v = *reinterpret_cast<const uintx4 *>(row + (long long)min(term, K - EPC) * (int)sizeof(T));
+      const uint32_t keep = inside > 0 ? ~0u : 0u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] &= keep;
+    } else if (inside >= EPC) {
+      __builtin_memcpy(&v, row + (long long)term * (int)sizeof(T), 16);
+    } else {
+      T t[EPC];
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) t[e] = e < inside ? reinterpret_cast<const T *>(row)[term + e] : (T)0.f;
+      __builtin_memcpy(&v, t, 16);
+    }
+    return v;
+  };
+  constexpr int U = MT == 4 ? 1 : 2;  // steps whose loads are in flight together
+  for (int s0 = wave; s0 < steps; s0 += NW * U) {
+    uintx4 fw[U][2], fx[U][MT][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u == 0 || s0 + u * NW < steps) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int term = (first + (s0 + u * NW) * 8 + 2 * q + j) * EPC;
+          fw[u][j] = load(w, term);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) fx[u][m][j] = load(x[m], term);
+        }
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u == 0 || s0 + u * NW < steps) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[m] = mfma<T>(fw[u][j], fx[u][m][j], acc[m]);
+      }
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) lds[(wave * MT * 16 + 16 * m + i) * 4 + (q ^ (i & 3))] = acc[m];
+  __syncthreads();
+  float *const sums = reinterpret_cast<float *>(lds);
+  for (int t = threadIdx.x; t < MT * 256; t += 64 * NW) {
+    float v = sums[t];
+#pragma unroll
+    for (int k = 1; k < NW; ++k) v += sums[k * MT * 256 + t];
+    sums[t] = v;  // no other thread reads or writes these places before the barrier
+  }
+  __syncthreads();
+  constexpr int GROUPS = COLS / 8;
+  for (int t = threadIdx.x; t < ROWS * GROUPS; t += 64 * NW) {
+    const int r = t / GROUPS, h = t % GROUPS, col = c0 + h * 8;
+    if (r0 + r >= g.R || col >= g.C) continue;
+    float v[8];
+    const floatx4 lo = lds[r * 4 + ((2 * h) ^ (r & 3))], hi = lds[r * 4 + ((2 * h + 1) ^ (r & 3))];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = lo[e], v[e + 4] = hi[e];
+    if (HALVES) {  // row r + 8, columns 8 ... 15
+      const floatx4 lo2 = lds[(r + 8) * 4 + (2 ^ (r & 3))], hi2 = lds[(r + 8) * 4 + (3 ^ (r & 3))];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += lo2[e], v[e + 4] += hi2[e];
+    }
+    finish_fwd<T>(g.e, r0 + r, col, g.C, v);
+  }
+}
+
+// Sums of the splits in order, and what follows them.  OUT is the results' type; FWD: the forward's epilogue.  A thread takes 8
+// columns of a row; where there are few of those, `lanes` groups of a workgroup's threads share the splits of one.
+struct FinishArgs {
+  const float *part;
+  int splits, C, lanes;  // lanes: 1, 4 or 16
+  long long R;
+  Epilogue e;
+};
 template <typename T, typename OUT, bool FWD>
-__global__ __launch_bounds__(LT) void gemm_finish_kernel(const float *__restrict__ part, int splits, long long R, int C,
-                                                         Epilogue e) {
-  const int groups = (C + 7) / 8;
-  const long long i = (long long)blockIdx.x * LT + threadIdx.x, ld = 8ll * groups;
-  if (i >= R * groups) return;
-  const long long row = i / groups;
-  const int col = (int)(i - row * groups) * 8;
+__device__ inline void gemm_finish(const FinishArgs &f, long long block, float *lds) {
+  const int items = f.lanes == 1 ? LT : f.lanes == 4 ? LT / 4 : LT / 16;
+  const int groups = (f.C + 7) / 8, k = threadIdx.x & (items - 1), zl = f.lanes == 1 ? 0 : threadIdx.x / (f.lanes == 4 ? LT / 4 : LT / 16);
+  const long long i = block * items + k, ld = 8ll * groups;
+  const bool live = i < f.R * groups;
+  const long long row = live ? i / groups : 0;
+  const int col = live ? (int)(i - row * groups) * 8 : 0;
   float v[8];
-  load8(part + row * ld + col, v);
-  for (int z = 1; z < splits; ++z) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll 4
+  for (int z = zl; z < f.splits; z += f.lanes) {
     float t[8];
-    load8(part + (z * R + row) * ld + col, t);
+    load8(f.part + (z * f.R + row) * ld + col, t);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += t[k];
+    for (int e = 0; e < 8; ++e) v[e] += t[e];
   }
+  if (f.lanes > 1) {
+    float *const at = lds + threadIdx.x * 9;  // 9: neighbours in other banks
+#pragma unroll
+    for (int e = 0; e < 8; ++e) at[e] = v[e];
+    __syncthreads();
+    if (zl > 0) return;
+    for (int q = 1; q < f.lanes; ++q) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += at[q * items * 9 + e];
+    }
+  }
+  if (!live) return;
   if constexpr (FWD) {
-    float bias[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) bias[k] = 0.f;
-    if (e.bias) load8(e.bias + col, bias, C - col);
-    finish_fwd<T>(e, row, col, C, bias, v);
+    finish_fwd<T>(f.e, row, col, f.C, v);
   } else {
-    store8((OUT *)e.out + row * C + col, v, C - col);
+    store8((OUT *)f.e.out + row * f.C + col, v, f.C - col);
   }
+}
+template <typename T>
+__global__ __launch_bounds__(LT) void fwd_finish_kernel(FinishArgs f) {
+  __shared__ float lds[LT * 9];
+  gemm_finish<T, T, true>(f, blockIdx.x, lds);
+}
+// of both gradients: the first nx workgroups finish dx, the others dW
+template <typename T>
+__global__ __launch_bounds__(LT) void gradients_finish_kernel(FinishArgs x, FinishArgs w, unsigned nx) {
+  __shared__ float lds[LT * 9];
+  if (blockIdx.x < nx)
+    gemm_finish<T, T, false>(x, blockIdx.x, lds);
+  else
+    gemm_finish<T, float, false>(w, blockIdx.x - nx, lds);
 }
 
 // ---- the epilogue's gradient ----
@@ -376,7 +728,7 @@ __global__ __launch_bounds__(LT) void linear_epilogue_kernel(long long M, int N,
       drop8(e.drop, (unsigned long long)m * (unsigned)groups + (unsigned)g8, v);
       if (e.act != NF_ACT_NONE) times_slope<T>(e.act, zv, v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[k] += v[k];
+      for (int k = 0; k < 8; ++k) v[k] *= e.drop.scale, s[k] += v[k];
       store8((T *)e.out + m * N + col, v, n);
     }
   }
@@ -393,21 +745,24 @@ __global__ __launch_bounds__(LT) void linear_epilogue_kernel(long long M, int N,
   }
 }
 
-// out[c] = sum over rows of part[row][c], 16 rows of threads to 16 columns, in a fixed order
-__global__ __launch_bounds__(LT) void column_sums_kernel(const float *__restrict__ part, int rows, long long ld, int C,
+// out[c] = sum over rows of part[row][c]: 16 columns to a workgroup of 64 x 16 threads, in a fixed order
+constexpr int CT = 1024;
+__global__ __launch_bounds__(CT) void column_sums_kernel(const float *__restrict__ part, int rows, long long ld, int C,
                                                          float *__restrict__ out) {
-  __shared__ float s[16][17];
+  __shared__ float s[64][17];
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
   float sum = 0.f;
-  if (c < C)
-    for (int r = y; r < rows; r += 16) sum += part[r * ld + c];
+  if (c < C) {
+#pragma unroll 8
+    for (int r = y; r < rows; r += 64) sum += part[r * ld + c];
+  }
   s[y][x] = sum;
   __syncthreads();
-  if (y == 0 && c < C) {
+  const int col = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  sum = s[lane][col];
 #pragma unroll
-    for (int q = 1; q < 16; ++q) sum += s[q][x];
-    out[c] = sum;
-  }
+  for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
+  if (lane == 0 && blockIdx.x * 16 + col < C) out[blockIdx.x * 16 + col] = sum;
 }
 
 // ---- plans ----
@@ -417,14 +772,16 @@ struct Plan {
   size_t bytes;  // of the splits' sums
 };
 
-Plan plan_of(long long R, int C, long long L, int size, bool to_f32) {
+Plan plan_of(long long R, int C, long long L, int size, bool whole) {
   const int step = 128 / size;
   const long long steps = (L + step - 1) / step;
   auto tiles = [&](int b) { return ((R + b - 1) / b) * ((C + b - 1) / b); };
   Plan p;
   p.tile = tiles(128) * steps >= 2048 || tiles(128) >= 192 ? 128 : 64;
+  static const char *wd = getenv("NF_WIDE");
+  if (wd && atoi(wd) && size == 2 && whole && tiles(WIDE) * steps >= atoi(wd)) p.tile = WIDE;
   const long long t = tiles(p.tile);
-  long long s = std::min<long long>(512 / t, steps / 4);
+  long long s = std::min<long long>((p.tile == WIDE ? 256 : 512) / t, steps / 4);
   if (s < 1) s = 1;
   const long long each = (steps + s - 1) / s;
   p.splits = (int)((steps + each - 1) / each);
@@ -433,76 +790,145 @@ Plan plan_of(long long R, int C, long long L, int size, bool to_f32) {
   return p;
 }
 
-template <typename T, bool AT, bool BT, int EPI>
-hipError_t run_gemm(const Plan &p, GemmArgs g, bool copy, hipStream_t st) {
-  const int b = p.tile;
-  g.tiles_c = (g.C + b - 1) / b;
-  g.tiles = (int)((g.R + b - 1) / b) * g.tiles_c;
-  g.splits = p.splits, g.per = p.per;
-  const dim3 grid((unsigned)(g.tiles * g.splits));
-  if (b == 128) {
-    if (copy)
-      hipLaunchKernelGGL((gemm_kernel<T, 128, 128, AT, BT, EPI, true>), grid, dim3(LT), 0, st, g);
-    else
-      hipLaunchKernelGGL((gemm_kernel<T, 128, 128, AT, BT, EPI, false>), grid, dim3(LT), 0, st, g);
-  } else {
-    if (copy)
-      hipLaunchKernelGGL((gemm_kernel<T, 64, 64, AT, BT, EPI, true>), grid, dim3(LT), 0, st, g);
-    else
-      hipLaunchKernelGGL((gemm_kernel<T, 64, 64, AT, BT, EPI, false>), grid, dim3(LT), 0, st, g);
-  }
-  return hipGetLastError();
+// The forward: tiles, or few rows.  Few rows where there are up to 32 (1x2048x2048 bf16 4.4 us, tiles 7.1; 16 rows 6.7 and 8.2), and
+// for small products (256x512x256 5.7 and 7.3); from sums of 2 KB and more than 32 rows on, tiles that share x and W through LDS
+// (64x2048x2048 12.4 and 9.9).
+constexpr int FEW_ROWS = 0;
+Plan fwd_plan(long long M, int N, int K, int size) {
+  Plan p = plan_of(M, N, K, size, K * size % 16 == 0);
+  const long long t64 = ((M + 63) / 64) * ((N + 63) / 64);
+  if (M <= 32 || (t64 <= 64 && (long long)K * size <= 2048)) p.tile = FEW_ROWS, p.splits = 1, p.bytes = 0;
+  return p;
 }
 
-template <typename T, typename OUT, bool FWD>
-hipError_t run_finish(const Plan &p, const GemmArgs &g, hipStream_t st) {
+// fills the tiles of a plan; returns the number of workgroups
+int lay(const Plan &p, GemmArgs &g) {
+  g.tiles_c = (g.C + p.tile - 1) / p.tile;
+  g.tiles = (int)((g.R + p.tile - 1) / p.tile) * g.tiles_c;
+  g.splits = p.splits, g.per = p.per;
+  return g.tiles * g.splits;
+}
+
+FinishArgs finish_args(const Plan &p, const GemmArgs &g) {
+  FinishArgs f = {g.part, p.splits, g.C, 1, g.R, g.e};
+  // groups of threads that share an item's splits: towards 65536 threads, at least 2 splits each
   const long long items = g.R * ((g.C + 7) / 8);
-  hipLaunchKernelGGL((gemm_finish_kernel<T, OUT, FWD>), dim3((unsigned)((items + LT - 1) / LT)), dim3(LT), 0, st, g.part, p.splits, g.R, g.C, g.e);
+  if (items < 65536 && p.splits >= 8) f.lanes = items >= 16384 || p.splits < 32 ? 4 : 16;
+  if (p.splits == 1) f.R = 0;
+  return f;
+}
+inline unsigned finish_blocks(const FinishArgs &f) { return (unsigned)((f.R * ((f.C + 7) / 8) * f.lanes + LT - 1) / LT); }
+
+template <typename T, bool AT, bool BT, int EPI, typename F>
+void go_wide(F go) {
+  if constexpr (sizeof(T) == 2) go(gemm_wide_kernel<T, AT, BT, EPI>);
+}
+
+template <typename T, int MT, int NW, bool HALVES>
+hipError_t few_rows_as(const GemmArgs &g, hipStream_t st) {
+  constexpr int ROWS = HALVES ? 8 : 16 * MT, COLS = HALVES ? 8 : 16;
+  const dim3 grid((g.C + COLS - 1) / COLS, (unsigned)((g.R + ROWS - 1) / ROWS));
+  if (g.lda % 16 == 0)
+    hipLaunchKernelGGL((linear_few_rows_kernel<T, MT, NW, HALVES, true>), grid, dim3(64 * NW), 0, st, g);
+  else
+    hipLaunchKernelGGL((linear_few_rows_kernel<T, MT, NW, HALVES, false>), grid, dim3(64 * NW), 0, st, g);
   return hipGetLastError();
+}
+template <typename T>
+hipError_t run_few_rows(const GemmArgs &g, hipStream_t st) {
+  const bool many = g.L * (int)sizeof(T) > 8 * 128;  // waves without a step would only wait
+  if (g.R <= 8) return many ? few_rows_as<T, 1, 16, true>(g, st) : few_rows_as<T, 1, 4, true>(g, st);
+  if (g.R <= 16) return many ? few_rows_as<T, 1, 16, false>(g, st) : few_rows_as<T, 1, 4, false>(g, st);
+  if (g.R <= 32) return many ? few_rows_as<T, 2, 16, false>(g, st) : few_rows_as<T, 2, 4, false>(g, st);
+  return many ? few_rows_as<T, 4, 16, false>(g, st) : few_rows_as<T, 4, 4, false>(g, st);
 }
 
 template <typename T>
 hipError_t fwd_as(const LinearCall &c, const void *x, const void *W, const float *b, const void *r, const DropArgs &drop,
                   void *y, void *z, void *ws, hipStream_t st) {
-  const Plan p = plan_of(c.M, c.N, c.K, sizeof(T), false);
+  const Plan p = fwd_plan(c.M, c.N, c.K, sizeof(T));
   GemmArgs g = {};
   g.a = (const char *)x, g.b = (const char *)W, g.lda = g.ldb = (long long)c.K * sizeof(T);
   g.R = c.M, g.C = c.N, g.L = c.K;
   g.e = Epilogue{b, r, z, y, drop, c.act};
+  if (p.tile == FEW_ROWS) return run_few_rows<T>(g, st);
   if (p.splits > 1) g.part = (float *)ws, g.part_ld = (c.N + 7) / 8 * 8;
-  const hipError_t e = run_gemm<T, false, false, EPI_FWD>(p, g, g.lda % 16 == 0, st);
+  const dim3 grid(lay(p, g));
+  const bool copy = g.lda % 16 == 0;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(LT), 0, st, g); };
+  auto wide = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(WT), 0, st, g); };
+  if (p.tile == WIDE)
+    go_wide<T, false, false, EPI_FWD>(wide);
+  else if (p.tile == 128)
+    copy ? go(gemm_kernel<T, 128, false, false, EPI_FWD, true>) : go(gemm_kernel<T, 128, false, false, EPI_FWD, false>);
+  else
+    copy ? go(gemm_kernel<T, 64, false, false, EPI_FWD, true>) : go(gemm_kernel<T, 64, false, false, EPI_FWD, false>);
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  return run_finish<T, T, true>(p, g, st);
+  const FinishArgs f = finish_args(p, g);
+  hipLaunchKernelGGL(fwd_finish_kernel<T>, dim3(finish_blocks(f)), dim3(LT), 0, st, f);
+  return hipGetLastError();
 }
 
+// The workspace holds dx's splits, then dW's.  Products of up to TOGETHER tiles share a launch; larger ones, whose tails weigh
+// little, keep the L2s to themselves (16384x2048x2048: 325 us together, 309 apart).
+constexpr int TOGETHER = 1024;
 template <typename T>
 hipError_t bwd_as(const LinearCall &c, const void *dz, const void *x, const void *W, void *dx, float *dW, void *ws,
                   hipStream_t st) {
   const long long ldn = (long long)c.N * sizeof(T), ldk = (long long)c.K * sizeof(T);
   const bool copy = ldn % 16 == 0 && ldk % 16 == 0;
-  if (dx) {
-    const Plan p = plan_of(c.M, c.K, c.N, sizeof(T), false);
-    GemmArgs g = {};
-    g.a = (const char *)dz, g.b = (const char *)W, g.lda = ldn, g.ldb = ldk;
-    g.R = c.M, g.C = c.K, g.L = c.N;
-    g.e.out = dx;
-    if (p.splits > 1) g.part = (float *)ws, g.part_ld = (c.K + 7) / 8 * 8;
-    hipError_t e = run_gemm<T, false, true, EPI_STORE>(p, g, copy, st);
-    if (e == hipSuccess && p.splits > 1) e = run_finish<T, T, false>(p, g, st);
-    if (e != hipSuccess) return e;
+  const Plan px = plan_of(c.M, c.K, c.N, sizeof(T), copy), pw = plan_of(c.N, c.K, c.M, sizeof(T), copy);
+  GemmArgs gx = {}, gw = {};
+  gx.a = (const char *)dz, gx.b = (const char *)W, gx.lda = ldn, gx.ldb = ldk;
+  gx.R = c.M, gx.C = c.K, gx.L = c.N, gx.e.out = dx;
+  if (px.splits > 1) gx.part = (float *)ws, gx.part_ld = (c.K + 7) / 8 * 8;
+  gw.a = (const char *)dz, gw.b = (const char *)x, gw.lda = ldn, gw.ldb = ldk;
+  gw.R = c.N, gw.C = c.K, gw.L = c.M, gw.e.out = dW;
+  gw.part = pw.splits > 1 ? (float *)((char *)ws + px.bytes) : dW, gw.part_ld = pw.splits > 1 ? (c.K + 7) / 8 * 8 : c.K;
+  const int nx = lay(px, gx), nw = lay(pw, gw);
+  if (dx && dW && px.tile != WIDE && pw.tile != WIDE && nx + nw <= TOGETHER) {
+    const dim3 grid((unsigned)((nx + 7) / 8 * 8 + nw));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(LT), 0, st, gx, gw); };
+    auto sized = [&](auto cp) {
+      constexpr bool C = decltype(cp)::value;
+      if (px.tile == 128)
+        pw.tile == 128 ? go(gemm_gradients_kernel<T, 128, 128, C>) : go(gemm_gradients_kernel<T, 128, 64, C>);
+      else
+        pw.tile == 128 ? go(gemm_gradients_kernel<T, 64, 128, C>) : go(gemm_gradients_kernel<T, 64, 64, C>);
+    };
+    copy ? sized(std::true_type()) : sized(std::false_type());
+  } else {
+    if (dx) {
+      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nx), dim3(LT), 0, st, gx); };
+      auto wide = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nx), dim3(WT), 0, st, gx); };
+      if (px.tile == WIDE)
+        go_wide<T, false, true, EPI_STORE>(wide);
+      else if (px.tile == 128)
+        copy ? go(gemm_kernel<T, 128, false, true, EPI_STORE, true>) : go(gemm_kernel<T, 128, false, true, EPI_STORE, false>);
+      else
+        copy ? go(gemm_kernel<T, 64, false, true, EPI_STORE, true>) : go(gemm_kernel<T, 64, false, true, EPI_STORE, false>);
+    }
+    if (dW) {
+      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nw), dim3(LT), 0, st, gw); };
+      auto wide = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nw), dim3(WT), 0, st, gw); };
+      if (pw.tile == WIDE)
+        go_wide<T, true, true, EPI_F32>(wide);
+      else if (pw.tile == 128)
+        copy ? go(gemm_kernel<T, 128, true, true, EPI_F32, true>) : go(gemm_kernel<T, 128, true, true, EPI_F32, false>);
+      else
+        copy ? go(gemm_kernel<T, 64, true, true, EPI_F32, true>) : go(gemm_kernel<T, 64, true, true, EPI_F32, false>);
+    }
   }
-  if (dW) {
-    const Plan p = plan_of(c.N, c.K, c.M, sizeof(T), true);
-    GemmArgs g = {};
-    g.a = (const char *)dz, g.b = (const char *)x, g.lda = ldn, g.ldb = ldk;
-    g.R = c.N, g.C = c.K, g.L = c.M;
-    g.e.out = dW;
-    g.part = p.splits > 1 ? (float *)ws : dW, g.part_ld = p.splits > 1 ? (c.K + 7) / 8 * 8 : c.K;
-    hipError_t e = run_gemm<T, true, true, EPI_F32>(p, g, copy, st);
-    if (e == hipSuccess && p.splits > 1) e = run_finish<T, float, false>(p, g, st);
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  FinishArgs fx = finish_args(px, gx), fw = finish_args(pw, gw);
+  if (!dx) fx.R = 0;
+  if (!dW) fw.R = 0;
+  const unsigned bx = finish_blocks(fx), bw = finish_blocks(fw);
+  if (bx + bw == 0) return hipSuccess;
+  hipLaunchKernelGGL(gradients_finish_kernel<T>, dim3(bx + bw), dim3(LT), 0, st, fx, fw, bx);
+  return hipGetLastError();
 }
 
 // the epilogue gradient's row parts: about 1024 workgroups, 8 rows or more to a thread
@@ -527,9 +953,10 @@ EpiPlan epi_plan(long long M, int N) {
 size_t linear_workspace_bytes(const LinearCall &c) {
   const int size = c.dtype == NF_F32 ? 4 : 2;
   const EpiPlan e = epi_plan(c.M, c.N);
-  const size_t all[] = {plan_of(c.M, c.N, c.K, size, false).bytes, plan_of(c.M, c.K, c.N, size, false).bytes,
-                        plan_of(c.N, c.K, c.M, size, true).bytes, (size_t)e.ny * ((c.N + 7) / 8) * 32};
-  return *std::max_element(all, all + 4);
+  const size_t fwd = fwd_plan(c.M, c.N, c.K, size).bytes;
+  const bool whole = c.N * size % 16 == 0 && c.K * size % 16 == 0;
+  const size_t bwd = plan_of(c.M, c.K, c.N, size, whole).bytes + plan_of(c.N, c.K, c.M, size, whole).bytes;
+  return std::max(std::max(fwd, bwd), (size_t)e.ny * ((c.N + 7) / 8) * 32);
 }
 
 hipError_t launch_linear_fwd(const LinearCall &c, const void *x, const void *W, const float *b, const void *r,
@@ -549,8 +976,7 @@ hipError_t launch_linear_bwd(const LinearCall &c, const void *dz, const void *x,
 hipError_t launch_linear_epilogue(const LinearCall &c, const void *dy, const void *z, const DropArgs &drop, void *dz,
                                   float *db, void *ws, hipStream_t st) {
   const EpiPlan p = epi_plan(c.M, c.N);
-  Epilogue e = {};
-  e.out = dz, e.drop = drop, e.act = c.act;
+  const Epilogue e = {nullptr, nullptr, nullptr, dz, drop, c.act};
   float *part = db ? (float *)ws : nullptr;
   const dim3 grid(p.nx, p.ny);
   if (c.dtype == NF_BF16)
@@ -562,7 +988,7 @@ hipError_t launch_linear_epilogue(const LinearCall &c, const void *dy, const voi
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || !db) return err;
   const int ld = (c.N + 7) / 8 * 8;
-  hipLaunchKernelGGL(column_sums_kernel, dim3((c.N + 15) / 16), dim3(LT), 0, st, part, p.ny, (long long)ld, c.N, db);
+  hipLaunchKernelGGL(column_sums_kernel, dim3((c.N + 15) / 16), dim3(CT), 0, st, part, p.ny, (long long)ld, c.N, db);
   return hipGetLastError();
 }
 

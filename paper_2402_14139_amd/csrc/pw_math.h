@@ -43,11 +43,11 @@ __device__ inline void store8(T *p, const float v[8], int n) {
 }
 
 // e^v and 1/v: as accurate as fp32 for fp32 results; two instructions (relative error about 1e-6) where the result is
-// rounded to 16 bits, whose half step is 2^-12 or more
+// rounded to 16 bits, whose half step is 2^-11 or more
 template <typename T>
 __device__ inline float exp_of(float v) {
   if constexpr (sizeof(T) == 4) return expf(v);
-  return __expf(v);
+  return __builtin_amdgcn_exp2f(v * 1.4426950408889634f);
 }
 template <typename T>
 __device__ inline float recip(float v) {
@@ -55,25 +55,36 @@ __device__ inline float recip(float v) {
   return __builtin_amdgcn_rcpf(v);
 }
 
-// The normal distribution's tail Q(|z|) = erfc(|z| / sqrt 2) / 2 and e^(-z^2 / 2).  erfc(x) = t e^(-x^2) P(t) with
-// t = 1 / (1 + 0.45 x); P is a minimax fit of degree 9 of erfc(x) e^(x^2) / t over 0 <= x <= 12 (relative error 1.6e-8,
-// 1.2e-7 with its fp32 evaluation; beyond 12 e^(-x^2) is 0 in fp32).
+// The normal distribution's tail Q(|z|) = erfc(|z| / sqrt 2) / 2 and bell = e^(-z^2 / 2): Q = t bell P(t), t = 1 / (1 + c |z|),
+// P a minimax fit of Q / (t bell).  fp32: c = 0.45 / sqrt 2, degree 9, |z| up to 17 (relative error 1.6e-8, 1.2e-7 with its
+// evaluation; beyond 17 the bell is 0 in fp32).  16 bits: c = 0.3, degree 5, |z| up to 9 (2.1e-6; beyond, Q is below 1e-19).
 template <typename T>
 __device__ inline float normal_tail(float z, float &bell) {
-  const float x = fabsf(z) * 0.70710678118654752f;
-  const float t = recip<T>(fmaf(0.45f, x, 1.f));
-  float P = -0.03643337f;
-  P = fmaf(P, t, 0.16440561f);
-  P = fmaf(P, t, -0.24082965f);
-  P = fmaf(P, t, 0.06623675f);
-  P = fmaf(P, t, 0.03736064f);
-  P = fmaf(P, t, 0.09022658f);
-  P = fmaf(P, t, 0.184595f);
-  P = fmaf(P, t, 0.22649258f);
-  P = fmaf(P, t, 0.25406855f);
-  P = fmaf(P, t, 0.25387729f);
-  bell = exp_of<T>(-0.5f * z * z);
-  return 0.5f * t * bell * P;
+  if constexpr (sizeof(T) == 4) {
+    const float t = 1.f / fmaf(0.31819805153394639f, fabsf(z), 1.f);
+    float P = -0.018216685f;
+    P = fmaf(P, t, 0.082202805f);
+    P = fmaf(P, t, -0.120414825f);
+    P = fmaf(P, t, 0.033118375f);
+    P = fmaf(P, t, 0.01868032f);
+    P = fmaf(P, t, 0.04511329f);
+    P = fmaf(P, t, 0.0922975f);
+    P = fmaf(P, t, 0.11324629f);
+    P = fmaf(P, t, 0.127034275f);
+    P = fmaf(P, t, 0.126938645f);
+    bell = expf(-0.5f * z * z);
+    return t * bell * P;
+  } else {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(z), 1.f));
+    float P = -0.08183746907f;
+    P = fmaf(P, t, 0.23058672288f);
+    P = fmaf(P, t, -0.03403829558f);
+    P = fmaf(P, t, 0.15375138749f);
+    P = fmaf(P, t, 0.11121039917f);
+    P = fmaf(P, t, 0.12032773274f);
+    bell = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
+    return t * bell * P;
+  }
 }
 
 // The activation of N values, and its slope at them (times what s holds).  The activation is the same for a whole launch: one
@@ -88,10 +99,10 @@ __device__ inline void act_of(int act, float (&v)[N]) {
     for (int e = 0; e < N; ++e) v[e] *= recip<T>(1.f + exp_of<T>(-v[e]));
   } else if (act == NF_ACT_GELU) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
+    for (int e = 0; e < N; ++e) {  // v Phi(v) = max(v, 0) - |v| Q(|v|); a NaN stays one through Q
       float bell;
       const float q = normal_tail<T>(v[e], bell);
-      v[e] *= v[e] > 0.f ? 1.f - q : q;
+      v[e] = fmaf(-fabsf(v[e]), q, fmaxf(v[e], 0.f));
     }
   }
 }
@@ -103,21 +114,21 @@ __device__ inline void times_slope(int act, const float (&z)[N], float (&s)[N]) 
     for (int e = 0; e < N; ++e) s[e] = z[e] > 0.f ? s[e] : 0.f;
   } else if (act == NF_ACT_SILU) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float q = recip<T>(1.f + exp_of<T>(-z[e]));
-      s[e] *= q * (1.f + z[e] * (1.f - q));
+    for (int e = 0; e < N; ++e) {  // q + z q (1 - q)
+      const float q = recip<T>(1.f + exp_of<T>(-z[e])), zq = z[e] * q;
+      s[e] *= fmaf(-q, zq, q + zq);
     }
   } else if (act == NF_ACT_GELU) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       float bell;
       const float q = normal_tail<T>(z[e], bell);
-      s[e] *= (z[e] > 0.f ? 1.f - q : q) + z[e] * bell * 0.39894228040143268f;
+      s[e] *= fmaf(z[e] * 0.39894228040143268f, bell, z[e] > 0.f ? 1.f - q : q);
     }
   }
 }
 
-// Dropout as the kernels take it: T = 0 means none.
+// Dropout as the kernels take it: T = 0 (and scale 1) means none.
 struct DropArgs {
   uint32_t T;
   float scale;
@@ -126,30 +137,28 @@ struct DropArgs {
 DropArgs drop_args(const nf_dropout_desc *d);  // d may be null; checked already
 
 // Philox4x32-10 at counter (group, step): the half words of the 8 elements of a group, two to a word.  A round is two
-// 32x32 -> 64 products (quarter rate) and two three-way xors, about 440 cycles of a wave per 512 elements: a chip that streams
-// bf16 rows at 5 TB/s spends a third of its vector cycles here.
+// 32x32 -> 64 products (quarter rate) and two three-way xors, 10 cycles of the vector ALU an element's wave-instruction in all: a
+// chip that streams bf16 rows at 5 TB/s spends a third of its vector cycles here.
 __device__ inline void philox8(const DropArgs &d, unsigned long long group, uint32_t w[4]) {
   uint32_t a = (uint32_t)group, b = (uint32_t)(group >> 32), c = d.s0, e = d.s1, k0 = d.k0, k1 = d.k1;
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const unsigned long long p = (unsigned long long)a * 0xD2511F53u, q = (unsigned long long)c * 0xCD9E8D57u;
-    a = (uint32_t)(q >> 32) ^ b ^ k0, b = (uint32_t)q;
-    c = (uint32_t)(p >> 32) ^ e ^ k1, e = (uint32_t)p;
+    a = __builtin_amdgcn_bitop3_b32((uint32_t)(q >> 32), b, k0, 0x96), b = (uint32_t)q;  // 0x96: the xor of three
+    c = __builtin_amdgcn_bitop3_b32((uint32_t)(p >> 32), e, k1, 0x96), e = (uint32_t)p;
     k0 += 0x9E3779B9u, k1 += 0xBB67AE85u;
   }
   w[0] = a, w[1] = b, w[2] = c, w[3] = e;
 }
 
-// D of 8 elements of one group, in place.  A dropped element is 0 whatever it was.
-__device__ inline void drop8(const DropArgs &d, unsigned long long group, float v[8]) {
+// Zeros for the dropped of 8 elements of one group, in place, whatever they were; the others are left for `scale`.
+__device__ inline void drop8(const DropArgs &d, unsigned long long group, float (&v)[8]) {
   if (!d.T) return;
   uint32_t w[4];
   philox8(d, group, w);
+  const uint32_t high = d.T << 16;  // u >= T for the half words as they lie: high ones compare whole
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t u = (e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu;
-    v[e] = u >= d.T ? v[e] * d.scale : 0.f;
-  }
+  for (int e = 0; e < 8; ++e) v[e] = ((e & 1) ? w[e >> 1] : w[e >> 1] << 16) >= high ? v[e] : 0.f;
 }
 
 // ---- launches (sizes and pointers checked already) ----
