@@ -7,8 +7,8 @@
 //   fragment    lane l holds row l % 16; with q = l / 16, the 8 terms 32 kk + 8 q + 0..7 of 16 bits (one 16x16x32 MFMA), or the
 //               4 terms 16 kk + 4 q + 0..3 of fp32, one to each of four 16x16x4 MFMAs: the MFMAs' own term order does not
 //               matter as long as A's and B's agree
-//   LDS         terms together: rows of 128 bytes, 16-byte chunk c of row r at c ^ ((r >> 1) & 7), so that the 16 rows of a
-//               fragment lie in 16 different bank groups; terms apart: see turned_swizzle
+//   LDS         rows of a step's bytes, or of a term's elements, whose chunks are exchanged so that those read together lie in
+//               different banks (Staged::swizzle, turned_swizzle)
 //   copies      memory to LDS without registers (buffer loads with LDS as their target, zeros for what lies outside) where rows
 //               are whole 16 bytes, else through registers
 //   order       the MFMA takes B's fragment first, so that a lane ends with 4 neighbouring columns of one row (write_sums)
@@ -82,11 +82,18 @@ __device__ inline int turned_swizzle(int row) {
 }
 
 // One operand's part of a tile: BR rows of results (or columns), one step of terms.
-template <typename T, int BR, bool APART>
+template <typename T, int BR, bool APART, int SB>
 struct Staged {
-  static constexpr int EPC = 16 / sizeof(T), STEP = 128 / sizeof(T);
-  static constexpr int ROWB = APART ? BR * (int)sizeof(T) : 128, CPR = ROWB / 16;
-  static constexpr int BYTES = BR * 128, PIECES = BYTES / 1024 / 4;  // pieces of 1024 bytes per wave
+  static constexpr int EPC = 16 / sizeof(T), STEP = SB / sizeof(T);
+  static constexpr int ROWB = APART ? BR * (int)sizeof(T) : SB, CPR = ROWB / 16;
+  static constexpr int BYTES = BR * SB, PIECES = BYTES / 1024 / 4;  // pieces of 1024 bytes per wave
+
+  // Terms together: the LDS serves 16 lanes of a 16-byte read at a time, lanes 0-3, 12-15, 20-23 and 24-27 together, and so on: rows
+  // 0-3 and 12-15 of one quarter, 4-11 of the next.  Their chunks lie in different banks with chunk c of a row of 128 bytes at
+  // c ^ (row / 2 % 8); of 64 bytes, at c ^ (0, 2, 3, 1 by row / 4 % 4).
+  static __device__ inline int swizzle(int row) {
+    return SB == 128 ? (row >> 1) & 7 : ((row >> 2 ^ row >> 3) & 1) << 1 | (row >> 3 & 1);
+  }
 
   // row and 16-byte chunk (in memory) that this lane brings for piece q
   static __device__ inline void place(int q, int wave, int lane, int &row, int &chunk) {
@@ -96,7 +103,7 @@ struct Staged {
     if constexpr (APART)
       chunk = c ^ (turned_swizzle<T, BR>(row) << (sizeof(T) == 4 ? 2 : 1));
     else
-      chunk = c ^ ((row >> 1) & 7);
+      chunk = c ^ swizzle(row);
   }
 
   // fragment of rows rb .. rb+15, half kk of the step
@@ -104,7 +111,7 @@ struct Staged {
     const int i = lane & 15, q = lane >> 4;
     if constexpr (!APART) {
       const int row = rb + i;
-      return *reinterpret_cast<const uintx4 *>(lds + row * 128 + (((kk * 4 + q) ^ ((row >> 1) & 7)) << 4));
+      return *reinterpret_cast<const uintx4 *>(lds + row * SB + (((kk * 4 + q) ^ swizzle(row)) << 4));
     } else if constexpr (sizeof(T) == 2) {
       uintx4 f;
 #pragma unroll
@@ -176,55 +183,22 @@ __device__ inline int xcd_run(int id, int n) {
 }
 
 // bytes of LDS of a tile: two stages
-template <int BM, int BN>
+template <int BM, int BN, int SB>
 constexpr int tile_lds() {
-  return 2 * (BM + BN) * 128;
+  return 2 * (BM + BN) * SB;
 }
 
-// A wave's sums, MT x NT fragments from row r0 and column c0 on, to where they go, straight from the registers.  A lane ends with 4
-// neighbouring columns of a row; it gives those of every second fragment to the lane 16 further and takes its for the
-// others, and then has 8: one 16-byte access of a 16-bit type and one Philox call.  KEPT: sums stay in the accumulator registers
-// until their turn (mfma_in_place).
+// A wave's sums, MT x NT fragments from row r0 and column c0 on, to where they go.  KEPT: sums stay in the accumulator registers until
+// their turn (mfma_in_place).
+// Gradients and parts of sums go straight from the registers.  A lane holds 4 neighbouring columns of a row; it gives those of every
+// second fragment to the lane 16 further and takes its for the others, and then has 8.
 template <typename T, int EPI, bool KEPT, int MT, int NT>
 __device__ inline void write_sums(const GemmArgs &g, int split, long long r0, int c0, int lane, floatx4 (&acc)[MT][NT]) {
-  const int i16 = lane & 15, q = lane >> 4;
+  const int i16 = lane & 15, q = lane >> 4, col0 = c0 + 16 * (q & 1) + 8 * (q >> 1);
 #pragma unroll
-  for (int p = 0; p < NT / 2; ++p) {
-    const int col = c0 + 32 * p + 16 * (q & 1) + 8 * (q >> 1), n = g.C - col;
-    float bias[8];
-    if (EPI == EPI_FWD) {
+  for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) bias[e] = 0.f;
-      if (g.e.bias && n > 0) load8(g.e.bias + col, bias, n);
-    }
-    struct Eight {
-      T v[8];
-    };
-    static_assert(MT % 4 == 0 || MT == 2, "");
-    constexpr int AHEAD = MT < 4 ? MT : 4;
-    uintx4 res[AHEAD][sizeof(T) / 2];  // of four rows, as they lie in memory: their reads are in flight together
-    const bool with = EPI == EPI_FWD && g.e.res && !g.part;
-    auto fetch = [&](int first) {
-      if (!with) return;
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const long long row = r0 + 16 * (first + i) + i16;
-        if (row < g.R && n > 0) {
-          const T *src = (const T *)g.e.res + row * g.C + col;
-          if (n >= 8) {
-            __builtin_memcpy(res[i], src, sizeof(Eight));
-          } else {
-            Eight t;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) t.v[e] = e < n ? src[e] : (T)0.f;
-            __builtin_memcpy(res[i], &t, sizeof(Eight));
-          }
-        }
-      }
-    };
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      if (i % 4 == 0) fetch(i);
+    for (int p = 0; p < NT / 2; ++p) {  // a row's fragments one after the other: its memory lines are whole soon
       if constexpr (KEPT) asm volatile("" : "+a"(acc[i][2 * p]), "+a"(acc[i][2 * p + 1]));
       float v[8];
 #pragma unroll
@@ -235,31 +209,99 @@ __device__ inline void write_sums(const GemmArgs &g, int split, long long r0, in
         v[e] = __builtin_bit_cast(float, own), v[e + 4] = __builtin_bit_cast(float, got);
       }
       const long long row = r0 + 16 * i + i16;
+      const int col = col0 + 32 * p, n = g.C - col;
       if (row >= g.R || n <= 0) continue;
-      if (EPI == EPI_F32 || g.part) {
+      if (EPI == EPI_F32 || g.part)
         store8(g.part + (split * g.R + row) * g.part_ld + col, v, (int)min(g.part_ld - col, 8ll));
-      } else if constexpr (EPI == EPI_FWD) {
-        float s[8];
-        if (with) {
-          Eight t;
-#pragma unroll
-          for (int w = 0; w < (int)sizeof(T) / 2; ++w) asm volatile("" : "+v"(res[i % AHEAD][w]));  // unpacked here, not before
-          __builtin_memcpy(&t, res[i % AHEAD], sizeof(Eight));
-#pragma unroll
-          for (int e = 0; e < 8; ++e) s[e] = (float)t.v[e];
-        }
-        finish_fwd<T>(g.e, row, col, g.C, bias, s, v);
-      } else {
+      else
         store8((T *)g.e.out + row * g.C + col, v, n);
+    }
+}
+
+// The forward's go through LDS that only this wave uses, all rows or half of them at a time (HALF fragments): its epilogue is a loop, not a copy of its code to every
+// fragment (80 KB of instructions, more than their cache holds), and a lane has 8 neighbours of a row: 16-byte accesses of 16 bits,
+// whole lines, and one Philox call.  lds: 16 rows x NT fragments x 1 KB per 16 rows; chunk c of row r at c ^ (r & 15).
+template <typename T, bool KEPT, int HALF, int MT, int NT>
+__device__ inline void write_fwd(const GemmArgs &g, long long r0, int c0, int lane, floatx4 (&acc)[MT][NT], floatx4 *lds) {
+  constexpr int CH = 4 * NT, ACROSS = 2 * NT, DOWN = 64 / ACROSS, TURNS = 16 * HALF / DOWN;
+  struct Eight {
+    uintx4 w[sizeof(T) / 2];
+  };
+  const int c8 = lane % ACROSS, rr = lane / ACROSS, col = c0 + 8 * c8, n = g.C - col;
+  float bias[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bias[e] = 0.f;
+  if (g.e.bias && n > 0) load8(g.e.bias + col, bias, n);
+  auto fetch = [&](long long row) {  // the residual as it lies in memory
+    Eight w = {};
+    if (g.e.res && row < g.R && n > 0) {
+      const T *src = (const T *)g.e.res + row * g.C + col;
+      if (n >= 8) {
+        __builtin_memcpy(&w, src, sizeof(w));
+      } else {
+        T t[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = e < n ? src[e] : (T)0.f;
+        __builtin_memcpy(&w, t, sizeof(w));
+      }
+    }
+    return w;
+  };
+  constexpr int AHEAD = TURNS < 4 ? TURNS : 4;  // turns whose residuals are in flight while as many are finished
+  Eight next[AHEAD];
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) next[u] = fetch(r0 + rr + u * DOWN);
+#pragma unroll 1
+  for (int h = 0; h < MT / HALF; ++h) {
+    auto put = [&](int from) {
+#pragma unroll
+      for (int i = 0; i < HALF; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          if constexpr (KEPT) asm volatile("" : "+a"(acc[from + i][j]));
+          const int r = 16 * i + (lane & 15), c = 4 * j + (lane >> 4);
+          lds[r * CH + (c ^ (r & (CH - 1) & 15))] = acc[from + i][j];
+        }
+    };
+    if (h == 0)
+      put(0);
+    else
+      put(MT - HALF);
+#pragma unroll 1
+    for (int k0 = 0; k0 < TURNS; k0 += AHEAD) {
+      Eight now[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) now[u] = next[u];
+      const long long first = r0 + rr + (h * TURNS + k0) * DOWN;  // turns run on through both halves
+      if (h * TURNS + k0 + AHEAD < MT / HALF * TURNS) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) next[u] = fetch(first + (AHEAD + u) * DOWN);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int r = (k0 + u) * DOWN + rr;
+        const floatx4 lo = lds[r * CH + ((2 * c8) ^ (r & (CH - 1) & 15))], hi = lds[r * CH + ((2 * c8 + 1) ^ (r & (CH - 1) & 15))];
+        const long long row = first + u * DOWN;
+        if (row >= g.R || n <= 0) continue;
+        float v[8], s[8];
+        T t[8];
+#pragma unroll
+        for (int w = 0; w < (int)sizeof(T) / 2; ++w) asm volatile("" : "+v"(now[u].w[w]));  // unpacked here, not before
+        __builtin_memcpy(t, &now[u], sizeof(Eight));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = lo[e], v[e + 4] = hi[e];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = (float)t[e];
+        finish_fwd<T>(g.e, row, col, g.C, bias, s, v);
       }
     }
   }
 }
 
-template <typename T, int BM, int BN, bool AT, bool BT, int EPI, bool COPY>
+template <typename T, int BM, int BN, int SB, bool AT, bool BT, int EPI, bool COPY>
 __device__ inline void gemm_tile(const GemmArgs &g, int id, char *lds) {
-  using A = Staged<T, BM, AT>;
-  using B = Staged<T, BN, BT>;
+  using A = Staged<T, BM, AT, SB>;
+  using B = Staged<T, BN, BT, SB>;
   constexpr int STEP = A::STEP, MT = BM / 32, NT = BN / 32, STAGE = A::BYTES + B::BYTES;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int split = id / g.tiles, tile = id - split * g.tiles, tr = tile / g.tiles_c;
@@ -290,7 +332,7 @@ __device__ inline void gemm_tile(const GemmArgs &g, int id, char *lds) {
   }
   const char *pa = g.a + (AT ? l0 * g.lda + r0 * (long long)sizeof(T) : r0 * g.lda + l0 * (long long)sizeof(T));
   const char *pb = g.b + (BT ? l0 * g.ldb + c0 * (long long)sizeof(T) : c0 * g.ldb + l0 * (long long)sizeof(T));
-  const long long sa = AT ? STEP * g.lda : 128, sb = BT ? STEP * g.ldb : 128;
+  const long long sa = AT ? STEP * g.lda : SB, sb = BT ? STEP * g.ldb : SB;
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 
   uintx4 hold[A::PIECES + B::PIECES];  // !COPY only
@@ -366,7 +408,7 @@ __device__ inline void gemm_tile(const GemmArgs &g, int id, char *lds) {
     barrier();
     const char *la = lds + cur * STAGE, *lb = la + A::BYTES;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
+    for (int kk = 0; kk < SB / 64; ++kk) {
       uintx4 fa[MT], fb[NT];
 #pragma unroll
       for (int i = 0; i < MT; ++i) fa[i] = A::fragment(la, wm + i * 16, kk, lane);
@@ -383,13 +425,16 @@ __device__ inline void gemm_tile(const GemmArgs &g, int id, char *lds) {
     barrier();
   }
 
-  write_sums<T, EPI, false>(g, split, r0 + wm, c0 + wn, lane, acc);
+  if (EPI == EPI_FWD && !g.part)
+    write_fwd<T, false, MT * NT * 4096 <= 2 * STAGE ? MT : MT / 2>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * (2 * STAGE / 64));
+  else
+    write_sums<T, EPI, false>(g, split, r0 + wm, c0 + wn, lane, acc);
 }
 
-template <typename T, int BLOCK, bool AT, bool BT, int EPI, bool COPY>
+template <typename T, int BLOCK, int SB, bool AT, bool BT, int EPI, bool COPY>
 __global__ __launch_bounds__(LT) void gemm_kernel(GemmArgs g) {
-  __shared__ __align__(1024) char lds[tile_lds<BLOCK, BLOCK>()];
-  gemm_tile<T, BLOCK, BLOCK, AT, BT, EPI, COPY>(g, xcd_run(blockIdx.x, gridDim.x), lds);
+  __shared__ __align__(1024) char lds[tile_lds<BLOCK, BLOCK, SB>()];
+  gemm_tile<T, BLOCK, BLOCK, SB, AT, BT, EPI, COPY>(g, xcd_run(blockIdx.x, gridDim.x), lds);
 }
 
 // ---- 256 x 256 tiles, 16 bits ----
@@ -408,9 +453,7 @@ struct StagedWide {
     const int c = at % CPR;
     chunk = APART ? c ^ (turned_swizzle<T, WIDE>(row) << 1) : c ^ swizzle(row);
   }
-  // terms together: the LDS serves 16 lanes of a 16-byte read at a time, lanes 0-3, 12-15, 20-23 and 24-27 together, and so on:
-  // rows 0-3 and 12-15 of one quarter, 4-11 of the next.  0, 2, 3, 1 by the row's fourth of 16 keeps those apart
-  static __device__ inline int swizzle(int row) { return ((row >> 2 ^ row >> 3) & 1) << 1 | (row >> 3 & 1); }
+  static __device__ inline int swizzle(int row) { return Staged<T, WIDE, false, 64>::swizzle(row); }
   // this lane's part of a fragment's address; fragment t of the wave's at rows w + 16 t
   static __device__ inline uint32_t lane_address(int w, int lane) {
     const int i = lane & 15, q = lane >> 4;
@@ -510,7 +553,7 @@ __global__ __launch_bounds__(WT, 2) void gemm_wide_kernel(GemmArgs g) {
     for (int q = 0; q < PIECES; ++q) copy_piece(s, s, q, ba, bb);
     pa += sa, pb += sb;
   }
-  wait_copies<2 * PIECES>();
+  wait_copies<(STAGES - 2) * PIECES>();
   barrier();
   settle_sums(acc);  // the zeros, too, are there before the first MFMA reads them
   uintx4 fa[2][8], fb[2][4];
@@ -518,29 +561,37 @@ __global__ __launch_bounds__(WT, 2) void gemm_wide_kernel(GemmArgs g) {
   for (int t = 0; t < 8; ++t) fa[0][t] = A::fragment(lds, at_a, t);
 #pragma unroll
   for (int t = 0; t < 4; ++t) fb[0][t] = B::fragment(lds, at_b, t);
-  for (int s0 = 0; s0 < steps; s0 += STAGES) {
+  // step s, the u-th of a turn, after which stages and sets of fragments are as before
+  auto step = [&](auto turn, int s) {
+    constexpr int u = decltype(turn)::value, cur = u & 1;
+    wait_copies<(STAGES - 3) * PIECES>();  // of step s + 1: this wave's
+    barrier();                             // everyone's; and step s - 1's fragments have been read
+    const uintx4 ba = buffer_of(pa), bb = buffer_of(pb);
+    pa += sa, pb += sb;
+    const char *const next = lds + (u + 1) % STAGES * STAGE;
 #pragma unroll
-    for (int u = 0; u < STAGES; ++u) {
-      const int s = s0 + u, cur = u & 1;
-      if (u > 0 && s >= steps) break;
-      wait_copies<PIECES>();  // of step s + 1: this wave's
-      barrier();              // everyone's; and step s - 1's fragments have been read
-      const uintx4 ba = buffer_of(pa), bb = buffer_of(pb);
-      pa += sa, pb += sb;
-      const char *const next = lds + ((u + 1) & 3) * STAGE;
+    for (int i = 0; i < 8; ++i) {
+      if (i % 2 == 0) copy_piece(s + STAGES - 1, (u + STAGES - 1) % STAGES, i / 2, ba, bb);
+      fa[cur ^ 1][i] = A::fragment(next, at_a, i);
+      if (i % 2 == 1) fb[cur ^ 1][i / 2] = B::fragment(next, at_b, i / 2);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (i % 2 == 0) copy_piece(s + 3, (u + 3) & 3, i / 2, ba, bb);
-        fa[cur ^ 1][i] = A::fragment(next, at_a, i);
-        if (i % 2 == 1) fb[cur ^ 1][i / 2] = B::fragment(next, at_b, i / 2);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mfma_in_place<T>(acc[i][j], fb[cur][j], fa[cur][i]);
-      }
+      for (int j = 0; j < 4; ++j) mfma_in_place<T>(acc[i][j], fb[cur][j], fa[cur][i]);
     }
+    return s + 1 < steps;
+  };
+  for (int s = 0;; s += STAGES) {
+    if (!step(std::integral_constant<int, 0>(), s)) break;
+    if (!step(std::integral_constant<int, 1>(), s + 1)) break;
+    if (!step(std::integral_constant<int, 2>(), s + 2)) break;
+    if (!step(std::integral_constant<int, 3>(), s + 3)) break;
   }
   wait_copies<0>();
   settle_sums(acc);
-  write_sums<T, EPI, true>(g, split, r0 + wm, c0 + wn, lane, acc);
+  barrier();  // every wave has read its last fragments
+  if (EPI == EPI_FWD && !g.part)
+    write_fwd<T, true, 4>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * 1024);
+  else
+    write_sums<T, EPI, true>(g, split, r0 + wm, c0 + wn, lane, acc);
 }
 
 // Both gradients in one launch: the first workgroups take dx's tiles, the others dW's.  Neither waits for the other, so the tail
@@ -548,13 +599,13 @@ __global__ __launch_bounds__(WT, 2) void gemm_wide_kernel(GemmArgs g) {
 template <typename T, int BX, int BW, bool COPY>
 __global__ __launch_bounds__(LT) void gemm_gradients_kernel(GemmArgs x, GemmArgs w) {
   constexpr int BIG = BX > BW ? BX : BW;
-  __shared__ __align__(1024) char lds[tile_lds<BIG, BIG>()];
+  __shared__ __align__(1024) char lds[tile_lds<BIG, BIG, 128>()];
   const int nx = x.tiles * x.splits, nx8 = (nx + 7) & ~7;  // dW starts at a multiple of the XCDs' number
   if ((int)blockIdx.x < nx8) {
     const int id = xcd_run(blockIdx.x, nx);
-    if ((int)blockIdx.x < nx) gemm_tile<T, BX, BX, false, true, EPI_STORE, COPY>(x, id, lds);
+    if ((int)blockIdx.x < nx) gemm_tile<T, BX, BX, 128, false, true, EPI_STORE, COPY>(x, id, lds);
   } else {
-    gemm_tile<T, BW, BW, true, true, EPI_F32, COPY>(w, xcd_run(blockIdx.x - nx8, w.tiles * w.splits), lds);
+    gemm_tile<T, BW, BW, 128, true, true, EPI_F32, COPY>(w, xcd_run(blockIdx.x - nx8, w.tiles * w.splits), lds);
   }
 }
 
@@ -772,16 +823,22 @@ struct Plan {
   size_t bytes;  // of the splits' sums
 };
 
+// Tiles of 256 (16 bits, whole 16-byte rows) where their rounds over the 256 CUs take less time than those of two 128s to a CU:
+// 1.55 us a step of 128 bytes and 13 more a round against 0.95 and 7.5 (65536x512x512 54 and 61 us, 8192x1024x1024, 128 tiles, 47 and 26);
+// not where the sum must be split, whose parts are four times as large.  Tiles of 64 for small results.  Sums are split so that
+// about 512 workgroups run, at least 4 steps to a part.
 Plan plan_of(long long R, int C, long long L, int size, bool whole) {
   const int step = 128 / size;
   const long long steps = (L + step - 1) / step;
   auto tiles = [&](int b) { return ((R + b - 1) / b) * ((C + b - 1) / b); };
   Plan p;
   p.tile = tiles(128) * steps >= 2048 || tiles(128) >= 192 ? 128 : 64;
-  static const char *wd = getenv("NF_WIDE");
-  if (wd && atoi(wd) && size == 2 && whole && tiles(WIDE) * steps >= atoi(wd)) p.tile = WIDE;
+  if (size == 2 && whole && tiles(WIDE) >= 128) {
+    const double wide = (double)((tiles(WIDE) + 255) / 256) * (1.55 * steps + 13), narrow = (double)((tiles(128) + 511) / 512) * (0.95 * steps + 7.5);
+    if (wide < narrow) p.tile = WIDE;
+  }
   const long long t = tiles(p.tile);
-  long long s = std::min<long long>((p.tile == WIDE ? 256 : 512) / t, steps / 4);
+  long long s = p.tile == WIDE ? 1 : std::min<long long>(512 / t, steps / 4);
   if (s < 1) s = 1;
   const long long each = (steps + s - 1) / s;
   p.splits = (int)((steps + each - 1) / each);
@@ -860,9 +917,9 @@ hipError_t fwd_as(const LinearCall &c, const void *x, const void *W, const float
   if (p.tile == WIDE)
     go_wide<T, false, false, EPI_FWD>(wide);
   else if (p.tile == 128)
-    copy ? go(gemm_kernel<T, 128, false, false, EPI_FWD, true>) : go(gemm_kernel<T, 128, false, false, EPI_FWD, false>);
+    copy ? go(gemm_kernel<T, 128, 128, false, false, EPI_FWD, true>) : go(gemm_kernel<T, 128, 128, false, false, EPI_FWD, false>);
   else
-    copy ? go(gemm_kernel<T, 64, false, false, EPI_FWD, true>) : go(gemm_kernel<T, 64, false, false, EPI_FWD, false>);
+    copy ? go(gemm_kernel<T, 64, 128, false, false, EPI_FWD, true>) : go(gemm_kernel<T, 64, 128, false, false, EPI_FWD, false>);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const FinishArgs f = finish_args(p, g);
@@ -905,9 +962,9 @@ hipError_t bwd_as(const LinearCall &c, const void *dz, const void *x, const void
       if (px.tile == WIDE)
         go_wide<T, false, true, EPI_STORE>(wide);
       else if (px.tile == 128)
-        copy ? go(gemm_kernel<T, 128, false, true, EPI_STORE, true>) : go(gemm_kernel<T, 128, false, true, EPI_STORE, false>);
+        copy ? go(gemm_kernel<T, 128, 128, false, true, EPI_STORE, true>) : go(gemm_kernel<T, 128, 128, false, true, EPI_STORE, false>);
       else
-        copy ? go(gemm_kernel<T, 64, false, true, EPI_STORE, true>) : go(gemm_kernel<T, 64, false, true, EPI_STORE, false>);
+        copy ? go(gemm_kernel<T, 64, 128, false, true, EPI_STORE, true>) : go(gemm_kernel<T, 64, 128, false, true, EPI_STORE, false>);
     }
     if (dW) {
       auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nw), dim3(LT), 0, st, gw); };
@@ -915,9 +972,9 @@ hipError_t bwd_as(const LinearCall &c, const void *dz, const void *x, const void
       if (pw.tile == WIDE)
         go_wide<T, true, true, EPI_F32>(wide);
       else if (pw.tile == 128)
-        copy ? go(gemm_kernel<T, 128, true, true, EPI_F32, true>) : go(gemm_kernel<T, 128, true, true, EPI_F32, false>);
+        copy ? go(gemm_kernel<T, 128, 128, true, true, EPI_F32, true>) : go(gemm_kernel<T, 128, 128, true, true, EPI_F32, false>);
       else
-        copy ? go(gemm_kernel<T, 64, true, true, EPI_F32, true>) : go(gemm_kernel<T, 64, true, true, EPI_F32, false>);
+        copy ? go(gemm_kernel<T, 64, 128, true, true, EPI_F32, true>) : go(gemm_kernel<T, 64, 128, true, true, EPI_F32, false>);
     }
   }
   const hipError_t e = hipGetLastError();
