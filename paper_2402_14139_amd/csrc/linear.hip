@@ -224,31 +224,18 @@ __device__ inline void write_sums(const GemmArgs &g, int split, long long r0, in
 template <typename T, bool KEPT, int HALF, int MT, int NT>
 __device__ inline void write_fwd(const GemmArgs &g, long long r0, int c0, int lane, floatx4 (&acc)[MT][NT], floatx4 *lds) {
   constexpr int CH = 4 * NT, ACROSS = 2 * NT, DOWN = 64 / ACROSS, TURNS = 16 * HALF / DOWN;
-  struct Eight {
-    uintx4 w[sizeof(T) / 2];
-  };
   const int c8 = lane % ACROSS, rr = lane / ACROSS, col = c0 + 8 * c8, n = g.C - col;
   float bias[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) bias[e] = 0.f;
   if (g.e.bias && n > 0) load8(g.e.bias + col, bias, n);
-  auto fetch = [&](long long row) {  // the residual as it lies in memory
-    Eight w = {};
-    if (g.e.res && row < g.R && n > 0) {
-      const T *src = (const T *)g.e.res + row * g.C + col;
-      if (n >= 8) {
-        __builtin_memcpy(&w, src, sizeof(w));
-      } else {
-        T t[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = e < n ? src[e] : (T)0.f;
-        __builtin_memcpy(&w, t, sizeof(w));
-      }
-    }
+  auto fetch = [&](long long row) {
+    Raw8<T> w = {};
+    if (g.e.res && row < g.R && n > 0) w = raw8((const T *)g.e.res + row * g.C + col, n);
     return w;
   };
   constexpr int AHEAD = TURNS < 4 ? TURNS : 4;  // turns whose residuals are in flight while as many are finished
-  Eight next[AHEAD];
+  Raw8<T> next[AHEAD];
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) next[u] = fetch(r0 + rr + u * DOWN);
 #pragma unroll 1
@@ -269,7 +256,7 @@ __device__ inline void write_fwd(const GemmArgs &g, long long r0, int c0, int la
       put(MT - HALF);
 #pragma unroll 1
     for (int k0 = 0; k0 < TURNS; k0 += AHEAD) {
-      Eight now[AHEAD];
+      Raw8<T> now[AHEAD];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) now[u] = next[u];
       const long long first = r0 + rr + (h * TURNS + k0) * DOWN;  // turns run on through both halves
@@ -284,14 +271,9 @@ __device__ inline void write_fwd(const GemmArgs &g, long long r0, int c0, int la
         const long long row = first + u * DOWN;
         if (row >= g.R || n <= 0) continue;
         float v[8], s[8];
-        T t[8];
-#pragma unroll
-        for (int w = 0; w < (int)sizeof(T) / 2; ++w) asm volatile("" : "+v"(now[u].w[w]));  // unpacked here, not before
-        __builtin_memcpy(t, &now[u], sizeof(Eight));
+        unpack8(now[u], s);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = lo[e], v[e + 4] = hi[e];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = (float)t[e];
         finish_fwd<T>(g.e, row, col, g.C, bias, s, v);
       }
     }
@@ -762,7 +744,7 @@ __global__ __launch_bounds__(LT) void gradients_finish_kernel(FinishArgs x, Fini
 // dz = act'(z) D(dy); a thread keeps 8 columns and walks the rows of its workgroup's part, so that the columns' sums stay in
 // registers.  part [row parts][groups * 8].  HBM-bound: 3 * sizeof(T) bytes an element.
 template <typename T>
-__global__ __launch_bounds__(LT) void linear_epilogue_kernel(long long M, int N, long long per, int tx, const T *dy, const T *z,
+__global__ __launch_bounds__(LT) void linear_epilogue_kernel(long long M, int N, long long per, int tx, const T *__restrict__ dy, const T *__restrict__ z,
                                                              Epilogue e, float *part) {
   __shared__ float sums[LT * 8];
   const int groups = (N + 7) / 8, ty = LT / tx;  // tx threads across, ty down
@@ -771,16 +753,33 @@ __global__ __launch_bounds__(LT) void linear_epilogue_kernel(long long M, int N,
 #pragma unroll
   for (int k = 0; k < 8; ++k) s[k] = 0.f;
   const long long m0 = blockIdx.y * per, m1 = min(M, m0 + per);
+  T *const out = (T *)e.out;
   if (g8 < groups && y < ty) {
-    for (long long m = m0 + y; m < m1; m += ty) {
-      float v[8], zv[8];
-      load8(dy + m * N + col, v, n);
-      if (e.act != NF_ACT_NONE) load8(z + m * N + col, zv, n);
-      drop8(e.drop, (unsigned long long)m * (unsigned)groups + (unsigned)g8, v);
-      if (e.act != NF_ACT_NONE) times_slope<T>(e.act, zv, v);
+    constexpr int U = 4;  // rows whose reads are in flight together
+    for (long long m = m0 + y; m < m1; m += U * ty) {
+      Raw8<T> d[U], zr[U];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] *= e.drop.scale, s[k] += v[k];
-      store8((T *)e.out + m * N + col, v, n);
+      for (int u = 0; u < U; ++u)
+        if (m + u * ty < m1) {
+          d[u] = raw8(dy + (m + u * ty) * N + col, n);
+          if (e.act != NF_ACT_NONE) zr[u] = raw8(z + (m + u * ty) * N + col, n);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (m + u * ty < m1) {
+          const long long row = m + u * ty;
+          float v[8];
+          unpack8(d[u], v);
+          drop8(e.drop, (unsigned long long)row * (unsigned)groups + (unsigned)g8, v);
+          if (e.act != NF_ACT_NONE) {
+            float zv[8];
+            unpack8(zr[u], zv);
+            times_slope<T>(e.act, zv, v);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] *= e.drop.scale, s[k] += v[k];
+          store8(out + row * N + col, v, n);
+        }
     }
   }
   if (!part) return;
@@ -988,7 +987,7 @@ hipError_t bwd_as(const LinearCall &c, const void *dz, const void *x, const void
   return hipGetLastError();
 }
 
-// the epilogue gradient's row parts: about 1024 workgroups, 8 rows or more to a thread
+// the epilogue gradient's row parts: up to 1024 workgroups, 4 rows or more to a thread
 struct EpiPlan {
   int tx, nx, ny;
   long long per;
@@ -999,7 +998,7 @@ EpiPlan epi_plan(long long M, int N) {
   p.tx = std::min(groups, LT);
   p.nx = (groups + p.tx - 1) / p.tx;
   const int ty = LT / p.tx;
-  long long ny = std::max<long long>(1, std::min<long long>(1024 / p.nx, M / (8ll * ty)));
+  long long ny = std::max<long long>(1, std::min<long long>(1024 / p.nx, M / (4ll * ty)));
   p.per = (M + ny - 1) / ny;
   p.ny = (int)((M + p.per - 1) / p.per);
   return p;

@@ -42,6 +42,35 @@ __device__ inline void store8(T *p, const float v[8], int n) {
     if (e < n) p[e] = (T)v[e];
 }
 
+// 8 elements as they lie in memory: half the registers of their fp32 forms for a 16-bit type.  unpack8 hides them from the
+// compiler, which would convert them as soon as they arrive.
+template <typename T>
+struct Raw8 {
+  uintx4 w[sizeof(T) / 2];
+};
+template <typename T>
+__device__ inline Raw8<T> raw8(const T *p, int n) {
+  Raw8<T> r;
+  if (n >= 8) {
+    __builtin_memcpy(&r, p, sizeof(r));
+  } else {
+    T t[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = e < n ? p[e] : (T)0.f;
+    __builtin_memcpy(&r, t, sizeof(r));
+  }
+  return r;
+}
+template <typename T>
+__device__ inline void unpack8(Raw8<T> r, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 2); ++i) asm volatile("" : "+v"(r.w[i]));
+  T t[8];
+  __builtin_memcpy(t, &r, sizeof(r));
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
+}
+
 // e^v and 1/v: as accurate as fp32 for fp32 results; two instructions (relative error about 1e-6) where the result is
 // rounded to 16 bits, whose half step is 2^-11 or more
 template <typename T>
