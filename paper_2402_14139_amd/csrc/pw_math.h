@@ -11,8 +11,8 @@ namespace nf {
 using floatx4 = __attribute__((ext_vector_type(4))) float;
 using uintx4 = __attribute__((ext_vector_type(4))) uint32_t;
 
-// 8 neighbouring elements as fp32.  A row may start at any element: the copies below carry no alignment, and the
-// memory system takes 16-byte accesses at element boundaries.
+// 8 neighbouring elements as fp32.  A row may start at any element: the copies below carry no alignment, and the memory
+// system takes 16-byte accesses at element boundaries.
 template <typename T>
 __device__ inline void load8(const T *p, float v[8]) {
   T t[8];
@@ -25,7 +25,12 @@ __device__ inline void store8(T *p, const float v[8]) {
   T t[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) t[e] = (T)v[e];  // to nearest, ties to even
-  __builtin_memcpy(p, t, sizeof(t));
+  uintx4 w[sizeof(T) / 2];
+  __builtin_memcpy(w, t, sizeof(t));
+  // whole: the compiler would share the first elements' store with the branch that writes fewer, and split this one
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 2); ++i) asm volatile("" : "+v"(w[i]));
+  __builtin_memcpy(p, w, sizeof(w));
 }
 // the first n of them (n may exceed 8); the others read as 0 and are not written
 template <typename T>
@@ -53,6 +58,7 @@ __device__ inline Raw8<T> raw8(const T *p, int n) {
   Raw8<T> r;
   if (n >= 8) {
     __builtin_memcpy(&r, p, sizeof(r));
+    asm volatile("");  // a branch of its own: its reads stay whole
   } else {
     T t[8];
 #pragma unroll
