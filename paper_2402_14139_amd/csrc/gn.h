@@ -30,6 +30,7 @@ __device__ inline uintx4 load_vec(const T *p, int n) {
     u = *reinterpret_cast<const uintx4 *>(p);
   } else if (n >= Vec<T>::N) {
     __builtin_memcpy(&u, p, 16);
+    asm volatile("");  // a branch of its own: its read stays whole
   } else {
     Vec<T> t;
 #pragma unroll
@@ -82,7 +83,9 @@ __device__ inline void store_vec(T *p, const uintx4 &u, int n) {
   if (WHOLE) {
     *reinterpret_cast<uintx4 *>(p) = u;
   } else if (n >= Vec<T>::N) {
-    __builtin_memcpy(p, &u, 16);
+    uintx4 w = u;
+    asm volatile("" : "+v"(w));  // likewise
+    __builtin_memcpy(p, &w, 16);
   } else {
     const Vec<T> t = __builtin_bit_cast(Vec<T>, u);
 #pragma unroll
@@ -108,7 +111,7 @@ __device__ inline void store_vec(T *p, const float (&f)[16 / sizeof(T)], int n) 
 enum { FUSED, STATS, APPLY };  // one launch; or a chunk's sums, and the results
 
 struct GnArgs {
-  int HW, C, G, Cg, W;  // W: channels of a slab
+  int HW, C, G, Cg, W;  // W: channels of a slab; the last of an image may have fewer
   int groups;           // of a slab
   int cv, px;           // vectors across a slab, pixels that the workgroup takes at once
   int chunks, per;      // chunks of an image, pixels of a chunk
@@ -153,27 +156,28 @@ __device__ inline void column_sums(const float *buf, int rows, int cols, int pit
 
 // Sums of the slab's groups from the threads' sums of their channels.  ONE: a vector lies in one group.
 // gsum[groups] is ready behind the last barrier; buf [px][cv or W, odd pitch], csum[W].
+// W, groups: this slab's.
 template <int VEC, bool ONE>
-__device__ inline void group_sums(const GnArgs &a, int pr, int cl, const float s[VEC], float *buf, float *csum, float *gsum) {
+__device__ inline void group_sums(const GnArgs &a, int W, int groups, int pr, int cl, const float s[VEC], float *buf, float *csum, float *gsum) {
   __syncthreads();  // the buffers may still be read
   if constexpr (ONE) {
     const int vg = a.Cg / VEC, c = cl / VEC, g = a.div_cg.div(cl);  // vectors of a group; rows are (pixel, vector of the group)
     float t = 0.f;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) t += s[e];
-    if (pr < a.px) buf[(pr * vg + c - g * vg) * (a.groups | 1) + g] = t;
+    if (pr < a.px && cl < W) buf[(pr * vg + c - g * vg) * (a.groups | 1) + g] = t;
     __syncthreads();
-    column_sums(buf, a.px * vg, a.groups, a.groups | 1, 1, a.share_g, gsum);
+    column_sums(buf, a.px * vg, groups, a.groups | 1, 1, a.share_g, gsum);
   } else {
     if (pr < a.px) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        if (cl + e < a.W) buf[pr * (a.W | 1) + cl + e] = s[e];
+        if (cl + e < W) buf[pr * (a.W | 1) + cl + e] = s[e];
     }
     __syncthreads();
-    column_sums(buf, a.px, a.W, a.W | 1, 1, a.share_w, csum);
+    column_sums(buf, a.px, W, a.W | 1, 1, a.share_w, csum);
     __syncthreads();
-    column_sums(csum, a.Cg, a.groups, 1, a.Cg, a.share_g, gsum);
+    column_sums(csum, a.Cg, groups, 1, a.Cg, a.share_g, gsum);
   }
   __syncthreads();
 }
@@ -216,17 +220,21 @@ GnPlan gn_plan(const GnShape &s, bool backward) {
     return (long long)(1024 / across(W)) * most >= s.HW && (long long)s.HW * s.C * size < (1ll << 31);
   };
   const int units = s.C / unit;
+  auto slabs = [&](int m) { return (units + m - 1) / m; };
   int m = 1;
   for (int k = 2; k <= units && k * unit * size <= 128; ++k)
-    if (units % k == 0 && fits(k * unit)) m = k;
-  for (int k = m - 1; k >= 1 && (long long)s.B * (units / m) < 512 && k * unit * size >= 32; --k)
-    if (units % k == 0) m = k;
+    if (fits(k * unit) && slabs(k) < slabs(m)) m = k;
+  while (m > 1 && (long long)s.B * slabs(m) < 512 && (m + 1) / 2 * unit * size >= 32) m = (m + 1) / 2;
   a.W = m * unit, a.groups = a.W / a.Cg, a.cv = across(a.W);
   p.split = !fits(a.W);
   int pixels = s.HW;
   a.chunks = 1;
   if (p.split) {
-    a.per = (int)std::min<long long>((1024 / a.cv) * std::min(most, 8), std::max<long long>(1, (1ll << 30) / ((long long)s.C * size)));
+    // pixels of a chunk: what 1024 threads hold, fewer where that leaves fewer than 512 workgroups; 30 bits of offset
+    const int at_once = 1024 / a.cv;
+    int deep = std::min(most, 8);
+    while (deep > 1 && (long long)s.B * slabs(m) * ((s.HW + at_once * deep - 1) / (at_once * deep)) < 512) --deep;
+    a.per = (int)std::min<long long>(at_once * deep, std::max<long long>(1, (1ll << 30) / ((long long)s.C * size)));
     a.chunks = (s.HW + a.per - 1) / a.per;
     a.per = (s.HW + a.chunks - 1) / a.chunks;
     a.chunks = (s.HW + a.per - 1) / a.per;
@@ -245,7 +253,7 @@ GnPlan gn_plan(const GnShape &s, bool backward) {
   a.px = p.nt / a.cv;
   p.tiny = !p.split && p.nt <= TINY && a.px >= s.HW;
   p.small = !p.split && p.nt <= 256 && (long long)a.px * 4 >= s.HW;
-  p.slabs = s.C / a.W;
+  p.slabs = slabs(m);
   auto share = [&](int cols) {  // all threads have a column, as far as 64 lanes to each go
     int k = 6;
     while (k > 0 && (cols << k) > p.nt) --k;
@@ -267,6 +275,80 @@ hipError_t by_type(const GnShape &s, const GnPlan &p, F run) {
   if (s.dtype == NF_BF16) return by_rows<__bf16>(p, run);
   if (s.dtype == NF_F16) return by_rows<_Float16>(p, run);
   return by_rows<float>(p, run);
+}
+
+// (x - mu) rs gamma + beta, k = rs gamma rounded, in two fp32 numbers: the roundings of sums and products are carried along.
+// Its sign, which decides whether a rectified element's dy counts, is right down to 2^-44 of the terms.
+__device__ inline float careful_z(float x, float mu, float rs, float gamma, float k, float beta) {
+#pragma clang fp contract(off)
+  const float d = x - mu, back = d - x, dl = (x - (d - back)) - (mu + back);
+  const float t = d * k, kl = fmaf(rs, gamma, -k);
+  const float tl = fmaf(d, k, -t) + fmaf(d, kl, dl * k);
+  const float sum = t + beta, from = sum - t;
+  return sum + (((t - (sum - from)) + (beta - from)) + tl);
+}
+
+// ---- small groups ----
+// A wave (four of them to a workgroup) or a workgroup of 256 or 1024 threads to a group, an element to a thread: threads go over the
+// group's channels first, then over `px` pixels, and up to FEW_R times further.  What a short launch waits for is mostly its
+// instructions' first fetch (a launch that does next to nothing takes 1.6 us, the slab kernels 5 to 7), and this is a fifth of
+// their code: 3x3x17 fp32 4.9 -> 2.0 us, 13x23x16 7.1 -> 3.1.
+constexpr int FEW_R = 16;
+struct GnFew {
+  int HW, C, G, Cg, px, units, act;
+  int threads;  // of a group: 64, 256 or 1024
+  int share;    // log2 of the threads that add up a channel's sums
+  float eps, inv;
+  FastDiv div_cg, div_g, div_px;
+};
+// Whether a shape goes this way: groups of up to 16 elements a thread, and up to FEW_ELEMENTS in all, beyond which accesses of single
+// elements cost more than the instructions
+constexpr long long FEW_ELEMENTS = 1 << 20;
+inline bool gn_few(const GnShape &s, GnFew *a) {
+  a->HW = s.HW, a->C = s.C, a->G = s.G, a->Cg = s.C / s.G, a->act = s.act, a->eps = s.eps;
+  static const char *fw = getenv("NF_FEW");
+  if ((long long)s.B * s.HW * s.C > (fw ? atoll(fw) : FEW_ELEMENTS)) return false;
+  a->threads = 0;
+  // few elements a thread, or the most threads
+  for (int nt : {64, 256, 1024})
+    if (a->Cg <= nt && s.HW <= (nt == 1024 ? FEW_R : 4) * (nt / a->Cg)) {
+      a->threads = nt;
+      break;
+    }
+  if (!a->threads) return false;
+  a->px = a->threads / a->Cg;
+  a->share = 6;
+  while (a->share > 0 && (a->Cg << a->share) > a->threads) --a->share;
+  a->units = s.B * s.G;
+  a->inv = (float)(1.0 / ((double)a->Cg * s.HW));
+  a->div_cg = FastDiv(a->Cg), a->div_g = FastDiv(s.G), a->div_px = FastDiv(a->px);
+  return true;
+}
+// (threads of a workgroup, threads of a group, elements of a thread)
+template <typename F>
+void gn_few_variant(const GnFew &a, F run) {
+  if (a.threads == 64)
+    run(std::integral_constant<int, 64>(), std::integral_constant<int, 4>(), dim3((a.units + 3) / 4), dim3(256));
+  else if (a.threads == 256)
+    run(std::integral_constant<int, 256>(), std::integral_constant<int, 4>(), dim3(a.units), dim3(256));
+  else if (a.HW <= 4 * a.px)
+    run(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>(), dim3(a.units), dim3(1024));
+  else
+    run(std::integral_constant<int, 1024>(), std::integral_constant<int, FEW_R>(), dim3(a.units), dim3(1024));
+}
+// the sum over a group's threads, on all of them; `slot` differs from one call of a kernel to the next
+template <int NT>
+__device__ inline float few_sum(float v, int slot) {
+  v = lanes_sum(v, 6);
+  if constexpr (NT > 64) {
+    __shared__ float parts[2][NT / 64];
+    if ((threadIdx.x & 63) == 0) parts[slot][threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) v += parts[slot][w];
+  }
+  return v;
 }
 
 }  // namespace

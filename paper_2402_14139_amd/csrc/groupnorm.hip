@@ -18,9 +18,10 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
   const int slabs = a.div_slabs.d;
   const int id = xcd_run(blockIdx.x, gridDim.x), bc = a.div_slabs.div(id), slab = id - bc * slabs;
   const int b = MODE == FUSED ? bc : (int)a.div_chunks.div(bc), chunk = MODE == FUSED ? 0 : bc - b * a.chunks;
-  const int c0 = slab * a.W, p0 = chunk * a.per, p1 = min(a.HW, p0 + a.per);
-  const int pr = a.div_cv.div(t), cl = (t - pr * a.cv) * VEC, n = a.W - cl;  // n: the slab's channels from here on
-  const bool live = pr < a.px;
+  const int c0 = slab * a.W, W = min(a.W, a.C - c0), groups = W == a.W ? a.groups : (int)a.div_cg.div(W);  // of this slab
+  const int p0 = chunk * a.per, p1 = min(a.HW, p0 + a.per);
+  const int pr = a.div_cv.div(t), cl = (t - pr * a.cv) * VEC, n = W - cl;  // n: the slab's channels from here on
+  const bool live = pr < a.px && n > 0;
   // offsets within the slab fit 32 bits (gn_plan)
   const long long first = ((long long)b * a.HW + p0) * a.C + c0;
   const char *const xs = (const char *)(x + first);
@@ -39,7 +40,7 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
       if (live && (WHOLE || e < n)) ga[e] = gamma[c0 + cl + e], be[e] = beta[c0 + cl + e];
     }
   }
-  auto group_of = [&](int e) { return ONE ? (int)a.div_cg.div(cl) : (int)a.div_cg.div(WHOLE ? cl + e : min(cl + e, a.W - 1)); };
+  auto group_of = [&](int e) { return ONE ? (int)a.div_cg.div(cl) : (int)a.div_cg.div(WHOLE ? cl + e : min(cl + e, W - 1)); };
   float mu[VEC], s[VEC];
   if (MODE != APPLY) {
 #pragma unroll
@@ -52,7 +53,7 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
 #pragma unroll
         for (int e = 0; e < VEC; ++e) s[e] += f[e];
       }
-    group_sums<VEC, ONE>(a, pr, cl, s, buf, csum, gm);
+    group_sums<VEC, ONE>(a, W, groups, pr, cl, s, buf, csum, gm);
     const float inv = MODE == FUSED ? a.inv : 1.f / ((float)(p1 - p0) * (float)a.Cg);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) mu[e] = live ? gm[group_of(e)] * inv : 0.f, s[e] = 0.f;
@@ -67,8 +68,8 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
           s[e] = fmaf(d, d, s[e]);
         }
       }
-    group_sums<VEC, ONE>(a, pr, cl, s, buf, csum, gr);
-    for (int g = t; g < a.groups; g += blockDim.x) {
+    group_sums<VEC, ONE>(a, W, groups, pr, cl, s, buf, csum, gr);
+    for (int g = t; g < groups; g += blockDim.x) {
       const long long o = (long long)bc * a.G + slab * a.groups + g;
       if (MODE == STATS) {
         part[2 * o] = gm[g] * inv, part[2 * o + 1] = gr[g];
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
     // chunks' means and squares to the image's: the squares about the image's mean are those about the chunks' plus
     // count * (chunk's mean - image's mean)^2
     const int lane = t & 63;
-    for (int g = t >> 6; g < a.groups; g += blockDim.x >> 6) {
+    for (int g = t >> 6; g < groups; g += blockDim.x >> 6) {
       const float *q = part + 2 * ((long long)b * a.chunks * a.G + slab * a.groups + g);
       float sum = 0.f, sq = 0.f;
       for (int k = lane; k < a.chunks; k += 64) sum += q[2ll * k * a.G] * (float)(min(a.HW, (k + 1) * a.per) - k * a.per);
@@ -145,6 +146,53 @@ hipError_t fwd_as(const GnShape &s, const GnPlan &p, const void *x, const float 
   return hipGetLastError();
 }
 
+// ---- small groups ----
+template <typename T, int NT, int R>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void gn_fwd_few_kernel(GnFew a, const T *__restrict__ x, const float *__restrict__ gamma,
+                                                                         const float *__restrict__ beta, T *__restrict__ y,
+                                                                         float *__restrict__ mean, float *__restrict__ rstd) {
+  const int t = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
+  const int unit = NT == 64 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
+  if (unit >= a.units) return;
+  const int b = a.div_g.div(unit), grp = unit - b * a.G;
+  const int p = a.div_cg.div(t), c = t - p * a.Cg, ch = grp * a.Cg + c;
+  const int mine = p < a.px ? (int)a.div_px.div(a.HW - p + a.px - 1) : 0;
+  const long long at = ((long long)b * a.HW + p) * a.C + ch, step = (long long)a.px * a.C;
+  float v[R], s = 0.f;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < mine) v[i] = (float)x[at + i * step];
+  float ga = 0.f, be = 0.f;
+  if (mine) ga = gamma[ch], be = beta[ch];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < mine) s += v[i];
+  const float mu = few_sum<NT>(s, 0) * a.inv;
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < mine) v[i] -= mu, s = fmaf(v[i], v[i], s);
+  const float rs = 1.f / sqrtf(few_sum<NT>(s, 1) * a.inv + a.eps);
+  if (t == 0) mean[unit] = mu, rstd[unit] = rs;
+  ga *= rs;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < mine) {
+      float z[1] = {fmaf(v[i], ga, be)};
+      act_of<T>(a.act, z);
+      y[at + i * step] = (T)z[0];
+    }
+}
+
+template <typename T>
+hipError_t fwd_few_as(const GnFew &a, const void *x, const float *gamma, const float *beta, void *y, float *mean, float *rstd,
+                      hipStream_t st) {
+  gn_few_variant(a, [&](auto nt, auto r, dim3 grid, dim3 block) {
+    hipLaunchKernelGGL((gn_fwd_few_kernel<T, decltype(nt)::value, decltype(r)::value>), grid, block, 0, st, a, (const T *)x, gamma, beta, (T *)y, mean, rstd);
+  });
+  return hipGetLastError();
+}
+
 }  // namespace
 
 size_t gn_workspace_bytes(const GnShape &s) {
@@ -154,6 +202,12 @@ size_t gn_workspace_bytes(const GnShape &s) {
 
 hipError_t launch_gn_fwd(const GnShape &s, const void *x, const float *gamma, const float *beta, void *y, float *mean,
                          float *rstd, void *ws, hipStream_t st) {
+  GnFew few;
+  if (gn_few(s, &few)) {
+    if (s.dtype == NF_BF16) return fwd_few_as<__bf16>(few, x, gamma, beta, y, mean, rstd, st);
+    if (s.dtype == NF_F16) return fwd_few_as<_Float16>(few, x, gamma, beta, y, mean, rstd, st);
+    return fwd_few_as<float>(few, x, gamma, beta, y, mean, rstd, st);
+  }
   const GnPlan p = gn_plan(s, false);
   return by_type(s, p, [&](auto t, auto whole, auto one) {
     return fwd_as<decltype(t), decltype(whole)::value, decltype(one)::value>(s, p, x, gamma, beta, y, mean, rstd, (float *)ws, st);

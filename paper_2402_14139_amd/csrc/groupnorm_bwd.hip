@@ -4,23 +4,13 @@
 namespace nf {
 namespace {
 
-// (x - mu) rs gamma + beta, k = rs gamma rounded, in two fp32 numbers: the roundings of sums and products are carried along.
-// Its sign, which decides whether a rectified element's dy counts, is right down to 2^-44 of the terms.
-__device__ inline float careful_z(float x, float mu, float rs, float gamma, float k, float beta) {
-#pragma clang fp contract(off)
-  const float d = x - mu, back = d - x, dl = (x - (d - back)) - (mu + back);
-  const float t = d * k, kl = fmaf(rs, gamma, -k);
-  const float tl = fmaf(d, k, -t) + fmaf(d, kl, dl * k);
-  const float sum = t + beta, from = sum - t;
-  return sum + (((t - (sum - from)) + (beta - from)) + tl);
-}
-
-// HBM-bound: 3 * sizeof(T) bytes an element.  part [image * chunks + chunk][2][C]: sums over pixels of g xh and g.
+// HBM-bound: 3 * sizeof(T) bytes an element.  sum_gx and sum_g, rows of 2 C floats per (image, chunk): sums over its pixels of g xh
+// and g.
 template <typename T, bool WHOLE, bool ONE, int MODE, int R, int NTMAX>
 __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__restrict__ dy, const T *__restrict__ x,
                                                        const float *__restrict__ gamma, const float *__restrict__ beta,
                                                        const float *__restrict__ mean, const float *__restrict__ rstd,
-                                                       T *__restrict__ dx, float *__restrict__ part) {
+                                                       T *__restrict__ dx, float *sum_gx, float *sum_g) {
   constexpr int VEC = Vec<T>::N, PV = ONE ? 1 : VEC;  // mean and deviation: one for the vector, or one per channel
   extern __shared__ float lds[];
   const int pitch = 2 * a.W + 1;
@@ -29,9 +19,10 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
   const int slabs = a.div_slabs.d;
   const int id = xcd_run(blockIdx.x, gridDim.x), bc = a.div_slabs.div(id), slab = id - bc * slabs;
   const int b = MODE == FUSED ? bc : (int)a.div_chunks.div(bc), chunk = MODE == FUSED ? 0 : bc - b * a.chunks;
-  const int c0 = slab * a.W, p0 = chunk * a.per, p1 = min(a.HW, p0 + a.per);
-  const int pr = a.div_cv.div(t), cl = (t - pr * a.cv) * VEC, n = a.W - cl;
-  const bool live = pr < a.px;
+  const int c0 = slab * a.W, W = min(a.W, a.C - c0), groups = W == a.W ? a.groups : (int)a.div_cg.div(W);  // of this slab
+  const int p0 = chunk * a.per, p1 = min(a.HW, p0 + a.per);
+  const int pr = a.div_cv.div(t), cl = (t - pr * a.cv) * VEC, n = W - cl;
+  const bool live = pr < a.px && n > 0;
   // offsets within the slab fit 32 bits (gn_plan)
   const long long first = ((long long)b * a.HW + p0) * a.C + c0;
   const char *const xs = (const char *)(x + first), *const ds = (const char *)(dy + first);
@@ -42,7 +33,7 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
 #pragma unroll
   for (int i = 0; i < R; ++i)
     if (i < mine) v[i] = load_vec<T, WHOLE>((const T *)(xs + (off + i * step)), n), d[i] = load_vec<T, WHOLE>((const T *)(ds + (off + i * step)), n);
-  auto group_of = [&](int e) { return ONE ? (int)a.div_cg.div(cl) : (int)a.div_cg.div(WHOLE ? cl + e : min(cl + e, a.W - 1)); };
+  auto group_of = [&](int e) { return ONE ? (int)a.div_cg.div(cl) : (int)a.div_cg.div(WHOLE ? cl + e : min(cl + e, W - 1)); };
   const long long first_group = (long long)b * a.G + slab * a.groups;
   float mu[PV], k[VEC], be[VEC];  // k = rs gamma
 #pragma unroll
@@ -56,17 +47,21 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
   auto grad = [&](int i, int h, float (&xc)[4], float (&g)[4]) {
     float z[4];
     unpack4<T>(v[i], h, xc), unpack4<T>(d[i], h, g);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) xc[e] -= mu[ONE ? 0 : 4 * h + e], z[e] = fmaf(xc[e], k[4 * h + e], be[4 * h + e]);
     if (a.act == NF_ACT_RELU) {
+      bool near = false;  // fp32's z is off by a few 2^-24 of beta there
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int q = 4 * h + e;
-        const float ga = WHOLE || q < n ? gamma[c0 + cl + q] : 0.f, rs = live ? rstd[first_group + group_of(q)] : 0.f;
-        z[e] = careful_z(xc[e], mu[ONE ? 0 : q], rs, ga, k[q], be[q]);
-        xc[e] -= mu[ONE ? 0 : q];
+      for (int e = 0; e < 4; ++e) near |= fabsf(z[e]) <= 1e-5f * fabsf(be[4 * h + e]);
+      if (near) {
+        float x[4];
+        unpack4<T>(v[i], h, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int q = 4 * h + e;
+          if (WHOLE || q < n) z[e] = careful_z(x[e], mu[ONE ? 0 : q], rstd[first_group + group_of(q)], gamma[c0 + cl + q], k[q], be[q]);
+        }
       }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) xc[e] -= mu[ONE ? 0 : 4 * h + e], z[e] = fmaf(xc[e], k[4 * h + e], be[4 * h + e]);
     }
     times_slope<T>(a.act, z, g);
   };
@@ -93,12 +88,17 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
     __syncthreads();
     column_sums(buf, a.px, 2 * a.W, pitch, 1, a.share_2w, csum);
     __syncthreads();
-    for (int c = t; c < 2 * a.W; c += blockDim.x) part[((long long)bc * 2 + (c >= a.W)) * a.C + c0 + (c >= a.W ? c - a.W : c)] = csum[c];
+    for (int c = t; c < 2 * a.W; c += blockDim.x) {
+      const int second = c >= a.W, ch = second ? c - a.W : c;
+      if (ch < W) (second ? sum_g : sum_gx)[(long long)bc * 2 * a.C + c0 + ch] = csum[c];
+    }
     if (MODE == STATS) return;
   } else {
     // the image's sums: the chunks' in order
     for (int c = t; c < 2 * a.W; c += blockDim.x) {
-      const float *q = part + ((long long)b * a.chunks * 2 + (c >= a.W)) * a.C + c0 + (c >= a.W ? c - a.W : c);
+      const int second = c >= a.W, ch = second ? c - a.W : c;
+      if (ch >= W) continue;
+      const float *q = (second ? sum_g : sum_gx) + (long long)b * a.chunks * 2 * a.C + c0 + ch;
       float s = 0.f;
       for (int k = 0; k < a.chunks; ++k) s += q[2ll * k * a.C];
       csum[c] = s;
@@ -108,12 +108,12 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
   // averages over the group of g gamma xh and g gamma
   {
     const int lane = t & 63;
-    for (int q = t >> 6; q < 2 * a.groups; q += blockDim.x >> 6) {
-      const int g = q >= a.groups ? q - a.groups : q;
+    for (int q = t >> 6; q < 2 * groups; q += blockDim.x >> 6) {
+      const int second = q >= groups, g = second ? q - groups : q;
       float s = 0.f;
-      for (int c = g * a.Cg + lane; c < (g + 1) * a.Cg; c += 64) s = fmaf(csum[(q >= a.groups ? a.W : 0) + c], gamma[c0 + c], s);
+      for (int c = g * a.Cg + lane; c < (g + 1) * a.Cg; c += 64) s = fmaf(csum[(second ? a.W : 0) + c], gamma[c0 + c], s);
       s = lanes_sum(s, 6);
-      if (lane == 0) gsum[q] = s * a.inv;
+      if (lane == 0) gsum[second * a.groups + g] = s * a.inv;
     }
   }
   __syncthreads();
@@ -171,12 +171,12 @@ __global__ __launch_bounds__(RT) void gn_params_kernel(const float *__restrict__
 
 template <typename T, bool WHOLE, bool ONE>
 hipError_t bwd_as(const GnShape &s, const GnPlan &p, const void *dy, const void *x, const float *gamma, const float *beta,
-                  const float *mean, const float *rstd, void *dx, float *part, hipStream_t st) {
+                  const float *mean, const float *rstd, void *dx, float *sum_gx, float *sum_g, hipStream_t st) {
   constexpr int R = ONE ? 8 : 4;
   const GnArgs &a = p.a;
   const size_t lds = 4 * ((size_t)a.px * (2 * a.W + 1) + 2 * a.W + 2 * a.groups);
   const dim3 grid((unsigned)(p.slabs * s.B * a.chunks)), nt(p.nt);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)dy, (const T *)x, gamma, beta, mean, rstd, (T *)dx, part); };
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)dy, (const T *)x, gamma, beta, mean, rstd, (T *)dx, sum_gx, sum_g); };
   if (p.split) {
     go(gn_bwd_kernel<T, WHOLE, ONE, STATS, R, 1024>);
     go(gn_bwd_kernel<T, WHOLE, ONE, APPLY, R, 1024>);
@@ -190,17 +190,91 @@ hipError_t bwd_as(const GnShape &s, const GnPlan &p, const void *dy, const void 
   return hipGetLastError();
 }
 
+// ---- small groups ----
+template <typename T, int NT, int R>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void gn_bwd_few_kernel(GnFew a, const T *__restrict__ dy, const T *__restrict__ x,
+                                                                         const float *__restrict__ gamma, const float *__restrict__ beta,
+                                                                         const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                                         T *__restrict__ dx, float *__restrict__ sum_gx,
+                                                                         float *__restrict__ sum_g) {
+  __shared__ float lds[2][NT < 256 ? 256 : NT];
+  const int t = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
+  const int unit = NT == 64 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
+  if (unit >= a.units) return;
+  const int b = a.div_g.div(unit), grp = unit - b * a.G;
+  const int p = a.div_cg.div(t), c = t - p * a.Cg, ch = grp * a.Cg + c;
+  const int mine = p < a.px ? (int)a.div_px.div(a.HW - p + a.px - 1) : 0;
+  const long long at = ((long long)b * a.HW + p) * a.C + ch, step = (long long)a.px * a.C;
+  float xv[R], g[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < mine) xv[i] = (float)x[at + i * step], g[i] = (float)dy[at + i * step];
+  float ga = 0.f, be = 0.f;
+  if (mine) ga = gamma[ch], be = beta[ch];
+  const float mu = mean[unit], rs = rstd[unit], k = rs * ga;
+  float s = 0.f, sx = 0.f;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < mine) {
+      const float x0 = xv[i];
+      xv[i] -= mu;
+      float z[1] = {fmaf(xv[i], k, be)}, v[1] = {g[i]};
+      if (a.act == NF_ACT_RELU && fabsf(z[0]) <= 1e-5f * fabsf(be)) z[0] = careful_z(x0, mu, rs, ga, k, be);
+      times_slope<T>(a.act, z, v);
+      g[i] = v[0];
+      s += g[i], sx = fmaf(g[i], xv[i], sx);
+    }
+  sx *= rs;
+  const float m1 = rs * few_sum<NT>(s * ga, 0) * a.inv, m2 = rs * rs * few_sum<NT>(sx * ga, 1) * a.inv;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < mine) dx[at + i * step] = (T)(fmaf(g[i], k, -m1) - xv[i] * m2);
+  // the channels' sums: [pixel][channel] in LDS, which only this wave uses where it is the whole group
+  const int base = NT == 64 ? threadIdx.x & ~63 : 0;
+  lds[0][base + t] = sx, lds[1][base + t] = s;
+  if constexpr (NT > 64) __syncthreads();
+  const int first = t & ((1 << a.share) - 1);
+  for (int q = t >> a.share; q < a.Cg; q += NT >> a.share) {
+    float gx = 0.f, g0 = 0.f;
+    for (int r = first; r < a.px; r += 1 << a.share) gx += lds[0][base + r * a.Cg + q], g0 += lds[1][base + r * a.Cg + q];
+    gx = lanes_sum(gx, a.share), g0 = lanes_sum(g0, a.share);
+    const long long o = (long long)b * 2 * a.C + grp * a.Cg + q;
+    if (first == 0) sum_gx[o] = gx, sum_g[o] = g0;
+  }
+}
+
+template <typename T>
+hipError_t bwd_few_as(const GnFew &a, const void *dy, const void *x, const float *gamma, const float *beta, const float *mean,
+                      const float *rstd, void *dx, float *sum_gx, float *sum_g, hipStream_t st) {
+  gn_few_variant(a, [&](auto nt, auto r, dim3 grid, dim3 block) {
+    hipLaunchKernelGGL((gn_bwd_few_kernel<T, decltype(nt)::value, decltype(r)::value>), grid, block, 0, st, a, (const T *)dy, (const T *)x, gamma, beta, mean, rstd, (T *)dx, sum_gx, sum_g);
+  });
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_gn_bwd(const GnShape &s, const void *dy, const void *x, const float *gamma, const float *beta,
                          const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta, void *ws,
                          hipStream_t st) {
+  GnFew few;
+  const bool is_few = gn_few(s, &few);
   const GnPlan p = gn_plan(s, true);
-  const hipError_t e = by_type(s, p, [&](auto t, auto whole, auto one) {
-    return bwd_as<decltype(t), decltype(whole)::value, decltype(one)::value>(s, p, dy, x, gamma, beta, mean, rstd, dx, (float *)ws, st);
-  });
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(gn_params_kernel, dim3((2 * s.C + 15) / 16), dim3(RT), 0, st, (const float *)ws, s.B * p.a.chunks, s.C, dgamma, dbeta);
+  const int rows = s.B * (is_few ? 1 : p.a.chunks);
+  // one row of sums is the result
+  float *const sum_gx = rows == 1 ? dgamma : (float *)ws, *const sum_g = rows == 1 ? dbeta : (float *)ws + s.C;
+  hipError_t e;
+  if (is_few) {
+    e = s.dtype == NF_BF16  ? bwd_few_as<__bf16>(few, dy, x, gamma, beta, mean, rstd, dx, sum_gx, sum_g, st)
+        : s.dtype == NF_F16 ? bwd_few_as<_Float16>(few, dy, x, gamma, beta, mean, rstd, dx, sum_gx, sum_g, st)
+                            : bwd_few_as<float>(few, dy, x, gamma, beta, mean, rstd, dx, sum_gx, sum_g, st);
+  } else {
+    e = by_type(s, p, [&](auto t, auto whole, auto one) {
+      return bwd_as<decltype(t), decltype(whole)::value, decltype(one)::value>(s, p, dy, x, gamma, beta, mean, rstd, dx, sum_gx, sum_g, st);
+    });
+  }
+  if (e != hipSuccess || rows == 1) return e;
+  hipLaunchKernelGGL(gn_params_kernel, dim3((2 * s.C + 15) / 16), dim3(RT), 0, st, (const float *)ws, rows, s.C, dgamma, dbeta);
   return hipGetLastError();
 }
 
