@@ -114,6 +114,7 @@ struct GnArgs {
   int HW, C, G, Cg, W;  // W: channels of a slab; the last of an image may have fewer
   int groups;           // of a slab
   int cv, px;           // vectors across a slab, pixels that the workgroup takes at once
+  int Wp;               // W in whole vectors: the length of the channels' parameters in LDS
   int chunks, per;      // chunks of an image, pixels of a chunk
   int act;
   float eps, inv;  // inv = 1 / (Cg HW)
@@ -154,6 +155,17 @@ __device__ inline void column_sums(const float *buf, int rows, int cols, int pit
   }
 }
 
+// a thread's channels' parameters
+template <int N>
+__device__ inline void read_channels(const float *lds, float (&f)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; e += 4) {
+    const floatx4 q = *reinterpret_cast<const floatx4 *>(lds + e);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) f[e + k] = q[k];
+  }
+}
+
 // Sums of the slab's groups from the threads' sums of their channels.  ONE: a vector lies in one group.
 // gsum[groups] is ready behind the last barrier; buf [px][cv or W, odd pitch], csum[W].
 // W, groups: this slab's.
@@ -182,8 +194,8 @@ __device__ inline void group_sums(const GnArgs &a, int W, int groups, int pr, in
   __syncthreads();
 }
 
-// floats of LDS before gsum: the matrix and the channels' sums
-inline int fwd_lds(const GnArgs &a, int vec, bool one) { return one ? a.px * (a.Cg / vec) * (a.groups | 1) : a.px * (a.W | 1) + a.W; }
+// floats of the matrix and the channels' sums
+inline int matrix_floats(const GnArgs &a, int vec, bool one) { return one ? a.px * (a.Cg / vec) * (a.groups | 1) : a.px * (a.W | 1) + a.W; }
 
 int gcd(int a, int b) {
   while (b) {
@@ -225,7 +237,7 @@ GnPlan gn_plan(const GnShape &s, bool backward) {
   for (int k = 2; k <= units && k * unit * size <= 128; ++k)
     if (fits(k * unit) && slabs(k) < slabs(m)) m = k;
   while (m > 1 && (long long)s.B * slabs(m) < 512 && (m + 1) / 2 * unit * size >= 32) m = (m + 1) / 2;
-  a.W = m * unit, a.groups = a.W / a.Cg, a.cv = across(a.W);
+  a.W = m * unit, a.groups = a.W / a.Cg, a.cv = across(a.W), a.Wp = a.cv * vec;
   p.split = !fits(a.W);
   int pixels = s.HW;
   a.chunks = 1;
@@ -303,7 +315,7 @@ struct GnFew {
 };
 // Whether a shape goes this way: groups of up to 16 elements a thread, and up to FEW_ELEMENTS in all, beyond which accesses of single
 // elements cost more than the instructions
-constexpr long long FEW_ELEMENTS = 1 << 20;
+constexpr long long FEW_ELEMENTS = 3 << 19;
 inline bool gn_few(const GnShape &s, GnFew *a) {
   a->HW = s.HW, a->C = s.C, a->G = s.G, a->Cg = s.C / s.G, a->act = s.act, a->eps = s.eps;
   static const char *fw = getenv("NF_FEW");

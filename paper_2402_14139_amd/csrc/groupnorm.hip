@@ -10,10 +10,12 @@ template <typename T, bool WHOLE, bool ONE, int MODE, int R, int NTMAX>
 __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__restrict__ x, const float *__restrict__ gamma,
                                                        const float *__restrict__ beta, T *__restrict__ y,
                                                        float *__restrict__ mean, float *__restrict__ rstd,
-                                                       float *__restrict__ part, int lds_floats) {
+                                                       float *__restrict__ part) {
   constexpr int VEC = Vec<T>::N;
   extern __shared__ float lds[];
-  float *const buf = lds, *const csum = buf + a.px * (a.W | 1), *const gm = lds + lds_floats, *const gr = gm + a.groups;
+  // the channels' means, rstd gamma and beta; the groups' sums; the matrix and the channels' sums
+  float *const pm = lds, *const pk = pm + a.Wp, *const pb = pk + a.Wp, *const gm = pb + a.Wp, *const gr = gm + a.groups;
+  float *const buf = gr + a.groups, *const csum = buf + a.px * (a.W | 1);
   const int t = threadIdx.x;
   const int slabs = a.div_slabs.d;
   const int id = xcd_run(blockIdx.x, gridDim.x), bc = a.div_slabs.div(id), slab = id - bc * slabs;
@@ -32,15 +34,9 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
 #pragma unroll
   for (int i = 0; i < R; ++i)
     if (i < mine) v[i] = load_vec<T, WHOLE>((const T *)(xs + (off + i * step)), n);
-  float ga[VEC], be[VEC];
   if (MODE != STATS) {
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      ga[e] = be[e] = 0.f;
-      if (live && (WHOLE || e < n)) ga[e] = gamma[c0 + cl + e], be[e] = beta[c0 + cl + e];
-    }
+    for (int c = t; c < a.Wp; c += blockDim.x) pk[c] = c < W ? gamma[c0 + c] : 0.f, pb[c] = c < W ? beta[c0 + c] : 0.f;
   }
-  auto group_of = [&](int e) { return ONE ? (int)a.div_cg.div(cl) : (int)a.div_cg.div(WHOLE ? cl + e : min(cl + e, W - 1)); };
   float mu[VEC], s[VEC];
   if (MODE != APPLY) {
 #pragma unroll
@@ -55,8 +51,11 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
       }
     group_sums<VEC, ONE>(a, W, groups, pr, cl, s, buf, csum, gm);
     const float inv = MODE == FUSED ? a.inv : 1.f / ((float)(p1 - p0) * (float)a.Cg);
+    for (int c = t; c < a.Wp; c += blockDim.x) pm[c] = c < W ? gm[a.div_cg.div(c)] * inv : 0.f;
+    __syncthreads();
+    read_channels(pm + (live ? cl : 0), mu);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) mu[e] = live ? gm[group_of(e)] * inv : 0.f, s[e] = 0.f;
+    for (int e = 0; e < VEC; ++e) s[e] = 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i)
       if (i < mine) {
@@ -79,9 +78,7 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
       }
     }
     if (MODE == STATS) return;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e)
-      if (live) ga[e] *= 1.f / sqrtf(gr[group_of(e)] * a.inv + a.eps);
+    for (int c = t; c < W; c += blockDim.x) pk[c] *= 1.f / sqrtf(gr[a.div_cg.div(c)] * a.inv + a.eps);
   } else {
     // chunks' means and squares to the image's: the squares about the image's mean are those about the chunks' plus
     // count * (chunk's mean - image's mean)^2
@@ -104,12 +101,13 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
       }
     }
     __syncthreads();
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      mu[e] = 0.f;
-      if (live) mu[e] = gm[group_of(e)], ga[e] *= gr[group_of(e)];
-    }
+    for (int c = t; c < W; c += blockDim.x) pm[c] = gm[a.div_cg.div(c)], pk[c] *= gr[a.div_cg.div(c)];
   }
+  __syncthreads();
+  if (!live) return;
+  float ga[VEC], be[VEC];
+  if (MODE == APPLY) read_channels(pm + cl, mu);
+  read_channels(pk + cl, ga), read_channels(pb + cl, be);
 #pragma unroll
   for (int i = 0; i < R; ++i)
     if (i < mine) {
@@ -129,10 +127,9 @@ template <typename T, bool WHOLE, bool ONE>
 hipError_t fwd_as(const GnShape &s, const GnPlan &p, const void *x, const float *gamma, const float *beta, void *y,
                   float *mean, float *rstd, float *part, hipStream_t st) {
   const GnArgs &a = p.a;
-  const int floats = fwd_lds(a, Vec<T>::N, ONE);
-  const size_t lds = 4 * (size_t)(floats + 2 * a.groups);
+  const size_t lds = 4 * (size_t)(3 * a.Wp + 2 * a.groups + matrix_floats(a, Vec<T>::N, ONE));
   const dim3 grid((unsigned)(p.slabs * s.B * a.chunks)), nt(p.nt);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)x, gamma, beta, (T *)y, mean, rstd, part, floats); };
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)x, gamma, beta, (T *)y, mean, rstd, part); };
   if (p.split) {
     go(gn_fwd_kernel<T, WHOLE, ONE, STATS, 8, 1024>);
     go(gn_fwd_kernel<T, WHOLE, ONE, APPLY, 8, 1024>);
@@ -197,7 +194,7 @@ hipError_t fwd_few_as(const GnFew &a, const void *x, const float *gamma, const f
 
 size_t gn_workspace_bytes(const GnShape &s) {
   const GnPlan f = gn_plan(s, false), b = gn_plan(s, true);
-  return std::max((size_t)s.B * b.a.chunks * 2 * s.C * 4, f.split ? (size_t)s.B * f.a.chunks * 2 * s.G * 4 : 0);
+  return std::max((size_t)s.B * (1 + (b.split ? b.a.chunks : 0)) * 2 * s.C * 4, f.split ? (size_t)s.B * f.a.chunks * 2 * s.G * 4 : 0);
 }
 
 hipError_t launch_gn_fwd(const GnShape &s, const void *x, const float *gamma, const float *beta, void *y, float *mean,

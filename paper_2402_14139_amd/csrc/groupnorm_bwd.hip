@@ -4,8 +4,8 @@
 namespace nf {
 namespace {
 
-// HBM-bound: 3 * sizeof(T) bytes an element.  sum_gx and sum_g, rows of 2 C floats per (image, chunk): sums over its pixels of g xh
-// and g.
+// HBM-bound: 3 * sizeof(T) bytes an element.  sum_gx and sum_g, rows of 2 C floats: sums over pixels of g xh and g, of
+// every (image, chunk); APPLY reads those of the images.
 template <typename T, bool WHOLE, bool ONE, int MODE, int R, int NTMAX>
 __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__restrict__ dy, const T *__restrict__ x,
                                                        const float *__restrict__ gamma, const float *__restrict__ beta,
@@ -14,7 +14,9 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
   constexpr int VEC = Vec<T>::N, PV = ONE ? 1 : VEC;  // mean and deviation: one for the vector, or one per channel
   extern __shared__ float lds[];
   const int pitch = 2 * a.W + 1;
-  float *const buf = lds, *const csum = buf + (MODE == APPLY ? 0 : a.px * pitch), *const gsum = csum + 2 * a.W;
+  // the channels' means, rstd gamma and beta, then averages in two of their places; rstd and gamma; sums of channels and groups; the matrix
+  float *const pm = lds, *const pk = pm + a.Wp, *const pb = pk + a.Wp, *const prs = pb + a.Wp, *const pg = prs + a.Wp;
+  float *const csum = pg + a.Wp, *const gsum = csum + 2 * a.W, *const buf = gsum + 2 * a.groups;
   const int t = threadIdx.x;
   const int slabs = a.div_slabs.d;
   const int id = xcd_run(blockIdx.x, gridDim.x), bc = a.div_slabs.div(id), slab = id - bc * slabs;
@@ -33,16 +35,23 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
 #pragma unroll
   for (int i = 0; i < R; ++i)
     if (i < mine) v[i] = load_vec<T, WHOLE>((const T *)(xs + (off + i * step)), n), d[i] = load_vec<T, WHOLE>((const T *)(ds + (off + i * step)), n);
-  auto group_of = [&](int e) { return ONE ? (int)a.div_cg.div(cl) : (int)a.div_cg.div(WHOLE ? cl + e : min(cl + e, W - 1)); };
   const long long first_group = (long long)b * a.G + slab * a.groups;
-  float mu[PV], k[VEC], be[VEC];  // k = rs gamma
-#pragma unroll
-  for (int e = 0; e < PV; ++e) mu[e] = live ? mean[first_group + group_of(e)] : 0.f;
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    k[e] = be[e] = 0.f;
-    if (live && (WHOLE || e < n)) k[e] = rstd[first_group + group_of(e)] * gamma[c0 + cl + e], be[e] = beta[c0 + cl + e];
+  for (int c = t; c < a.Wp; c += blockDim.x) {
+    float m = 0.f, r = 0.f, g = 0.f, bt = 0.f;
+    if (c < W) {
+      const int q = a.div_cg.div(c);
+      m = mean[first_group + q], r = rstd[first_group + q], g = gamma[c0 + c], bt = beta[c0 + c];
+    }
+    pm[c] = m, pk[c] = r * g, pb[c] = bt, prs[c] = r, pg[c] = g;
   }
+  __syncthreads();
+  float mu[PV], k[VEC], be[VEC];  // k = rs gamma
+  const int at = live ? cl : 0;
+  if constexpr (ONE)
+    mu[0] = pm[at];
+  else
+    read_channels(pm + at, mu);
+  read_channels(pk + at, k), read_channels(pb + at, be);
   // of 4 elements of the vector at pixel i: xc = x - mu and g = dy act'(z), z = xc k + beta
   auto grad = [&](int i, int h, float (&xc)[4], float (&g)[4]) {
     float z[4];
@@ -59,7 +68,7 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int q = 4 * h + e;
-          if (WHOLE || q < n) z[e] = careful_z(x[e], mu[ONE ? 0 : q], rstd[first_group + group_of(q)], gamma[c0 + cl + q], k[q], be[q]);
+          if (WHOLE || q < n) z[e] = careful_z(x[e], mu[ONE ? 0 : q], prs[cl + q], pg[cl + q], k[q], be[q]);
         }
       }
     }
@@ -81,7 +90,7 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int q = 4 * h + e;
-          if (WHOLE || q < n) buf[pr * pitch + cl + q] = sx[e] * rstd[first_group + group_of(q)], buf[pr * pitch + a.W + cl + q] = s[e];
+          if (WHOLE || q < n) buf[pr * pitch + cl + q] = sx[e], buf[pr * pitch + a.W + cl + q] = s[e];
         }
       }
     }
@@ -90,18 +99,17 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
     __syncthreads();
     for (int c = t; c < 2 * a.W; c += blockDim.x) {
       const int second = c >= a.W, ch = second ? c - a.W : c;
-      if (ch < W) (second ? sum_g : sum_gx)[(long long)bc * 2 * a.C + c0 + ch] = csum[c];
+      if (ch >= W) continue;
+      const float v = second ? csum[c] : csum[c] * prs[ch];
+      csum[c] = v;
+      (second ? sum_g : sum_gx)[(long long)bc * 2 * a.C + c0 + ch] = v;
     }
     if (MODE == STATS) return;
+    __syncthreads();
   } else {
-    // the image's sums: the chunks' in order
     for (int c = t; c < 2 * a.W; c += blockDim.x) {
       const int second = c >= a.W, ch = second ? c - a.W : c;
-      if (ch >= W) continue;
-      const float *q = (second ? sum_g : sum_gx) + (long long)b * a.chunks * 2 * a.C + c0 + ch;
-      float s = 0.f;
-      for (int k = 0; k < a.chunks; ++k) s += q[2ll * k * a.C];
-      csum[c] = s;
+      if (ch < W) csum[c] = (second ? sum_g : sum_gx)[(long long)b * 2 * a.C + c0 + ch];
     }
     __syncthreads();
   }
@@ -111,21 +119,23 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
     for (int q = t >> 6; q < 2 * groups; q += blockDim.x >> 6) {
       const int second = q >= groups, g = second ? q - groups : q;
       float s = 0.f;
-      for (int c = g * a.Cg + lane; c < (g + 1) * a.Cg; c += 64) s = fmaf(csum[(second ? a.W : 0) + c], gamma[c0 + c], s);
+      for (int c = g * a.Cg + lane; c < (g + 1) * a.Cg; c += 64) s = fmaf(csum[(second ? a.W : 0) + c], pg[c], s);
       s = lanes_sum(s, 6);
       if (lane == 0) gsum[second * a.groups + g] = s * a.inv;
     }
   }
   __syncthreads();
-  float m1[PV], m2[PV];  // rs avg(g gamma), rs^2 avg(g gamma xh)
-#pragma unroll
-  for (int e = 0; e < PV; ++e) {
-    m1[e] = m2[e] = 0.f;
-    if (live) {
-      const float rs = rstd[first_group + group_of(e)];
-      m1[e] = rs * gsum[a.groups + group_of(e)], m2[e] = rs * rs * gsum[group_of(e)];
-    }
+  for (int c = t; c < W; c += blockDim.x) {  // rs avg(g gamma), rs^2 avg(g gamma xh)
+    const int q = a.div_cg.div(c);
+    const float r = prs[c];
+    pm[c] = r * gsum[a.groups + q], pk[c] = r * r * gsum[q];
   }
+  __syncthreads();
+  float m1[PV], m2[PV];
+  if constexpr (ONE)
+    m1[0] = pm[at], m2[0] = pk[at];
+  else
+    read_channels(pm + at, m1), read_channels(pk + at, m2);
 #pragma unroll
   for (int h = 0; h < VEC / 4; ++h) {
 #pragma unroll
@@ -144,41 +154,46 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
   }
 }
 
-// dgamma[c] and dbeta[c]: sums over the rows of part [rows][2][C], 16 columns by 64 lanes each, in a fixed order
+// Sums over `rows` rows of part [blockIdx.y][rows][2][C], by 16 columns to 64 lanes each, in a fixed order: chunks to images' sums,
+// images to dgamma and dbeta
 constexpr int RT = 1024;
-__global__ __launch_bounds__(RT) void gn_params_kernel(const float *__restrict__ part, int rows, int C,
-                                                       float *__restrict__ dgamma, float *__restrict__ dbeta) {
+__global__ __launch_bounds__(RT) void gn_rows_kernel(const float *__restrict__ part, int rows, int C, float *__restrict__ out0,
+                                                     float *__restrict__ out1, long long out_stride) {
   __shared__ float s[64][17];
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;  // columns of [2][C]
+  const float *const p = part + (long long)blockIdx.y * rows * 2 * C;
   float sum = 0.f;
   if (c < 2 * C) {
 #pragma unroll 4
-    for (int r = y; r < rows; r += 64) sum += part[(long long)r * 2 * C + c];
+    for (int r = y; r < rows; r += 64) sum += p[(long long)r * 2 * C + c];
   }
   s[y][x] = sum;
   __syncthreads();
   const int col = threadIdx.x >> 6, lane = threadIdx.x & 63, o = blockIdx.x * 16 + col;
-  sum = s[lane][col];
-#pragma unroll
-  for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
+  sum = lanes_sum(s[lane][col], 6);
   if (lane == 0 && o < 2 * C) {
     if (o < C)
-      dgamma[o] = sum;
+      out0[blockIdx.y * out_stride + o] = sum;
     else
-      dbeta[o - C] = sum;
+      out1[blockIdx.y * out_stride + o - C] = sum;
   }
+}
+void sum_rows(const float *part, int images, int rows, int C, float *out0, float *out1, hipStream_t st) {
+  hipLaunchKernelGGL(gn_rows_kernel, dim3((2 * C + 15) / 16, images), dim3(RT), 0, st, part, rows, C, out0, out1, 2ll * C);
 }
 
 template <typename T, bool WHOLE, bool ONE>
 hipError_t bwd_as(const GnShape &s, const GnPlan &p, const void *dy, const void *x, const float *gamma, const float *beta,
-                  const float *mean, const float *rstd, void *dx, float *sum_gx, float *sum_g, hipStream_t st) {
+                  const float *mean, const float *rstd, void *dx, float *part, float *sum_gx, float *sum_g, hipStream_t st) {
   constexpr int R = ONE ? 8 : 4;
   const GnArgs &a = p.a;
-  const size_t lds = 4 * ((size_t)a.px * (2 * a.W + 1) + 2 * a.W + 2 * a.groups);
+  const size_t lds = 4 * ((size_t)a.px * (2 * a.W + 1) + 5 * a.Wp + 2 * a.W + 2 * a.groups);
   const dim3 grid((unsigned)(p.slabs * s.B * a.chunks)), nt(p.nt);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)dy, (const T *)x, gamma, beta, mean, rstd, (T *)dx, sum_gx, sum_g); };
+  auto launch = [&](auto kernel, float *gx, float *g) { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)dy, (const T *)x, gamma, beta, mean, rstd, (T *)dx, gx, g); };
+  auto go = [&](auto kernel) { launch(kernel, sum_gx, sum_g); };
   if (p.split) {
-    go(gn_bwd_kernel<T, WHOLE, ONE, STATS, R, 1024>);
+    launch(gn_bwd_kernel<T, WHOLE, ONE, STATS, R, 1024>, part, part + s.C);
+    sum_rows(part, s.B, a.chunks, s.C, sum_gx, sum_g, st);
     go(gn_bwd_kernel<T, WHOLE, ONE, APPLY, R, 1024>);
   } else if (p.tiny) {
     go(gn_bwd_kernel<T, WHOLE, ONE, FUSED, 1, TINY>);
@@ -260,9 +275,9 @@ hipError_t launch_gn_bwd(const GnShape &s, const void *dy, const void *x, const 
   GnFew few;
   const bool is_few = gn_few(s, &few);
   const GnPlan p = gn_plan(s, true);
-  const int rows = s.B * (is_few ? 1 : p.a.chunks);
-  // one row of sums is the result
-  float *const sum_gx = rows == 1 ? dgamma : (float *)ws, *const sum_g = rows == 1 ? dbeta : (float *)ws + s.C;
+  // the images' sums [B][2][C], of which one image's are the result; the chunks' lie behind
+  float *const sums = (float *)ws, *const part = sums + (size_t)s.B * 2 * s.C;
+  float *const sum_gx = s.B == 1 ? dgamma : sums, *const sum_g = s.B == 1 ? dbeta : sums + s.C;
   hipError_t e;
   if (is_few) {
     e = s.dtype == NF_BF16  ? bwd_few_as<__bf16>(few, dy, x, gamma, beta, mean, rstd, dx, sum_gx, sum_g, st)
@@ -270,11 +285,11 @@ hipError_t launch_gn_bwd(const GnShape &s, const void *dy, const void *x, const 
                             : bwd_few_as<float>(few, dy, x, gamma, beta, mean, rstd, dx, sum_gx, sum_g, st);
   } else {
     e = by_type(s, p, [&](auto t, auto whole, auto one) {
-      return bwd_as<decltype(t), decltype(whole)::value, decltype(one)::value>(s, p, dy, x, gamma, beta, mean, rstd, dx, sum_gx, sum_g, st);
+      return bwd_as<decltype(t), decltype(whole)::value, decltype(one)::value>(s, p, dy, x, gamma, beta, mean, rstd, dx, part, sum_gx, sum_g, st);
     });
   }
-  if (e != hipSuccess || rows == 1) return e;
-  hipLaunchKernelGGL(gn_params_kernel, dim3((2 * s.C + 15) / 16), dim3(RT), 0, st, (const float *)ws, rows, s.C, dgamma, dbeta);
+  if (e != hipSuccess || s.B == 1) return e;
+  sum_rows(sums, 1, s.B, s.C, dgamma, dbeta, st);
   return hipGetLastError();
 }
 

@@ -171,7 +171,7 @@ def test_linear_gradient_against_differences():
 
 
 NORMS = [(1, 1, 1, 1), (1, 1, 8, 1), (2, 7, 3, 3), (3, 25, 12, 4), (8, 64, 16, 4), (2, 675, 72, 12), (5, 49, 100, 1), (1, 4096, 64, 32),
-         (2, 130, 1024, 32), (3, 33, 37, 37), (2, 1024, 130, 5), (1, 3000, 256, 1), (40, 4, 2056, 8), (2, 300, 515, 1)]
+         (2, 130, 1024, 32), (3, 33, 37, 37), (2, 1024, 130, 5), (1, 3000, 256, 1), (40, 4, 2056, 8), (2, 300, 515, 1), (2, 40, 4096, 2), (3, 1200, 24, 24), (1, 700, 1536, 3)]
 
 
 @pytest.mark.parametrize("t", TYPES)
