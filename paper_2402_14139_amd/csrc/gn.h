@@ -318,8 +318,7 @@ struct GnFew {
 constexpr long long FEW_ELEMENTS = 3 << 19;
 inline bool gn_few(const GnShape &s, GnFew *a) {
   a->HW = s.HW, a->C = s.C, a->G = s.G, a->Cg = s.C / s.G, a->act = s.act, a->eps = s.eps;
-  static const char *fw = getenv("NF_FEW");
-  if ((long long)s.B * s.HW * s.C > (fw ? atoll(fw) : FEW_ELEMENTS)) return false;
+  if ((long long)s.B * s.HW * s.C > FEW_ELEMENTS) return false;
   a->threads = 0;
   // few elements a thread, or the most threads
   for (int nt : {64, 256, 1024})

@@ -1,0 +1,129 @@
+"""A pointwise residual block over channels-last activations, trained from a quantised activation cache: group norm with its
+activation, a widening linear layer (activation, dropout), a linear layer back with dropout and the residual sum.  Host
+bookkeeping only: every arithmetic step but the example's squared-error loss is a call of include/nf.h.
+
+    h = act(GN(x));  a = D1(act(h W1^T + b1));  y = x + D2(a W2^T + b2)
+
+``python -m paper_2402_14139_amd.pointwise`` fits such a block to a map that another one computes, from an int8 cache.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+from . import binding as nf
+
+TYPES = {nf.NF_F32: torch.float32, nf.NF_BF16: torch.bfloat16, nf.NF_F16: torch.float16}
+
+
+class QuantisedCache:
+    """``capacity`` rows of n elements in 8 or 4 bits, with their labels (nf_qcache_write / nf_qcache_read)."""
+
+    def __init__(self, fmt, capacity: int, n: int, device="cuda"):
+        code, scale = nf.nf_qcache_row_bytes(fmt, n)
+        self.fmt, self.capacity, self.n = fmt, capacity, n
+        self.codes = torch.empty((capacity, code), dtype=torch.uint8, device=device)
+        self.scales = torch.empty((capacity, scale), dtype=torch.uint8, device=device)
+        self.labels = torch.zeros(capacity, dtype=torch.int32, device=device)
+
+    def write(self, dtype, first: int, x, labels):
+        nf.nf_qcache_write(self.fmt, dtype, self.codes, self.scales, self.labels, self.capacity, self.n, first, x.shape[0], x,
+                           labels)
+
+    def read(self, dtype, idx, x_out, labels_out):
+        nf.nf_qcache_read(self.fmt, dtype, self.codes, self.scales, self.labels, self.capacity, self.n, 0, idx, idx.shape[0],
+                          x_out, labels_out)
+
+
+class PointwiseBlock:
+    """Parameters (fp32; the weights also in the activations' type), gradients and buffers of one block for batches of up to
+    ``B`` maps of ``HW`` pixels and ``C`` channels, ``H`` hidden ones."""
+
+    def __init__(self, dtype, B: int, HW: int, C: int, H: int, groups: int, act=nf.NF_ACT_GELU, p: float = 0.0, seed: int = 0,
+                 device="cuda"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("PointwiseBlock needs a GPU: the library has no CPU path")
+        self.dtype, self.B, self.HW, self.C, self.H, self.p, self.seed = dtype, B, HW, C, H, p, seed
+        T = TYPES[dtype]
+        self.norm = nf.GroupNormDesc(dtype=dtype, C=C, G=groups, act=act, HW=HW, eps=1e-5)
+        self.up = nf.LinearDesc(dtype=dtype, K=C, N=H, act=act)
+        self.down = nf.LinearDesc(dtype=dtype, K=H, N=C, act=nf.NF_ACT_NONE)
+        g = torch.Generator().manual_seed(seed)
+        self.p32 = {"gamma": torch.ones(C), "beta": torch.zeros(C), "W1": torch.randn(H, C, generator=g) / math.sqrt(C),
+                    "b1": torch.zeros(H), "W2": torch.randn(C, H, generator=g) / math.sqrt(H), "b2": torch.zeros(C)}
+        self.p32 = {k: v.to(device) for k, v in self.p32.items()}
+        self.grad = {k: torch.zeros_like(v) for k, v in self.p32.items()}
+        self.w = {k: self.p32[k].to(T) for k in ("W1", "W2")}
+        M = B * HW
+        new = lambda *s, d=T: torch.empty(s, dtype=d, device=device)  # noqa: E731
+        self.h, self.z1, self.a, self.y = new(M, C), new(M, H), new(M, H), new(M, C)
+        self.dz2, self.da, self.dh, self.dx = new(M, C), new(M, H), new(M, C), new(M, C)
+        self.mean, self.rstd = new(B, groups, d=torch.float32), new(B, groups, d=torch.float32)
+        need = max(nf.nf_groupnorm_workspace_bytes(self.norm, B), *(nf.nf_linear_workspace_bytes(d, m) for d in (self.up, self.down)
+                                                                    for m in {M, HW}))
+        self.ws = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+
+    def _drop(self, which: int, step: int):
+        return nf.DropoutDesc(p=self.p, seed=self.seed * 2 + which, step=step) if self.p else None
+
+    def forward(self, x, step: int = 0, train: bool = True):
+        """y [B, HW, C] of x [B, HW, C]; ``step`` chooses the dropout masks."""
+        B = x.shape[0]
+        M, P = B * self.HW, self.p32
+        d1, d2 = (self._drop(0, step), self._drop(1, step)) if train else (None, None)
+        nf.nf_groupnorm_fwd(self.norm, B, x, P["gamma"], P["beta"], self.h, self.mean, self.rstd, self.ws)
+        nf.nf_linear_fwd(self.up, M, self.h, self.w["W1"], P["b1"], None, d1, self.a, self.z1, self.ws)
+        nf.nf_linear_fwd(self.down, M, self.a, self.w["W2"], P["b2"], x, d2, self.y, None, self.ws)
+        return self.y[:M].view(B, self.HW, self.C)
+
+    def backward(self, x, dy, step: int = 0):
+        """Gradients of the parameters (``grad``) and of x but for the residual's part, which is dy itself."""
+        B = x.shape[0]
+        M, P, g = B * self.HW, self.p32, self.grad
+        nf.nf_linear_bwd_epilogue(self.down, M, dy, None, self._drop(1, step), self.dz2, g["b2"], self.ws)
+        nf.nf_linear_bwd(self.down, M, self.dz2, self.a, self.w["W2"], self.da, g["W2"], self.ws)
+        nf.nf_linear_bwd_epilogue(self.up, M, self.da, self.z1, self._drop(0, step), self.a, g["b1"], self.ws)  # a is not needed again
+        nf.nf_linear_bwd(self.up, M, self.a, self.h, self.w["W1"], self.dh, g["W1"], self.ws)
+        nf.nf_groupnorm_bwd(self.norm, B, self.dh, x, P["gamma"], P["beta"], self.mean, self.rstd, self.dx, g["gamma"], g["beta"],
+                            self.ws)
+        return self.dx[:M].view(B, self.HW, self.C)
+
+    def sgd(self, lr: float):
+        names = list(self.p32)
+        nf.nf_sgd_update(lr, 0.0, [self.p32[k] for k in names], [self.grad[k] for k in names], None)
+        for k, v in self.w.items():
+            v.copy_(self.p32[k])
+
+
+def fit(dtype=nf.NF_BF16, fmt=nf.NF_Q_INT8, items=256, B=64, HW=64, C=64, H=128, groups=8, epochs=6, lr=0.5, p=0.0, seed=3):
+    """Trains a block towards another one's outputs on rows of a quantised cache; the mean loss of every epoch."""
+    T = TYPES[dtype]
+    teacher, block = (PointwiseBlock(dtype, B, HW, C, H, groups, p=q, seed=s) for s, q in ((seed, 0.0), (seed + 1, p)))
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    cache = QuantisedCache(fmt, items, HW * C)
+    labels = torch.arange(items, dtype=torch.int32, device="cuda")
+    for first in range(0, items, B):
+        rows = min(B, items - first)
+        x = torch.randn((rows, HW * C), generator=g, device="cuda").to(T)
+        cache.write(dtype, first, x, labels[first:first + rows].clone())
+    x, lab = torch.empty((B, HW, C), dtype=T, device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")
+    losses, step = [], 0
+    for _ in range(epochs):
+        order, total = torch.randperm(items, generator=g, device="cuda"), 0.0
+        for first in range(0, items - B + 1, B):
+            cache.read(dtype, order[first:first + B].clone(), x, lab)   # clone: 16-byte aligned
+            want = teacher.forward(x, train=False)
+            got = block.forward(x, step)
+            off = got.float() - want.float()
+            block.backward(x, (off * (2.0 / off.numel() * C)).to(T), step)
+            block.sgd(lr / C)
+            total += off.square().mean().item()
+            step += 1
+        losses.append(total / (items // B))
+    return losses
+
+
+if __name__ == "__main__":
+    for name, fmt in (("int8", nf.NF_Q_INT8), ("e4m3", nf.NF_Q_E4M3), ("e2m1", nf.NF_Q_E2M1)):
+        print(name, " ".join(f"{v:.4f}" for v in fit(fmt=fmt)))
