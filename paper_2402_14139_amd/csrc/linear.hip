@@ -742,10 +742,10 @@ __global__ __launch_bounds__(LT) void gradients_finish_kernel(FinishArgs x, Fini
 
 // ---- the epilogue's gradient ----
 // dz = act'(z) D(dy); a thread keeps 8 columns and walks the rows of its workgroup's part, so that the columns' sums stay in
-// registers.  part [row parts][groups * 8].  HBM-bound: 3 * sizeof(T) bytes an element.
+// registers.  part [row parts][ld], or db itself where there is one row part.  HBM-bound: 3 * sizeof(T) bytes an element.
 template <typename T>
 __global__ __launch_bounds__(LT) void linear_epilogue_kernel(long long M, int N, long long per, int tx, const T *__restrict__ dy, const T *__restrict__ z,
-                                                             Epilogue e, float *part) {
+                                                             Epilogue e, float *part, int ld) {
   __shared__ float sums[LT * 8];
   const int groups = (N + 7) / 8, ty = LT / tx;  // tx threads across, ty down
   const int x = threadIdx.x % tx, y = threadIdx.x / tx, g8 = blockIdx.x * tx + x, col = g8 * 8, n = N - col;
@@ -791,7 +791,7 @@ __global__ __launch_bounds__(LT) void linear_epilogue_kernel(long long M, int N,
     float t = 0.f;
     for (int q = 0; q < ty; ++q) t += sums[q * across + c];
     const int cc = blockIdx.x * across + c;
-    if (cc < groups * 8) part[(long long)blockIdx.y * groups * 8 + cc] = t;
+    if (cc < ld) part[(long long)blockIdx.y * ld + cc] = t;
   }
 }
 
@@ -1033,17 +1033,18 @@ hipError_t launch_linear_epilogue(const LinearCall &c, const void *dy, const voi
                                   float *db, void *ws, hipStream_t st) {
   const EpiPlan p = epi_plan(c.M, c.N);
   const Epilogue e = {nullptr, nullptr, nullptr, dz, drop, c.act};
-  float *part = db ? (float *)ws : nullptr;
+  // one row part's sums are db
+  const int ld = p.ny == 1 ? c.N : (c.N + 7) / 8 * 8;
+  float *part = !db ? nullptr : p.ny == 1 ? db : (float *)ws;
   const dim3 grid(p.nx, p.ny);
   if (c.dtype == NF_BF16)
-    hipLaunchKernelGGL((linear_epilogue_kernel<__bf16>), grid, dim3(LT), 0, st, c.M, c.N, p.per, p.tx, (const __bf16 *)dy, (const __bf16 *)z, e, part);
+    hipLaunchKernelGGL((linear_epilogue_kernel<__bf16>), grid, dim3(LT), 0, st, c.M, c.N, p.per, p.tx, (const __bf16 *)dy, (const __bf16 *)z, e, part, ld);
   else if (c.dtype == NF_F16)
-    hipLaunchKernelGGL((linear_epilogue_kernel<_Float16>), grid, dim3(LT), 0, st, c.M, c.N, p.per, p.tx, (const _Float16 *)dy, (const _Float16 *)z, e, part);
+    hipLaunchKernelGGL((linear_epilogue_kernel<_Float16>), grid, dim3(LT), 0, st, c.M, c.N, p.per, p.tx, (const _Float16 *)dy, (const _Float16 *)z, e, part, ld);
   else
-    hipLaunchKernelGGL((linear_epilogue_kernel<float>), grid, dim3(LT), 0, st, c.M, c.N, p.per, p.tx, (const float *)dy, (const float *)z, e, part);
+    hipLaunchKernelGGL((linear_epilogue_kernel<float>), grid, dim3(LT), 0, st, c.M, c.N, p.per, p.tx, (const float *)dy, (const float *)z, e, part, ld);
   hipError_t err = hipGetLastError();
-  if (err != hipSuccess || !db) return err;
-  const int ld = (c.N + 7) / 8 * 8;
+  if (err != hipSuccess || !db || p.ny == 1) return err;
   hipLaunchKernelGGL(column_sums_kernel, dim3((c.N + 15) / 16), dim3(CT), 0, st, part, p.ny, (long long)ld, c.N, db);
   return hipGetLastError();
 }

@@ -92,11 +92,12 @@ __device__ inline float recip(float v) {
 
 // The normal distribution's tail Q(|z|) = erfc(|z| / sqrt 2) / 2 and bell = e^(-z^2 / 2): Q = t bell P(t), t = 1 / (1 + c |z|),
 // P a minimax fit of Q / (t bell).  fp32: c = 0.45 / sqrt 2, degree 9, |z| up to 17 (relative error 1.6e-8, 1.2e-7 with its
-// evaluation; beyond 17 the bell is 0 in fp32).  16 bits: c = 0.3, degree 5, |z| up to 9 (2.1e-6; beyond, Q is below 1e-19).
-template <typename T>
+// evaluation; beyond 17 the bell is 0 in fp32).  Results of 16 bits: c = 0.3, degree 5, |z| up to 9 (2.1e-6; beyond, Q is below
+// 1e-19).  Slopes take the first form (FINE), since their sums are fp32 results.
+template <typename T, bool FINE>
 __device__ inline float normal_tail(float z, float &bell) {
-  if constexpr (sizeof(T) == 4) {
-    const float t = 1.f / fmaf(0.31819805153394639f, fabsf(z), 1.f);
+  if constexpr (sizeof(T) == 4 || FINE) {
+    const float t = recip<T>(fmaf(0.31819805153394639f, fabsf(z), 1.f));
     float P = -0.018216685f;
     P = fmaf(P, t, 0.082202805f);
     P = fmaf(P, t, -0.120414825f);
@@ -107,7 +108,7 @@ __device__ inline float normal_tail(float z, float &bell) {
     P = fmaf(P, t, 0.11324629f);
     P = fmaf(P, t, 0.127034275f);
     P = fmaf(P, t, 0.126938645f);
-    bell = expf(-0.5f * z * z);
+    bell = sizeof(T) == 4 ? expf(-0.5f * z * z) : __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
     return t * bell * P;
   } else {
     const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(z), 1.f));
@@ -136,7 +137,7 @@ __device__ inline void act_of(int act, float (&v)[N]) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {  // v Phi(v) = max(v, 0) - |v| Q(|v|); a NaN stays one through Q
       float bell;
-      const float q = normal_tail<T>(v[e], bell);
+      const float q = normal_tail<T, false>(v[e], bell);
       v[e] = fmaf(-fabsf(v[e]), q, fmaxf(v[e], 0.f));
     }
   }
@@ -157,7 +158,7 @@ __device__ inline void times_slope(int act, const float (&z)[N], float (&s)[N]) 
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       float bell;
-      const float q = normal_tail<T>(z[e], bell);
+      const float q = normal_tail<T, true>(z[e], bell);
       s[e] *= fmaf(z[e] * 0.39894228040143268f, bell, z[e] > 0.f ? 1.f - q : q);
     }
   }
