@@ -353,7 +353,8 @@ int32_t nf_dropout_fwd(const nf_dropout_desc *drop, int32_t dtype, int64_t rows,
 int32_t nf_dropout_bwd(const nf_dropout_desc *drop, int32_t dtype, int64_t rows, int64_t cols, const void *dy,
                        void *dx, void *stream);
 
-/* A layer of N filters on rows of K channels: x [M][K], W [N][K], y [M][N].  1 <= M, N, K, M < 2^31 - 512, K, N <= 2^20. */
+/* A layer of N filters on rows of K channels: x [M][K], W [N][K], y [M][N].  1 <= M, N, K, M < 2^31 - 512,
+ * K, N <= 2^20, and the tiles of 64 along the longest of M, K, N times those along max(K, N) stay below 2^23. */
 typedef struct {
   int32_t dtype, K, N, act;
 } nf_linear_desc;

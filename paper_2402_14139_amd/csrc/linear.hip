@@ -317,24 +317,38 @@ __device__ inline void gemm_tile(const GemmArgs &g, int id, char *lds) {
   const long long sa = AT ? STEP * g.lda : SB, sb = BT ? STEP * g.ldb : SB;
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 
-  uintx4 hold[A::PIECES + B::PIECES];  // !COPY only
-  // elements of a chunk that lie inside: the chunk's own terms or neighbours may end in its middle
-  auto edge16 = [&](const char *p, uint32_t off, int inside) -> uintx4 {
-    uintx4 v = {0, 0, 0, 0};
-    if (off == OUTSIDE) return v;
-    if (inside >= A::EPC) {
-      __builtin_memcpy(&v, p + off, 16);
-    } else {
-      T t[A::EPC];
+  // !COPY: through registers.  A chunk may begin at any element and end, as its row or the results do, in its middle: 16 bytes are read
+  // all the same, from the neighbours behind it or, at the operand's last element, from those before it, without a branch
+  // that would wait for them; they are shifted and cut when they go to LDS.
+  uintx4 hold[A::PIECES + B::PIECES];
+  int held[A::PIECES + B::PIECES];  // elements of it that lie inside, and from bit 8 on those read before it
+  auto read16 = [&](int q, const char *p, const char *end, uint32_t off, int inside) {  // operands of 16 bytes or more (gemm_short)
+    const int most = (int)min(end - p - 16, 0x7FFFFFF0ll), at = min((int)min(off, 0x7FFFFFFFu), most);
+    held[q] = off == OUTSIDE ? 0 : max(min(inside, A::EPC), 0) | ((int)off - at) / (int)sizeof(T) << 8;
+    __builtin_memcpy(&hold[q], p + at, 16);
+  };
+  auto cut = [&](int q) {
+    asm volatile("" : "+v"(hold[q])::"memory");
+    uintx4 v = hold[q];
+    for (int d = held[q] >> 8; d > 0; --d) {
+      if constexpr (sizeof(T) == 4)
+        v[0] = v[1], v[1] = v[2], v[2] = v[3];
+      else
+        v[0] = v[0] >> 16 | v[1] << 16, v[1] = v[1] >> 16 | v[2] << 16, v[2] = v[2] >> 16 | v[3] << 16, v[3] >>= 16;
+    }
+    const int n = held[q] & 255;
+    if (n < A::EPC) {
 #pragma unroll
-      for (int e = 0; e < A::EPC; ++e) t[e] = (T)0.f;
-#pragma unroll
-      for (int e = 0; e < A::EPC; ++e)
-        if (e < inside) t[e] = reinterpret_cast<const T *>(p + off)[e];
-      __builtin_memcpy(&v, t, 16);
+      for (int w = 0; w < 4; ++w) {
+        if constexpr (sizeof(T) == 4)
+          v[w] = n > w ? v[w] : 0u;
+        else
+          v[w] = n > 2 * w + 1 ? v[w] : n == 2 * w + 1 ? v[w] & 0xFFFFu : 0u;
+      }
     }
     return v;
   };
+  const char *const end_a = g.a + (AT ? g.L : g.R) * g.lda, *const end_b = g.b + (BT ? g.L : (long long)g.C) * g.ldb;
   auto fetch = [&](int s, int stage) {
     const bool last = s + 1 == steps;
     const char *qa = pa + s * sa, *qb = pb + s * sb;
@@ -351,22 +365,22 @@ __device__ inline void gemm_tile(const GemmArgs &g, int id, char *lds) {
       for (int q = 0; q < A::PIECES; ++q) {
         int row, chunk;
         A::place(q, wave, lane, row, chunk);
-        hold[q] = edge16(qa, last ? avl[q] : av[q], (AT ? (int)min(rows_left, 1ll << 30) : terms) - chunk * A::EPC);
+        read16(q, qa, end_a, last ? avl[q] : av[q], (AT ? (int)min(rows_left, 1ll << 30) : terms) - chunk * A::EPC);
       }
 #pragma unroll
       for (int q = 0; q < B::PIECES; ++q) {
         int row, chunk;
         B::place(q, wave, lane, row, chunk);
-        hold[A::PIECES + q] = edge16(qb, last ? bvl[q] : bv[q], (BT ? cols_left : terms) - chunk * B::EPC);
+        read16(A::PIECES + q, qb, end_b, last ? bvl[q] : bv[q], (BT ? cols_left : terms) - chunk * B::EPC);
       }
     }
   };
   auto put = [&](int stage) {
     char *to = lds + stage * STAGE + wave * 1024 + lane * 16;
 #pragma unroll
-    for (int q = 0; q < A::PIECES; ++q) *reinterpret_cast<uintx4 *>(to + q * 4096) = hold[q];
+    for (int q = 0; q < A::PIECES; ++q) *reinterpret_cast<uintx4 *>(to + q * 4096) = cut(q);
 #pragma unroll
-    for (int q = 0; q < B::PIECES; ++q) *reinterpret_cast<uintx4 *>(to + A::BYTES + q * 4096) = hold[A::PIECES + q];
+    for (int q = 0; q < B::PIECES; ++q) *reinterpret_cast<uintx4 *>(to + A::BYTES + q * 4096) = cut(A::PIECES + q);
   };
 
   const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
@@ -401,8 +415,10 @@ __device__ inline void gemm_tile(const GemmArgs &g, int id, char *lds) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = mfma<T>(fb[j], fa[i], acc[i][j]);
     }
-    if constexpr (!COPY)
-      if (s + 1 < steps) put(cur ^ 1);  // read last a step ago, behind the barrier above
+    if constexpr (!COPY) {
+      __builtin_amdgcn_sched_barrier(0);  // the reads are waited for here, not before the step's products
+      if (s + 1 < steps) put(cur ^ 1);    // read last a step ago, behind the barrier above
+    }
     wait_lds();
     barrier();
   }
@@ -681,6 +697,19 @@ __global__ __launch_bounds__(64 * NW) void linear_few_rows_kernel(GemmArgs g) {
   }
 }
 
+// Gradients with an operand of less than 16 bytes: sums of at most 7 terms, a thread each.  Strides in elements.
+template <typename T, typename OUT>
+__global__ __launch_bounds__(LT) void gemm_short_kernel(const T *__restrict__ a, long long ra, long long la, const T *__restrict__ b,
+                                                        long long cb, long long lb, OUT *__restrict__ out, long long R, int C, int L) {
+  const long long i = (long long)blockIdx.x * LT + threadIdx.x;
+  if (i >= R * C) return;
+  const long long r = i / C;
+  const int c = (int)(i - r * C);
+  float s = 0.f;
+  for (int l = 0; l < L; ++l) s = fmaf((float)a[r * ra + l * la], (float)b[c * cb + l * lb], s);
+  out[i] = (OUT)s;
+}
+
 // Sums of the splits in order, and what follows them.  OUT is the results' type; FWD: the forward's epilogue.  A thread takes 8
 // columns of a row; where there are few of those, `lanes` groups of a workgroup's threads share the splits of one.
 struct FinishArgs {
@@ -853,7 +882,7 @@ constexpr int FEW_ROWS = 0;
 Plan fwd_plan(long long M, int N, int K, int size) {
   Plan p = plan_of(M, N, K, size, K * size % 16 == 0);
   const long long t64 = ((M + 63) / 64) * ((N + 63) / 64);
-  if (M <= 32 || (t64 <= 64 && (long long)K * size <= 2048)) p.tile = FEW_ROWS, p.splits = 1, p.bytes = 0;
+  if (M <= 32 || (t64 <= 64 && (long long)K * size <= 2048) || (long long)N * K * size < 16) p.tile = FEW_ROWS, p.splits = 1, p.bytes = 0;
   return p;
 }
 
@@ -926,6 +955,9 @@ hipError_t fwd_as(const LinearCall &c, const void *x, const void *W, const float
   return hipGetLastError();
 }
 
+// whether an operand of a product, of a or b elements, is shorter than the 16 bytes that the tile kernel reads at a time
+inline bool gemm_short(long long a, long long b, int size) { return std::min(a, b) * size < 16; }
+
 // The workspace holds dx's splits, then dW's.  Products of up to TOGETHER tiles share a launch; larger ones, whose tails weigh
 // little, keep the L2s to themselves (16384x2048x2048: 325 us together, 309 apart).
 constexpr int TOGETHER = 1024;
@@ -934,6 +966,18 @@ hipError_t bwd_as(const LinearCall &c, const void *dz, const void *x, const void
                   hipStream_t st) {
   const long long ldn = (long long)c.N * sizeof(T), ldk = (long long)c.K * sizeof(T);
   const bool copy = ldn % 16 == 0 && ldk % 16 == 0;
+  auto blocks = [](long long n) { return dim3((unsigned)((n + LT - 1) / LT)); };
+  if (dx && gemm_short(c.M * c.N, (long long)c.N * c.K, sizeof(T))) {
+    hipLaunchKernelGGL((gemm_short_kernel<T, T>), blocks(c.M * c.K), dim3(LT), 0, st, (const T *)dz, (long long)c.N, 1ll, (const T *)W, 1ll,
+                       (long long)c.K, (T *)dx, c.M, c.K, c.N);
+    dx = nullptr;
+  }
+  if (dW && gemm_short(c.M * c.N, c.M * c.K, sizeof(T))) {
+    hipLaunchKernelGGL((gemm_short_kernel<T, float>), blocks((long long)c.N * c.K), dim3(LT), 0, st, (const T *)dz, 1ll, (long long)c.N,
+                       (const T *)x, 1ll, (long long)c.K, dW, (long long)c.N, c.K, (int)c.M);
+    dW = nullptr;
+  }
+  if (!dx && !dW) return hipGetLastError();
   const Plan px = plan_of(c.M, c.K, c.N, sizeof(T), copy), pw = plan_of(c.N, c.K, c.M, sizeof(T), copy);
   GemmArgs gx = {}, gw = {};
   gx.a = (const char *)dz, gx.b = (const char *)W, gx.lda = ldn, gx.ldb = ldk;

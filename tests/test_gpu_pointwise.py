@@ -71,7 +71,7 @@ def linear_case(t, M, K, N, act, p, res, z, seed=3):
         assert (got[keep == 0] == 0).all()
 
 
-SHAPES = [(1, 1, 1), (1, 2048, 40), (3, 5, 7), (2, 16, 129), (17, 33, 100), (65, 64, 72), (64, 2048, 64), (129, 100, 130), (300, 24, 8),
+SHAPES = [(1, 1, 1), (700, 1, 3), (5000, 2, 1), (3, 1, 900), (2, 700, 1), (1, 3, 4000), (1, 2048, 40), (3, 5, 7), (2, 16, 129), (17, 33, 100), (65, 64, 72), (64, 2048, 64), (129, 100, 130), (300, 24, 8),
           (200, 136, 264), (257, 1000, 65), (2100, 72, 1600)]
 
 
@@ -141,6 +141,22 @@ def test_linear_gradients(t, M, K, N):
     nf.nf_linear_bwd(d, M, dz, None, W, only_x.t, None, ws)
     nf.nf_linear_bwd(d, M, dz, x, None, None, only_w.t, ws)
     assert torch.equal(only_x.cpu(), dx.cpu()) and torch.equal(only_w.cpu(), dW.cpu())
+
+
+def test_linear_of_long_odd_rows():
+    """Rows of 0.7 MB that begin at any 4 bytes: the reads of a tile lie up to 90 MB apart."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    M, K, N = 130, 180001, 135
+    x, W = torch.randn(M, K, generator=g, device="cuda"), torch.randn(N, K, generator=g, device="cuda")
+    d = nf.LinearDesc(dtype=nf.NF_F32, K=K, N=N, act=0)
+    ws, y, dx = workspace(nf.nf_linear_workspace_bytes(d, M)), Out(M, N), Out(M, K)
+    nf.nf_linear_fwd(d, M, x, W, None, None, None, y.t, None, ws)
+    X, w = x.double(), W.double()
+    close("y", y.cpu(), (X @ w.t()).cpu(), ((K + 2) * SUM * (X.abs() @ w.t().abs())).cpu())
+    dz = randn(torch.Generator().manual_seed(6), M, N)
+    nf.nf_linear_bwd(d, M, dz, None, W, dx.t, None, ws)
+    D = dz.double()
+    close("dx", dx.cpu(), (D @ w).cpu(), ((N + 2) * SUM * (D.abs() @ w.abs())).cpu())
 
 
 def test_linear_gradient_against_differences():
