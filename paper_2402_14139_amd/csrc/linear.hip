@@ -851,24 +851,47 @@ struct Plan {
   size_t bytes;  // of the splits' sums
 };
 
+// What a product in tiles of 128 or 64 takes, its sum in `splits` parts, in us: the first copies and the results, then steps of 128
+// bytes.  With c workgroups on the busiest CU a step takes c times the CU's own time for it, or a single step's latency; parts are
+// written and read again (6.3 TB/s) in a launch of their own.  The figures are a fit to 900 runs of products from 300x300x4000
+// to 128x128x65536.  By them the choice is on average 1 % behind the fastest tiles and parts measured, at most 15 %; splitting until 512
+// workgroups run, whatever the parts weigh, was 30 % (16 bits) and 16 % behind (4096x1024x1024 bf16 26.6 us in 512 workgroups, 16.2 in 1024
+// of tiles of 64 without parts).
+struct TileTimes {
+  double first, latency, rate;
+};
+double product_time(long long tiles, long long steps, int splits, double results, bool large, int size, bool whole) {
+  constexpr TileTimes T16[2][2] = {{{5.5, 0.93, 0.39}, {8, 1.63, 1.0}}, {{5, 0.26, 0.19}, {8, 0.5, 0.4}}};
+  constexpr TileTimes T32[2][2] = {{{7.5, 1.17, 0.74}, {10, 2.9, 2.45}}, {{6, 0.63, 0.52}, {9, 2.0, 1.9}}};
+  const TileTimes &t = size == 2 ? T16[whole][large] : T32[whole][large];
+  const double each = (double)((steps + splits - 1) / splits), c = (double)((tiles * splits + 255) / 256);
+  return t.first + each * std::max(t.latency, t.rate * c) + (splits > 1 ? 2.5 + splits * results * 8 / 6.3e6 : 0.0);
+}
+
 // Tiles of 256 (16 bits, whole 16-byte rows) where their rounds over the 256 CUs take less time than those of two 128s to a CU:
 // 1.55 us a step of 128 bytes and 13 more a round against 0.95 and 7.5 (65536x512x512 54 and 61 us, 8192x1024x1024, 128 tiles, 47 and 26);
-// not where the sum must be split, whose parts are four times as large.  Tiles of 64 for small results.  Sums are split so that
-// about 512 workgroups run, at least 4 steps to a part.
+// not where the sum must be split, whose parts are four times as large.  Else the quickest of tiles of 128 or 64 and of 1 to 512 parts.
 Plan plan_of(long long R, int C, long long L, int size, bool whole) {
   const int step = 128 / size;
   const long long steps = (L + step - 1) / step;
   auto tiles = [&](int b) { return ((R + b - 1) / b) * ((C + b - 1) / b); };
   Plan p;
-  p.tile = tiles(128) * steps >= 2048 || tiles(128) >= 192 ? 128 : 64;
-  if (size == 2 && whole && tiles(WIDE) >= 128) {
-    const double wide = (double)((tiles(WIDE) + 255) / 256) * (1.55 * steps + 13), narrow = (double)((tiles(128) + 511) / 512) * (0.95 * steps + 7.5);
-    if (wide < narrow) p.tile = WIDE;
+  p.tile = 128, p.splits = 1;
+  bool wide = size == 2 && whole && tiles(WIDE) >= 128;
+  if (wide) wide = (double)((tiles(WIDE) + 255) / 256) * (1.55 * steps + 13) < (double)((tiles(128) + 511) / 512) * (0.95 * steps + 7.5);
+  if (wide) {
+    p.tile = WIDE;
+  } else {
+    double best = 1e300;
+    for (const int b : {128, 64}) {
+      const long long t = tiles(b);
+      for (int s = 1; s <= steps && (s == 1 || (s <= 512 && t * s <= 2048)); s += s < 4 ? 1 : (s & (s - 1)) ? s / 3 : s / 2) {
+        const double time = product_time(t, steps, s, (double)R * C, b == 128, size, whole);
+        if (time < best) best = time, p.tile = b, p.splits = s;
+      }
+    }
   }
-  const long long t = tiles(p.tile);
-  long long s = p.tile == WIDE ? 1 : std::min<long long>(512 / t, steps / 4);
-  if (s < 1) s = 1;
-  const long long each = (steps + s - 1) / s;
+  const long long each = (steps + p.splits - 1) / p.splits;
   p.splits = (int)((steps + each - 1) / each);
   p.per = each * step;
   p.bytes = p.splits > 1 ? (size_t)p.splits * R * ((C + 7) / 8 * 8) * 4 : 0;
@@ -877,7 +900,7 @@ Plan plan_of(long long R, int C, long long L, int size, bool whole) {
 
 // The forward: tiles, or few rows.  Few rows where there are up to 32 (1x2048x2048 bf16 4.4 us, tiles 7.1; 16 rows 6.7 and 8.2), and
 // for small products (256x512x256 5.7 and 7.3); from sums of 2 KB and more than 32 rows on, tiles that share x and W through LDS
-// (64x2048x2048 12.4 and 9.9).
+// (64x2048x2048 12.4 and 9.9).  And weights of less than the 16 bytes that the tile kernel reads at a time.
 constexpr int FEW_ROWS = 0;
 Plan fwd_plan(long long M, int N, int K, int size) {
   Plan p = plan_of(M, N, K, size, K * size % 16 == 0);
@@ -958,9 +981,7 @@ hipError_t fwd_as(const LinearCall &c, const void *x, const void *W, const float
 // whether an operand of a product, of a or b elements, is shorter than the 16 bytes that the tile kernel reads at a time
 inline bool gemm_short(long long a, long long b, int size) { return std::min(a, b) * size < 16; }
 
-// The workspace holds dx's splits, then dW's.  Products of up to TOGETHER tiles share a launch; larger ones, whose tails weigh
-// little, keep the L2s to themselves (16384x2048x2048: 325 us together, 309 apart).
-constexpr int TOGETHER = 1024;
+// The workspace holds dx's splits, then dW's.  Products in the same kind of tiles share a launch.
 template <typename T>
 hipError_t bwd_as(const LinearCall &c, const void *dz, const void *x, const void *W, void *dx, float *dW, void *ws,
                   hipStream_t st) {
@@ -987,7 +1008,7 @@ hipError_t bwd_as(const LinearCall &c, const void *dz, const void *x, const void
   gw.R = c.N, gw.C = c.K, gw.L = c.M, gw.e.out = dW;
   gw.part = pw.splits > 1 ? (float *)((char *)ws + px.bytes) : dW, gw.part_ld = pw.splits > 1 ? (c.K + 7) / 8 * 8 : c.K;
   const int nx = lay(px, gx), nw = lay(pw, gw);
-  if (dx && dW && px.tile != WIDE && pw.tile != WIDE && nx + nw <= TOGETHER) {
+  if (dx && dW && px.tile != WIDE && pw.tile != WIDE) {
     const dim3 grid((unsigned)((nx + 7) / 8 * 8 + nw));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(LT), 0, st, gx, gw); };
     auto sized = [&](auto cp) {
