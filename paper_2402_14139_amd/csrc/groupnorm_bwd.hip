@@ -5,7 +5,9 @@ namespace nf {
 namespace {
 
 // HBM-bound: 3 * sizeof(T) bytes an element.  sum_gx and sum_g, rows of 2 C floats: sums over pixels of g xh and g, of
-// every (image, chunk); APPLY reads those of the images.
+// every (image, chunk); APPLY reads those of the images.  64x1024x512 bf16 in 32 groups with SiLU 74.5 us, 2.7 TB/s: two rounds of
+// slabs that load, compute (36 vector instructions an element) and store in step; 33x675x72 fp16 11.9 us, the
+// latency of unaligned slabs.
 template <typename T, bool WHOLE, bool ONE, int MODE, int R, int NTMAX>
 __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__restrict__ dy, const T *__restrict__ x,
                                                        const float *__restrict__ gamma, const float *__restrict__ beta,
@@ -155,7 +157,7 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
 }
 
 // Sums over `rows` rows of part [blockIdx.y][rows][2][C], by 16 columns to 64 lanes each, in a fixed order: chunks to images' sums,
-// images to dgamma and dbeta
+// images to dgamma and dbeta.  A launch's latency: 3.8 us for 33 images of 72 channels, 5.2 for 64 of 512.
 constexpr int RT = 1024;
 __global__ __launch_bounds__(RT) void gn_rows_kernel(const float *__restrict__ part, int rows, int C, float *__restrict__ out0,
                                                      float *__restrict__ out1, long long out_stride) {

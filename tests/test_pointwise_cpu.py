@@ -21,7 +21,7 @@ def L():
 
 
 def test_philox_known_answers():
-    """The generator's published vectors (Random123), through both forms of the reference."""
+    """The generator's published vectors, through both forms of the reference."""
     assert ref.philox([0] * 4, [0, 0]) == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
     assert ref.philox([0xFFFFFFFF] * 4, [0xFFFFFFFF] * 2) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
     seed, step = 0x1234567890ABCDEF, 0xFEDCBA0987654321
