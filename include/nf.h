@@ -336,7 +336,8 @@ int32_t nf_select_exit(int32_t n_exits, const int64_t *n_correct, const int64_t 
  * inputs, but for dropout's y, which may be x or r (and dx, which may be dy).  Results do not depend on the order
  * in which workgroups run. */
 enum { NF_F32 = 0, NF_BF16 = 1, NF_F16 = 2 };
-/* relu: max(v, 0), its slope at 0 is 0; silu: v / (1 + e^-v); gelu: v Phi(v), Phi the normal distribution's. */
+/* relu: max(v, 0), its slope at 0 is 0; silu: v / (1 + e^-v); gelu: v Phi(v), Phi the normal distribution's.  At infinities they
+ * and their slopes are the limits (inf and 0, 1 and 0). */
 enum { NF_ACT_NONE = 0, NF_ACT_RELU = 1, NF_ACT_SILU = 2, NF_ACT_GELU = 3 };
 
 /* D: an element of a row-major matrix is dropped (0) where u < T = rint(65536 p), else scaled by

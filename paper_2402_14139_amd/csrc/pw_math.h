@@ -77,8 +77,8 @@ __device__ inline void unpack8(Raw8<T> r, float (&v)[8]) {
   for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
 }
 
-// e^v and 1/v: as accurate as fp32 for fp32 results; two instructions (relative error about 1e-6) where the result is
-// rounded to 16 bits, whose half step is 2^-11 or more
+// e^v and 1/v: as accurate as fp32 for fp32 results; two instructions and one (e^v off by up to (|v| + 1) 2^-23 of itself, 1/v by 2^-23) where
+// the result is rounded to 16 bits, whose half step is 2^-11 or more
 template <typename T>
 __device__ inline float exp_of(float v) {
   if constexpr (sizeof(T) == 4) return expf(v);
@@ -90,14 +90,14 @@ __device__ inline float recip(float v) {
   return __builtin_amdgcn_rcpf(v);
 }
 
-// The normal distribution's tail Q(|z|) = erfc(|z| / sqrt 2) / 2 and bell = e^(-z^2 / 2): Q = t bell P(t), t = 1 / (1 + c |z|),
-// P a minimax fit of Q / (t bell).  fp32: c = 0.45 / sqrt 2, degree 9, |z| up to 17 (relative error 1.6e-8, 1.2e-7 with its
+// The normal distribution's tail Q(|z|) = erfc(|z| / sqrt 2) / 2 in its factors: Q = t bell P(t), bell = e^(-z^2 / 2), t = 1 / (1 + c |z|),
+// P a minimax fit of Q / (t bell), which is returned.  fp32: c = 0.45 / sqrt 2, degree 9, |z| up to 17 (relative error 1.6e-8, 1.2e-7 with its
 // evaluation; beyond 17 the bell is 0 in fp32).  Results of 16 bits: c = 0.3, degree 5, |z| up to 9 (2.1e-6; beyond, Q is below
 // 1e-19).  Slopes take the first form (FINE), since their sums are fp32 results.
 template <typename T, bool FINE>
-__device__ inline float normal_tail(float z, float &bell) {
+__device__ inline float normal_tail(float z, float &bell, float &t) {
   if constexpr (sizeof(T) == 4 || FINE) {
-    const float t = recip<T>(fmaf(0.31819805153394639f, fabsf(z), 1.f));
+    t = recip<T>(fmaf(0.31819805153394639f, fabsf(z), 1.f));
     float P = -0.018216685f;
     P = fmaf(P, t, 0.082202805f);
     P = fmaf(P, t, -0.120414825f);
@@ -109,9 +109,9 @@ __device__ inline float normal_tail(float z, float &bell) {
     P = fmaf(P, t, 0.127034275f);
     P = fmaf(P, t, 0.126938645f);
     bell = sizeof(T) == 4 ? expf(-0.5f * z * z) : __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
-    return t * bell * P;
+    return P;
   } else {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(z), 1.f));
+    t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(z), 1.f));
     float P = -0.08183746907f;
     P = fmaf(P, t, 0.23058672288f);
     P = fmaf(P, t, -0.03403829558f);
@@ -119,9 +119,14 @@ __device__ inline float normal_tail(float z, float &bell) {
     P = fmaf(P, t, 0.11121039917f);
     P = fmaf(P, t, 0.12032773274f);
     bell = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
-    return t * bell * P;
+    return P;
   }
 }
+
+// v f where 0 times anything is 0: an activation's vanishing factor (q, the bell) holds against an infinite v or e^-v, so that
+// infinities give the limits (activations inf and 0, slopes 1 and 0) and not 0 * inf.  A NaN is one in both factors and stays.
+__device__ float mul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
+__device__ inline float fading(float v, float f) { return mul_legacy(v, f); }
 
 // The activation of N values, and its slope at them (times what s holds).  The activation is the same for a whole launch: one
 // branch to a vector, not to an element.
@@ -132,13 +137,13 @@ __device__ inline void act_of(int act, float (&v)[N]) {
     for (int e = 0; e < N; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];  // a NaN stays one
   } else if (act == NF_ACT_SILU) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] *= recip<T>(1.f + exp_of<T>(-v[e]));
+    for (int e = 0; e < N; ++e) v[e] = fading(v[e], recip<T>(1.f + exp_of<T>(-v[e])));
   } else if (act == NF_ACT_GELU) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {  // v Phi(v) = max(v, 0) - |v| Q(|v|); a NaN stays one through Q
-      float bell;
-      const float q = normal_tail<T, false>(v[e], bell);
-      v[e] = fmaf(-fabsf(v[e]), q, fmaxf(v[e], 0.f));
+      float bell, t;
+      const float P = normal_tail<T, false>(v[e], bell, t);
+      v[e] = fmaf(-fading(fabsf(v[e]), bell) * t, P, fmaxf(v[e], 0.f));
     }
   }
 }
@@ -150,16 +155,16 @@ __device__ inline void times_slope(int act, const float (&z)[N], float (&s)[N]) 
     for (int e = 0; e < N; ++e) s[e] = z[e] > 0.f ? s[e] : 0.f;
   } else if (act == NF_ACT_SILU) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {  // q + z q (1 - q)
-      const float q = recip<T>(1.f + exp_of<T>(-z[e])), zq = z[e] * q;
-      s[e] *= fmaf(-q, zq, q + zq);
+    for (int e = 0; e < N; ++e) {  // q + z q (1 - q), q = 1 / (1 + a), a = e^-z; 1 - q is a q, which keeps its digits where q is next to 1
+      const float a = exp_of<T>(-z[e]), q = recip<T>(1.f + a);
+      s[e] *= fmaf(fading(z[e], fading(a, q)), q, q);
     }
   } else if (act == NF_ACT_GELU) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      float bell;
-      const float q = normal_tail<T, true>(z[e], bell);
-      s[e] *= fmaf(z[e] * 0.39894228040143268f, bell, z[e] > 0.f ? 1.f - q : q);
+      float bell, t;
+      const float P = normal_tail<T, true>(z[e], bell, t), Q = t * bell * P;
+      s[e] *= fmaf(fading(z[e], bell), 0.39894228040143268f, z[e] > 0.f ? 1.f - Q : Q);
     }
   }
 }
