@@ -17,6 +17,12 @@ from . import binding as nf
 TYPES = {nf.NF_F32: torch.float32, nf.NF_BF16: torch.bfloat16, nf.NF_F16: torch.float16}
 
 
+def _check(name: str, t, T, device, rows: int, row: int):
+    """The kernels see addresses only: ``t`` has to hold ``rows`` dense rows of ``row`` elements of type ``T`` there."""
+    if t.device != device or t.dtype != T or not t.is_contiguous() or t.shape[:1] != (rows,) or t.numel() != rows * row:
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}; want {rows} dense rows of {row} {T} on {device}")
+
+
 class QuantisedCache:
     """``capacity`` rows of n elements in 8 or 4 bits, with their labels (nf_qcache_write / nf_qcache_read)."""
 
@@ -28,11 +34,17 @@ class QuantisedCache:
         self.labels = torch.zeros(capacity, dtype=torch.int32, device=device)
 
     def write(self, dtype, first: int, x, labels):
+        _check("x", x, TYPES[dtype], self.codes.device, x.shape[0], self.n)
+        _check("labels", labels, torch.int32, self.codes.device, x.shape[0], 1)
         nf.nf_qcache_write(self.fmt, dtype, self.codes, self.scales, self.labels, self.capacity, self.n, first, x.shape[0], x,
                            labels)
 
     def read(self, dtype, idx, x_out, labels_out):
-        nf.nf_qcache_read(self.fmt, dtype, self.codes, self.scales, self.labels, self.capacity, self.n, 0, idx, idx.shape[0],
+        B = idx.shape[0]
+        _check("idx", idx, torch.int64, self.codes.device, B, 1)
+        _check("x_out", x_out, TYPES[dtype], self.codes.device, B, self.n)
+        _check("labels_out", labels_out, torch.int32, self.codes.device, B, 1)
+        nf.nf_qcache_read(self.fmt, dtype, self.codes, self.scales, self.labels, self.capacity, self.n, 0, idx, B,
                           x_out, labels_out)
 
 
@@ -64,12 +76,18 @@ class PointwiseBlock:
                                                                     for m in {M, HW}))
         self.ws = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
 
+    def _maps(self, name: str, t, B: int):
+        if not 1 <= B <= self.B:
+            raise ValueError(f"{name}: a batch of {B}; this block's buffers hold 1 to {self.B}")
+        _check(name, t, TYPES[self.dtype], self.ws.device, B, self.HW * self.C)
+
     def _drop(self, which: int, step: int):
         return nf.DropoutDesc(p=self.p, seed=self.seed * 2 + which, step=step) if self.p else None
 
     def forward(self, x, step: int = 0, train: bool = True):
         """y [B, HW, C] of x [B, HW, C]; ``step`` chooses the dropout masks."""
         B = x.shape[0]
+        self._maps("x", x, B)
         M, P = B * self.HW, self.p32
         d1, d2 = (self._drop(0, step), self._drop(1, step)) if train else (None, None)
         nf.nf_groupnorm_fwd(self.norm, B, x, P["gamma"], P["beta"], self.h, self.mean, self.rstd, self.ws)
@@ -80,6 +98,8 @@ class PointwiseBlock:
     def backward(self, x, dy, step: int = 0):
         """Gradients of the parameters (``grad``) and of x but for the residual's part, which is dy itself."""
         B = x.shape[0]
+        self._maps("x", x, B)
+        self._maps("dy", dy, B)
         M, P, g = B * self.HW, self.p32, self.grad
         nf.nf_linear_bwd_epilogue(self.down, M, dy, None, self._drop(1, step), self.dz2, g["b2"], self.ws)
         nf.nf_linear_bwd(self.down, M, self.dz2, self.a, self.w["W2"], self.da, g["W2"], self.ws)

@@ -1,0 +1,73 @@
+"""The pointwise block and the quantised cache without a GPU: what they refuse before any kernel gets an address."""
+import pytest
+import torch
+
+from paper_2402_14139_amd import binding as nf
+from paper_2402_14139_amd import pointwise as pw
+
+BF16 = torch.bfloat16
+
+
+@pytest.fixture
+def no_kernels(monkeypatch):
+    def called(*a, **k):
+        raise AssertionError("a kernel would run")
+    for name in nf.EXPORTS:
+        if not name.endswith("_bytes"):
+            monkeypatch.setattr(nf, name, called, raising=False)
+
+
+def block(B=4, HW=6, C=8):
+    b = object.__new__(pw.PointwiseBlock)   # without the buffers, which need a GPU
+    b.dtype, b.B, b.HW, b.C, b.H, b.p, b.seed = nf.NF_BF16, B, HW, C, 16, 0.0, 0
+    b.p32, b.grad = {}, {}
+    b.ws = torch.empty(1, dtype=torch.uint8)
+    return b
+
+
+BAD = {"more maps than the buffers": torch.zeros(5, 6, 8, dtype=BF16), "no maps": torch.zeros(0, 6, 8, dtype=BF16),
+       "other type": torch.zeros(4, 6, 8), "strided": torch.zeros(4, 8, 6, dtype=BF16).transpose(1, 2),
+       "short rows": torch.zeros(4, 6, 7, dtype=BF16), "other device": torch.zeros(4, 6, 8, dtype=BF16, device="meta")}
+
+
+@pytest.mark.parametrize("why", BAD)
+def test_block_refuses(no_kernels, why):
+    b, good = block(), torch.zeros(4, 6, 8, dtype=BF16)
+    with pytest.raises(ValueError):
+        b.forward(BAD[why])
+    with pytest.raises(ValueError):
+        b.backward(BAD[why], good)
+    with pytest.raises(ValueError):
+        b.backward(good, BAD[why])
+
+
+def test_block_refuses_a_gradient_of_another_batch(no_kernels):
+    with pytest.raises(ValueError):
+        block().backward(torch.zeros(3, 6, 8, dtype=BF16), torch.zeros(2, 6, 8, dtype=BF16))
+
+
+def test_cache_refuses(no_kernels):
+    c = pw.QuantisedCache(nf.NF_Q_INT8, 10, 48, device="cpu")
+    x, lab, idx = torch.zeros(3, 48, dtype=BF16), torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)
+    for bad in (x.float(), torch.zeros(3, 47, dtype=BF16), x.t().contiguous().t(), x.to("meta")):
+        with pytest.raises(ValueError):
+            c.write(nf.NF_BF16, 0, bad, lab)
+        with pytest.raises(ValueError):
+            c.read(nf.NF_BF16, idx, bad, lab)
+    for bad in (lab[:2], lab.long(), torch.zeros(6, dtype=torch.int32)[::2], lab.to("meta")):
+        with pytest.raises(ValueError):
+            c.write(nf.NF_BF16, 0, x, bad)
+        with pytest.raises(ValueError):
+            c.read(nf.NF_BF16, idx, x, bad)
+    for bad in (idx.int(), torch.zeros(4, dtype=torch.int64), idx.to("meta")):
+        with pytest.raises(ValueError):
+            c.read(nf.NF_BF16, bad, x, lab)
+
+
+def test_good_arguments_reach_the_kernels(no_kernels):
+    c = pw.QuantisedCache(nf.NF_Q_INT8, 10, 48, device="cpu")
+    x, lab, idx = torch.zeros(3, 48, dtype=BF16), torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)
+    with pytest.raises(AssertionError):
+        c.write(nf.NF_BF16, 0, x.view(3, 6, 8), lab)
+    with pytest.raises(AssertionError):
+        c.read(nf.NF_BF16, idx, x, lab)
