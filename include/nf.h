@@ -359,7 +359,8 @@ int32_t nf_dropout_bwd(const nf_dropout_desc *drop, int32_t dtype, int64_t rows,
 typedef struct {
   int32_t dtype, K, N, act;
 } nf_linear_desc;
-/* Bytes of workspace that the three calls below want at M rows. */
+/* Bytes of workspace that the three calls below want at M rows.  They do not grow steadily with M: a sum is cut into other parts at
+ * other sizes, and fewer rows may want more.  A buffer for several M holds the largest of their sizes. */
 int32_t nf_linear_workspace_bytes(const nf_linear_desc *d, int64_t M, size_t *out);
 /* z = x W^T + b, y = r + D(act(z)).  b (fp32), r and drop may be NULL; z may be NULL (else it receives the sums before
  * the activation, rounded to the type, which the backward epilogue reads). */
@@ -381,6 +382,7 @@ typedef struct {
   int32_t dtype, C, G, act, HW;
   float eps;
 } nf_groupnorm_desc;
+/* Not steady in B, either: fewer images are cut into more chunks. */
 int32_t nf_groupnorm_workspace_bytes(const nf_groupnorm_desc *d, int32_t B, size_t *out);
 /* y = act((x - mean) rstd gamma + beta), rstd = (var + eps)^-1/2, var the mean square about the mean; mean and rstd
  * [B][G] are written too. */

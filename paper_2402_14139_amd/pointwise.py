@@ -48,6 +48,12 @@ class QuantisedCache:
                           x_out, labels_out)
 
 
+def workspace_bytes(norm, up, down, B: int) -> int:
+    """Bytes for batches of 1 to ``B`` maps: fewer rows are cut into other parts and may want more than many do."""
+    return max(max(nf.nf_groupnorm_workspace_bytes(norm, b), *(nf.nf_linear_workspace_bytes(d, b * norm.HW) for d in (up, down)))
+               for b in range(1, B + 1))
+
+
 class PointwiseBlock:
     """Parameters (fp32; the weights also in the activations' type), gradients and buffers of one block for batches of up to
     ``B`` maps of ``HW`` pixels and ``C`` channels, ``H`` hidden ones."""
@@ -72,9 +78,7 @@ class PointwiseBlock:
         self.h, self.z1, self.a, self.y = new(M, C), new(M, H), new(M, H), new(M, C)
         self.dz2, self.da, self.dh, self.dx = new(M, C), new(M, H), new(M, C), new(M, C)
         self.mean, self.rstd = new(B, groups, d=torch.float32), new(B, groups, d=torch.float32)
-        need = max(nf.nf_groupnorm_workspace_bytes(self.norm, B), *(nf.nf_linear_workspace_bytes(d, m) for d in (self.up, self.down)
-                                                                    for m in {M, HW}))
-        self.ws = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+        self.ws = torch.empty(max(workspace_bytes(self.norm, self.up, self.down, B), 1), dtype=torch.uint8, device=device)
 
     def _maps(self, name: str, t, B: int):
         if not 1 <= B <= self.B:

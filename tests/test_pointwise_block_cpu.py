@@ -71,3 +71,22 @@ def test_good_arguments_reach_the_kernels(no_kernels):
         c.write(nf.NF_BF16, 0, x.view(3, 6, 8), lab)
     with pytest.raises(AssertionError):
         c.read(nf.NF_BF16, idx, x, lab)
+
+
+@pytest.mark.parametrize("dtype", [nf.NF_F32, nf.NF_BF16, nf.NF_F16])
+@pytest.mark.parametrize("B,HW,C,H,G", [(64, 64, 64, 128, 8), (48, 100, 72, 100, 12), (9, 4096, 32, 64, 4), (33, 675, 72, 100, 12),
+                                        (100, 16, 512, 512, 32), (3, 1 << 16, 16, 32, 2)])
+def test_workspace_holds_every_batch(dtype, B, HW, C, H, G):
+    norm = nf.GroupNormDesc(dtype=dtype, C=C, G=G, act=0, HW=HW, eps=1e-5)
+    up, down = nf.LinearDesc(dtype=dtype, K=C, N=H, act=0), nf.LinearDesc(dtype=dtype, K=H, N=C, act=0)
+    have = pw.workspace_bytes(norm, up, down, B)
+    need = [max(nf.nf_groupnorm_workspace_bytes(norm, b), nf.nf_linear_workspace_bytes(up, b * HW), nf.nf_linear_workspace_bytes(down, b * HW))
+            for b in range(1, B + 1)]
+    assert have == max(need)
+
+
+def test_a_smaller_batch_may_want_more():
+    """What the sizing is for: 48 maps of 64 pixels want more than 64 and more than one."""
+    up = nf.LinearDesc(dtype=nf.NF_BF16, K=64, N=128, act=0)
+    need = {b: nf.nf_linear_workspace_bytes(up, b * 64) for b in (1, 48, 64)}
+    assert need[48] > max(need[1], need[64])
