@@ -362,6 +362,8 @@ typedef struct {
 /* Bytes of workspace that the three calls below want at M rows.  They do not grow steadily with M: a sum is cut into other parts at
  * other sizes, and fewer rows may want more.  A buffer for several M holds the largest of their sizes. */
 int32_t nf_linear_workspace_bytes(const nf_linear_desc *d, int64_t M, size_t *out);
+/* What nf_linear_fwd alone wants: at most that, and often nothing (65536 rows of 512 to 512: 0 and 33.6 MB). */
+int32_t nf_linear_fwd_workspace_bytes(const nf_linear_desc *d, int64_t M, size_t *out);
 /* z = x W^T + b, y = r + D(act(z)).  b (fp32), r and drop may be NULL; z may be NULL (else it receives the sums before
  * the activation, rounded to the type, which the backward epilogue reads). */
 int32_t nf_linear_fwd(const nf_linear_desc *d, int64_t M, const void *x, const void *W, const float *b, const void *r,
@@ -384,6 +386,8 @@ typedef struct {
 } nf_groupnorm_desc;
 /* Not steady in B, either: fewer images are cut into more chunks. */
 int32_t nf_groupnorm_workspace_bytes(const nf_groupnorm_desc *d, int32_t B, size_t *out);
+/* what nf_groupnorm_fwd alone wants */
+int32_t nf_groupnorm_fwd_workspace_bytes(const nf_groupnorm_desc *d, int32_t B, size_t *out);
 /* y = act((x - mean) rstd gamma + beta), rstd = (var + eps)^-1/2, var the mean square about the mean; mean and rstd
  * [B][G] are written too. */
 int32_t nf_groupnorm_fwd(const nf_groupnorm_desc *d, int32_t B, const void *x, const float *gamma, const float *beta,

@@ -27,8 +27,8 @@ EXPORTS = ("nf_strerror", "nf_layer_out_dims", "nf_workspace_bytes", "nf_layer_f
            "nf_profile_layer", "nf_partition", "nf_aux_predict", "nf_block_evaluate", "nf_select_exit",
            "nf_device_info", "nf_local_step_static", "nf_contraction", "nf_block_graph_create",
            "nf_block_graph_launch", "nf_block_graph_destroy", "nf_dropout_fwd", "nf_dropout_bwd",
-           "nf_linear_workspace_bytes", "nf_linear_fwd", "nf_linear_bwd_epilogue", "nf_linear_bwd",
-           "nf_groupnorm_workspace_bytes", "nf_groupnorm_fwd", "nf_groupnorm_bwd", "nf_qcache_row_bytes",
+           "nf_linear_workspace_bytes", "nf_linear_fwd_workspace_bytes", "nf_linear_fwd", "nf_linear_bwd_epilogue", "nf_linear_bwd",
+           "nf_groupnorm_workspace_bytes", "nf_groupnorm_fwd_workspace_bytes", "nf_groupnorm_fwd", "nf_groupnorm_bwd", "nf_qcache_row_bytes",
            "nf_qcache_write", "nf_qcache_read")
 
 NF_WS_AUX_ACT, NF_WS_POOL_ARG, NF_WS_HEAD_ARG = 0, 1, 2
@@ -174,10 +174,12 @@ def lib():
         L.nf_dropout_fwd.argtypes = [C.POINTER(DropoutDesc), i32, i64, i64, ptr, ptr, ptr, ptr]
         L.nf_dropout_bwd.argtypes = [C.POINTER(DropoutDesc), i32, i64, i64, ptr, ptr, ptr]
         L.nf_linear_workspace_bytes.argtypes = [C.POINTER(LinearDesc), i64, C.POINTER(size)]
+        L.nf_linear_fwd_workspace_bytes.argtypes = L.nf_linear_workspace_bytes.argtypes
         L.nf_linear_fwd.argtypes = [C.POINTER(LinearDesc), i64, ptr, ptr, ptr, ptr, C.POINTER(DropoutDesc), ptr, ptr, ptr, size, ptr]
         L.nf_linear_bwd_epilogue.argtypes = [C.POINTER(LinearDesc), i64, ptr, ptr, C.POINTER(DropoutDesc), ptr, ptr, ptr, size, ptr]
         L.nf_linear_bwd.argtypes = [C.POINTER(LinearDesc), i64, ptr, ptr, ptr, ptr, ptr, ptr, size, ptr]
         L.nf_groupnorm_workspace_bytes.argtypes = [C.POINTER(GroupNormDesc), i32, C.POINTER(size)]
+        L.nf_groupnorm_fwd_workspace_bytes.argtypes = L.nf_groupnorm_workspace_bytes.argtypes
         L.nf_groupnorm_fwd.argtypes = [C.POINTER(GroupNormDesc), i32, ptr, ptr, ptr, ptr, ptr, ptr, ptr, size, ptr]
         L.nf_groupnorm_bwd.argtypes = [C.POINTER(GroupNormDesc), i32] + [ptr] * 10 + [size, ptr]
         L.nf_qcache_row_bytes.argtypes = [i32, i64, C.POINTER(size), C.POINTER(size)]
@@ -492,6 +494,12 @@ def nf_linear_workspace_bytes(d: LinearDesc, M: int) -> int:
     return int(out.value)
 
 
+def nf_linear_fwd_workspace_bytes(d: LinearDesc, M: int) -> int:
+    out = C.c_size_t()
+    _check(lib().nf_linear_fwd_workspace_bytes(_ref(d), M, C.byref(out)), "nf_linear_fwd_workspace_bytes")
+    return int(out.value)
+
+
 def nf_linear_fwd(d: LinearDesc, M, x, W, b, r, drop, y, z, ws, stream=None):
     wp, wn = _ws(ws)
     _check(lib().nf_linear_fwd(_ref(d), M, _ptr(x), _ptr(W), _ptr(b), _ptr(r), _ref(drop), _ptr(y), _ptr(z), wp, wn,
@@ -513,6 +521,12 @@ def nf_linear_bwd(d: LinearDesc, M, dz, x, W, dx, dW, ws, stream=None):
 def nf_groupnorm_workspace_bytes(d: GroupNormDesc, B: int) -> int:
     out = C.c_size_t()
     _check(lib().nf_groupnorm_workspace_bytes(_ref(d), B, C.byref(out)), "nf_groupnorm_workspace_bytes")
+    return int(out.value)
+
+
+def nf_groupnorm_fwd_workspace_bytes(d: GroupNormDesc, B: int) -> int:
+    out = C.c_size_t()
+    _check(lib().nf_groupnorm_fwd_workspace_bytes(_ref(d), B, C.byref(out)), "nf_groupnorm_fwd_workspace_bytes")
     return int(out.value)
 
 

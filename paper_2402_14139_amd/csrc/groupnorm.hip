@@ -192,9 +192,14 @@ hipError_t fwd_few_as(const GnFew &a, const void *x, const float *gamma, const f
 
 }  // namespace
 
+size_t gn_fwd_workspace_bytes(const GnShape &s) {
+  const GnPlan p = gn_plan(s, false);
+  return p.split ? (size_t)s.B * p.a.chunks * 2 * s.G * 4 : 0;
+}
+
 size_t gn_workspace_bytes(const GnShape &s) {
-  const GnPlan f = gn_plan(s, false), b = gn_plan(s, true);
-  return std::max((size_t)s.B * (1 + (b.split ? b.a.chunks : 0)) * 2 * s.C * 4, f.split ? (size_t)s.B * f.a.chunks * 2 * s.G * 4 : 0);
+  const GnPlan b = gn_plan(s, true);
+  return std::max((size_t)s.B * (1 + (b.split ? b.a.chunks : 0)) * 2 * s.C * 4, gn_fwd_workspace_bytes(s));
 }
 
 hipError_t launch_gn_fwd(const GnShape &s, const void *x, const float *gamma, const float *beta, void *y, float *mean,

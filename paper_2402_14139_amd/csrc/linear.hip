@@ -1077,10 +1077,12 @@ EpiPlan epi_plan(long long M, int N) {
 
 }  // namespace
 
+size_t linear_fwd_workspace_bytes(const LinearCall &c) { return fwd_plan(c.M, c.N, c.K, c.dtype == NF_F32 ? 4 : 2).bytes; }
+
 size_t linear_workspace_bytes(const LinearCall &c) {
   const int size = c.dtype == NF_F32 ? 4 : 2;
   const EpiPlan e = epi_plan(c.M, c.N);
-  const size_t fwd = fwd_plan(c.M, c.N, c.K, size).bytes;
+  const size_t fwd = linear_fwd_workspace_bytes(c);
   const bool whole = c.N * size % 16 == 0 && c.K * size % 16 == 0;
   const size_t bwd = plan_of(c.M, c.K, c.N, size, whole).bytes + plan_of(c.N, c.K, c.M, size, whole).bytes;
   return std::max(std::max(fwd, bwd), (size_t)e.ny * ((c.N + 7) / 8) * 32);

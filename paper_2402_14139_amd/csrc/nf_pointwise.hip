@@ -110,6 +110,15 @@ int32_t nf_linear_workspace_bytes(const nf_linear_desc *d, int64_t M, size_t *ou
   return NF_OK;
 }
 
+int32_t nf_linear_fwd_workspace_bytes(const nf_linear_desc *d, int64_t M, size_t *out) {
+  LinearCall c;
+  const int32_t rc = check_linear(d, M, &c);
+  if (rc) return rc;
+  if (!out) return NF_ERR_NULL;
+  *out = linear_fwd_workspace_bytes(c);
+  return NF_OK;
+}
+
 int32_t nf_linear_fwd(const nf_linear_desc *d, int64_t M, const void *x, const void *W, const float *b, const void *r,
                       const nf_dropout_desc *drop, void *y, void *z, void *ws, size_t ws_bytes, void *stream) {
   LinearCall c;
@@ -118,7 +127,7 @@ int32_t nf_linear_fwd(const nf_linear_desc *d, int64_t M, const void *x, const v
   if (!x || !W || !y) return NF_ERR_NULL;
   if (drop && (rc = check_drop(drop))) return rc;
   if (!all_aligned16(x, W, b, r, y, z)) return NF_ERR_BAD_DESC;
-  if ((rc = check_ws(ws, ws_bytes, linear_workspace_bytes(c)))) return rc;
+  if ((rc = check_ws(ws, ws_bytes, linear_fwd_workspace_bytes(c)))) return rc;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const double m = (double)M, mn = m * c.N;
   NF_RUN(st, "linear_fwd", 2.0 * mn * c.K, size_of(c.dtype) * (m * c.K + (double)c.N * c.K + mn * (1 + (r != nullptr) + (z != nullptr))),
@@ -167,6 +176,15 @@ int32_t nf_groupnorm_workspace_bytes(const nf_groupnorm_desc *d, int32_t B, size
   return NF_OK;
 }
 
+int32_t nf_groupnorm_fwd_workspace_bytes(const nf_groupnorm_desc *d, int32_t B, size_t *out) {
+  GnShape s;
+  const int32_t rc = check_groupnorm(d, B, &s);
+  if (rc) return rc;
+  if (!out) return NF_ERR_NULL;
+  *out = gn_fwd_workspace_bytes(s);
+  return NF_OK;
+}
+
 int32_t nf_groupnorm_fwd(const nf_groupnorm_desc *d, int32_t B, const void *x, const float *gamma, const float *beta,
                          void *y, float *mean, float *rstd, void *ws, size_t ws_bytes, void *stream) {
   GnShape s;
@@ -174,7 +192,7 @@ int32_t nf_groupnorm_fwd(const nf_groupnorm_desc *d, int32_t B, const void *x, c
   if (rc) return rc;
   if (!x || !gamma || !beta || !y || !mean || !rstd) return NF_ERR_NULL;
   if (!all_aligned16(x, gamma, beta, y, mean, rstd)) return NF_ERR_BAD_DESC;
-  if ((rc = check_ws(ws, ws_bytes, gn_workspace_bytes(s)))) return rc;
+  if ((rc = check_ws(ws, ws_bytes, gn_fwd_workspace_bytes(s)))) return rc;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   NF_RUN(st, "groupnorm_fwd", 0.0, 2.0 * size_of(s.dtype) * B * s.HW * s.C,
          launch_gn_fwd(s, x, gamma, beta, y, mean, rstd, ws, st));

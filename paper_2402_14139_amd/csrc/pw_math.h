@@ -223,6 +223,7 @@ struct GnShape {
   float eps;
 };
 size_t gn_workspace_bytes(const GnShape &s);
+size_t gn_fwd_workspace_bytes(const GnShape &s);
 hipError_t launch_gn_fwd(const GnShape &s, const void *x, const float *gamma, const float *beta, void *y, float *mean,
                          float *rstd, void *ws, hipStream_t st);
 hipError_t launch_gn_bwd(const GnShape &s, const void *dy, const void *x, const float *gamma, const float *beta,
@@ -235,6 +236,7 @@ struct LinearCall {
   int K, N;
 };
 size_t linear_workspace_bytes(const LinearCall &c);
+size_t linear_fwd_workspace_bytes(const LinearCall &c);
 hipError_t launch_linear_fwd(const LinearCall &c, const void *x, const void *W, const float *b, const void *r,
                              const DropArgs &drop, void *y, void *z, void *ws, hipStream_t st);
 hipError_t launch_linear_epilogue(const LinearCall &c, const void *dy, const void *z, const DropArgs &drop, void *dz,
