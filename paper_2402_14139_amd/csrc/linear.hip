@@ -616,13 +616,17 @@ __global__ __launch_bounds__(LT) void gemm_gradients_kernel(GemmArgs x, GemmArgs
 // need not follow the MFMA's term order (any order that x and W share will do): the four lanes of a row take 128 neighbouring bytes.
 // Up to 8 rows (HALVES): the MFMA's 16 x 16 results hold 8 columns of W's first half of terms by x's, and 8 of the second by the
 // second, so that twice as many workgroups share W.  Latency-bound; reads of W bound it from some MB on.
+// Weights of a few elements (fwd_plan) come here with any number of rows: a grid's second axis ends at 65535, so 2^FEW_DOWN
+// workgroups lie along it and the rest along the third.
+constexpr int FEW_DOWN = 15;
 template <typename T, int MT, int NW, bool HALVES, bool ALIGNED>
 __global__ __launch_bounds__(64 * NW) void linear_few_rows_kernel(GemmArgs g) {
   constexpr int EPC = 16 / sizeof(T), ROWS = HALVES ? 8 : 16 * MT, COLS = HALVES ? 8 : 16;
   __shared__ floatx4 lds[NW * MT * 64];  // [wave][row of 16][4 chunks of 4 columns], chunk c at c ^ (row & 3)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
   const int c0 = blockIdx.x * COLS;
-  const long long r0 = (long long)blockIdx.y * ROWS;
+  const long long r0 = (long long)(blockIdx.z << FEW_DOWN | blockIdx.y) * ROWS;
+  if (r0 >= g.R) return;
   const int K = (int)g.L, all = (K * (int)sizeof(T) + 127) / 128, steps = HALVES ? (all + 1) / 2 : all;
   const int own = HALVES ? i & 7 : i, first = HALVES && i >= 8 ? steps * 8 : 0;  // first chunk
   const char *const w = g.b + min(c0 + own, g.C - 1) * g.ldb;  // rows beyond the last read it again; their results are not used
@@ -941,7 +945,8 @@ void go_wide(F go) {
 template <typename T, int MT, int NW, bool HALVES>
 hipError_t few_rows_as(const GemmArgs &g, hipStream_t st) {
   constexpr int ROWS = HALVES ? 8 : 16 * MT, COLS = HALVES ? 8 : 16;
-  const dim3 grid((g.C + COLS - 1) / COLS, (unsigned)((g.R + ROWS - 1) / ROWS));
+  const unsigned down = (unsigned)((g.R + ROWS - 1) / ROWS);
+  const dim3 grid((g.C + COLS - 1) / COLS, std::min(down, 1u << FEW_DOWN), (down + (1u << FEW_DOWN) - 1) >> FEW_DOWN);
   if (g.lda % 16 == 0)
     hipLaunchKernelGGL((linear_few_rows_kernel<T, MT, NW, HALVES, true>), grid, dim3(64 * NW), 0, st, g);
   else
