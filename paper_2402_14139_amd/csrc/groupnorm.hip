@@ -18,7 +18,7 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
   float *const buf = gr + a.groups, *const csum = buf + a.px * (a.W | 1);
   const int t = threadIdx.x;
   const int slabs = a.div_slabs.d;
-  const int id = xcd_run(blockIdx.x, gridDim.x), bc = a.div_slabs.div(id), slab = id - bc * slabs;
+  const int id = xcd_run(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y), bc = a.div_slabs.div(id), slab = id - bc * slabs;
   const int b = MODE == FUSED ? bc : (int)a.div_chunks.div(bc), chunk = MODE == FUSED ? 0 : bc - b * a.chunks;
   const int c0 = slab * a.W, W = min(a.W, a.C - c0), groups = W == a.W ? a.groups : (int)a.div_cg.div(W);  // of this slab
   const int p0 = chunk * a.per, p1 = min(a.HW, p0 + a.per);
@@ -128,7 +128,7 @@ hipError_t fwd_as(const GnShape &s, const GnPlan &p, const void *x, const float 
                   float *mean, float *rstd, float *part, hipStream_t st) {
   const GnArgs &a = p.a;
   const size_t lds = 4 * (size_t)(3 * a.Wp + 2 * a.groups + matrix_floats(a, Vec<T>::N, ONE));
-  const dim3 grid((unsigned)(p.slabs * s.B * a.chunks)), nt(p.nt);
+  const dim3 grid(p.slabs * a.chunks, s.B), nt(p.nt);  // a grid's axis ends at 2^32 threads
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)x, gamma, beta, (T *)y, mean, rstd, part); };
   if (p.split) {
     go(gn_fwd_kernel<T, WHOLE, ONE, STATS, 8, 1024>);

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__rest
   float *const csum = pg + a.Wp, *const gsum = csum + 2 * a.W, *const buf = gsum + 2 * a.groups;
   const int t = threadIdx.x;
   const int slabs = a.div_slabs.d;
-  const int id = xcd_run(blockIdx.x, gridDim.x), bc = a.div_slabs.div(id), slab = id - bc * slabs;
+  const int id = xcd_run(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y), bc = a.div_slabs.div(id), slab = id - bc * slabs;
   const int b = MODE == FUSED ? bc : (int)a.div_chunks.div(bc), chunk = MODE == FUSED ? 0 : bc - b * a.chunks;
   const int c0 = slab * a.W, W = min(a.W, a.C - c0), groups = W == a.W ? a.groups : (int)a.div_cg.div(W);  // of this slab
   const int p0 = chunk * a.per, p1 = min(a.HW, p0 + a.per);
@@ -190,7 +190,7 @@ hipError_t bwd_as(const GnShape &s, const GnPlan &p, const void *dy, const void 
   constexpr int R = ONE ? 8 : 4;
   const GnArgs &a = p.a;
   const size_t lds = 4 * ((size_t)a.px * (2 * a.W + 1) + 5 * a.Wp + 2 * a.W + 2 * a.groups);
-  const dim3 grid((unsigned)(p.slabs * s.B * a.chunks)), nt(p.nt);
+  const dim3 grid(p.slabs * a.chunks, s.B), nt(p.nt);  // a grid's axis ends at 2^32 threads
   auto launch = [&](auto kernel, float *gx, float *g) { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)dy, (const T *)x, gamma, beta, mean, rstd, (T *)dx, gx, g); };
   auto go = [&](auto kernel) { launch(kernel, sum_gx, sum_g); };
   if (p.split) {
