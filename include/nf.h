@@ -447,7 +447,7 @@ int32_t nf_partition(int32_t n_layers, const nf_linear_model *R, double M, int32
  * that blocks the host), and returns one record per kernel: launches, summed duration (ms),
  * summed algorithmic FLOPs and bytes.  Records are sorted by duration, at most `cap` are
  * written, *n receives the number of distinct kernels.  Kernels that a call puts into one launch (the two
- * weight gradients of small steps) are launched and recorded one by one after nf_prof_begin;
+ * weight gradients of small steps, both gradients of a linear layer) are launched and recorded one by one after nf_prof_begin;
  * nf_prof_begin_as_run records the launches that a call makes without a measurement, such a one under
  * a name of its own.  Process-wide state (one recording at a time;
  * the record list is guarded by a mutex so that launches from several host threads may be recorded),

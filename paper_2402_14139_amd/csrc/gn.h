@@ -11,6 +11,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "nf_enqueue.h"
 #include "pw_math.h"
 
 namespace nf {
@@ -276,6 +277,14 @@ GnPlan gn_plan(const GnShape &s, bool backward) {
   return p;
 }
 
+// names of the slab kernels: a group to a vector, several, rows of any alignment
+enum { TINY_SLAB, SMALL_SLAB, SLAB, SLAB_STATS, SLAB_APPLY };
+using SlabNames = const char *const[5][3];
+template <typename T>
+double gn_bytes(const GnShape &s, double passes) {  // passes: tensors read and written
+  return passes * sizeof(T) * s.B * s.HW * s.C;
+}
+
 template <typename T, typename F>
 hipError_t by_rows(const GnPlan &p, F run) {
   if (p.one) return run((T)0.f, std::true_type(), std::true_type());
@@ -335,17 +344,20 @@ inline bool gn_few(const GnShape &s, GnFew *a) {
   a->div_cg = FastDiv(a->Cg), a->div_g = FastDiv(s.G), a->div_px = FastDiv(a->px);
   return true;
 }
-// (threads of a workgroup, threads of a group, elements of a thread)
+// run(threads of a group, elements of a thread, workgroups, their threads), recorded under one of the names
 template <typename F>
-void gn_few_variant(const GnFew &a, F run) {
-  if (a.threads == 64)
-    run(std::integral_constant<int, 64>(), std::integral_constant<int, 4>(), dim3((a.units + 3) / 4), dim3(256));
-  else if (a.threads == 256)
-    run(std::integral_constant<int, 256>(), std::integral_constant<int, 4>(), dim3(a.units), dim3(256));
-  else if (a.HW <= 4 * a.px)
-    run(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>(), dim3(a.units), dim3(1024));
-  else
-    run(std::integral_constant<int, 1024>(), std::integral_constant<int, FEW_R>(), dim3(a.units), dim3(1024));
+hipError_t gn_few_variant(const GnFew &a, const char *const (&names)[4], double bytes, hipStream_t st, F run) {
+  const int k = a.threads == 64 ? 0 : a.threads == 256 ? 1 : a.HW <= 4 * a.px ? 2 : 3;
+  return recorded(st, names[k], 0.0, bytes, [&] {
+    if (k == 0)
+      run(std::integral_constant<int, 64>(), std::integral_constant<int, 4>(), dim3((a.units + 3) / 4), dim3(256));
+    else if (k == 1)
+      run(std::integral_constant<int, 256>(), std::integral_constant<int, 4>(), dim3(a.units), dim3(256));
+    else if (k == 2)
+      run(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>(), dim3(a.units), dim3(1024));
+    else
+      run(std::integral_constant<int, 1024>(), std::integral_constant<int, FEW_R>(), dim3(a.units), dim3(1024));
+  });
 }
 // the sum over a group's threads, on all of them; `slot` differs from one call of a kernel to the next
 template <int NT>

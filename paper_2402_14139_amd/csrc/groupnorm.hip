@@ -123,24 +123,29 @@ __global__ __launch_bounds__(NTMAX) void gn_fwd_kernel(GnArgs a, const T *__rest
     }
 }
 
+constexpr SlabNames FWD_NAMES = {{"groupnorm_fwd_tiny", "groupnorm_fwd_tiny_mixed", "groupnorm_fwd_tiny_odd"},
+                                 {"groupnorm_fwd_small", "groupnorm_fwd_small_mixed", "groupnorm_fwd_small_odd"},
+                                 {"groupnorm_fwd_slab", "groupnorm_fwd_slab_mixed", "groupnorm_fwd_slab_odd"},
+                                 {"groupnorm_fwd_stats", "groupnorm_fwd_stats_mixed", "groupnorm_fwd_stats_odd"},
+                                 {"groupnorm_fwd_apply", "groupnorm_fwd_apply_mixed", "groupnorm_fwd_apply_odd"}};
+
 template <typename T, bool WHOLE, bool ONE>
 hipError_t fwd_as(const GnShape &s, const GnPlan &p, const void *x, const float *gamma, const float *beta, void *y,
                   float *mean, float *rstd, float *part, hipStream_t st) {
   const GnArgs &a = p.a;
   const size_t lds = 4 * (size_t)(3 * a.Wp + 2 * a.groups + matrix_floats(a, Vec<T>::N, ONE));
   const dim3 grid(p.slabs * a.chunks, s.B), nt(p.nt);  // a grid's axis ends at 2^32 threads
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)x, gamma, beta, (T *)y, mean, rstd, part); };
+  auto go = [&](int which, double passes, auto kernel) {
+    return recorded(st, FWD_NAMES[which][ONE ? 0 : WHOLE ? 1 : 2], 0.0, gn_bytes<T>(s, passes),
+                    [&] { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)x, gamma, beta, (T *)y, mean, rstd, part); });
+  };
   if (p.split) {
-    go(gn_fwd_kernel<T, WHOLE, ONE, STATS, 8, 1024>);
-    go(gn_fwd_kernel<T, WHOLE, ONE, APPLY, 8, 1024>);
-  } else if (p.tiny) {
-    go(gn_fwd_kernel<T, WHOLE, ONE, FUSED, 1, TINY>);
-  } else if (p.small) {
-    go(gn_fwd_kernel<T, WHOLE, ONE, FUSED, 4, 256>);
-  } else {
-    go(gn_fwd_kernel<T, WHOLE, ONE, FUSED, 16, 1024>);
+    const hipError_t e = go(SLAB_STATS, 1.0, gn_fwd_kernel<T, WHOLE, ONE, STATS, 8, 1024>);
+    return e != hipSuccess ? e : go(SLAB_APPLY, 2.0, gn_fwd_kernel<T, WHOLE, ONE, APPLY, 8, 1024>);
   }
-  return hipGetLastError();
+  if (p.tiny) return go(TINY_SLAB, 2.0, gn_fwd_kernel<T, WHOLE, ONE, FUSED, 1, TINY>);
+  if (p.small) return go(SMALL_SLAB, 2.0, gn_fwd_kernel<T, WHOLE, ONE, FUSED, 4, 256>);
+  return go(SLAB, 2.0, gn_fwd_kernel<T, WHOLE, ONE, FUSED, 16, 1024>);
 }
 
 // ---- small groups ----
@@ -184,10 +189,10 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void gn_fwd_few_kernel(GnFew a
 template <typename T>
 hipError_t fwd_few_as(const GnFew &a, const void *x, const float *gamma, const float *beta, void *y, float *mean, float *rstd,
                       hipStream_t st) {
-  gn_few_variant(a, [&](auto nt, auto r, dim3 grid, dim3 block) {
+  static const char *const names[4] = {"groupnorm_fwd_few_64", "groupnorm_fwd_few_256", "groupnorm_fwd_few_1024", "groupnorm_fwd_few_1024_deep"};
+  return gn_few_variant(a, names, 2.0 * sizeof(T) * a.units * a.HW * a.Cg, st, [&](auto nt, auto r, dim3 grid, dim3 block) {
     hipLaunchKernelGGL((gn_fwd_few_kernel<T, decltype(nt)::value, decltype(r)::value>), grid, block, 0, st, a, (const T *)x, gamma, beta, (T *)y, mean, rstd);
   });
-  return hipGetLastError();
 }
 
 }  // namespace

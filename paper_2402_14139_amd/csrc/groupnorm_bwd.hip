@@ -180,9 +180,17 @@ __global__ __launch_bounds__(RT) void gn_rows_kernel(const float *__restrict__ p
       out1[blockIdx.y * out_stride + o - C] = sum;
   }
 }
-void sum_rows(const float *part, int images, int rows, int C, float *out0, float *out1, hipStream_t st) {
-  hipLaunchKernelGGL(gn_rows_kernel, dim3((2 * C + 15) / 16, images), dim3(RT), 0, st, part, rows, C, out0, out1, 2ll * C);
+hipError_t sum_rows(const char *name, const float *part, int images, int rows, int C, float *out0, float *out1, hipStream_t st) {
+  return recorded(st, name, 0.0, 8.0 * C * images * (rows + 1.0), [&] {
+    hipLaunchKernelGGL(gn_rows_kernel, dim3((2 * C + 15) / 16, images), dim3(RT), 0, st, part, rows, C, out0, out1, 2ll * C);
+  });
 }
+
+constexpr SlabNames BWD_NAMES = {{"groupnorm_bwd_tiny", "groupnorm_bwd_tiny_mixed", "groupnorm_bwd_tiny_odd"},
+                                 {"groupnorm_bwd_small", "groupnorm_bwd_small_mixed", "groupnorm_bwd_small_odd"},
+                                 {"groupnorm_bwd_slab", "groupnorm_bwd_slab_mixed", "groupnorm_bwd_slab_odd"},
+                                 {"groupnorm_bwd_stats", "groupnorm_bwd_stats_mixed", "groupnorm_bwd_stats_odd"},
+                                 {"groupnorm_bwd_apply", "groupnorm_bwd_apply_mixed", "groupnorm_bwd_apply_odd"}};
 
 template <typename T, bool WHOLE, bool ONE>
 hipError_t bwd_as(const GnShape &s, const GnPlan &p, const void *dy, const void *x, const float *gamma, const float *beta,
@@ -191,20 +199,19 @@ hipError_t bwd_as(const GnShape &s, const GnPlan &p, const void *dy, const void 
   const GnArgs &a = p.a;
   const size_t lds = 4 * ((size_t)a.px * (2 * a.W + 1) + 5 * a.Wp + 2 * a.W + 2 * a.groups);
   const dim3 grid(p.slabs * a.chunks, s.B), nt(p.nt);  // a grid's axis ends at 2^32 threads
-  auto launch = [&](auto kernel, float *gx, float *g) { hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)dy, (const T *)x, gamma, beta, mean, rstd, (T *)dx, gx, g); };
-  auto go = [&](auto kernel) { launch(kernel, sum_gx, sum_g); };
+  auto go = [&](int which, double passes, auto kernel, float *gx, float *g) {
+    return recorded(st, BWD_NAMES[which][ONE ? 0 : WHOLE ? 1 : 2], 0.0, gn_bytes<T>(s, passes), [&] {
+      hipLaunchKernelGGL(kernel, grid, nt, lds, st, a, (const T *)dy, (const T *)x, gamma, beta, mean, rstd, (T *)dx, gx, g);
+    });
+  };
   if (p.split) {
-    launch(gn_bwd_kernel<T, WHOLE, ONE, STATS, R, 1024>, part, part + s.C);
-    sum_rows(part, s.B, a.chunks, s.C, sum_gx, sum_g, st);
-    go(gn_bwd_kernel<T, WHOLE, ONE, APPLY, R, 1024>);
-  } else if (p.tiny) {
-    go(gn_bwd_kernel<T, WHOLE, ONE, FUSED, 1, TINY>);
-  } else if (p.small) {
-    go(gn_bwd_kernel<T, WHOLE, ONE, FUSED, 4, 256>);
-  } else {
-    go(gn_bwd_kernel<T, WHOLE, ONE, FUSED, R, 1024>);
+    hipError_t e = go(SLAB_STATS, 2.0, gn_bwd_kernel<T, WHOLE, ONE, STATS, R, 1024>, part, part + s.C);
+    if (e == hipSuccess) e = sum_rows("groupnorm_bwd_chunk_sums", part, s.B, a.chunks, s.C, sum_gx, sum_g, st);
+    return e != hipSuccess ? e : go(SLAB_APPLY, 3.0, gn_bwd_kernel<T, WHOLE, ONE, APPLY, R, 1024>, sum_gx, sum_g);
   }
-  return hipGetLastError();
+  if (p.tiny) return go(TINY_SLAB, 3.0, gn_bwd_kernel<T, WHOLE, ONE, FUSED, 1, TINY>, sum_gx, sum_g);
+  if (p.small) return go(SMALL_SLAB, 3.0, gn_bwd_kernel<T, WHOLE, ONE, FUSED, 4, 256>, sum_gx, sum_g);
+  return go(SLAB, 3.0, gn_bwd_kernel<T, WHOLE, ONE, FUSED, R, 1024>, sum_gx, sum_g);
 }
 
 // ---- small groups ----
@@ -263,10 +270,10 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void gn_bwd_few_kernel(GnFew a
 template <typename T>
 hipError_t bwd_few_as(const GnFew &a, const void *dy, const void *x, const float *gamma, const float *beta, const float *mean,
                       const float *rstd, void *dx, float *sum_gx, float *sum_g, hipStream_t st) {
-  gn_few_variant(a, [&](auto nt, auto r, dim3 grid, dim3 block) {
+  static const char *const names[4] = {"groupnorm_bwd_few_64", "groupnorm_bwd_few_256", "groupnorm_bwd_few_1024", "groupnorm_bwd_few_1024_deep"};
+  return gn_few_variant(a, names, 3.0 * sizeof(T) * a.units * a.HW * a.Cg, st, [&](auto nt, auto r, dim3 grid, dim3 block) {
     hipLaunchKernelGGL((gn_bwd_few_kernel<T, decltype(nt)::value, decltype(r)::value>), grid, block, 0, st, a, (const T *)dy, (const T *)x, gamma, beta, mean, rstd, (T *)dx, sum_gx, sum_g);
   });
-  return hipGetLastError();
 }
 
 }  // namespace
@@ -291,8 +298,7 @@ hipError_t launch_gn_bwd(const GnShape &s, const void *dy, const void *x, const 
     });
   }
   if (e != hipSuccess || s.B == 1) return e;
-  sum_rows(sums, 1, s.B, s.C, dgamma, dbeta, st);
-  return hipGetLastError();
+  return sum_rows("groupnorm_bwd_sums", sums, 1, s.B, s.C, dgamma, dbeta, st);
 }
 
 }  // namespace nf

@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "nf_enqueue.h"
 #include "pw_math.h"
 
 namespace nf {
@@ -942,25 +943,46 @@ void go_wide(F go) {
   if constexpr (sizeof(T) == 2) go(gemm_wide_kernel<T, AT, BT, EPI>);
 }
 
+// bytes of a product's operands and results
+template <typename T>
+double product_bytes(const GemmArgs &g, double result_size) {
+  return sizeof(T) * ((double)g.R * g.L + (double)g.C * g.L) + result_size * g.R * g.C;
+}
+inline double product_flops(const GemmArgs &g) { return 2.0 * g.R * g.C * g.L; }
+
 template <typename T, int MT, int NW, bool HALVES>
-hipError_t few_rows_as(const GemmArgs &g, hipStream_t st) {
+hipError_t few_rows_as(const GemmArgs &g, const char *const (&names)[2], hipStream_t st) {
   constexpr int ROWS = HALVES ? 8 : 16 * MT, COLS = HALVES ? 8 : 16;
   const unsigned down = (unsigned)((g.R + ROWS - 1) / ROWS);
   const dim3 grid((g.C + COLS - 1) / COLS, std::min(down, 1u << FEW_DOWN), (down + (1u << FEW_DOWN) - 1) >> FEW_DOWN);
-  if (g.lda % 16 == 0)
-    hipLaunchKernelGGL((linear_few_rows_kernel<T, MT, NW, HALVES, true>), grid, dim3(64 * NW), 0, st, g);
-  else
-    hipLaunchKernelGGL((linear_few_rows_kernel<T, MT, NW, HALVES, false>), grid, dim3(64 * NW), 0, st, g);
-  return hipGetLastError();
+  const bool aligned = g.lda % 16 == 0;
+  return recorded(st, names[!aligned], product_flops(g), product_bytes<T>(g, sizeof(T) * (1.0 + (g.e.res != nullptr) + (g.e.z != nullptr))), [&] {
+    if (aligned)
+      hipLaunchKernelGGL((linear_few_rows_kernel<T, MT, NW, HALVES, true>), grid, dim3(64 * NW), 0, st, g);
+    else
+      hipLaunchKernelGGL((linear_few_rows_kernel<T, MT, NW, HALVES, false>), grid, dim3(64 * NW), 0, st, g);
+  });
 }
 template <typename T>
 hipError_t run_few_rows(const GemmArgs &g, hipStream_t st) {
+  static const char *const names[4][2][2] = {
+      {{"linear_fwd_8_rows", "linear_fwd_8_rows_odd"}, {"linear_fwd_8_rows_long", "linear_fwd_8_rows_long_odd"}},
+      {{"linear_fwd_16_rows", "linear_fwd_16_rows_odd"}, {"linear_fwd_16_rows_long", "linear_fwd_16_rows_long_odd"}},
+      {{"linear_fwd_32_rows", "linear_fwd_32_rows_odd"}, {"linear_fwd_32_rows_long", "linear_fwd_32_rows_long_odd"}},
+      {{"linear_fwd_64_rows", "linear_fwd_64_rows_odd"}, {"linear_fwd_64_rows_long", "linear_fwd_64_rows_long_odd"}}};
   const bool many = g.L * (int)sizeof(T) > 8 * 128;  // waves without a step would only wait
-  if (g.R <= 8) return many ? few_rows_as<T, 1, 16, true>(g, st) : few_rows_as<T, 1, 4, true>(g, st);
-  if (g.R <= 16) return many ? few_rows_as<T, 1, 16, false>(g, st) : few_rows_as<T, 1, 4, false>(g, st);
-  if (g.R <= 32) return many ? few_rows_as<T, 2, 16, false>(g, st) : few_rows_as<T, 2, 4, false>(g, st);
-  return many ? few_rows_as<T, 4, 16, false>(g, st) : few_rows_as<T, 4, 4, false>(g, st);
+  if (g.R <= 8) return many ? few_rows_as<T, 1, 16, true>(g, names[0][1], st) : few_rows_as<T, 1, 4, true>(g, names[0][0], st);
+  if (g.R <= 16) return many ? few_rows_as<T, 1, 16, false>(g, names[1][1], st) : few_rows_as<T, 1, 4, false>(g, names[1][0], st);
+  if (g.R <= 32) return many ? few_rows_as<T, 2, 16, false>(g, names[2][1], st) : few_rows_as<T, 2, 4, false>(g, names[2][0], st);
+  return many ? few_rows_as<T, 4, 16, false>(g, names[3][1], st) : few_rows_as<T, 4, 4, false>(g, names[3][0], st);
 }
+
+// names of the tile kernels of a product: tiles of 256, of 128 and of 64, those for rows of any alignment behind
+using TileNames = const char *const[5];
+inline const char *tile_name(const TileNames &n, int tile, bool copy) { return n[tile == WIDE ? 0 : (tile == 128 ? 1 : 2) + (copy ? 0 : 2)]; }
+constexpr TileNames FWD_NAMES = {"linear_fwd_256x256", "linear_fwd_128x128", "linear_fwd_64x64", "linear_fwd_128x128_odd", "linear_fwd_64x64_odd"};
+constexpr TileNames DX_NAMES = {"linear_dx_256x256", "linear_dx_128x128", "linear_dx_64x64", "linear_dx_128x128_odd", "linear_dx_64x64_odd"};
+constexpr TileNames DW_NAMES = {"linear_dw_256x256", "linear_dw_128x128", "linear_dw_64x64", "linear_dw_128x128_odd", "linear_dw_64x64_odd"};
 
 template <typename T>
 hipError_t fwd_as(const LinearCall &c, const void *x, const void *W, const float *b, const void *r, const DropArgs &drop,
@@ -976,50 +998,61 @@ hipError_t fwd_as(const LinearCall &c, const void *x, const void *W, const float
   const bool copy = g.lda % 16 == 0;
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(LT), 0, st, g); };
   auto wide = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(WT), 0, st, g); };
-  if (p.tile == WIDE)
-    go_wide<T, false, false, EPI_FWD>(wide);
-  else if (p.tile == 128)
-    copy ? go(gemm_kernel<T, 128, 128, false, false, EPI_FWD, true>) : go(gemm_kernel<T, 128, 128, false, false, EPI_FWD, false>);
-  else
-    copy ? go(gemm_kernel<T, 64, 128, false, false, EPI_FWD, true>) : go(gemm_kernel<T, 64, 128, false, false, EPI_FWD, false>);
-  hipError_t e = hipGetLastError();
+  const double ends = sizeof(T) * (1.0 + (r != nullptr) + (z != nullptr));
+  const hipError_t e = recorded(st, tile_name(FWD_NAMES, p.tile, copy), product_flops(g), product_bytes<T>(g, p.splits > 1 ? 4.0 * p.splits : ends), [&] {
+    if (p.tile == WIDE)
+      go_wide<T, false, false, EPI_FWD>(wide);
+    else if (p.tile == 128)
+      copy ? go(gemm_kernel<T, 128, 128, false, false, EPI_FWD, true>) : go(gemm_kernel<T, 128, 128, false, false, EPI_FWD, false>);
+    else
+      copy ? go(gemm_kernel<T, 64, 128, false, false, EPI_FWD, true>) : go(gemm_kernel<T, 64, 128, false, false, EPI_FWD, false>);
+  });
   if (e != hipSuccess || p.splits == 1) return e;
   const FinishArgs f = finish_args(p, g);
-  hipLaunchKernelGGL(fwd_finish_kernel<T>, dim3(finish_blocks(f)), dim3(LT), 0, st, f);
-  return hipGetLastError();
+  return recorded(st, "linear_fwd_finish", 0.0, (4.0 * p.splits + ends) * g.R * g.C,
+                  [&] { hipLaunchKernelGGL(fwd_finish_kernel<T>, dim3(finish_blocks(f)), dim3(LT), 0, st, f); });
 }
 
 // whether an operand of a product, of a or b elements, is shorter than the 16 bytes that the tile kernel reads at a time
 inline bool gemm_short(long long a, long long b, int size) { return std::min(a, b) * size < 16; }
 
-// The workspace holds dx's splits, then dW's.  Products in the same kind of tiles share a launch.
+// The workspace holds dx's splits, then dW's.  Products in the same kind of tiles share a launch, and so does what adds up their
+// splits; a measurement that wants them one by one gets them so.
 template <typename T>
 hipError_t bwd_as(const LinearCall &c, const void *dz, const void *x, const void *W, void *dx, float *dW, void *ws,
                   hipStream_t st) {
   const long long ldn = (long long)c.N * sizeof(T), ldk = (long long)c.K * sizeof(T);
-  const bool copy = ldn % 16 == 0 && ldk % 16 == 0;
+  const bool copy = ldn % 16 == 0 && ldk % 16 == 0, apart = g_prof.on && g_prof.apart;
   auto blocks = [](long long n) { return dim3((unsigned)((n + LT - 1) / LT)); };
-  if (dx && gemm_short(c.M * c.N, (long long)c.N * c.K, sizeof(T))) {
-    hipLaunchKernelGGL((gemm_short_kernel<T, T>), blocks(c.M * c.K), dim3(LT), 0, st, (const T *)dz, (long long)c.N, 1ll, (const T *)W, 1ll,
-                       (long long)c.K, (T *)dx, c.M, c.K, c.N);
-    dx = nullptr;
-  }
-  if (dW && gemm_short(c.M * c.N, c.M * c.K, sizeof(T))) {
-    hipLaunchKernelGGL((gemm_short_kernel<T, float>), blocks((long long)c.N * c.K), dim3(LT), 0, st, (const T *)dz, 1ll, (long long)c.N,
-                       (const T *)x, 1ll, (long long)c.K, dW, (long long)c.N, c.K, (int)c.M);
-    dW = nullptr;
-  }
-  if (!dx && !dW) return hipGetLastError();
-  const Plan px = plan_of(c.M, c.K, c.N, sizeof(T), copy), pw = plan_of(c.N, c.K, c.M, sizeof(T), copy);
   GemmArgs gx = {}, gw = {};
   gx.a = (const char *)dz, gx.b = (const char *)W, gx.lda = ldn, gx.ldb = ldk;
   gx.R = c.M, gx.C = c.K, gx.L = c.N, gx.e.out = dx;
-  if (px.splits > 1) gx.part = (float *)ws, gx.part_ld = (c.K + 7) / 8 * 8;
   gw.a = (const char *)dz, gw.b = (const char *)x, gw.lda = ldn, gw.ldb = ldk;
   gw.R = c.N, gw.C = c.K, gw.L = c.M, gw.e.out = dW;
+  hipError_t e = hipSuccess;
+  if (dx && gemm_short(c.M * c.N, (long long)c.N * c.K, sizeof(T))) {
+    e = recorded(st, "linear_dx_short", product_flops(gx), product_bytes<T>(gx, sizeof(T)), [&] {
+      hipLaunchKernelGGL((gemm_short_kernel<T, T>), blocks(c.M * c.K), dim3(LT), 0, st, (const T *)dz, (long long)c.N, 1ll, (const T *)W, 1ll,
+                         (long long)c.K, (T *)dx, c.M, c.K, c.N);
+    });
+    dx = nullptr;
+  }
+  if (e == hipSuccess && dW && gemm_short(c.M * c.N, c.M * c.K, sizeof(T))) {
+    e = recorded(st, "linear_dw_short", product_flops(gw), product_bytes<T>(gw, 4.0), [&] {
+      hipLaunchKernelGGL((gemm_short_kernel<T, float>), blocks((long long)c.N * c.K), dim3(LT), 0, st, (const T *)dz, 1ll, (long long)c.N,
+                         (const T *)x, 1ll, (long long)c.K, dW, (long long)c.N, c.K, (int)c.M);
+    });
+    dW = nullptr;
+  }
+  if (e != hipSuccess || (!dx && !dW)) return e;
+  const Plan px = plan_of(c.M, c.K, c.N, sizeof(T), copy), pw = plan_of(c.N, c.K, c.M, sizeof(T), copy);
+  if (px.splits > 1) gx.part = (float *)ws, gx.part_ld = (c.K + 7) / 8 * 8;
   gw.part = pw.splits > 1 ? (float *)((char *)ws + px.bytes) : dW, gw.part_ld = pw.splits > 1 ? (c.K + 7) / 8 * 8 : c.K;
   const int nx = lay(px, gx), nw = lay(pw, gw);
-  if (dx && dW && px.tile != WIDE && pw.tile != WIDE) {
+  const double bytes_x = product_bytes<T>(gx, px.splits > 1 ? 4.0 * px.splits : sizeof(T)), bytes_w = product_bytes<T>(gw, 4.0 * pw.splits);
+  if (dx && dW && px.tile != WIDE && pw.tile != WIDE && !apart) {
+    static const char *const names[2][2][2] = {{{"linear_gradients_64_64", "linear_gradients_64_64_odd"}, {"linear_gradients_64_128", "linear_gradients_64_128_odd"}},
+                                               {{"linear_gradients_128_64", "linear_gradients_128_64_odd"}, {"linear_gradients_128_128", "linear_gradients_128_128_odd"}}};
     const dim3 grid((unsigned)((nx + 7) / 8 * 8 + nw));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(LT), 0, st, gx, gw); };
     auto sized = [&](auto cp) {
@@ -1029,38 +1062,47 @@ hipError_t bwd_as(const LinearCall &c, const void *dz, const void *x, const void
       else
         pw.tile == 128 ? go(gemm_gradients_kernel<T, 64, 128, C>) : go(gemm_gradients_kernel<T, 64, 64, C>);
     };
-    copy ? sized(std::true_type()) : sized(std::false_type());
+    e = recorded(st, names[px.tile == 128][pw.tile == 128][!copy], product_flops(gx) + product_flops(gw), bytes_x + bytes_w,
+                 [&] { copy ? sized(std::true_type()) : sized(std::false_type()); });
   } else {
     if (dx) {
       auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nx), dim3(LT), 0, st, gx); };
       auto wide = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nx), dim3(WT), 0, st, gx); };
-      if (px.tile == WIDE)
-        go_wide<T, false, true, EPI_STORE>(wide);
-      else if (px.tile == 128)
-        copy ? go(gemm_kernel<T, 128, 128, false, true, EPI_STORE, true>) : go(gemm_kernel<T, 128, 128, false, true, EPI_STORE, false>);
-      else
-        copy ? go(gemm_kernel<T, 64, 128, false, true, EPI_STORE, true>) : go(gemm_kernel<T, 64, 128, false, true, EPI_STORE, false>);
+      e = recorded(st, tile_name(DX_NAMES, px.tile, copy), product_flops(gx), bytes_x, [&] {
+        if (px.tile == WIDE)
+          go_wide<T, false, true, EPI_STORE>(wide);
+        else if (px.tile == 128)
+          copy ? go(gemm_kernel<T, 128, 128, false, true, EPI_STORE, true>) : go(gemm_kernel<T, 128, 128, false, true, EPI_STORE, false>);
+        else
+          copy ? go(gemm_kernel<T, 64, 128, false, true, EPI_STORE, true>) : go(gemm_kernel<T, 64, 128, false, true, EPI_STORE, false>);
+      });
     }
-    if (dW) {
+    if (e == hipSuccess && dW) {
       auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nw), dim3(LT), 0, st, gw); };
       auto wide = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nw), dim3(WT), 0, st, gw); };
-      if (pw.tile == WIDE)
-        go_wide<T, true, true, EPI_F32>(wide);
-      else if (pw.tile == 128)
-        copy ? go(gemm_kernel<T, 128, 128, true, true, EPI_F32, true>) : go(gemm_kernel<T, 128, 128, true, true, EPI_F32, false>);
-      else
-        copy ? go(gemm_kernel<T, 64, 128, true, true, EPI_F32, true>) : go(gemm_kernel<T, 64, 128, true, true, EPI_F32, false>);
+      e = recorded(st, tile_name(DW_NAMES, pw.tile, copy), product_flops(gw), bytes_w, [&] {
+        if (pw.tile == WIDE)
+          go_wide<T, true, true, EPI_F32>(wide);
+        else if (pw.tile == 128)
+          copy ? go(gemm_kernel<T, 128, 128, true, true, EPI_F32, true>) : go(gemm_kernel<T, 128, 128, true, true, EPI_F32, false>);
+        else
+          copy ? go(gemm_kernel<T, 64, 128, true, true, EPI_F32, true>) : go(gemm_kernel<T, 64, 128, true, true, EPI_F32, false>);
+      });
     }
   }
-  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   FinishArgs fx = finish_args(px, gx), fw = finish_args(pw, gw);
   if (!dx) fx.R = 0;
   if (!dW) fw.R = 0;
+  auto finish = [&](const char *name, unsigned bx, unsigned bw) {
+    return recorded(st, name, 0.0, (4.0 * px.splits + sizeof(T)) * (bx ? (double)gx.R * gx.C : 0.0) + 4.0 * (pw.splits + 1) * (bw ? (double)gw.R * gw.C : 0.0),
+                    [&] { hipLaunchKernelGGL(gradients_finish_kernel<T>, dim3(bx + bw), dim3(LT), 0, st, fx, fw, bx); });
+  };
   const unsigned bx = finish_blocks(fx), bw = finish_blocks(fw);
-  if (bx + bw == 0) return hipSuccess;
-  hipLaunchKernelGGL(gradients_finish_kernel<T>, dim3(bx + bw), dim3(LT), 0, st, fx, fw, bx);
-  return hipGetLastError();
+  if (bx && bw && !apart) return finish("linear_gradients_finish", bx, bw);
+  if (bx) e = finish("linear_dx_finish", bx, 0);
+  if (e == hipSuccess && bw) e = finish("linear_dw_finish", 0, bw);
+  return e;
 }
 
 // the epilogue gradient's row parts: up to 1024 workgroups, 4 rows or more to a thread
@@ -1115,16 +1157,23 @@ hipError_t launch_linear_epilogue(const LinearCall &c, const void *dy, const voi
   const int ld = p.ny == 1 ? c.N : (c.N + 7) / 8 * 8;
   float *part = !db ? nullptr : p.ny == 1 ? db : (float *)ws;
   const dim3 grid(p.nx, p.ny);
-  if (c.dtype == NF_BF16)
-    hipLaunchKernelGGL((linear_epilogue_kernel<__bf16>), grid, dim3(LT), 0, st, c.M, c.N, p.per, p.tx, (const __bf16 *)dy, (const __bf16 *)z, e, part, ld);
-  else if (c.dtype == NF_F16)
-    hipLaunchKernelGGL((linear_epilogue_kernel<_Float16>), grid, dim3(LT), 0, st, c.M, c.N, p.per, p.tx, (const _Float16 *)dy, (const _Float16 *)z, e, part, ld);
-  else
-    hipLaunchKernelGGL((linear_epilogue_kernel<float>), grid, dim3(LT), 0, st, c.M, c.N, p.per, p.tx, (const float *)dy, (const float *)z, e, part, ld);
-  hipError_t err = hipGetLastError();
+  const double size = c.dtype == NF_F32 ? 4.0 : 2.0;
+  const hipError_t err = recorded(st, "linear_bwd_epilogue", 0.0, size * (c.act != NF_ACT_NONE ? 3.0 : 2.0) * c.M * c.N, [&] {
+    auto go = [&](auto t) {
+      using T = decltype(t);
+      hipLaunchKernelGGL((linear_epilogue_kernel<T>), grid, dim3(LT), 0, st, c.M, c.N, p.per, p.tx, (const T *)dy, (const T *)z, e, part, ld);
+    };
+    if (c.dtype == NF_BF16)
+      go((__bf16)0.f);
+    else if (c.dtype == NF_F16)
+      go((_Float16)0.f);
+    else
+      go(0.f);
+  });
   if (err != hipSuccess || !db || p.ny == 1) return err;
-  hipLaunchKernelGGL(column_sums_kernel, dim3((c.N + 15) / 16), dim3(CT), 0, st, part, p.ny, (long long)ld, c.N, db);
-  return hipGetLastError();
+  return recorded(st, "linear_bias_sums", 0.0, 4.0 * (p.ny + 1) * c.N, [&] {
+    hipLaunchKernelGGL(column_sums_kernel, dim3((c.N + 15) / 16), dim3(CT), 0, st, part, p.ny, (long long)ld, c.N, db);
+  });
 }
 
 }  // namespace nf

@@ -49,6 +49,16 @@ struct ProfScope {
   }
 };
 
+// The same for a file that has its launches to itself: a launch, its error, its record.
+template <typename F>
+inline hipError_t recorded(hipStream_t st, const char *name, double flops, double bytes, F launch) {
+  ProfScope sc(st);
+  launch();
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) sc.done(name, flops, bytes);
+  return e;
+}
+
 }  // namespace nf
 
 #define NF_RUN(st, name, flops, bytes, call) \

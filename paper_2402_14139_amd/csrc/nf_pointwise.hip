@@ -129,9 +129,7 @@ int32_t nf_linear_fwd(const nf_linear_desc *d, int64_t M, const void *x, const v
   if (!all_aligned16(x, W, b, r, y, z)) return NF_ERR_BAD_DESC;
   if ((rc = check_ws(ws, ws_bytes, linear_fwd_workspace_bytes(c)))) return rc;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const double m = (double)M, mn = m * c.N;
-  NF_RUN(st, "linear_fwd", 2.0 * mn * c.K, size_of(c.dtype) * (m * c.K + (double)c.N * c.K + mn * (1 + (r != nullptr) + (z != nullptr))),
-         launch_linear_fwd(c, x, W, b, r, drop_args(drop), y, z, ws, st));
+  NF_HIP(launch_linear_fwd(c, x, W, b, r, drop_args(drop), y, z, ws, st));
   return NF_OK;
 }
 
@@ -146,8 +144,7 @@ int32_t nf_linear_bwd_epilogue(const nf_linear_desc *d, int64_t M, const void *d
   if (!all_aligned16(dy, z, dz, db)) return NF_ERR_BAD_DESC;
   if ((rc = check_ws(ws, ws_bytes, linear_workspace_bytes(c)))) return rc;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  NF_RUN(st, "linear_bwd_epilogue", 0.0, size_of(c.dtype) * (c.act != NF_ACT_NONE ? 3.0 : 2.0) * M * c.N,
-         launch_linear_epilogue(c, dy, z, drop_args(drop), dz, db, ws, st));
+  NF_HIP(launch_linear_epilogue(c, dy, z, drop_args(drop), dz, db, ws, st));
   return NF_OK;
 }
 
@@ -160,10 +157,7 @@ int32_t nf_linear_bwd(const nf_linear_desc *d, int64_t M, const void *dz, const 
   if (!all_aligned16(dz, x, W, dx, dW)) return NF_ERR_BAD_DESC;
   if ((rc = check_ws(ws, ws_bytes, linear_workspace_bytes(c)))) return rc;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const double m = (double)M, e = size_of(c.dtype), nk = (double)c.N * c.K;
-  NF_RUN(st, "linear_bwd", 2.0 * m * nk * ((dx != nullptr) + (dW != nullptr)),
-         e * m * c.N + (dx ? e * (m * c.K + nk) : 0.0) + (dW ? e * m * c.K + 4.0 * nk : 0.0),
-         launch_linear_bwd(c, dz, x, W, dx, dW, ws, st));
+  NF_HIP(launch_linear_bwd(c, dz, x, W, dx, dW, ws, st));
   return NF_OK;
 }
 
@@ -194,8 +188,7 @@ int32_t nf_groupnorm_fwd(const nf_groupnorm_desc *d, int32_t B, const void *x, c
   if (!all_aligned16(x, gamma, beta, y, mean, rstd)) return NF_ERR_BAD_DESC;
   if ((rc = check_ws(ws, ws_bytes, gn_fwd_workspace_bytes(s)))) return rc;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  NF_RUN(st, "groupnorm_fwd", 0.0, 2.0 * size_of(s.dtype) * B * s.HW * s.C,
-         launch_gn_fwd(s, x, gamma, beta, y, mean, rstd, ws, st));
+  NF_HIP(launch_gn_fwd(s, x, gamma, beta, y, mean, rstd, ws, st));
   return NF_OK;
 }
 
@@ -209,8 +202,7 @@ int32_t nf_groupnorm_bwd(const nf_groupnorm_desc *d, int32_t B, const void *dy, 
   if (!all_aligned16(dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta)) return NF_ERR_BAD_DESC;
   if ((rc = check_ws(ws, ws_bytes, gn_workspace_bytes(s)))) return rc;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  NF_RUN(st, "groupnorm_bwd", 0.0, 3.0 * size_of(s.dtype) * B * s.HW * s.C,
-         launch_gn_bwd(s, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, ws, st));
+  NF_HIP(launch_gn_bwd(s, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, ws, st));
   return NF_OK;
 }
 
