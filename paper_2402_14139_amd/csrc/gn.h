@@ -322,12 +322,22 @@ struct GnFew {
   float eps, inv;
   FastDiv div_cg, div_g, div_px;
 };
-// Whether a shape goes this way: groups of up to 16 elements a thread, and up to FEW_ELEMENTS in all, beyond which accesses of single
-// elements cost more than the instructions
-constexpr long long FEW_ELEMENTS = 3 << 19;
-inline bool gn_few(const GnShape &s, GnFew *a) {
+// Whether a shape goes this way: groups of up to 16 elements a thread, and not so many elements that accesses of single ones cost more
+// than the slab kernels' instructions (us of a call here and in slabs, at thousands of elements):
+//   a wave to a group, pixels of 8 bytes or more: no barriers.  20x36 in 6 groups fp32, 1573 forward 6.8 and 9.4, gradients 14.4 and 15.9;
+//     64x128 in 32 1573 6.1 and 5.7, 11.3 and 10.7, 2097 7.4 and 6.6, 12.8 and 11.6
+//   pixels of fewer bytes: 50x40 in 40 fp32, 524 7.7 and 5.4, 11.9 and 9.5
+//   several waves, slabs of whole vectors to a group: 144x96 in 8 fp32, forward 524 5.1 and 5.1, 786 5.8 and 5.3; gradients 393 8.0 and 7.8,
+//     524 9.2 and 7.9 (256x128 in 32, 1573 13.8 and 6.7, 22.7 and 10.7)
+//   several waves, slabs that mix groups in a vector: 100x48 in 4 bf16, forward 786 5.9 and 6.3, 1049 7.3 and 6.4; gradients 524 7.9 and 8.4, 786
+//     11.3 and 9.0
+inline long long few_most(int threads, int pixel_bytes, bool backward) {
+  if (pixel_bytes < 8) return 1 << 18;
+  if (threads == 64) return 3 << 19;
+  return pixel_bytes % 16 == 0 ? (backward ? 3 << 17 : 1 << 19) : (backward ? 1 << 19 : 3 << 18);
+}
+inline bool gn_few(const GnShape &s, bool backward, GnFew *a) {
   a->HW = s.HW, a->C = s.C, a->G = s.G, a->Cg = s.C / s.G, a->act = s.act, a->eps = s.eps;
-  if ((long long)s.B * s.HW * s.C > FEW_ELEMENTS) return false;
   a->threads = 0;
   // few elements a thread, or the most threads
   for (int nt : {64, 256, 1024})
@@ -335,7 +345,7 @@ inline bool gn_few(const GnShape &s, GnFew *a) {
       a->threads = nt;
       break;
     }
-  if (!a->threads) return false;
+  if (!a->threads || (long long)s.B * s.HW * s.C > few_most(a->threads, a->Cg * (s.dtype == NF_F32 ? 4 : 2), backward)) return false;
   a->px = a->threads / a->Cg;
   a->share = 6;
   while (a->share > 0 && (a->Cg << a->share) > a->threads) --a->share;

@@ -210,7 +210,7 @@ size_t gn_workspace_bytes(const GnShape &s) {
 hipError_t launch_gn_fwd(const GnShape &s, const void *x, const float *gamma, const float *beta, void *y, float *mean,
                          float *rstd, void *ws, hipStream_t st) {
   GnFew few;
-  if (gn_few(s, &few)) {
+  if (gn_few(s, false, &few)) {
     if (s.dtype == NF_BF16) return fwd_few_as<__bf16>(few, x, gamma, beta, y, mean, rstd, st);
     if (s.dtype == NF_F16) return fwd_few_as<_Float16>(few, x, gamma, beta, y, mean, rstd, st);
     return fwd_few_as<float>(few, x, gamma, beta, y, mean, rstd, st);

@@ -282,7 +282,7 @@ hipError_t launch_gn_bwd(const GnShape &s, const void *dy, const void *x, const 
                          const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta, void *ws,
                          hipStream_t st) {
   GnFew few;
-  const bool is_few = gn_few(s, &few);
+  const bool is_few = gn_few(s, true, &few);
   const GnPlan p = gn_plan(s, true);
   // the images' sums [B][2][C], of which one image's are the result; the chunks' lie behind
   float *const sums = (float *)ws, *const part = sums + (size_t)s.B * 2 * s.C;

@@ -78,3 +78,17 @@ def test_every_kernel_is_among_these_cases():
     kinds = {k + r for k in ("tiny", "small", "slab", "split") for r in ("", "_mixed", "_odd")} | {"few_64", "few_256", "few_1024", "few_1024_deep"}
     for i in range(4):
         assert {c[i] for c in CASES.values()} == kinds, i
+
+
+@pytest.mark.parametrize("t,shape,fwd,bwd", [
+    ("f32", (384, 16, 256, 16), True, True), ("f32", (385, 16, 256, 16), False, False),          # waves
+    ("f32", (131, 50, 40, 40), True, True), ("f32", (132, 50, 40, 40), False, False),            # waves, 4 bytes of a pixel
+    ("f32", (28, 144, 96, 8), True, True), ("f32", (29, 144, 96, 8), True, False), ("f32", (38, 144, 96, 8), False, False),
+    ("bf16", (109, 100, 48, 4), True, True), ("bf16", (110, 100, 48, 4), True, False), ("bf16", (164, 100, 48, 4), False, False)])
+def test_both_sides_of_the_rule_for_small_groups(t, shape, fwd, bwd):
+    nf.nf_prof_begin()
+    try:
+        tp.test_group_norm(t, *shape)
+    finally:
+        got = {r["kernel"] for r in nf.nf_prof_end() if not r["kernel"].endswith("sums")}
+    assert {k.split("_")[1]: "_few_" in k for k in got} == {"fwd": fwd, "bwd": bwd}, got
