@@ -880,16 +880,24 @@ double product_time(long long tiles, long long steps, int splits, double results
 }
 
 // Tiles of 256 (16 bits, whole 16-byte rows) where their rounds over the 256 CUs take less time than those of two 128s to a CU:
-// 1.55 us a step of 128 bytes and 13 more a round against 0.95 and 7.5 (65536x512x512 54 and 61 us, 8192x1024x1024, 128 tiles, 47 and 26);
-// not where the sum must be split, whose parts are four times as large.  Else the quickest of tiles of 128 or 64 and of 1 to 512 parts.
-Plan plan_of(long long R, int C, long long L, int size, bool whole) {
+// 1.55 us a step of 128 bytes and 13 more a round against 0.95 and 7.5; not where the sum must be split, whose parts are four times as
+// large, nor where a tile's columns or rows are a quarter empty (33770x512x136 forward 28 us, in tiles of 128 and 64 17).  And only in
+// rounds that are nearly whole, since smaller tiles share out what is left (us in tiles of 256, and of 128 and 64):
+//   forward, whose epilogue a round waits for: 7/8 of the last round and 4 steps.  65536x1024x256 51 and 58, 65536x192x256 26 and 25, 65536x64x512 41
+//     and 35; 20000x256x512, 158 tiles, 25 and 18; 40000x1024x1000, 628 tiles, 128 and 116
+//   gradients: 3/4 of it, or 8 steps.  dx 65536x256x1024 39 and 50, 65536x256x32 11 and 12; 20000x512x1024, 158 tiles, 28 and 30, 20000x512x192 13
+//     and 12; dW 3000x4000 of 1024 rows, 192 tiles, 36 and 39, of 128 19 and 18
+// (8192x1024x1024, 128 tiles, 39 and 25: their times decide.)  Else the quickest of tiles of 128 or 64 and of 1 to 512 parts.
+Plan plan_of(long long R, int C, long long L, int size, bool whole, bool fwd) {
   const int step = 128 / size;
   const long long steps = (L + step - 1) / step;
   auto tiles = [&](int b) { return ((R + b - 1) / b) * ((C + b - 1) / b); };
   Plan p;
   p.tile = 128, p.splits = 1;
-  bool wide = size == 2 && whole && tiles(WIDE) >= 128;
-  if (wide) wide = (double)((tiles(WIDE) + 255) / 256) * (1.55 * steps + 13) < (double)((tiles(128) + 511) / 512) * (0.95 * steps + 7.5);
+  const long long large = tiles(WIDE), rounds = (large + 255) / 256;
+  const bool wide = size == 2 && whole && large >= 128 && 4 * R * C >= 3 * large * WIDE * WIDE &&
+                    (fwd ? steps >= 4 && 8 * large >= 7 * 256 * rounds : steps >= 8 || 4 * large >= 3 * 256 * rounds) &&
+                    (double)rounds * (1.55 * steps + 13) < (double)((tiles(128) + 511) / 512) * (0.95 * steps + 7.5);
   if (wide) {
     p.tile = WIDE;
   } else {
@@ -914,7 +922,7 @@ Plan plan_of(long long R, int C, long long L, int size, bool whole) {
 // (64x2048x2048 12.4 and 9.9).  And weights of less than the 16 bytes that the tile kernel reads at a time.
 constexpr int FEW_ROWS = 0;
 Plan fwd_plan(long long M, int N, int K, int size) {
-  Plan p = plan_of(M, N, K, size, K * size % 16 == 0);
+  Plan p = plan_of(M, N, K, size, K * size % 16 == 0, true);
   const long long t64 = ((M + 63) / 64) * ((N + 63) / 64);
   if (M <= 32 || (t64 <= 64 && (long long)K * size <= 2048) || (long long)N * K * size < 16) p.tile = FEW_ROWS, p.splits = 1, p.bytes = 0;
   return p;
@@ -1045,7 +1053,7 @@ hipError_t bwd_as(const LinearCall &c, const void *dz, const void *x, const void
     dW = nullptr;
   }
   if (e != hipSuccess || (!dx && !dW)) return e;
-  const Plan px = plan_of(c.M, c.K, c.N, sizeof(T), copy), pw = plan_of(c.N, c.K, c.M, sizeof(T), copy);
+  const Plan px = plan_of(c.M, c.K, c.N, sizeof(T), copy, false), pw = plan_of(c.N, c.K, c.M, sizeof(T), copy, false);
   if (px.splits > 1) gx.part = (float *)ws, gx.part_ld = (c.K + 7) / 8 * 8;
   gw.part = pw.splits > 1 ? (float *)((char *)ws + px.bytes) : dW, gw.part_ld = pw.splits > 1 ? (c.K + 7) / 8 * 8 : c.K;
   const int nx = lay(px, gx), nw = lay(pw, gw);
@@ -1131,7 +1139,7 @@ size_t linear_workspace_bytes(const LinearCall &c) {
   const EpiPlan e = epi_plan(c.M, c.N);
   const size_t fwd = linear_fwd_workspace_bytes(c);
   const bool whole = c.N * size % 16 == 0 && c.K * size % 16 == 0;
-  const size_t bwd = plan_of(c.M, c.K, c.N, size, whole).bytes + plan_of(c.N, c.K, c.M, size, whole).bytes;
+  const size_t bwd = plan_of(c.M, c.K, c.N, size, whole, false).bytes + plan_of(c.N, c.K, c.M, size, whole, false).bytes;
   return std::max(std::max(fwd, bwd), (size_t)e.ny * ((c.N + 7) / 8) * 32);
 }
 

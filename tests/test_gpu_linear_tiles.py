@@ -60,7 +60,7 @@ def forward(t, M, K, N, names, act="gelu", p=0.1, res=True, z=True):
     close("y", y, Y, tol + (HALF[t] + 2 * SUM) * (Y.abs() + tol) + SUM * v.abs() + TINY[t])
 
 
-WIDE = [(33770, 8, 136), (33770, 72, 136), (33770, 264, 136), (8300, 104, 1032), (8300, 1000, 1032)]
+WIDE = [(60101, 200, 200), (28901, 264, 456), (14401, 1000, 1000)]
 
 
 @pytest.mark.parametrize("t", ["bf16", "f16"])
@@ -71,9 +71,9 @@ def test_forward_in_tiles_of_256(t, M, K, N):
 
 @pytest.mark.parametrize("t", ["bf16", "f16"])
 def test_forward_in_tiles_of_256_without_its_epilogue(t):
-    forward(t, 33770, 136, 136, ["linear_fwd_256x256"], act="none", p=0.0, res=False, z=False)
-    forward(t, 33770, 136, 136, ["linear_fwd_256x256"], act="relu", p=0.0, res=True, z=False)
-    forward(t, 33770, 136, 136, ["linear_fwd_256x256"], act="silu", p=0.25, res=False, z=True)
+    forward(t, 60101, 200, 200, ["linear_fwd_256x256"], act="none", p=0.0, res=False, z=False)
+    forward(t, 60101, 200, 200, ["linear_fwd_256x256"], act="relu", p=0.0, res=True, z=False)
+    forward(t, 60101, 200, 200, ["linear_fwd_256x256"], act="silu", p=0.25, res=False, z=True)
 
 
 BOTH = ("bf16", "f16")
@@ -108,8 +108,8 @@ def test_forward_of_few_rows(t, M, rows, form, K):
 
 # shape, dx's tiles, dW's, "odd" rows, parts of dx and of dW
 GRADIENTS = [
-    (BOTH, 33483, 136, 8, 256, 64, False, False, True), (BOTH, 33483, 136, 40, 256, 64, False, False, True), (BOTH, 33483, 136, 264, 256, 64, False, False, True),
-    (BOTH, 34, 2696, 2952, 64, 256, False, True, False), (BOTH, 201, 2696, 2952, None, 256, False, None, False), (BOTH, 2213, 3864, 2168, 256, 256, False, False, False),
+    (BOTH, 50001, 200, 8, 256, 64, False, False, True), (BOTH, 50001, 200, 40, 256, 64, False, False, True), (BOTH, 50001, 200, 264, 256, 64, False, False, True),
+    (BOTH, 34, 3496, 4008, 64, 256, False, None, False), (BOTH, 201, 3496, 4008, None, 256, False, None, False), (BOTH, 2213, 3864, 2168, 256, 256, False, False, False),
     (BOTH, 2935, 1368, 712, 128, 128, False, False, True), (BOTH, 1127, 944, 2864, 128, None, False, True, None), (BOTH, 1732, 1784, 736, 128, 64, False, False, False),
     (BOTH, 721, 1712, 1848, 64, 128, False, False, False), (BOTH, 1676, 1207, 1827, 128, 128, True, True, True), (BOTH, 2066, 2978, 206, 128, None, True, False, None),
     (BOTH, 195, 1764, 3520, None, 128, True, None, False), (BOTH, 920, 1130, 2173, 128, 64, True, True, False), (BOTH, 2197, 791, 1236, 64, 128, True, False, True),
@@ -147,16 +147,29 @@ def test_gradients(t, M, K, N, bx, bw, odd, px, pw):
 @pytest.mark.parametrize("t", ["bf16", "f16"])
 def test_infinities_stay_in_their_rows_and_columns(t):
     """A row of x with an infinity and a NaN in W, in the last terms of tiles of 256: their products only."""
-    M, K, N = 33770, 72, 136
+    M, K, N = 60101, 200, 200
     T = TYPES[t]
     x, W = torch.ones(M, K, dtype=T, device="cuda"), torch.ones(N, K, dtype=T, device="cuda")
-    x[33769, 71], x[255, 0], W[135, 71] = float("inf"), float("-inf"), float("nan")
+    x[60100, 199], x[255, 0], W[199, 199] = float("inf"), float("-inf"), float("nan")
     d = nf.LinearDesc(dtype=DT[t], K=K, N=N, act=0)
     y = torch.empty(M, N, dtype=T, device="cuda")
     assert recorded(lambda: nf.nf_linear_fwd(d, M, x, W, None, None, None, y, None, None)) == {"linear_fwd_256x256"}
-    want = torch.full((M, N), 72.0, device="cuda")
-    want[33769], want[255], want[:, 135] = float("inf"), float("-inf"), float("nan")
+    want = torch.full((M, N), 200.0, device="cuda")
+    want[60100], want[255], want[:, 199] = float("inf"), float("-inf"), float("nan")
     assert torch.equal(y.float().nan_to_num(9.0, 1e9, -1e9), want.nan_to_num(9.0, 1e9, -1e9))
+
+
+@pytest.mark.parametrize("M,K,N,name", [(60101, 200, 200, "256x256"), (60101, 192, 200, "128x128"), (60101, 200, 184, "64x64"), (20000, 256, 512, "64x64"),
+                                        (33770, 512, 136, "64x64"), (40000, 1024, 1000, "128x128"), (65536, 512, 512, "256x256")])
+def test_both_sides_of_the_forward_rule_for_256(M, K, N, name):
+    """Empty quarters of tiles, short sums and rounds that are not nearly whole go to smaller tiles."""
+    x, W = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda"), torch.zeros(N, K, dtype=torch.bfloat16, device="cuda")
+    x[:, 3], W[:, 3] = 2, 3
+    y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    d = nf.LinearDesc(dtype=nf.NF_BF16, K=K, N=N, act=0)
+    ws = workspace(nf.nf_linear_fwd_workspace_bytes(d, M))
+    assert recorded(lambda: nf.nf_linear_fwd(d, M, x, W, None, None, None, y, None, ws)) == {"linear_fwd_" + name}
+    assert (y == 6).all()
 
 
 def test_every_kernel_is_among_these_cases():
