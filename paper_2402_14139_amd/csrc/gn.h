@@ -322,22 +322,36 @@ struct GnFew {
   float eps, inv;
   FastDiv div_cg, div_g, div_px;
 };
-// Whether a shape goes this way: groups of up to 16 elements a thread, and not so many elements that accesses of single ones cost more
-// than the slab kernels' instructions (us of a call here and in slabs, at thousands of elements):
-//   a wave to a group, pixels of 8 bytes or more: no barriers.  20x36 in 6 groups fp32, 1573 forward 6.8 and 9.4, gradients 14.4 and 15.9;
-//     64x128 in 32 1573 6.1 and 5.7, 11.3 and 10.7, 2097 7.4 and 6.6, 12.8 and 11.6
-//   pixels of fewer bytes: 50x40 in 40 fp32, 524 7.7 and 5.4, 11.9 and 9.5
-//   several waves, slabs of whole vectors to a group: 144x96 in 8 fp32, forward 524 5.1 and 5.1, 786 5.8 and 5.3; gradients 393 8.0 and 7.8,
-//     524 9.2 and 7.9 (256x128 in 32, 1573 13.8 and 6.7, 22.7 and 10.7)
-//   several waves, slabs that mix groups in a vector: 100x48 in 4 bf16, forward 786 5.9 and 6.3, 1049 7.3 and 6.4; gradients 524 7.9 and 8.4, 786
-//     11.3 and 9.0
-inline long long few_most(int threads, int pixel_bytes, bool backward) {
-  if (pixel_bytes < 8) return 1 << 18;
-  if (threads == 64) return 3 << 19;
-  return pixel_bytes % 16 == 0 ? (backward ? 3 << 17 : 1 << 19) : (backward ? 1 << 19 : 3 << 18);
+// What a call takes this way and in slabs, in us with the launch, by least squares over 48000 calls (24000 shapes of 2^16 to 2^21
+// elements; one standard deviation is 9 to 17 %): turns of a thread; thousands of waves times turns, more of them beyond 8 and with several waves
+// to a group; the same by how short a pixel's run is.  Slabs: turns, which SiLU and GELU lengthen; thousands of waves times turns; turns of the sums over
+// groups (backward).  By them the choice is on average 2 % behind the faster of the two and 4 % faster than one limit of 1.5 * 2^20 elements:
+//   256x128 in 32 groups fp32, 48 images     forward 13.8 and in slabs 6.7    gradients 22.7 and 10.7
+//   100x48 in 4 bf16, 109 and 218 images     4.9 and 5.9, 7.3 and 6.4         7.9 and 8.4, 12.9 and 9.1
+//   16x512 in 32 fp32, 192 images            5.6 and 6.5                      9.4 and 11.2
+//   905x64 in 8 bf16 with GELU, 7 images, 28 slabs                            10.7 and 14.9
+inline double few_time(const GnFew &a, int pixel_bytes, bool backward) {
+  constexpr double T[2][5] = {{5.3, 0.11, 0.04, 0.026, 0.044}, {8.5, 0.09, 0.035, 0.12, 0.068}};
+  const double *t = T[backward];
+  const int turns = (a.HW + a.px - 1) / a.px;
+  const double work = (double)a.units * (a.threads / 64) * turns * 1e-3;
+  return t[0] + t[1] * turns + (a.threads > 64 ? t[2] * work + t[3] * std::max(0.0, work - 8) : 0.0) + t[4] * work * std::min(16.0 / pixel_bytes, 4.0);
 }
-inline bool gn_few(const GnShape &s, bool backward, GnFew *a) {
+inline double slab_time(const GnPlan &p, int images, bool backward) {
+  constexpr double T[2][3][5] = {{{5.8, 0.23, 0.25, 0.14, 0}, {5.5, 0.49, 0.41, 0.24, 0}, {5.4, 0.9, 0.32, 0.25, 0}},
+                                 {{8.7, 0.15, 0.5, 0.39, 0.165}, {8, 0.4, 0.55, 0.46, 0.19}, {8.1, 0.8, 0.5, 0.55, 0.19}}};
+  const double *t = T[backward][p.one ? 0 : p.whole ? 1 : 2];
+  const GnArgs &a = p.a;
+  const int turns = p.split ? 4 : (a.HW + a.px - 1) / a.px, waves = p.nt / 64;
+  const double groups = (double)images * p.slabs * (p.split ? (double)a.HW / (4.0 * a.px) : 1.0);
+  return t[0] + (t[1] + (a.act >= NF_ACT_SILU ? t[2] : 0.0)) * turns + t[3] * groups * waves * turns * 1e-3 + t[4] * ((2 * a.groups + waves - 1) / waves);
+}
+// Whether a shape goes this way: groups of up to 16 elements a thread, up to 1.5 * 2^20 in all (beyond, slabs were faster or within 10 %); always up
+// to 2^16, where a call is its launch and first fetches
+inline bool gn_few(const GnShape &s, bool backward, const GnPlan &slabs, GnFew *a) {
   a->HW = s.HW, a->C = s.C, a->G = s.G, a->Cg = s.C / s.G, a->act = s.act, a->eps = s.eps;
+  const long long elements = (long long)s.B * s.HW * s.C;
+  if (elements > 3 << 19) return false;
   a->threads = 0;
   // few elements a thread, or the most threads
   for (int nt : {64, 256, 1024})
@@ -345,14 +359,14 @@ inline bool gn_few(const GnShape &s, bool backward, GnFew *a) {
       a->threads = nt;
       break;
     }
-  if (!a->threads || (long long)s.B * s.HW * s.C > few_most(a->threads, a->Cg * (s.dtype == NF_F32 ? 4 : 2), backward)) return false;
+  if (!a->threads) return false;
   a->px = a->threads / a->Cg;
   a->share = 6;
   while (a->share > 0 && (a->Cg << a->share) > a->threads) --a->share;
   a->units = s.B * s.G;
   a->inv = (float)(1.0 / ((double)a->Cg * s.HW));
   a->div_cg = FastDiv(a->Cg), a->div_g = FastDiv(s.G), a->div_px = FastDiv(a->px);
-  return true;
+  return elements <= 1 << 16 || few_time(*a, a->Cg * (s.dtype == NF_F32 ? 4 : 2), backward) <= slab_time(slabs, s.B, backward);
 }
 // run(threads of a group, elements of a thread, workgroups, their threads), recorded under one of the names
 template <typename F>

@@ -209,13 +209,13 @@ size_t gn_workspace_bytes(const GnShape &s) {
 
 hipError_t launch_gn_fwd(const GnShape &s, const void *x, const float *gamma, const float *beta, void *y, float *mean,
                          float *rstd, void *ws, hipStream_t st) {
+  const GnPlan p = gn_plan(s, false);
   GnFew few;
-  if (gn_few(s, false, &few)) {
+  if (gn_few(s, false, p, &few)) {
     if (s.dtype == NF_BF16) return fwd_few_as<__bf16>(few, x, gamma, beta, y, mean, rstd, st);
     if (s.dtype == NF_F16) return fwd_few_as<_Float16>(few, x, gamma, beta, y, mean, rstd, st);
     return fwd_few_as<float>(few, x, gamma, beta, y, mean, rstd, st);
   }
-  const GnPlan p = gn_plan(s, false);
   return by_type(s, p, [&](auto t, auto whole, auto one) {
     return fwd_as<decltype(t), decltype(whole)::value, decltype(one)::value>(s, p, x, gamma, beta, y, mean, rstd, (float *)ws, st);
   });

@@ -281,9 +281,9 @@ hipError_t bwd_few_as(const GnFew &a, const void *dy, const void *x, const float
 hipError_t launch_gn_bwd(const GnShape &s, const void *dy, const void *x, const float *gamma, const float *beta,
                          const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta, void *ws,
                          hipStream_t st) {
-  GnFew few;
-  const bool is_few = gn_few(s, true, &few);
   const GnPlan p = gn_plan(s, true);
+  GnFew few;
+  const bool is_few = gn_few(s, true, p, &few);
   // the images' sums [B][2][C], of which one image's are the result; the chunks' lie behind
   float *const sums = (float *)ws, *const part = sums + (size_t)s.B * 2 * s.C;
   float *const sum_gx = s.B == 1 ? dgamma : sums, *const sum_g = s.B == 1 ? dbeta : sums + s.C;

@@ -81,10 +81,9 @@ def test_every_kernel_is_among_these_cases():
 
 
 @pytest.mark.parametrize("t,shape,fwd,bwd", [
-    ("f32", (384, 16, 256, 16), True, True), ("f32", (385, 16, 256, 16), False, False),          # waves
-    ("f32", (131, 50, 40, 40), True, True), ("f32", (132, 50, 40, 40), False, False),            # waves, 4 bytes of a pixel
-    ("f32", (28, 144, 96, 8), True, True), ("f32", (29, 144, 96, 8), True, False), ("f32", (38, 144, 96, 8), False, False),
-    ("bf16", (109, 100, 48, 4), True, True), ("bf16", (110, 100, 48, 4), True, False), ("bf16", (164, 100, 48, 4), False, False)])
+    ("f32", (192, 16, 512, 32), True, True), ("f32", (384, 16, 256, 16), True, True), ("f32", (385, 16, 256, 16), False, False),
+    ("f32", (48, 256, 128, 32), False, False), ("bf16", (218, 100, 48, 4), False, False), ("bf16", (7, 905, 64, 8), True, True),
+    ("bf16", (39, 105, 264, 8), True, True), ("f16", (28, 144, 96, 8), True, False), ("f32", (16, 64, 64, 8), True, True)])
 def test_both_sides_of_the_rule_for_small_groups(t, shape, fwd, bwd):
     nf.nf_prof_begin()
     try:
