@@ -5,9 +5,10 @@ namespace nf {
 namespace {
 
 // HBM-bound: 3 * sizeof(T) bytes an element.  sum_gx and sum_g, rows of 2 C floats: sums over pixels of g xh and g, of
-// every (image, chunk); APPLY reads those of the images.  64x1024x512 bf16 in 32 groups with SiLU 74.5 us, 2.7 TB/s: two rounds of
-// slabs that load, compute (36 vector instructions an element) and store in step; 33x675x72 fp16 11.9 us, the
-// latency of unaligned slabs.
+// every (image, chunk); APPLY reads those of the images.  64x1024x512 bf16 in 32 groups with SiLU 75 us, 2.7 TB/s: one workgroup of 1024 threads
+// to a CU and two rounds of them, which load, compute (36 vector instructions an element: each pass evaluates the slope) and store in
+// step, so that the times of memory and of the vector ALU add up.  33x675x72 fp16 in 12 groups 11.9 us: 99 slabs (24 channels: no
+// whole vectors in fewer) leave 157 of 256 CUs idle.
 template <typename T, bool WHOLE, bool ONE, int MODE, int R, int NTMAX>
 __global__ __launch_bounds__(NTMAX) void gn_bwd_kernel(GnArgs a, const T *__restrict__ dy, const T *__restrict__ x,
                                                        const float *__restrict__ gamma, const float *__restrict__ beta,

@@ -431,7 +431,8 @@ __device__ inline void gemm_tile(const GemmArgs &g, int id, char *lds) {
 }
 
 // Two workgroups of 128x128 or five of 64x64 to a CU, whose waits overlap.  8192x1024x1024 bf16 24 us (717 TFLOP/s), fp32 133 (129);
-// dW of 16384x2048x2048 bf16 140 (980); 22275x72x100 fp32 with its epilogue 12 us, the latency of 3 steps.
+// dW of 16384x2048x2048 bf16 140 (980); 22275x72x100 fp32 with its epilogue 12 us: a sum of 288 bytes is three steps, the last of 8 terms, that each
+// wait for memory and two barriers, and the second tile of columns holds 36 of 64.
 template <typename T, int BLOCK, int SB, bool AT, bool BT, int EPI, bool COPY>
 __global__ __launch_bounds__(LT) void gemm_kernel(GemmArgs g) {
   __shared__ __align__(1024) char lds[tile_lds<BLOCK, BLOCK, SB>()];
@@ -497,8 +498,8 @@ __device__ inline void settle_sums(floatx4 (&c)[8][N]) {
   for (int i = 0; i < 8 * N; ++i) asm volatile("" : "+a"(c[i / N][i % N]));
 }
 
-// One workgroup to a CU: dx of 16384x2048x2048 bf16 113-130 us (1060-1210 TFLOP/s, bound by the matrix pipe and one barrier a step);
-// 65536x512x512 forward 54 us, with GELU, dropout, residual and z 85 (bound by the epilogue behind the main loop).
+// One workgroup to a CU: dx of 16384x2048x2048 bf16 112 us called by itself (1230 TFLOP/s), 127-131 between dW's kernels (1050-1080), bound by the
+// matrix pipe and one barrier a step; 65536x512x512 forward 54 us, with GELU, dropout, residual and z 85 (bound by the epilogue behind the main loop).
 template <typename T, bool AT, bool BT, int EPI>
 __global__ __launch_bounds__(WT, 2) void gemm_wide_kernel(GemmArgs g) {
   using A = StagedWide<T, AT>;
