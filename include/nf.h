@@ -331,10 +331,10 @@ int32_t nf_select_exit(int32_t n_exits, const int64_t *n_correct, const int64_t 
  * The operators around a 1x1 layer of channels-last activations, forward and backward, in three types: a
  * dtype of NF_F32, NF_BF16 or NF_F16 is that of the activations and of the weights W; biases, gamma, beta,
  * statistics and the gradients of parameters are fp32.  Products, sums, statistics and activations are formed
- * in fp32 (an activation of a 16-bit type may be off by 8e-6 of its argument) and each result is rounded once.  Rows are dense.  Every pointer is 16-byte aligned at its base; rows
- * need no alignment (any K, N, C, cols, n).  A workspace of 0 bytes may be NULL.  Outputs must not overlap
- * inputs, but for dropout's y, which may be x or r (and dx, which may be dy).  Results do not depend on the order
- * in which workgroups run. */
+ * in fp32 (an activation of a 16-bit type may be off by 8e-6 of its argument) and each result is rounded once.
+ * Rows are dense.  Every pointer is 16-byte aligned at its base; rows need no alignment (any K, N, C, cols, n).
+ * A workspace of 0 bytes may be NULL.  Outputs must not overlap inputs, but for dropout's y, which may be x or
+ * r (and dx, which may be dy).  Results do not depend on the order in which workgroups run. */
 enum { NF_F32 = 0, NF_BF16 = 1, NF_F16 = 2 };
 /* relu: max(v, 0), its slope at 0 is 0; silu: v / (1 + e^-v); gelu: v Phi(v), Phi the normal distribution's.  At infinities they
  * and their slopes are the limits (inf and 0, 1 and 0). */
