@@ -43,14 +43,14 @@ def test_training_from_a_quantised_cache(fmt, p):
     assert all(0 < v < 10 for v in losses) and losses[-1] < 0.7 * losses[0], losses
 
 
-@pytest.mark.parametrize("B", [1, 31, 48, 63])
+@pytest.mark.parametrize("B", [1, 31, 41, 47])
 def test_a_smaller_batch_than_the_blocks(B):
-    """A block of 64 maps on fewer: all calls run in its workspace, to the bits that a block of that batch gives."""
+    """A block of 48 maps on fewer: all calls run in its workspace, to the bits that a block of that batch gives."""
     from paper_2402_14139_amd.pointwise import PointwiseBlock
-    args = dict(HW=64, C=64, H=128, groups=8, p=0.1, seed=2)
-    large, own = PointwiseBlock(nf.NF_BF16, 64, **args), PointwiseBlock(nf.NF_BF16, B, **args)
+    args = dict(HW=49, C=72, H=100, groups=12, p=0.1, seed=2)
+    large, own = PointwiseBlock(nf.NF_BF16, 48, **args), PointwiseBlock(nf.NF_BF16, B, **args)
     g = torch.Generator().manual_seed(B)
-    x, dy = (torch.randn(B, 64, 64, generator=g).bfloat16().cuda() for _ in range(2))
+    x, dy = (torch.randn(B, 49, 72, generator=g).bfloat16().cuda() for _ in range(2))
     for b in (large, own):
         b.out = b.forward(x, 3).clone(), b.backward(x, dy, 3).clone()
     assert all(torch.equal(u, v) for u, v in zip(large.out, own.out))

@@ -74,7 +74,7 @@ def test_good_arguments_reach_the_kernels(no_kernels):
 
 
 @pytest.mark.parametrize("dtype", [nf.NF_F32, nf.NF_BF16, nf.NF_F16])
-@pytest.mark.parametrize("B,HW,C,H,G", [(64, 64, 64, 128, 8), (48, 100, 72, 100, 12), (9, 4096, 32, 64, 4), (33, 675, 72, 100, 12),
+@pytest.mark.parametrize("B,HW,C,H,G", [(48, 49, 72, 100, 12), (40, 100, 72, 144, 12), (9, 4096, 32, 64, 4), (33, 675, 72, 100, 12),
                                         (100, 16, 512, 512, 32), (3, 1 << 16, 16, 32, 2)])
 def test_workspace_holds_every_batch(dtype, B, HW, C, H, G):
     norm = nf.GroupNormDesc(dtype=dtype, C=C, G=G, act=0, HW=HW, eps=1e-5)
@@ -86,7 +86,7 @@ def test_workspace_holds_every_batch(dtype, B, HW, C, H, G):
 
 
 def test_a_smaller_batch_may_want_more():
-    """What the sizing is for: 48 maps of 64 pixels want more than 64 and more than one."""
-    up = nf.LinearDesc(dtype=nf.NF_BF16, K=64, N=128, act=0)
-    need = {b: nf.nf_linear_workspace_bytes(up, b * 64) for b in (1, 48, 64)}
-    assert need[48] > max(need[1], need[64])
+    """What the sizing is for: 41 maps of 49 pixels want more than 48 and more than one."""
+    up, down = nf.LinearDesc(dtype=nf.NF_BF16, K=72, N=100, act=0), nf.LinearDesc(dtype=nf.NF_BF16, K=100, N=72, act=0)
+    need = {b: max(nf.nf_linear_workspace_bytes(d, b * 49) for d in (up, down)) for b in (1, 41, 48)}
+    assert need[41] > max(need[1], need[48])
