@@ -212,12 +212,12 @@ def _plan(s):
         s["ws"] = room(nf.nf_layernorm_workspace_bytes(s["d"], c["M"])) if k == "ln_bwd" else None
     elif k == "mx_fwd":
         s["d"] = nf.LinearDesc(dtype=s["dt"], K=c["K"], N=c["N"], act=ACTS.index(c["act"]))
-        s["ws"] = room(nf.nf_mx4_linear_workspace_bytes(s["d"], c["M"]))
+        s["ws"] = room(nf.nf_mx_linear_workspace_bytes(s["d"], c["M"]))
     elif k == "mx_bwd":
         M, K, N = c["M"], c["K"], c["N"]
         s["for_dx"] = nf.LinearDesc(dtype=s["dt"], K=N, N=K, act=nf.NF_ACT_NONE)
         s["for_dW"] = nf.LinearDesc(dtype=nf.NF_F32, K=M, N=K, act=nf.NF_ACT_NONE)
-        s["ws"] = room(max(nf.nf_mx4_product_workspace_bytes(s["for_dx"], M), nf.nf_mx4_product_workspace_bytes(s["for_dW"], N)))
+        s["ws"] = room(max(nf.nf_mx_product_workspace_bytes(s["for_dx"], M), nf.nf_mx_product_workspace_bytes(s["for_dW"], N)))
         s["dz_rows"], s["dz_cols"], s["x_cols"] = held(M, N), held(N, M), held(K, M)
     else:
         s["orth"] = nf.orth_desc([COEF] * STEPS, ORTH_EPS)
@@ -237,14 +237,14 @@ def _run_own(s):
         nf.nf_layernorm_bwd(s["d"], c["M"], s["dy"], s["x"], s["gamma"], s["mean"], s["rstd"], s["dr"], s["dx"], s["dgamma"], s["dbeta"], s["ws"])
         return [s["dx"], s["dgamma"], s["dbeta"]]
     if k == "mx_fwd":
-        nf.nf_mx4_linear_fwd(s["d"], c["M"], s["x"], *s["w"], s["b"], s["r"], None, s["y"], None, s["ws"])
+        nf.nf_mx_linear_fwd(s["d"], c["M"], s["x"], *s["w"], s["b"], s["r"], None, s["y"], None, s["ws"])
         return [s["y"]]
     if k == "mx_bwd":
         M, K, N = c["M"], c["K"], c["N"]
-        nf.nf_mx4_quantise(s["dt"], M, N, s["dz"], *s["dz_rows"], *s["dz_cols"])
-        nf.nf_mx4_quantise(s["dt"], M, K, s["x"], None, None, *s["x_cols"])
-        nf.nf_mx4_product(s["for_dx"], M, *s["dz_rows"], *s["w_t"], None, None, s["dx"], s["ws"])
-        nf.nf_mx4_product(s["for_dW"], N, *s["dz_cols"], *s["x_cols"], None, None, s["dW"], s["ws"])
+        nf.nf_mx_quantise(s["dt"], M, N, s["dz"], *s["dz_rows"], *s["dz_cols"])
+        nf.nf_mx_quantise(s["dt"], M, K, s["x"], None, None, *s["x_cols"])
+        nf.nf_mx_product(s["for_dx"], M, *s["dz_rows"], *s["w_t"], None, None, s["dx"], s["ws"])
+        nf.nf_mx_product(s["for_dW"], N, *s["dz_cols"], *s["x_cols"], None, None, s["dW"], s["ws"])
         return [s["dx"], s["dW"]]
     if k == "orth":
         nf.nf_orthogonalise(s["orth"], s["dt"], [s["g"]], [s["y"]], s["ws"])
