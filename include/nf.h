@@ -327,7 +327,7 @@ int32_t nf_block_evaluate(const nf_block *blk, int32_t exit_layer, int32_t B, in
                           int32_t *pred_out, int32_t *n_correct, void *ws, size_t ws_bytes, void *stream);
 int32_t nf_select_exit(int32_t n_exits, const int64_t *n_correct, const int64_t *n_params, int32_t *exit_out);
 
-/* ---- pointwise layers: linear with a fused epilogue, group norm, dropout, a quantised cache --------------
+/* ---- pointwise layers: linear with a fused epilogue, group and layer norm, dropout, a quantised cache ----
  * The operators around a 1x1 layer of channels-last activations, forward and backward, in three types: a
  * dtype of NF_F32, NF_BF16 or NF_F16 is that of the activations and of the weights W; biases, gamma, beta,
  * statistics and the gradients of parameters are fp32.  Products, sums, statistics and activations are formed
@@ -398,6 +398,24 @@ int32_t nf_groupnorm_fwd(const nf_groupnorm_desc *d, int32_t B, const void *x, c
 int32_t nf_groupnorm_bwd(const nf_groupnorm_desc *d, int32_t B, const void *dy, const void *x, const float *gamma,
                          const float *beta, const float *mean, const float *rstd, void *dx, float *dgamma,
                          float *dbeta, void *ws, size_t ws_bytes, void *stream);
+
+/* Layer norm over the rows of x [M][C].  1 <= M < 2^40, C <= 2^16, eps >= 0. */
+typedef struct {
+  int32_t dtype, C;
+  float eps;
+} nf_layernorm_desc;
+/* What nf_layernorm_bwd wants for dgamma and dbeta (the forward wants none).  Not steady in M. */
+int32_t nf_layernorm_workspace_bytes(const nf_layernorm_desc *d, int64_t M, size_t *out);
+/* y = (x - mean) rstd gamma + beta, rstd = (var + eps)^-1/2, var the mean square about the mean.  gamma (else 1) and beta (else 0)
+ * may be NULL; mean and rstd [M] are written unless both are NULL.  y may be x. */
+int32_t nf_layernorm_fwd(const nf_layernorm_desc *d, int64_t M, const void *x, const float *gamma, const float *beta,
+                         void *y, float *mean, float *rstd, void *stream);
+/* With xh = (x - mean) rstd and g = dy gamma: dx = rstd (g - avg(g) - xh avg(g xh)) + dr, averages over the row; dgamma = sum dy xh,
+ * dbeta = sum dy over the rows.  mean and rstd are what the forward wrote.  gamma may be NULL (1), dr too (a residual path's
+ * gradient, read in the same pass; dx may be dy or dr).  Any of dx, dgamma, dbeta may be NULL, not all; ws is wanted where dgamma or dbeta is given. */
+int32_t nf_layernorm_bwd(const nf_layernorm_desc *d, int64_t M, const void *dy, const void *x, const float *gamma,
+                         const float *mean, const float *rstd, const void *dr, void *dx, float *dgamma, float *dbeta,
+                         void *ws, size_t ws_bytes, void *stream);
 
 /* The activation cache in 8 or 4 bits an element.  A row of n elements is cut into groups of 32 (the last may be
  * shorter); group j has the exponent byte scales[row][j] = E + 127 and its elements are code * 2^E:

@@ -28,7 +28,8 @@ EXPORTS = ("nf_strerror", "nf_layer_out_dims", "nf_workspace_bytes", "nf_layer_f
            "nf_device_info", "nf_local_step_static", "nf_contraction", "nf_block_graph_create",
            "nf_block_graph_launch", "nf_block_graph_destroy", "nf_dropout_fwd", "nf_dropout_bwd",
            "nf_linear_workspace_bytes", "nf_linear_fwd_workspace_bytes", "nf_linear_fwd", "nf_linear_bwd_epilogue", "nf_linear_bwd",
-           "nf_groupnorm_workspace_bytes", "nf_groupnorm_fwd_workspace_bytes", "nf_groupnorm_fwd", "nf_groupnorm_bwd", "nf_qcache_row_bytes",
+           "nf_groupnorm_workspace_bytes", "nf_groupnorm_fwd_workspace_bytes", "nf_groupnorm_fwd", "nf_groupnorm_bwd", "nf_layernorm_workspace_bytes",
+           "nf_layernorm_fwd", "nf_layernorm_bwd", "nf_qcache_row_bytes",
            "nf_qcache_write", "nf_qcache_read")
 
 NF_WS_AUX_ACT, NF_WS_POOL_ARG, NF_WS_HEAD_ARG = 0, 1, 2
@@ -85,6 +86,10 @@ class LinearDesc(C.Structure):
 
 class GroupNormDesc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "C", "G", "act", "HW")] + [("eps", C.c_float)]
+
+
+class LayerNormDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("C", C.c_int32), ("eps", C.c_float)]
 
 
 class LinearModel(C.Structure):
@@ -182,6 +187,9 @@ def lib():
         L.nf_groupnorm_fwd_workspace_bytes.argtypes = L.nf_groupnorm_workspace_bytes.argtypes
         L.nf_groupnorm_fwd.argtypes = [C.POINTER(GroupNormDesc), i32, ptr, ptr, ptr, ptr, ptr, ptr, ptr, size, ptr]
         L.nf_groupnorm_bwd.argtypes = [C.POINTER(GroupNormDesc), i32] + [ptr] * 10 + [size, ptr]
+        L.nf_layernorm_workspace_bytes.argtypes = [C.POINTER(LayerNormDesc), i64, C.POINTER(size)]
+        L.nf_layernorm_fwd.argtypes = [C.POINTER(LayerNormDesc), i64] + [ptr] * 7
+        L.nf_layernorm_bwd.argtypes = [C.POINTER(LayerNormDesc), i64] + [ptr] * 10 + [size, ptr]
         L.nf_qcache_row_bytes.argtypes = [i32, i64, C.POINTER(size), C.POINTER(size)]
         L.nf_qcache_write.argtypes = [i32, i32, ptr, ptr, ptr, i64, i64, i64, i32, ptr, ptr, ptr]
         L.nf_qcache_read.argtypes = [i32, i32, ptr, ptr, ptr, i64, i64, i64, ptr, i32, ptr, ptr, ptr]
@@ -540,6 +548,23 @@ def nf_groupnorm_bwd(d: GroupNormDesc, B, dy, x, gamma, beta, mean, rstd, dx, dg
     wp, wn = _ws(ws)
     _check(lib().nf_groupnorm_bwd(_ref(d), B, _ptr(dy), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd),
                                   _ptr(dx), _ptr(dgamma), _ptr(dbeta), wp, wn, _stream(stream)), "nf_groupnorm_bwd")
+
+
+def nf_layernorm_workspace_bytes(d: LayerNormDesc, M: int) -> int:
+    out = C.c_size_t()
+    _check(lib().nf_layernorm_workspace_bytes(_ref(d), M, C.byref(out)), "nf_layernorm_workspace_bytes")
+    return int(out.value)
+
+
+def nf_layernorm_fwd(d: LayerNormDesc, M, x, gamma, beta, y, mean, rstd, stream=None):
+    _check(lib().nf_layernorm_fwd(_ref(d), M, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
+                                  _stream(stream)), "nf_layernorm_fwd")
+
+
+def nf_layernorm_bwd(d: LayerNormDesc, M, dy, x, gamma, mean, rstd, dr, dx, dgamma, dbeta, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check(lib().nf_layernorm_bwd(_ref(d), M, _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dr), _ptr(dx),
+                                  _ptr(dgamma), _ptr(dbeta), wp, wn, _stream(stream)), "nf_layernorm_bwd")
 
 
 def nf_qcache_row_bytes(fmt: int, n: int):

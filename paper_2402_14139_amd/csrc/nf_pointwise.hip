@@ -56,6 +56,14 @@ int32_t check_groupnorm(const nf_groupnorm_desc *d, int32_t B, GnShape *s) {
   return NF_OK;
 }
 
+int32_t check_layernorm(const nf_layernorm_desc *d, int64_t M, LnShape *s) {
+  if (!d) return NF_ERR_NULL;
+  if (!dtype_ok(d->dtype) || d->C <= 0 || M <= 0 || !(d->eps >= 0.f)) return NF_ERR_BAD_DESC;
+  if (d->C > (1 << 16) || M >= (1ll << 40)) return NF_ERR_UNSUPPORTED;
+  *s = LnShape{d->dtype, M, d->C, d->eps};
+  return NF_OK;
+}
+
 int32_t check_qcache(int32_t format, int32_t dtype, const void *codes, const void *scales, const void *clab,
                      int64_t capacity, int64_t n, int64_t first, int32_t B, const void *buf, const void *lab, bool by_index,
                      QcacheRows *q) {
@@ -203,6 +211,41 @@ int32_t nf_groupnorm_bwd(const nf_groupnorm_desc *d, int32_t B, const void *dy, 
   if ((rc = check_ws(ws, ws_bytes, gn_workspace_bytes(s)))) return rc;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   NF_HIP(launch_gn_bwd(s, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, ws, st));
+  return NF_OK;
+}
+
+int32_t nf_layernorm_workspace_bytes(const nf_layernorm_desc *d, int64_t M, size_t *out) {
+  LnShape s;
+  const int32_t rc = check_layernorm(d, M, &s);
+  if (rc) return rc;
+  if (!out) return NF_ERR_NULL;
+  *out = ln_workspace_bytes(s);
+  return NF_OK;
+}
+
+int32_t nf_layernorm_fwd(const nf_layernorm_desc *d, int64_t M, const void *x, const float *gamma, const float *beta,
+                         void *y, float *mean, float *rstd, void *stream) {
+  LnShape s;
+  const int32_t rc = check_layernorm(d, M, &s);
+  if (rc) return rc;
+  if (!x || !y || (mean == nullptr) != (rstd == nullptr)) return NF_ERR_NULL;
+  if (!all_aligned16(x, gamma, beta, y, mean, rstd)) return NF_ERR_BAD_DESC;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  NF_HIP(launch_ln_fwd(s, x, gamma, beta, y, mean, rstd, st));
+  return NF_OK;
+}
+
+int32_t nf_layernorm_bwd(const nf_layernorm_desc *d, int64_t M, const void *dy, const void *x, const float *gamma,
+                         const float *mean, const float *rstd, const void *dr, void *dx, float *dgamma, float *dbeta,
+                         void *ws, size_t ws_bytes, void *stream) {
+  LnShape s;
+  int32_t rc = check_layernorm(d, M, &s);
+  if (rc) return rc;
+  if (!dy || !x || !mean || !rstd || (!dx && !dgamma && !dbeta)) return NF_ERR_NULL;
+  if (!all_aligned16(dy, x, gamma, mean, rstd, dr, dx, dgamma, dbeta)) return NF_ERR_BAD_DESC;
+  if ((dgamma || dbeta) && (rc = check_ws(ws, ws_bytes, ln_workspace_bytes(s)))) return rc;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  NF_HIP(launch_ln_bwd(s, dy, x, gamma, mean, rstd, dr, dx, dgamma, dbeta, ws, st));
   return NF_OK;
 }
 

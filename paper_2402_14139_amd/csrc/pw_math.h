@@ -230,6 +230,17 @@ hipError_t launch_gn_bwd(const GnShape &s, const void *dy, const void *x, const 
                          const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta, void *ws,
                          hipStream_t st);
 
+struct LnShape {
+  int dtype;
+  long long M;
+  int C;
+  float eps;
+};
+size_t ln_workspace_bytes(const LnShape &s);
+hipError_t launch_ln_fwd(const LnShape &s, const void *x, const float *gamma, const float *beta, void *y, float *mean, float *rstd, hipStream_t st);
+hipError_t launch_ln_bwd(const LnShape &s, const void *dy, const void *x, const float *gamma, const float *mean, const float *rstd, const void *dr, void *dx,
+                         float *dgamma, float *dbeta, void *ws, hipStream_t st);
+
 struct LinearCall {
   int dtype, act;
   long long M;
