@@ -436,6 +436,28 @@ int32_t nf_qcache_read(int32_t format, int32_t dtype, const uint8_t *codes, cons
                        const int32_t *cache_labels, int64_t capacity, int64_t n, int64_t first, const int64_t *idx,
                        int32_t B, void *x_out, int32_t *labels_out, void *stream);
 
+/* Matrices in 4 bits, and their products.  A matrix [rows][cols] is held as the rows of an NF_Q_E2M1 cache of n = cols (the same codes, exponents and
+ * row strides: nf_qcache_row_bytes; nf_qcache_write fills and nf_qcache_read reads one, too).  nf_mx_quantise writes x [rows][cols], of
+ * type dtype, by rows into codes and scales, and by columns, that is as the matrix [cols][rows], into codes_t and scales_t; either pair may be
+ * NULL.  Codes behind a row's last element, up to a whole group, are 0; other bytes between a row's end and its stride are left as they
+ * are, and products read none of them as numbers.  Rows and columns beyond 2^44 elements in all: NF_ERR_UNSUPPORTED. */
+int32_t nf_mx_quantise(int32_t dtype, int64_t rows, int64_t cols, const void *x, uint8_t *codes, uint8_t *scales,
+                       uint8_t *codes_t, uint8_t *scales_t, void *stream);
+/* y = r + act(a b^T + bias) [M][N]: a holds M rows of K, b N rows of K, both in 4 bits; d->dtype is that of y and r; bias and r may be
+ * NULL.  Sums are fp32 (a group that reads back as NaN makes its results NaN).  A linear layer's gradients are such products, each operand
+ * quantised along the axis that is summed over: dx = product(dz by rows, W by columns), dW = product(dz by columns, x by columns).
+ * 1 <= M < 2^31 - 512, N <= 2^20, K <= 2^24, and the tiles of 64 along M times those along N stay below 2^23. */
+int32_t nf_mx_product_workspace_bytes(const nf_linear_desc *d, int64_t M, size_t *out);
+int32_t nf_mx_product(const nf_linear_desc *d, int64_t M, const uint8_t *a, const uint8_t *a_scales, const uint8_t *b,
+                      const uint8_t *b_scales, const float *bias, const void *r, void *y, void *ws, size_t ws_bytes,
+                      void *stream);
+/* nf_linear_fwd with W [N][K] in 4 bits: x [M][K], of type dtype, is quantised by rows on the way (up to 32 rows within the product's
+ * launch, else into the workspace).  b, r, drop, z as there.  The results are those of nf_mx_quantise and nf_mx_product. */
+int32_t nf_mx_linear_workspace_bytes(const nf_linear_desc *d, int64_t M, size_t *out);
+int32_t nf_mx_linear_fwd(const nf_linear_desc *d, int64_t M, const void *x, const uint8_t *W, const uint8_t *W_scales,
+                         const float *b, const void *r, const nf_dropout_desc *drop, void *y, void *z, void *ws,
+                         size_t ws_bytes, void *stream);
+
 /* ---- Profiler and Partitioner ("Modules", Algorithm 1): host functions, no device work ---------
  * The Profiler's measured memory is replaced by the exact device bytes of one local step with
  * this library: parameters + gradients (+ momentum buffers) of the layer and its head, the input,

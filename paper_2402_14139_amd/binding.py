@@ -30,7 +30,8 @@ EXPORTS = ("nf_strerror", "nf_layer_out_dims", "nf_workspace_bytes", "nf_layer_f
            "nf_linear_workspace_bytes", "nf_linear_fwd_workspace_bytes", "nf_linear_fwd", "nf_linear_bwd_epilogue", "nf_linear_bwd",
            "nf_groupnorm_workspace_bytes", "nf_groupnorm_fwd_workspace_bytes", "nf_groupnorm_fwd", "nf_groupnorm_bwd", "nf_layernorm_workspace_bytes",
            "nf_layernorm_fwd", "nf_layernorm_bwd", "nf_qcache_row_bytes",
-           "nf_qcache_write", "nf_qcache_read")
+           "nf_qcache_write", "nf_qcache_read", "nf_mx_quantise", "nf_mx_product_workspace_bytes", "nf_mx_product",
+           "nf_mx_linear_workspace_bytes", "nf_mx_linear_fwd")
 
 NF_WS_AUX_ACT, NF_WS_POOL_ARG, NF_WS_HEAD_ARG = 0, 1, 2
 NF_HEAD_POOL_AVG, NF_HEAD_POOL_MAX = 0, 1
@@ -193,6 +194,10 @@ def lib():
         L.nf_qcache_row_bytes.argtypes = [i32, i64, C.POINTER(size), C.POINTER(size)]
         L.nf_qcache_write.argtypes = [i32, i32, ptr, ptr, ptr, i64, i64, i64, i32, ptr, ptr, ptr]
         L.nf_qcache_read.argtypes = [i32, i32, ptr, ptr, ptr, i64, i64, i64, ptr, i32, ptr, ptr, ptr]
+        L.nf_mx_quantise.argtypes = [i32, i64, i64, ptr, ptr, ptr, ptr, ptr, ptr]
+        L.nf_mx_product_workspace_bytes.argtypes = L.nf_mx_linear_workspace_bytes.argtypes = [C.POINTER(LinearDesc), i64, C.POINTER(size)]
+        L.nf_mx_product.argtypes = [C.POINTER(LinearDesc), i64] + [ptr] * 8 + [size, ptr]
+        L.nf_mx_linear_fwd.argtypes = [C.POINTER(LinearDesc), i64, ptr, ptr, ptr, ptr, ptr, C.POINTER(DropoutDesc), ptr, ptr, ptr, size, ptr]
         _lib = L
     return _lib
 
@@ -582,3 +587,35 @@ def nf_qcache_write(fmt, dtype, codes, scales, cache_labels, capacity, n, first,
 def nf_qcache_read(fmt, dtype, codes, scales, cache_labels, capacity, n, first, idx, B, x_out, labels_out, stream=None):
     _check(lib().nf_qcache_read(fmt, dtype, _ptr(codes), _ptr(scales), _ptr(cache_labels), capacity, n, first,
                                 _ptr(idx), B, _ptr(x_out), _ptr(labels_out), _stream(stream)), "nf_qcache_read")
+
+
+# ---- matrices in 4 bits ----
+
+def nf_mx_quantise(dtype, rows, cols, x, codes, scales, codes_t, scales_t, stream=None):
+    """By rows into ``codes`` and ``scales``, by columns into ``codes_t`` and ``scales_t``; either pair may be None."""
+    _check(lib().nf_mx_quantise(dtype, rows, cols, _ptr(x), _ptr(codes), _ptr(scales), _ptr(codes_t), _ptr(scales_t),
+                                _stream(stream)), "nf_mx_quantise")
+
+
+def nf_mx_product_workspace_bytes(d: LinearDesc, M: int) -> int:
+    out = C.c_size_t()
+    _check(lib().nf_mx_product_workspace_bytes(_ref(d), M, C.byref(out)), "nf_mx_product_workspace_bytes")
+    return int(out.value)
+
+
+def nf_mx_product(d: LinearDesc, M, a, a_scales, b, b_scales, bias, r, y, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check(lib().nf_mx_product(_ref(d), M, _ptr(a), _ptr(a_scales), _ptr(b), _ptr(b_scales), _ptr(bias), _ptr(r), _ptr(y),
+                               wp, wn, _stream(stream)), "nf_mx_product")
+
+
+def nf_mx_linear_workspace_bytes(d: LinearDesc, M: int) -> int:
+    out = C.c_size_t()
+    _check(lib().nf_mx_linear_workspace_bytes(_ref(d), M, C.byref(out)), "nf_mx_linear_workspace_bytes")
+    return int(out.value)
+
+
+def nf_mx_linear_fwd(d: LinearDesc, M, x, W, W_scales, b, r, drop, y, z, ws, stream=None):
+    wp, wn = _ws(ws)
+    _check(lib().nf_mx_linear_fwd(_ref(d), M, _ptr(x), _ptr(W), _ptr(W_scales), _ptr(b), _ptr(r), _ref(drop), _ptr(y),
+                                  _ptr(z), wp, wn, _stream(stream)), "nf_mx_linear_fwd")

@@ -1,0 +1,440 @@
+// Matrices in 4 bits an element with an exponent to every 32 (rows as those of the e2m1 cache): quantisation by rows and by columns, and
+// products of two such matrices, y = r + D(act(a b^T + bias)), on the scaled matrix instructions.
+#include <algorithm>
+
+#include "linear.h"
+#include "nf_enqueue.h"
+#include "q_codes.h"
+
+namespace nf {
+namespace {
+
+constexpr int QT = 256;
+
+// ---- quantisation ----
+// A tile of 128 rows x 64 columns to a workgroup: a thread reads pieces of 8 elements, 4 neighbours of a row share an exponent and write their
+// codes; for the columns the tile goes through LDS as it lies, and a thread takes 32 rows of a column.  Memory-bound: sizeof(T) and 1/2 + 1/32
+// bytes an element, twice the latter where both forms are wanted.
+constexpr int TR = 128, TC = 64;
+
+struct QuantArgs {
+  long long rows, cols, tiles_c;
+  uint8_t *codes, *scales, *codes_t, *scales_t;  // one pair may be null
+  long long cb, sb, cbt, sbt;                    // row strides
+};
+
+template <typename T, bool BY_ROWS, bool BY_COLS>
+__global__ __launch_bounds__(QT) void mx_quantise_kernel(QuantArgs a, const T *__restrict__ x) {
+  constexpr int LD = TC + 4 / sizeof(T);
+  __shared__ T lds[BY_COLS ? TR * LD : 1];
+  const long long tr = blockIdx.x / a.tiles_c, r0 = tr * TR, c0 = (blockIdx.x - tr * a.tiles_c) * TC;
+  const int j = threadIdx.x & 7, down = threadIdx.x >> 3;
+  const long long col = c0 + 8 * j;
+  const int n = (int)min(max(a.cols - col, 0ll), 8ll);
+  Raw8<T> raw[TR / 32] = {};
+#pragma unroll
+  for (int k = 0; k < TR / 32; ++k) {
+    const long long row = r0 + k * 32 + down;
+    if (row < a.rows && n > 0) raw[k] = raw8(x + row * a.cols + col, n);
+  }
+#pragma unroll
+  for (int k = 0; k < TR / 32; ++k) {
+    const long long row = r0 + k * 32 + down;
+    if constexpr (BY_COLS) __builtin_memcpy(&lds[(k * 32 + down) * LD + 8 * j], &raw[k], sizeof(raw[k]));
+    if constexpr (BY_ROWS) {
+      float v[8], top = 0.f;
+      unpack8(raw[k], v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fabsf(v[e]) <= INFINITY ? fmaxf(top, fabsf(v[e])) : INFINITY;  // a NaN counts as infinite
+      top = fmaxf(top, __shfl_xor(top, 1));
+      top = fmaxf(top, __shfl_xor(top, 2));
+      const int eb = exponent_byte<NF_Q_E2M1>(top);
+      uint32_t w[2] = {0, 0};
+      if (eb < 255) encode8<NF_Q_E2M1>(v, eb - 127, w);
+      if (row < a.rows && (col & ~31ll) < a.cols) {  // whole groups: zeros behind the last element
+        *reinterpret_cast<uint32_t *>(a.codes + row * a.cb + col / 2) = w[0];
+        if ((j & 3) == 0) a.scales[row * a.sb + col / GROUP] = (uint8_t)eb;
+      }
+    }
+  }
+  if constexpr (BY_COLS) {
+    __syncthreads();
+    const int c = threadIdx.x & 63, k = threadIdx.x >> 6;
+    const long long first = r0 + k * 32;
+    if (c0 + c >= a.cols || first >= a.rows) return;
+    float v[4][8], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float t = (float)lds[(k * 32 + i) * LD + c];
+      v[i >> 3][i & 7] = t;
+      top = fabsf(t) <= INFINITY ? fmaxf(top, fabsf(t)) : INFINITY;
+    }
+    const int eb = exponent_byte<NF_Q_E2M1>(top);
+    uintx4 out = {0, 0, 0, 0};
+    if (eb < 255) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        uint32_t w[2];
+        encode8<NF_Q_E2M1>(v[h], eb - 127, w);
+        out[h] = w[0];
+      }
+    }
+    *reinterpret_cast<uintx4 *>(a.codes_t + (c0 + c) * a.cbt + first / 2) = out;
+    a.scales_t[(c0 + c) * a.sbt + first / GROUP] = (uint8_t)eb;
+  }
+}
+
+// ---- products ----
+// results[r][c] = sum over groups g of 2^(Ea + Eb) sum over a group's elements of a b.  One 16x16x128 instruction takes 16 rows of each operand by 4
+// groups: lane l holds group l / 16 of row l % 16, 16 bytes, and its exponent byte.  A group that held no number has the exponent byte 255,
+// which the instruction reads as NaN.
+using intx8 = __attribute__((ext_vector_type(8))) int;
+
+__device__ inline floatx4 mx_mfma(const uintx4 &a, uint32_t sa, const uintx4 &b, uint32_t sb, floatx4 c) {
+  const intx8 x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, (int)sa, 0, (int)sb);  // 4: e2m1; exponents in the low byte
+}
+
+struct MxArgs {
+  GemmArgs g;  // strides of codes; L = groups, per = groups of a split
+  const uint8_t *sa, *sb;
+  long long lsa, lsb;
+  int K;
+};
+
+// the codes of a row's last group, of which n elements count
+__device__ inline uintx4 first_codes(uintx4 v, int n) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int k = n - 8 * w;
+    v[w] &= k >= 8 ? ~0u : k <= 0 ? 0u : (1u << 4 * k) - 1;
+  }
+  return v;
+}
+
+// 4 bytes per lane from memory to LDS at `to` + 4 * lane
+__device__ inline void copy4(const uintx4 &buf, uint32_t voff, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(buf) : "memory");
+}
+
+// A tile of BLOCK x BLOCK by four waves of BLOCK/2 x BLOCK/2; a step is 8 groups of the sum: 128 bytes of codes and 8 of exponents to a row.  A row's chunks
+// of 16 bytes (groups) are exchanged in LDS so that the 16 rows of a fragment's read lie in different banks.
+constexpr int STEP = 8;  // groups
+template <int BLOCK>
+struct MxTile {
+  static constexpr int CODES = BLOCK * 128, SCALES = BLOCK * STEP, STAGE = 2 * (CODES + SCALES), PIECES = BLOCK / 32;
+};
+__device__ inline int mx_swizzle(int row) { return (row >> 1) & 7; }
+
+template <typename T, int BLOCK>
+__global__ __launch_bounds__(LT) void mx_gemm_kernel(MxArgs m) {
+  using S = MxTile<BLOCK>;
+  constexpr int MT = BLOCK / 32, PIECES = S::PIECES;
+  __shared__ __align__(1024) char lds[2 * S::STAGE];
+  const GemmArgs &g = m.g;
+  const int id = xcd_run(blockIdx.x, gridDim.x);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, q = lane >> 4;
+  const int split = id / g.tiles, tile = id - split * g.tiles, tr = tile / g.tiles_c;
+  const long long r0 = (long long)tr * BLOCK, l0 = split * g.per, l1 = min(g.L, l0 + g.per);
+  const int c0 = (tile - tr * g.tiles_c) * BLOCK;
+  const int steps = (int)((l1 - l0 + STEP - 1) / STEP);
+  const long long rows_left = g.R - r0;
+  const int cols_left = g.C - c0;
+  // what this lane brings: chunks of codes, and a word of exponents of each operand (tiles of 64: waves 0 and 1 of A's, 2 and 3 of B's)
+  uint32_t av[PIECES], bv[PIECES];
+  int chunk[PIECES];
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    const int at = (p * 4 + wave) * 64 + lane, row = at >> 3;
+    chunk[p] = (at & 7) ^ mx_swizzle(row);
+    av[p] = row < rows_left ? (uint32_t)(row * g.lda + chunk[p] * 16) : OUTSIDE;
+    bv[p] = row < cols_left ? (uint32_t)(row * g.ldb + chunk[p] * 16) : OUTSIDE;
+  }
+  const int srow = BLOCK == 128 ? tid >> 1 : (tid & 127) >> 1;
+  const uint32_t half = (tid & 1) * 4;
+  const uint32_t sav = srow < rows_left ? (uint32_t)(srow * m.lsa) + half : OUTSIDE, sbv = srow < cols_left ? (uint32_t)(srow * m.lsb) + half : OUTSIDE;
+  const char *const pa = g.a + r0 * g.lda + l0 * 16, *const pb = g.b + c0 * g.ldb + l0 * 16;
+  const char *const psa = (const char *)m.sa + r0 * m.lsa + l0, *const psb = (const char *)m.sb + c0 * m.lsb + l0;
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+  auto fetch = [&](int s, int stage) {
+    const int inside = (int)(l1 - l0) - s * STEP;  // groups of this step
+    const uintx4 ba = buffer_of(pa + s * 128ll), bb = buffer_of(pb + s * 128ll);
+    const uint32_t to = base + stage * S::STAGE;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) copy16(ba, chunk[p] < inside ? av[p] : OUTSIDE, to + (p * 4 + wave) * 1024);
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) copy16(bb, chunk[p] < inside ? bv[p] : OUTSIDE, to + S::CODES + (p * 4 + wave) * 1024);
+    if constexpr (BLOCK == 128) {
+      copy4(buffer_of(psa + s * STEP), sav, to + 2 * S::CODES + wave * 256);
+      copy4(buffer_of(psb + s * STEP), sbv, to + 2 * S::CODES + S::SCALES + wave * 256);
+    } else {
+      copy4(buffer_of((wave < 2 ? psa : psb) + s * STEP), wave < 2 ? sav : sbv, to + 2 * S::CODES + wave * 256);
+    }
+  };
+  const int wm = (wave >> 1) * (BLOCK / 2), wn = (wave & 1) * (BLOCK / 2);
+  floatx4 acc[MT][MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  fetch(0, 0);
+  for (int s = 0; s < steps; ++s) {
+    if (s + 1 < steps) {
+      fetch(s + 1, (s + 1) & 1);
+      wait_copies<2 * PIECES + (BLOCK == 128 ? 2 : 1)>();
+    } else {
+      wait_copies<0>();
+    }
+    wait_lds();
+    barrier();
+    const char *const la = lds + (s & 1) * S::STAGE, *const lb = la + S::CODES;
+    const char *const ea = la + 2 * S::CODES, *const eb = ea + S::SCALES;
+    const bool last = l0 + (s + 1) * STEP >= g.L;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      uintx4 fa[MT], fb[MT];
+      uint32_t xa[MT], xb[MT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int ra = wm + 16 * i + i16, rb = wn + 16 * i + i16;
+        fa[i] = *reinterpret_cast<const uintx4 *>(la + ra * 128 + (((kk * 4 + q) ^ mx_swizzle(ra)) << 4));
+        fb[i] = *reinterpret_cast<const uintx4 *>(lb + rb * 128 + (((kk * 4 + q) ^ mx_swizzle(rb)) << 4));
+        xa[i] = *reinterpret_cast<const uint32_t *>(ea + ra * STEP + kk * 4) >> (8 * q);
+        xb[i] = *reinterpret_cast<const uint32_t *>(eb + rb * STEP + kk * 4) >> (8 * q);
+      }
+      if (last) {  // what lies behind a row's last element may be anything
+        const long long group = l0 + s * STEP + kk * 4 + q;
+        const int n = (int)min(max(m.K - group * GROUP, 0ll), (long long)GROUP);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          fa[i] = first_codes(fa[i], n);
+          xa[i] = n ? xa[i] : 0u, xb[i] = n ? xb[i] : 0u;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = mx_mfma(fb[j], xb[j], fa[i], xa[i], acc[i][j]);
+    }
+    wait_lds();
+    barrier();
+  }
+  if (!g.part)
+    write_fwd<T, false, MT>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * MT * MT * 64);
+  else
+    write_sums<T, EPI_FWD, false>(g, split, r0 + wm, c0 + wn, lane, acc);
+}
+
+// Few rows: 16 columns and up to 32 rows to a workgroup, whose waves share the sum's axis; fragments come from memory without LDS.  x is quantised on the
+// way where it is not held in 4 bits yet (RAW): a lane's fragment is a group, whose 32 elements it reads and codes by itself.  Up to 8 rows
+// (HALVES) the instruction's 16 x 16 results hold 8 columns of W's first half of groups by x's, and 8 of the second by the second, so
+// that twice as many workgroups share W.
+template <typename T, int MT, int NW, bool HALVES, bool RAW>
+__global__ __launch_bounds__(64 * NW) void mx_few_rows_kernel(MxArgs m) {
+  constexpr int ROWS = HALVES ? 8 : 16 * MT, COLS = HALVES ? 8 : 16;
+  __shared__ floatx4 lds[NW * MT * 64];  // [wave][row of 16][4 chunks of 4 columns], chunk c at c ^ (row & 3)
+  const GemmArgs &g = m.g;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
+  const int c0 = blockIdx.x * COLS, groups = (int)g.L;
+  const int all = (groups + 3) / 4, steps = HALVES ? (all + 1) / 2 : all;
+  const int own = HALVES ? i & 7 : i, first = HALVES && i >= 8 ? steps * 4 : 0;
+  const long long wr = min(c0 + own, g.C - 1);  // rows beyond the last read it again; their results are not used
+  const char *const w = g.b + wr * g.ldb;
+  const uint8_t *const ws = m.sb + wr * m.lsb;
+  floatx4 acc[MT];
+#pragma unroll
+  for (int k = 0; k < MT; ++k) acc[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int s = wave; s < steps; s += NW) {
+    const int group = first + s * 4 + q, n = min(max(m.K - group * GROUP, 0), GROUP);
+    uintx4 fw = {0, 0, 0, 0}, fx[MT];
+    uint32_t ew = 0, ex[MT];
+    if (n > 0) fw = *reinterpret_cast<const uintx4 *>(w + group * 16ll), ew = ws[group];
+#pragma unroll
+    for (int k = 0; k < MT; ++k) {
+      const long long row = min((long long)16 * k + own, g.R - 1);
+      fx[k] = uintx4{0, 0, 0, 0}, ex[k] = 0;
+      if (n <= 0) continue;
+      if constexpr (RAW) {
+        float v[4][8], top = 0.f;
+        const T *const p = (const T *)(g.a + row * g.lda) + (long long)group * GROUP;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) load8(p + 8 * h, v[h], n - 8 * h);
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = fabsf(v[h][e]) <= INFINITY ? fmaxf(top, fabsf(v[h][e])) : INFINITY;
+        const int eb = exponent_byte<NF_Q_E2M1>(top);
+        ex[k] = eb;
+        if (eb < 255) {
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            uint32_t c[2];
+            encode8<NF_Q_E2M1>(v[h], eb - 127, c);
+            fx[k][h] = c[0];
+          }
+        }
+      } else {
+        fx[k] = first_codes(*reinterpret_cast<const uintx4 *>(g.a + row * g.lda + group * 16ll), n);
+        ex[k] = m.sa[row * m.lsa + group];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < MT; ++k) acc[k] = mx_mfma(fw, ew, fx[k], ex[k], acc[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < MT; ++k) lds[(wave * MT * 16 + 16 * k + i) * 4 + (q ^ (i & 3))] = acc[k];
+  __syncthreads();
+  float *const sums = reinterpret_cast<float *>(lds);
+  for (int t = threadIdx.x; t < MT * 256; t += 64 * NW) {
+    float v = sums[t];
+#pragma unroll
+    for (int k = 1; k < NW; ++k) v += sums[k * MT * 256 + t];
+    sums[t] = v;  // no other thread reads or writes these places before the barrier
+  }
+  __syncthreads();
+  constexpr int GROUPS = COLS / 8;
+  for (int t = threadIdx.x; t < ROWS * GROUPS; t += 64 * NW) {
+    const int r = t / GROUPS, h = t % GROUPS, col = c0 + h * 8;
+    if (r >= g.R || col >= g.C) continue;
+    float v[8];
+    const floatx4 lo = lds[r * 4 + ((2 * h) ^ (r & 3))], hi = lds[r * 4 + ((2 * h + 1) ^ (r & 3))];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = lo[e], v[e + 4] = hi[e];
+    if (HALVES) {  // row r + 8, columns 8 ... 15
+      const floatx4 lo2 = lds[(r + 8) * 4 + (2 ^ (r & 3))], hi2 = lds[(r + 8) * 4 + (3 ^ (r & 3))];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += lo2[e], v[e + 4] += hi2[e];
+    }
+    finish_fwd<T>(g.e, r, col, g.C, v);
+  }
+}
+
+// ---- plans ----
+constexpr int FEW = 32;  // rows
+struct MxPlan {
+  int tile, splits;
+  long long per;  // groups of a split
+  size_t bytes;   // of the splits' sums
+};
+MxPlan mx_plan(long long M, int N, long long K) {
+  MxPlan p = {0, 1, 0, 0};
+  if (M <= FEW) return p;
+  const long long steps = ((K + GROUP - 1) / GROUP + STEP - 1) / STEP;
+  auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
+  p.tile = tiles(128) >= 256 ? 128 : 64;
+  const long long t = tiles(p.tile);
+  long long splits = std::max<long long>(1, std::min<long long>(512 / t, steps / 4));
+  const long long each = (steps + splits - 1) / splits;
+  p.splits = (int)((steps + each - 1) / each), p.per = each * STEP;
+  p.bytes = p.splits > 1 ? (size_t)p.splits * M * ((N + 7) / 8 * 8) * 4 : 0;
+  return p;
+}
+inline size_t whole256(size_t n) { return (n + 255) / 256 * 256; }
+
+template <typename T>
+hipError_t product_as(const MxCall &c, const void *raw, const MxRows &a, const MxRows &b, const Epilogue &e, void *ws, hipStream_t st) {
+  const MxPlan p = mx_plan(c.M, c.N, c.K);
+  MxArgs m = {};
+  GemmArgs &g = m.g;
+  g.a = raw ? (const char *)raw : (const char *)a.codes, g.b = (const char *)b.codes, g.lda = raw ? (long long)c.K * sizeof(T) : a.cb, g.ldb = b.cb;
+  m.sa = a.scales, m.sb = b.scales, m.lsa = a.sb, m.lsb = b.sb, m.K = (int)c.K;
+  g.R = c.M, g.C = c.N, g.L = (c.K + GROUP - 1) / GROUP, g.e = e;
+  const double flops = 2.0 * c.M * c.N * c.K, ends = sizeof(T) * (1.0 + (e.res != nullptr) + (e.z != nullptr)) * c.M * c.N;
+  const double bytes = (raw ? sizeof(T) : 0.53) * c.M * c.K + 0.53 * c.N * c.K;
+  if (!p.tile) {
+    auto go = [&](auto kernel, int threads, int cols) { hipLaunchKernelGGL(kernel, dim3((c.N + cols - 1) / cols), dim3(threads), 0, st, m); };
+    return recorded(st, raw ? "mx_linear_few_rows" : "mx_product_few_rows", flops, bytes + ends, [&] {
+      if (c.M <= 8)
+        raw ? go(mx_few_rows_kernel<T, 1, 8, true, true>, 512, 8) : go(mx_few_rows_kernel<T, 1, 8, true, false>, 512, 8);
+      else if (c.M <= 16)
+        raw ? go(mx_few_rows_kernel<T, 1, 8, false, true>, 512, 16) : go(mx_few_rows_kernel<T, 1, 8, false, false>, 512, 16);
+      else
+        raw ? go(mx_few_rows_kernel<T, 2, 8, false, true>, 512, 16) : go(mx_few_rows_kernel<T, 2, 8, false, false>, 512, 16);
+    });
+  }
+  g.tiles_c = (c.N + p.tile - 1) / p.tile, g.tiles = (int)((c.M + p.tile - 1) / p.tile) * g.tiles_c;
+  g.splits = p.splits, g.per = p.per;
+  if (p.splits > 1) g.part = (float *)ws, g.part_ld = (c.N + 7) / 8 * 8;
+  const hipError_t err = recorded(st, p.tile == 128 ? "mx_product_128x128" : "mx_product_64x64", flops, bytes + (p.splits > 1 ? 4.0 * p.splits * c.M * c.N : ends), [&] {
+    const dim3 grid((unsigned)(g.tiles * g.splits));
+    if (p.tile == 128)
+      hipLaunchKernelGGL((mx_gemm_kernel<T, 128>), grid, dim3(LT), 0, st, m);
+    else
+      hipLaunchKernelGGL((mx_gemm_kernel<T, 64>), grid, dim3(LT), 0, st, m);
+  });
+  if (err != hipSuccess || p.splits == 1) return err;
+  const FinishArgs f = finish_args(p.splits, g);
+  return recorded(st, "mx_product_finish", 0.0, 4.0 * p.splits * c.M * c.N + ends,
+                  [&] { hipLaunchKernelGGL(fwd_finish_kernel<T>, dim3(finish_blocks(f)), dim3(LT), 0, st, f); });
+}
+
+template <typename T>
+hipError_t quantise_as(const QuantArgs &a, const T *x, hipStream_t st) {
+  const dim3 grid((unsigned)(a.tiles_c * ((a.rows + TR - 1) / TR)));
+  const double n = (double)a.rows * a.cols;
+  return recorded(st, "mx_quantise", 0.0, n * (sizeof(T) + (a.codes ? 0.53 : 0.0) + (a.codes_t ? 0.53 : 0.0)), [&] {
+    if (a.codes && a.codes_t)
+      hipLaunchKernelGGL((mx_quantise_kernel<T, true, true>), grid, dim3(QT), 0, st, a, x);
+    else if (a.codes)
+      hipLaunchKernelGGL((mx_quantise_kernel<T, true, false>), grid, dim3(QT), 0, st, a, x);
+    else
+      hipLaunchKernelGGL((mx_quantise_kernel<T, false, true>), grid, dim3(QT), 0, st, a, x);
+  });
+}
+
+MxRows rows_at(void *codes, void *scales, long long n) {
+  MxRows r = {(uint8_t *)codes, (uint8_t *)scales, 0, 0};
+  qcache_row_bytes(NF_Q_E2M1, n, &r.cb, &r.sb);
+  return r;
+}
+
+}  // namespace
+
+bool mx_quantise_fits(long long rows, long long cols) {
+  return (double)((rows + TR - 1) / TR) * (double)((cols + TC - 1) / TC) < 2147483648.0;
+}
+
+size_t mx_product_workspace_bytes(const MxCall &c) { return mx_plan(c.M, c.N, c.K).bytes; }
+size_t mx_linear_workspace_bytes(const MxCall &c) {
+  const MxPlan p = mx_plan(c.M, c.N, c.K);
+  if (!p.tile) return 0;
+  const MxRows r = rows_at(nullptr, nullptr, c.K);
+  return whole256(p.bytes) + whole256((size_t)c.M * r.cb) + (size_t)c.M * r.sb;
+}
+
+hipError_t launch_mx_quantise(int dtype, long long rows, long long cols, const void *x, void *codes, void *scales, void *codes_t, void *scales_t, hipStream_t st) {
+  const MxRows r = rows_at(codes, scales, cols), t = rows_at(codes_t, scales_t, rows);
+  const QuantArgs a = {rows, cols, (cols + TC - 1) / TC, r.codes, r.scales, t.codes, t.scales, r.cb, r.sb, t.cb, t.sb};
+  if (dtype == NF_BF16) return quantise_as(a, (const __bf16 *)x, st);
+  if (dtype == NF_F16) return quantise_as(a, (const _Float16 *)x, st);
+  return quantise_as(a, (const float *)x, st);
+}
+
+hipError_t launch_mx_product(const MxCall &c, const void *a, const void *as, const void *b, const void *bs, const float *bias, const void *r, const DropArgs &drop,
+                             void *y, void *z, void *ws, hipStream_t st) {
+  const Epilogue e = {bias, r, z, y, drop, c.act};
+  const MxRows ra = rows_at((void *)a, (void *)as, c.K), rb = rows_at((void *)b, (void *)bs, c.K);
+  if (c.dtype == NF_BF16) return product_as<__bf16>(c, nullptr, ra, rb, e, ws, st);
+  if (c.dtype == NF_F16) return product_as<_Float16>(c, nullptr, ra, rb, e, ws, st);
+  return product_as<float>(c, nullptr, ra, rb, e, ws, st);
+}
+
+// The workspace holds the splits' sums, then x's codes and exponents.
+hipError_t launch_mx_linear(const MxCall &c, const void *x, const void *W, const void *Ws, const float *bias, const void *r, const DropArgs &drop, void *y, void *z,
+                            void *ws, hipStream_t st) {
+  const MxPlan p = mx_plan(c.M, c.N, c.K);
+  if (p.tile) {
+    const MxRows sizes = rows_at(nullptr, nullptr, c.K);
+    char *const codes = (char *)ws + whole256(p.bytes), *const scales = codes + whole256((size_t)c.M * sizes.cb);
+    const hipError_t e = launch_mx_quantise(c.dtype, c.M, c.K, x, codes, scales, nullptr, nullptr, st);
+    return e != hipSuccess ? e : launch_mx_product(c, codes, scales, W, Ws, bias, r, drop, y, z, ws, st);
+  }
+  const Epilogue e = {bias, r, z, y, drop, c.act};
+  const MxRows none = {}, rb = rows_at((void *)W, (void *)Ws, c.K);
+  if (c.dtype == NF_BF16) return product_as<__bf16>(c, x, none, rb, e, ws, st);
+  if (c.dtype == NF_F16) return product_as<_Float16>(c, x, none, rb, e, ws, st);
+  return product_as<float>(c, x, none, rb, e, ws, st);
+}
+
+}  // namespace nf

@@ -80,6 +80,15 @@ int32_t check_qcache(int32_t format, int32_t dtype, const void *codes, const voi
   return NF_OK;
 }
 
+int32_t check_mx(const nf_linear_desc *d, int64_t M, MxCall *c) {
+  if (!d) return NF_ERR_NULL;
+  if (!dtype_ok(d->dtype) || !act_ok(d->act) || d->K <= 0 || d->N <= 0 || M <= 0) return NF_ERR_BAD_DESC;
+  if (d->K > (1 << 24) || d->N > (1 << 20) || M >= (1ll << 31) - 512) return NF_ERR_UNSUPPORTED;
+  if (((M + 63) / 64) * ((d->N + 63) / 64) >= (1ll << 31) / 256) return NF_ERR_UNSUPPORTED;
+  *c = MxCall{d->dtype, d->act, M, d->N, d->K};
+  return NF_OK;
+}
+
 }  // namespace
 }  // namespace nf
 
@@ -280,6 +289,62 @@ int32_t nf_qcache_read(int32_t format, int32_t dtype, const uint8_t *codes, cons
   const hipStream_t st = static_cast<hipStream_t>(stream);
   NF_RUN(st, "qcache_read", 0.0, (double)B * (size_of(dtype) * n + n * (format == NF_Q_E2M1 ? 0.5 : 1.0) + n / 32.0),
          launch_qcache_read(format, dtype, q, reinterpret_cast<const long long *>(idx), B, x_out, labels_out, st));
+  return NF_OK;
+}
+
+int32_t nf_mx_quantise(int32_t dtype, int64_t rows, int64_t cols, const void *x, uint8_t *codes, uint8_t *scales,
+                       uint8_t *codes_t, uint8_t *scales_t, void *stream) {
+  if (!x || (codes == nullptr) != (scales == nullptr) || (codes_t == nullptr) != (scales_t == nullptr) || (!codes && !codes_t)) return NF_ERR_NULL;
+  if (!dtype_ok(dtype) || rows <= 0 || cols <= 0) return NF_ERR_BAD_DESC;
+  if (rows > (1ll << 44) / cols || !mx_quantise_fits(rows, cols)) return NF_ERR_UNSUPPORTED;
+  if (!all_aligned16(x, codes, scales, codes_t, scales_t)) return NF_ERR_BAD_DESC;
+  NF_HIP(launch_mx_quantise(dtype, rows, cols, x, codes, scales, codes_t, scales_t, static_cast<hipStream_t>(stream)));
+  return NF_OK;
+}
+
+int32_t nf_mx_product_workspace_bytes(const nf_linear_desc *d, int64_t M, size_t *out) {
+  MxCall c;
+  const int32_t rc = check_mx(d, M, &c);
+  if (rc) return rc;
+  if (!out) return NF_ERR_NULL;
+  *out = mx_product_workspace_bytes(c);
+  return NF_OK;
+}
+
+int32_t nf_mx_product(const nf_linear_desc *d, int64_t M, const uint8_t *a, const uint8_t *a_scales, const uint8_t *b,
+                      const uint8_t *b_scales, const float *bias, const void *r, void *y, void *ws, size_t ws_bytes,
+                      void *stream) {
+  MxCall c;
+  int32_t rc = check_mx(d, M, &c);
+  if (rc) return rc;
+  if (!a || !a_scales || !b || !b_scales || !y) return NF_ERR_NULL;
+  if (!all_aligned16(a, a_scales, b, b_scales, bias, r, y)) return NF_ERR_BAD_DESC;
+  if ((rc = check_ws(ws, ws_bytes, mx_product_workspace_bytes(c)))) return rc;
+  NF_HIP(launch_mx_product(c, a, a_scales, b, b_scales, bias, r, drop_args(nullptr), y, nullptr, ws, static_cast<hipStream_t>(stream)));
+  return NF_OK;
+}
+
+int32_t nf_mx_linear_workspace_bytes(const nf_linear_desc *d, int64_t M, size_t *out) {
+  MxCall c;
+  const int32_t rc = check_mx(d, M, &c);
+  if (rc) return rc;
+  if (!out) return NF_ERR_NULL;
+  *out = mx_linear_workspace_bytes(c);
+  return NF_OK;
+}
+
+int32_t nf_mx_linear_fwd(const nf_linear_desc *d, int64_t M, const void *x, const uint8_t *W, const uint8_t *W_scales,
+                         const float *b, const void *r, const nf_dropout_desc *drop, void *y, void *z, void *ws,
+                         size_t ws_bytes, void *stream) {
+  MxCall c;
+  int32_t rc = check_mx(d, M, &c);
+  if (rc) return rc;
+  if (!x || !W || !W_scales || !y) return NF_ERR_NULL;
+  if (drop && (rc = check_drop(drop))) return rc;
+  if (!mx_quantise_fits(M, d->K)) return NF_ERR_UNSUPPORTED;
+  if (!all_aligned16(x, W, W_scales, b, r, y, z)) return NF_ERR_BAD_DESC;
+  if ((rc = check_ws(ws, ws_bytes, mx_linear_workspace_bytes(c)))) return rc;
+  NF_HIP(launch_mx_linear(c, x, W, W_scales, b, r, drop_args(drop), y, z, ws, static_cast<hipStream_t>(stream)));
   return NF_OK;
 }
 

@@ -255,4 +255,23 @@ hipError_t launch_linear_epilogue(const LinearCall &c, const void *dy, const voi
 hipError_t launch_linear_bwd(const LinearCall &c, const void *dz, const void *x, const void *W, void *dx, float *dW,
                              void *ws, hipStream_t st);
 
+struct MxRows {
+  uint8_t *codes, *scales;
+  long long cb, sb;  // row strides
+};
+struct MxCall {
+  int dtype, act;
+  long long M;
+  int N;
+  long long K;
+};
+bool mx_quantise_fits(long long rows, long long cols);
+hipError_t launch_mx_quantise(int dtype, long long rows, long long cols, const void *x, void *codes, void *scales, void *codes_t, void *scales_t, hipStream_t st);
+size_t mx_product_workspace_bytes(const MxCall &c);
+size_t mx_linear_workspace_bytes(const MxCall &c);
+hipError_t launch_mx_product(const MxCall &c, const void *a, const void *as, const void *b, const void *bs, const float *bias, const void *r, const DropArgs &drop,
+                             void *y, void *z, void *ws, hipStream_t st);
+hipError_t launch_mx_linear(const MxCall &c, const void *x, const void *W, const void *Ws, const float *bias, const void *r, const DropArgs &drop, void *y, void *z,
+                            void *ws, hipStream_t st);
+
 }  // namespace nf

@@ -1,0 +1,278 @@
+"""Matrices in 4 bits on the GPU: codes to the bit, products against 64 bits.  A product's tolerance is one step of fp32 for each term of a
+sum, relative to the sum of the terms' magnitudes, and half a step of the result's type."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2402_14139_amd import binding as nf
+from tests import mx_ref
+from tests import pointwise_ref as ref
+from tests.pointwise_ref import ACTS, DT, FUNC, HALF, SUM, TINY, TYPES
+from tests.test_gpu_pointwise import Out, close, workspace
+
+pytestmark = pytest.mark.gpu
+REST = 0xA5
+
+
+def strides(n):
+    return nf.nf_qcache_row_bytes(nf.NF_Q_E2M1, n)
+
+
+def held(rows, n):
+    return tuple(torch.full((rows, b), REST, dtype=torch.uint8, device="cuda") for b in strides(n))
+
+
+def check_codes(pair, x):
+    """Codes and exponents of rows x, zeros up to a whole group, every other byte as it was."""
+    codes, scales = (p.cpu() for p in pair)
+    rows, n = x.shape
+    groups = -(-n // 32)
+    code, byte, _ = mx_ref.quantise(x)
+    assert np.array_equal(scales[:, :groups].numpy(), byte)
+    got = mx_ref.unpack(codes, groups * 32)
+    assert np.array_equal(got[:, :n], code) and not got[:, n:].any()
+    assert (codes[:, groups * 16:] == REST).all() and (scales[:, groups:] == REST).all()
+
+
+def quantised(t, x, rows=True, cols=True):
+    R, n = x.shape
+    a, b = held(R, n), held(n, R)
+    nf.nf_mx_quantise(DT[t], R, n, x.cuda(), *(a if rows else (None, None)), *(b if cols else (None, None)))
+    return a, b
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("R,n", [(1, 1), (1, 2048), (2048, 1), (3, 33), (31, 32), (32, 31), (33, 65), (100, 72), (127, 64), (128, 63), (129, 129), (300, 200), (70, 1000)])
+def test_codes(t, R, n):
+    g = torch.Generator().manual_seed(R * 3 + n)
+    x = (torch.randn(R, n, generator=g) * torch.exp2(torch.randint(-9, 5, (R, n), generator=g).float())).to(TYPES[t])
+    a, b = quantised(t, x)
+    check_codes(a, x.double().numpy())
+    check_codes(b, x.double().t().numpy())
+    for rows, cols in ((True, False), (False, True)):
+        p, q = quantised(t, x, rows, cols)
+        assert torch.equal(p[0], a[0]) == rows and torch.equal(q[1], b[1]) == cols
+        if rows:
+            check_codes(p, x.double().numpy())
+        else:
+            check_codes(q, x.double().t().numpy())
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_codes_of_edges(t):
+    """Every border between codes, zeros of both signs, the smallest and largest numbers, infinities and NaN."""
+    T = TYPES[t]
+    f = torch.finfo(T)
+    x = torch.zeros(40, 96, dtype=torch.float64)
+    steps = torch.tensor([0.0, 0.25, 0.5, 0.75, 1, 1.25, 1.5, 1.75, 2, 2.5, 3, 3.5, 4, 5, 6], dtype=torch.float64)
+    near = torch.cat([steps, steps * (1 + f.eps), steps * (1 - f.eps)])[:32]
+    for r, scale in enumerate([1, 2.0 ** -12, 2.0 ** 10, 1.5, -1]):
+        x[r, :32], x[r, 31] = near * scale, 6 * scale
+    x[5, :32] = torch.tensor([f.max, -f.max] * 16, dtype=torch.float64)
+    x[6, 0] = f.tiny
+    x[7, 0] = f.tiny * f.eps   # the smallest subnormal number
+    x[8, 3], x[9, 40], x[10, 95] = float("inf"), float("nan"), float("-inf")
+    x[11, :] = -0.0
+    x[12, 5], x[12, 6] = f.max, f.tiny
+    x[13, :32] = 7.0 * 2.0 ** torch.arange(-16, 16).double().clamp(-14, 12)
+    x = x.to(T)
+    a, b = quantised(t, x)
+    check_codes(a, x.double().numpy())
+    check_codes(b, x.double().t().numpy())
+    same = held(40, 96)
+    nf.nf_qcache_write(nf.NF_Q_E2M1, DT[t], *same, None, 40, 96, 0, 40, x.cuda(), None)
+    assert torch.equal(same[0], a[0]) and torch.equal(same[1], a[1])
+
+
+def operand(g, rows, n, spread=4):
+    """A random matrix in 4 bits, anything behind its rows' ends (255: exponents that would be NaN), and its values."""
+    code = torch.randint(0, 16, (rows, n), generator=g).numpy().astype(np.uint8)
+    byte = torch.randint(127 - spread, 128 + spread, (rows, -(-n // 32)), generator=g).numpy().astype(np.uint8)
+    packed = mx_ref.pack(code, byte, strides(n))
+    return tuple(p.cuda() for p in packed), torch.from_numpy(mx_ref.values(code, byte))
+
+
+def product_case(t, M, K, N, act="none", bias=False, res=False, seed=1):
+    g = torch.Generator().manual_seed(seed + M * 13 + K * 5 + N)
+    a, A = operand(g, M, K)
+    b, B = operand(g, N, K)
+    d = nf.LinearDesc(dtype=DT[t], K=K, N=N, act=ACTS.index(act))
+    scale = float(K) ** 0.5
+    v = (scale * torch.randn(N, generator=g)).cuda() if bias else None
+    r = (scale * torch.randn(M, N, generator=g)).to(TYPES[t]).cuda() if res else None
+    y = Out(M, N, dtype=TYPES[t])
+    nf.nf_mx_product(d, M, *a, *b, v, r, y.t, workspace(nf.nf_mx_product_workspace_bytes(d, M)))
+    Z = A @ B.t() + (v.double().cpu() if bias else 0)
+    err = (K + 2) * SUM * (A.abs() @ B.abs().t() + (v.double().cpu().abs() if bias else 0))
+    w = ref.act(act, Z)
+    Y = w + r.double().cpu() if res else w
+    tol = 1.13 * err + FUNC * Z.abs() * (act != "none")
+    close_or_beyond(t, y.cpu(), Y, tol + (HALF[t] + 2 * SUM) * (Y.abs() + tol) + SUM * w.abs() + TINY[t])
+
+
+def close_or_beyond(t, got, want, tol):
+    """A result from half a step above the type's largest number on (fp16: 65520) rounds to an infinity: the large sums of 4100 and more terms do."""
+    T = torch.finfo(TYPES[t])
+    beyond = T.max * (1 + T.eps / 4)
+    over, under = want.abs() - tol >= beyond, want.abs() + tol < beyond
+    assert torch.equal(got[over], torch.copysign(torch.full_like(got[over], float("inf")), want[over]))
+    close("y", got[under], want[under], tol[under])
+
+
+SHAPES = [(1, 1, 1), (1, 2048, 40), (3, 31, 7), (8, 100, 9), (9, 256, 20), (16, 33, 129), (17, 1000, 33), (32, 4100, 70), (33, 1, 5), (33, 64, 64), (64, 72, 100), (65, 257, 130),
+          (129, 700, 63), (300, 8, 24), (257, 1030, 65), (2100, 40, 1600), (64, 40000, 72), (5000, 512, 3)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("M,K,N", SHAPES)
+def test_product(t, M, K, N):
+    product_case(t, M, K, N)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("act,bias,res", [("relu", True, True), ("silu", True, False), ("gelu", False, True), ("none", True, True)])
+@pytest.mark.parametrize("M,K,N", [(1, 40, 24), (20, 515, 33), (70, 88, 61), (300, 520, 256), (64, 20000, 50)])
+def test_product_epilogue(t, act, bias, res, M, K, N):
+    product_case(t, M, K, N, act, bias, res)
+
+
+@pytest.mark.parametrize("M", [2, 20, 70])
+def test_all_exponents(M):
+    """Operands' exponents from -127 to 127 whose products are near 1: fp32 results, sums of one term, to the bit."""
+    K, N = 8 * 32, 16
+    code = np.zeros((M, K), np.uint8)
+    for r in range(M):
+        code[r, (r % 8) * 32 + 3] = 1 + r % 15
+    ea = np.random.RandomState(M).randint(0, 255, (M, 8)).astype(np.uint8)
+    other = np.full((N, K), 3, np.uint8)
+    eb = np.zeros((N, 8), np.uint8)
+    for c in range(N):
+        eb[c] = 254 - ea[c % M]
+    a, b = (tuple(p.cuda() for p in mx_ref.pack(q, e, strides(K))) for q, e in ((code, ea), (other, eb)))
+    y = torch.empty(M, N, device="cuda")
+    d = nf.LinearDesc(dtype=nf.NF_F32, K=K, N=N, act=0)
+    nf.nf_mx_product(d, M, *a, *b, None, None, y, workspace(nf.nf_mx_product_workspace_bytes(d, M)))
+    want = torch.from_numpy(mx_ref.values(code, ea) @ mx_ref.values(other, eb).T)
+    for c in range(N):
+        for r in range(c % M, M, M):   # those whose exponents cancel; the others may leave fp32's range
+            assert y[r, c].item() == want[r, c].item(), (r, c)
+    fits = (want.abs() < 1e38) & ((want.abs() > 1e-37) | (want == 0))
+    assert torch.equal(y.cpu().double()[fits], want[fits])
+
+
+@pytest.mark.parametrize("M", [5, 100])
+def test_a_group_without_numbers(M):
+    g = torch.Generator().manual_seed(9)
+    x, w = torch.randn(M, 200, generator=g), torch.randn(40, 200, generator=g)
+    x[3, 199], w[7, 0] = float("inf"), float("nan")
+    d = nf.LinearDesc(dtype=nf.NF_F32, K=200, N=40, act=0)
+    W, _ = quantised("f32", w, cols=False)
+    y = torch.empty(M, 40, device="cuda")
+    nf.nf_mx_linear_fwd(d, M, x.cuda(), *W, None, None, None, y, None, workspace(nf.nf_mx_linear_workspace_bytes(d, M)))
+    bad = torch.zeros(M, 40, dtype=torch.bool)
+    bad[3], bad[:, 7] = True, True
+    assert torch.equal(y.cpu().isnan(), bad)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("M,K,N", [(1, 2048, 2048), (1, 70, 9), (7, 200, 65), (8, 2040, 40), (12, 333, 50), (31, 96, 200), (33, 72, 100), (100, 1000, 130), (2000, 520, 72)])
+def test_linear_is_quantisation_and_product(t, M, K, N):
+    """The bits of the two calls, for rows that are quantised within the product's launch too."""
+    g = torch.Generator().manual_seed(M + K + N)
+    T = TYPES[t]
+    x, w = (torch.randn(M, K, generator=g) * torch.exp(torch.randn(K, generator=g))).to(T), torch.randn(N, K, generator=g)
+    b, r = torch.randn(N, generator=g).cuda(), torch.randn(M, N, generator=g).to(T).cuda()
+    W, _ = quantised("f32", w, cols=False)
+    X, _ = quantised(t, x, cols=False)
+    d = nf.LinearDesc(dtype=DT[t], K=K, N=N, act=nf.NF_ACT_SILU)
+    y, z, want = Out(M, N, dtype=T), Out(M, N, dtype=T), Out(M, N, dtype=T)
+    nf.nf_mx_linear_fwd(d, M, x.cuda(), *W, b, r, None, y.t, z.t, workspace(nf.nf_mx_linear_workspace_bytes(d, M)))
+    nf.nf_mx_product(d, M, *X, *W, b, r, want.t, workspace(nf.nf_mx_product_workspace_bytes(d, M)))
+    assert torch.equal(y.cpu(), want.cpu())
+    A, B = torch.from_numpy(mx_ref.quantise(x.double().numpy())[2]), torch.from_numpy(mx_ref.quantise(w.double().numpy())[2])
+    Z = A @ B.t() + b.double().cpu()
+    err = (K + 2) * SUM * (A.abs() @ B.abs().t() + b.double().cpu().abs())
+    close("z", z.cpu(), Z, err + HALF[t] * (Z.abs() + err) + TINY[t])
+
+
+@pytest.mark.parametrize("M", [6, 150])
+def test_linear_with_dropout(M):
+    g = torch.Generator().manual_seed(M)
+    K, N, p = 136, 44, 0.3
+    x, w = torch.randn(M, K, generator=g), torch.randn(N, K, generator=g)
+    W, _ = quantised("f32", w, cols=False)
+    d, y = nf.LinearDesc(dtype=nf.NF_F32, K=K, N=N, act=nf.NF_ACT_GELU), Out(M, N)
+    nf.nf_mx_linear_fwd(d, M, x.cuda(), *W, None, None, nf.DropoutDesc(p, 55, 66), y.t, None, workspace(nf.nf_mx_linear_workspace_bytes(d, M)))
+    A, B = (torch.from_numpy(mx_ref.quantise(v.double().numpy())[2]) for v in (x, w))
+    Z, keep = A @ B.t(), ref.keep_scale(M, N, p, 55, 66)
+    err = (K + 4) * SUM * (A.abs() @ B.abs().t())
+    Y = ref.act("gelu", Z) * keep
+    got = y.cpu()
+    close("y", got, Y, (1.13 * err + FUNC * Z.abs()) * keep + 2 * SUM * Y.abs())
+    assert (got[keep == 0] == 0).all()
+
+
+def test_a_layers_gradients():
+    """dx = Q(dz) Q(W) and dW = Q(dz)^T Q(x), each operand's groups along the axis that is summed over."""
+    g = torch.Generator().manual_seed(12)
+    M, K, N = 333, 100, 70
+    dz, x, w = torch.randn(M, N, generator=g).bfloat16(), torch.randn(M, K, generator=g).bfloat16(), torch.randn(N, K, generator=g)
+    dz_rows, dz_cols = quantised("bf16", dz)
+    _, x_cols = quantised("bf16", x, rows=False)
+    _, w_cols = quantised("f32", w, rows=False)
+    dx, dW = Out(M, K, dtype=torch.bfloat16), Out(N, K)
+    for_dx, for_dW = nf.LinearDesc(dtype=nf.NF_BF16, K=N, N=K, act=0), nf.LinearDesc(dtype=nf.NF_F32, K=M, N=K, act=0)
+    nf.nf_mx_product(for_dx, M, *dz_rows, *w_cols, None, None, dx.t, workspace(nf.nf_mx_product_workspace_bytes(for_dx, M)))
+    nf.nf_mx_product(for_dW, N, *dz_cols, *x_cols, None, None, dW.t, workspace(nf.nf_mx_product_workspace_bytes(for_dW, N)))
+    q = lambda v: torch.from_numpy(mx_ref.quantise(v.double().numpy())[2])  # noqa: E731
+    for name, got, A, B, t in (("dx", dx, q(dz), q(w.t()), "bf16"), ("dW", dW, q(dz.t()), q(x.t()), "f32")):
+        Z, err = A @ B.t(), (A.shape[1] + 2) * SUM * (A.abs() @ B.abs().t())
+        close(name, got.cpu(), Z, err + HALF[t] * (Z.abs() + err))
+
+
+def test_more_rows_than_a_grids_second_axis():
+    product_case("bf16", 300000, 40, 8)
+
+
+def test_another_stream_and_a_graph():
+    g = torch.Generator().manual_seed(4)
+    M, K, N = 500, 1000, 72
+    x, w = torch.randn(M, K, generator=g).bfloat16().cuda(), torch.randn(N, K, generator=g).cuda()
+    W, Wt, Xt = held(N, K), held(K, N), held(K, M)
+    d, dW = nf.LinearDesc(dtype=nf.NF_BF16, K=K, N=N, act=nf.NF_ACT_GELU), nf.LinearDesc(dtype=nf.NF_F32, K=M, N=K, act=0)
+    y, out = torch.empty(M, N, dtype=torch.bfloat16, device="cuda"), torch.empty(N, K, device="cuda")
+    Yt = held(N, M)
+    ws = workspace(max(nf.nf_mx_linear_workspace_bytes(d, M), nf.nf_mx_product_workspace_bytes(dW, N)))
+
+    def all_calls(stream):
+        nf.nf_mx_quantise(nf.NF_F32, N, K, w, *W, *Wt, stream)
+        nf.nf_mx_linear_fwd(d, M, x, *W, None, None, None, y, None, ws, stream)
+        nf.nf_mx_quantise(nf.NF_BF16, M, N, y, None, None, *Yt, stream)
+        nf.nf_mx_quantise(nf.NF_BF16, M, K, x, None, None, *Xt, stream)
+        nf.nf_mx_product(dW, N, *Yt, *Xt, None, None, out, ws, stream)
+
+    outs = (*W, *Wt, *Xt, *Yt, y, out)
+    all_calls(None)
+    torch.cuda.synchronize()
+    want = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    for o in outs:
+        o.fill_(REST)
+    side.wait_stream(torch.cuda.current_stream())
+    all_calls(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        all_calls(torch.cuda.current_stream())
+    for turn in range(3):
+        for o in outs:
+            o.fill_(REST)
+        if turn:
+            all_calls(None)
+            torch.cuda.synchronize()
+            for o in outs:
+                o.fill_(REST)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), turn
