@@ -183,6 +183,36 @@ int32_t nf_local_bwd_wgrad(const nf_layer_desc *d, const nf_aux_desc *a, int32_t
 int32_t nf_sgd_update(const nf_sgd_desc *s, int32_t n_tensors, float *const *w, const float *const *g,
                       float *const *v, const int64_t *numel, void *stream);
 
+/* Updates made orthogonal.  A matrix G [rows][cols], dense, goes through `steps` Newton-Schulz steps,
+ *   X = G / (|G| + eps), |G| the root of the sum of squares;  X <- a X + (b A + c A^2) X with A = X X^T (rows <= cols; else X^T X),
+ * step k with a[k], b[k], c[k].  They drive the singular values towards those that the polynomial x (a + b x^2 + c x^4) repeats.  Products keep 22 bits of their
+ * operands and sums are fp32, as errors of small singular values grow by the a's product.  Every step's results have to stay bounded (by 1e9) where the
+ * singular values begin at most at 1: else NF_ERR_UNSUPPORTED.  1 <= steps <= NF_ORTH_STEPS, eps >= 0.
+ * n_matrices (<= NF_ORTH_MATRICES) share the launches; rows, cols, and the arrays of device pointers are HOST arrays.  rows, cols <= 2^20, the lesser of them
+ * <= 2^14.  A matrix with an infinity or a NaN gives NaN throughout, and so does one of zeros where eps is 0. */
+#define NF_ORTH_STEPS 12
+#define NF_ORTH_MATRICES 32
+typedef struct {
+  int32_t steps;
+  float eps, a[NF_ORTH_STEPS], b[NF_ORTH_STEPS], c[NF_ORTH_STEPS];
+} nf_orth_desc;
+int32_t nf_orthogonalise_workspace_bytes(const nf_orth_desc *d, int32_t n_matrices, const int32_t *rows,
+                                         const int32_t *cols, size_t *out);
+/* y = the last X, in G's type (NF_F32, NF_BF16, NF_F16).  y may be g; no two y may be the same. */
+int32_t nf_orthogonalise(const nf_orth_desc *d, int32_t dtype, int32_t n_matrices, const void *const *g, void *const *y,
+                         const int32_t *rows, const int32_t *cols, void *ws, size_t ws_bytes, void *stream);
+/* nf_sgd_update for weight matrices, the update made orthogonal (filters [C_out][R][S][C_in] are matrices of C_out rows):
+ *   v = momentum v + g;  u = g + momentum v (nesterov != 0) or v;  w = (1 - lr weight_decay) w - lr sqrt(max(1, rows / cols)) X(u)
+ * v == NULL or momentum == 0: u = g.  All fp32.  The workspace is nf_orthogonalise's.  No two w, and no two v, may be the same. */
+typedef struct {
+  float lr, momentum, weight_decay;
+  int32_t nesterov;
+  nf_orth_desc orth;
+} nf_muon_desc;
+int32_t nf_muon_update(const nf_muon_desc *d, int32_t n_matrices, float *const *w, const float *const *g,
+                       float *const *v, const int32_t *rows, const int32_t *cols, void *ws, size_t ws_bytes,
+                       void *stream);
+
 /* Activation cache.  cache [capacity][sample_elems], cache_labels [capacity] (may be NULL
  * together with labels).  Write stores batch rows at [first, first+B).  Read gathers B rows:
  * idx == NULL -> rows first..first+B-1, else rows idx[0..B) (device int64) — B is the

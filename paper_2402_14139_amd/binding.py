@@ -31,7 +31,7 @@ EXPORTS = ("nf_strerror", "nf_layer_out_dims", "nf_workspace_bytes", "nf_layer_f
            "nf_groupnorm_workspace_bytes", "nf_groupnorm_fwd_workspace_bytes", "nf_groupnorm_fwd", "nf_groupnorm_bwd", "nf_layernorm_workspace_bytes",
            "nf_layernorm_fwd", "nf_layernorm_bwd", "nf_qcache_row_bytes",
            "nf_qcache_write", "nf_qcache_read", "nf_mx_quantise", "nf_mx_product_workspace_bytes", "nf_mx_product",
-           "nf_mx_linear_workspace_bytes", "nf_mx_linear_fwd")
+           "nf_mx_linear_workspace_bytes", "nf_mx_linear_fwd", "nf_orthogonalise_workspace_bytes", "nf_orthogonalise", "nf_muon_update")
 
 NF_WS_AUX_ACT, NF_WS_POOL_ARG, NF_WS_HEAD_ARG = 0, 1, 2
 NF_HEAD_POOL_AVG, NF_HEAD_POOL_MAX = 0, 1
@@ -39,6 +39,7 @@ NF_LOSS_CE, NF_LOSS_MSE = 0, 1
 NF_F32, NF_BF16, NF_F16 = 0, 1, 2
 NF_ACT_NONE, NF_ACT_RELU, NF_ACT_SILU, NF_ACT_GELU = 0, 1, 2, 3
 NF_Q_INT8, NF_Q_E4M3, NF_Q_E2M1 = 0, 1, 2
+NF_ORTH_STEPS, NF_ORTH_MATRICES = 12, 32
 
 
 class NfError(RuntimeError):
@@ -62,6 +63,14 @@ class AuxDesc(C.Structure):
 
 class SgdDesc(C.Structure):
     _fields_ = [("lr", C.c_float), ("momentum", C.c_float)]
+
+
+class OrthDesc(C.Structure):
+    _fields_ = [("steps", C.c_int32), ("eps", C.c_float)] + [(n, C.c_float * NF_ORTH_STEPS) for n in "abc"]
+
+
+class MuonDesc(C.Structure):
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32), ("orth", OrthDesc)]
 
 
 class LayerParams(C.Structure):
@@ -198,6 +207,10 @@ def lib():
         L.nf_mx_product_workspace_bytes.argtypes = L.nf_mx_linear_workspace_bytes.argtypes = [C.POINTER(LinearDesc), i64, C.POINTER(size)]
         L.nf_mx_product.argtypes = [C.POINTER(LinearDesc), i64] + [ptr] * 8 + [size, ptr]
         L.nf_mx_linear_fwd.argtypes = [C.POINTER(LinearDesc), i64, ptr, ptr, ptr, ptr, ptr, C.POINTER(DropoutDesc), ptr, ptr, ptr, size, ptr]
+        ptrs, dims = C.POINTER(ptr), C.POINTER(i32)
+        L.nf_orthogonalise_workspace_bytes.argtypes = [C.POINTER(OrthDesc), i32, dims, dims, C.POINTER(size)]
+        L.nf_orthogonalise.argtypes = [C.POINTER(OrthDesc), i32, i32, ptrs, ptrs, dims, dims, ptr, size, ptr]
+        L.nf_muon_update.argtypes = [C.POINTER(MuonDesc), i32, ptrs, ptrs, ptrs, dims, dims, ptr, size, ptr]
         _lib = L
     return _lib
 
@@ -619,3 +632,47 @@ def nf_mx_linear_fwd(d: LinearDesc, M, x, W, W_scales, b, r, drop, y, z, ws, str
     wp, wn = _ws(ws)
     _check(lib().nf_mx_linear_fwd(_ref(d), M, _ptr(x), _ptr(W), _ptr(W_scales), _ptr(b), _ptr(r), _ref(drop), _ptr(y),
                                   _ptr(z), wp, wn, _stream(stream)), "nf_mx_linear_fwd")
+
+
+# ---- updates made orthogonal ----
+
+def orth_desc(steps, eps: float = 1e-7) -> OrthDesc:
+    """``steps``: (a, b, c) of every Newton-Schulz step."""
+    d = OrthDesc(steps=len(steps), eps=eps)
+    for k, (a, b, c) in enumerate(steps[:NF_ORTH_STEPS]):
+        d.a[k], d.b[k], d.c[k] = a, b, c
+    return d
+
+
+def _dims(shapes):
+    n = len(shapes)
+    return (C.c_int32 * n)(*[int(s[0]) for s in shapes]), (C.c_int32 * n)(*[int(s[1]) for s in shapes])
+
+
+def _as_matrices(ts):
+    """(rows, cols) of tensors whose first axis counts the rows."""
+    return _dims([(t.shape[0], t.numel() // max(t.shape[0], 1)) for t in ts])
+
+
+def nf_orthogonalise_workspace_bytes(d: OrthDesc, shapes) -> int:
+    """``shapes``: (rows, cols) of every matrix."""
+    out = C.c_size_t()
+    _check(lib().nf_orthogonalise_workspace_bytes(_ref(d), len(shapes), *_dims(shapes), C.byref(out)), "nf_orthogonalise_workspace_bytes")
+    return int(out.value)
+
+
+def nf_orthogonalise(d: OrthDesc, dtype, g, y, ws, stream=None):
+    """g, y: lists of torch tensors, rows along the first axis."""
+    wp, wn = _ws(ws)
+    n = len(g)
+    arr = lambda ts: (C.c_void_p * n)(*[_ptr(t) for t in ts])  # noqa: E731
+    _check(lib().nf_orthogonalise(_ref(d), dtype, n, arr(g), arr(y), *_as_matrices(g), wp, wn, _stream(stream)), "nf_orthogonalise")
+
+
+def nf_muon_update(d: MuonDesc, w, g, v, ws, stream=None):
+    """w, g, v: lists of torch tensors (v None without momentum), rows along the first axis."""
+    wp, wn = _ws(ws)
+    n = len(w)
+    arr = lambda ts: (C.c_void_p * n)(*[_ptr(t) for t in ts])  # noqa: E731
+    _check(lib().nf_muon_update(_ref(d), n, arr(w), arr(g), arr(v) if v is not None else None, *_as_matrices(w), wp, wn,
+                                _stream(stream)), "nf_muon_update")

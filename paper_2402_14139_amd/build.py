@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnf.so")
 SOURCES = ["nf_api.hip", "nf_block.hip", "nf_partition.hip", "igemm_fwd.hip", "igemm_fwd_fast.hip", "igemm_fwd_split.hip", "wino_fwd.hip", "wino_wgrad.hip", "igemm_wgrad.hip", "igemm_wgrad_fast.hip", "igemm_wgrad_split.hip", "igemm_wgrad_small.hip", "head.hip", "elementwise.hip", "stem.hip",
-           "nf_pointwise.hip", "linear.hip", "groupnorm.hip", "groupnorm_bwd.hip", "layernorm.hip", "dropout.hip", "qcache.hip", "mx.hip"]
+           "nf_pointwise.hip", "linear.hip", "groupnorm.hip", "groupnorm_bwd.hip", "layernorm.hip", "dropout.hip", "qcache.hip", "mx.hip", "nf_update.hip", "orth.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-parameter"]

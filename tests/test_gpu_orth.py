@@ -1,0 +1,193 @@
+"""Orthogonal updates on the GPU against 64 bits.  The steps amplify the roundings of whoever carries them out, by how much depends on the matrix: the
+tolerance is taken from the same steps in fp32 on the CPU, whose operands are rounded at 2^-24 where the kernels' two fp16 pieces are at 2^-22, four
+times that, and doubled, as both errors are random; and 2^-20 of the result, some roundings of its own size, where fp32 happens to be nearly exact."""
+import pytest
+import torch
+
+from paper_2402_14139_amd import binding as nf
+from tests import orth_ref as ref
+from tests.pointwise_ref import DT, HALF, TINY, TYPES
+from tests.test_gpu_pointwise import Out, workspace
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def tolerance(g, steps, eps):
+    """The result in 64 bits, and how far (2-norm) fp32 pieces may be off."""
+    want = ref.steps(g.double(), steps, eps)
+    off = (ref.steps(g.float(), steps, eps).double() - want).norm()
+    return want, 8 * off + 2.0 ** -20 * want.norm()
+
+
+def run(t, gs, steps, eps=1e-7, ws=None):
+    d = nf.orth_desc(steps, eps)
+    outs = [Out(*g.shape, dtype=TYPES[t]) for g in gs]
+    ws = workspace(nf.nf_orthogonalise_workspace_bytes(d, [g.shape for g in gs])) if ws is None else ws
+    nf.nf_orthogonalise(d, DT[t], [g.cuda() for g in gs], [o.t for o in outs], ws)
+    return [o.cpu() for o in outs]
+
+
+def check(t, g, got, steps, eps=1e-7):
+    want, tol = tolerance(g, steps, eps)
+    assert torch.isfinite(got).all()
+    off = (got - want).norm()
+    assert off <= tol * (1 + HALF[t]) + HALF[t] * want.norm() + TINY[t] * g.numel() ** 0.5, (off / want.norm(), tol / want.norm())
+
+
+SHAPES = [(1, 1), (1, 7), (7, 1), (3, 5), (16, 27), (27, 16), (64, 64), (65, 63), (63, 200), (100, 576), (577, 100), (130, 130), (512, 300), (64, 4608), (4000, 10), (700, 1030), (1500, 1100)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_orthogonalise(t, rows, cols):
+    g = ref.gradient(torch.Generator().manual_seed(rows * 3 + cols), rows, cols).to(TYPES[t])
+    check(t, g, run(t, [g], ref.MUON)[0], ref.MUON)
+
+
+@pytest.mark.parametrize("steps", [ref.MUON[:1], ref.MUON[:2], ref.CUBIC, ref.QUINTIC, [(8.28721, -23.59589, 17.30039), (4.10706, -2.94785, 0.54484), (2.0, -1.5, 0.5)],
+                                   [(0.5, 0.0, 0.0), (3.0, -1.0, 0.0)], [(0.0, 1.0, 0.0)]])
+@pytest.mark.parametrize("rows,cols", [(40, 90), (200, 70)])
+def test_other_steps(steps, rows, cols):
+    g = torch.randn(rows, cols, generator=torch.Generator().manual_seed(7))
+    check("f32", g, run("f32", [g], steps)[0], steps)
+
+
+def test_singular_values_become_one():
+    """Steps that converge: a matrix of singular values 0.5 to 2 gives an orthogonal one."""
+    gen = torch.Generator().manual_seed(3)
+    q, _ = torch.linalg.qr(torch.randn(96, 96, generator=gen, dtype=torch.float64))
+    p, _ = torch.linalg.qr(torch.randn(240, 96, generator=gen, dtype=torch.float64))
+    g = ((q * torch.linspace(0.5, 2, 96, dtype=torch.float64)) @ p.t()).float()
+    for m in (g, g.t().contiguous()):
+        y = run("f32", [m], [(15 / 8, -10 / 8, 3 / 8)] * 12)[0]
+        gram = y @ y.t() if m is g else y.t() @ y
+        assert (gram - torch.eye(96)).abs().max() < 1e-5   # 12 steps from 0.05 on; what is left are roundings
+        assert (y - ((q @ p.t()) if m is g else (q @ p.t()).t())).abs().max() < 1e-5
+
+
+STACK = [(16, 27), (64, 27), (64, 576), (576, 64), (128, 1152), (10, 512), (256, 256), (1, 9), (300, 2304)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_many_matrices(t):
+    gen = torch.Generator().manual_seed(5)
+    gs = [ref.gradient(gen, *s).to(TYPES[t]) for s in STACK]
+    got = run(t, gs, ref.MUON)
+    for g, y in zip(gs, got):
+        check(t, g, y, ref.MUON)
+    again = run(t, gs, ref.MUON)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+def test_as_many_as_fit():
+    gen = torch.Generator().manual_seed(6)
+    gs = [ref.gradient(gen, 8 + k, 90 - 2 * k) for k in range(nf.NF_ORTH_MATRICES)]
+    for g, y in zip(gs, run("f32", gs, ref.MUON)):
+        check("f32", g, y, ref.MUON)
+
+
+def test_scale_does_not_matter():
+    """Powers of two leave the bits alone, up to the ends of fp32's range; eps is what changes a small matrix."""
+    g = torch.randn(70, 130, generator=torch.Generator().manual_seed(1))
+    y = run("f32", [g], ref.MUON, eps=0.0)[0]
+    for e in (-100, -60, 60, 110):
+        assert torch.equal(run("f32", [g * 2.0 ** e], ref.MUON, eps=0.0)[0], y), e
+    check("f32", g * 1e-6, run("f32", [g * 1e-6], ref.MUON, eps=1e-3)[0], ref.MUON, eps=1e-3)
+
+
+def test_zeros_and_what_is_no_number():
+    z = torch.zeros(30, 50)
+    assert not run("f32", [z], ref.MUON)[0].any()
+    assert run("f32", [z], ref.MUON, eps=0.0)[0].isnan().all()
+    gen = torch.Generator().manual_seed(2)
+    for rows, cols in ((30, 50), (130, 40)):
+        for bad in (float("nan"), float("inf")):
+            good, g = ref.gradient(gen, 20, 70), ref.gradient(gen, rows, cols)
+            g[rows - 1, 3] = bad
+            y = run("f32", [g, good], ref.MUON)
+            assert y[0].isnan().all()
+            check("f32", good, y[1], ref.MUON)
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 100), (100, 40), (200, 200)])
+def test_in_place(rows, cols):
+    gen = torch.Generator().manual_seed(4)
+    gs = [ref.gradient(gen, rows, cols).cuda(), ref.gradient(gen, 33, 70).cuda()]
+    want = run("f32", [g.cpu() for g in gs], ref.MUON)
+    d = nf.orth_desc(ref.MUON)
+    nf.nf_orthogonalise(d, nf.NF_F32, gs, gs, workspace(nf.nf_orthogonalise_workspace_bytes(d, [g.shape for g in gs])))
+    assert all(torch.equal(g.cpu().double(), w) for g, w in zip(gs, want))
+
+
+@pytest.mark.parametrize("momentum,nesterov,decay", [(0.95, 1, 0.0), (0.9, 0, 0.1), (0.0, 1, 0.01), (None, 0, 0.0)])
+def test_muon(momentum, nesterov, decay):
+    """Weights and momentum against the definition; filters [C_out][R][S][C_in] are matrices of C_out rows."""
+    gen = torch.Generator().manual_seed(11)
+    shapes = [(16, 3, 3, 3), (64, 3, 3, 64), (300, 40), (40, 300), (10, 10)]
+    rn = lambda s: torch.randn(*s, generator=gen)  # noqa: E731
+    w = [rn(s) * 0.05 for s in shapes]
+    g = [ref.gradient(gen, s[0], rn(s).numel() // s[0]).reshape(s) for s in shapes]
+    v = [ref.gradient(gen, s[0], rn(s).numel() // s[0]).reshape(s) for s in shapes]
+    mu, lr = float(torch.tensor(momentum or 0.0)), float(torch.tensor(0.02))
+    W, V = [Out(*s) for s in shapes], [Out(*s) for s in shapes]
+    for o, x in zip(W + V, w + v):
+        o.t.copy_(x)
+    d = nf.MuonDesc(lr=lr, momentum=mu, weight_decay=decay, nesterov=nesterov, orth=nf.orth_desc(ref.MUON))
+    nf.nf_muon_update(d, [o.t for o in W], [x.cuda() for x in g], None if momentum is None else [o.t for o in V],
+                      workspace(nf.nf_orthogonalise_workspace_bytes(d.orth, [(s[0], rn(s).numel() // s[0]) for s in shapes])))
+    for k, s in enumerate(shapes):
+        G, V0, W0 = (x[k].double().reshape(s[0], -1) for x in (g, v, w))
+        v1 = mu * V0 + G if mu else V0
+        got_v = V[k].cpu().reshape(s[0], -1)
+        assert ((got_v - v1).abs() <= 2 * U * (mu * V0.abs() + G.abs()) * bool(mu)).all()
+        u = (G + mu * v1 if nesterov else v1) if mu else G
+        O, tol = tolerance(u.float(), ref.MUON, 1e-7)   # u is off by roundings of fp32, as any matrix of fp32 numbers is
+        scale = lr * max(1.0, O.shape[0] / O.shape[1]) ** 0.5
+        keep = 1 - lr * float(torch.tensor(decay))
+        want = keep * W0 - scale * O
+        off = (W[k].cpu().reshape(s[0], -1) - want).norm()
+        assert off <= scale * tol + 4 * U * (W0.norm() + scale * O.norm()), k
+
+
+def test_another_stream_and_a_graph():
+    gen = torch.Generator().manual_seed(8)
+    shapes = [(64, 27), (128, 300), (200, 60)]
+    start = [[torch.randn(*s, generator=gen).cuda() for s in shapes] for _ in range(2)]
+    g = [ref.gradient(gen, *s).cuda() for s in shapes]
+    w, v = [t.clone() for t in start[0]], [t.clone() for t in start[1]]
+    y = [torch.empty_like(t) for t in g]
+    d = nf.MuonDesc(lr=0.1, momentum=0.9, weight_decay=0.1, nesterov=1, orth=nf.orth_desc(ref.MUON))
+    ws = workspace(nf.nf_orthogonalise_workspace_bytes(d.orth, shapes))
+
+    def both(stream):
+        nf.nf_muon_update(d, w, g, v, ws, stream)
+        nf.nf_orthogonalise(d.orth, nf.NF_F32, g, y, ws, stream)
+
+    def again():
+        for a, b in zip(w + v, start[0] + start[1]):
+            a.copy_(b)
+        for a in y:
+            a.zero_()
+
+    both(None)
+    torch.cuda.synchronize()
+    want = [t.clone() for t in w + v + y]
+    again()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    both(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(w + v + y, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(torch.cuda.current_stream())
+    for turn in range(3):
+        again()
+        if turn:
+            both(None)
+            torch.cuda.synchronize()
+            again()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(w + v + y, want)), turn
