@@ -4,7 +4,7 @@
 // matrix is held as two fp16 pieces, h + l = v 2^s to 22 bits, and a product is h h + h l + l h on the fp16 matrix instructions, summed in fp32.  That is
 // three products at 1.4 PFLOP/s where the fp32 instructions reach 150 TFLOP/s.  s is chosen from a bound of the singular values after each step
 // (orth_scales), so that the largest element fits fp16 and what falls below its smallest is 2^-39 of that.
-//   layout   [row][32 columns' h, their l]: a row's step of 32 columns is 128 bytes; sides are padded with zeros to whole tiles
+//   layout   [row][32 columns' h, their l]: a row's step of 32 columns is 128 bytes; sides are padded with zeros to 32
 //   a step   A = X X^T and P = b A + c A^2, both symmetric: the tiles on and above the diagonal, each written twice; X' = a X + P X
 //   a long side lies along the columns: a tall G is held transposed and written back so
 // All matrices of a call share the launches.
@@ -18,7 +18,6 @@
 namespace nf {
 namespace {
 
-using halfx4 = __attribute__((ext_vector_type(4))) _Float16;
 using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 using shortx4 = __attribute__((ext_vector_type(4))) short;
 
@@ -60,25 +59,21 @@ __device__ inline void split(float v, V &h, V &l) {
   h = (_Float16)v;
   l = (_Float16)(v - (float)h);
 }
-__device__ inline void load4(const char *p, float (&v)[4]) {
-  const halfx4 h = *reinterpret_cast<const halfx4 *>(p), l = *reinterpret_cast<const halfx4 *>(p + 64);
+// 8 neighbours of a row
+__device__ inline void get8(const char *p, float (&v)[8]) {
+  const f16x8 h = *reinterpret_cast<const f16x8 *>(p), l = *reinterpret_cast<const f16x8 *>(p + 64);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = (float)h[e] + (float)l[e];
+  for (int e = 0; e < 8; ++e) v[e] = (float)h[e] + (float)l[e];
 }
-__device__ inline void store4(char *p, const float (&v)[4]) {
-  halfx4 h, l;
+__device__ inline void put8(char *p, const float (&v)[8]) {
+  f16x8 h, l;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < 8; ++e) {
     _Float16 x, y;
     split(v[e], x, y);
     h[e] = x, l[e] = y;
   }
-  *reinterpret_cast<halfx4 *>(p) = h, *reinterpret_cast<halfx4 *>(p + 64) = l;
-}
-__device__ inline void store1(char *p, float v) {
-  _Float16 h, l;
-  split(v, h, l);
-  *reinterpret_cast<_Float16 *>(p) = h, *reinterpret_cast<_Float16 *>(p + 64) = l;
+  *reinterpret_cast<f16x8 *>(p) = h, *reinterpret_cast<f16x8 *>(p + 64) = l;
 }
 
 // ---- |G|^2, and the momentum ----
@@ -136,7 +131,7 @@ __global__ __launch_bounds__(NT) void orth_start_kernel(Args a, Tensors t) {
   __shared__ float tile[64][65];
   const int k = item_of(a, blockIdx.x);
   const Item &it = a.it[k];
-  const int id = blockIdx.x - a.first[k], across = it.mp / 64, tr = id / across, r0 = tr * 64, c0 = (id - tr * across) * 64;
+  const int id = blockIdx.x - a.first[k], across = (it.mp + 63) / 64, tr = id / across, r0 = tr * 64, c0 = (id - tr * across) * 64;
   double s = 0;
   const double *const squares = reinterpret_cast<const double *>(a.ws + it.squares);
   for (int i = threadIdx.x; i < it.square_parts; i += NT) s += squares[i];
@@ -152,10 +147,13 @@ __global__ __launch_bounds__(NT) void orth_start_kernel(Args a, Tensors t) {
   }
   __syncthreads();
   char *const X = a.ws + it.x[0];
-  for (int i = threadIdx.x; i < 1024; i += NT) {
-    const int r = i >> 4, c = (i & 15) * 4;
-    const float w[4] = {tile[r][c], tile[r][c + 1], tile[r][c + 2], tile[r][c + 3]};
-    store4(piece(X, 4ll * it.mp, r0 + r, c0 + c), w);
+  for (int i = threadIdx.x; i < 512; i += NT) {
+    const int r = i >> 3, c = (i & 7) * 8;
+    if (r0 + r >= it.np || c0 + c >= it.mp) continue;
+    float w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = tile[r][c + e];
+    put8(piece(X, 4ll * it.mp, r0 + r, c0 + c), w);
   }
 }
 
@@ -164,7 +162,10 @@ enum { GRAM, POLY, APPLY, LAST };
 
 template <int BLOCK>
 struct Tile {
-  static constexpr int BYTES = BLOCK * 128, STAGE = 2 * BYTES, PIECES = BLOCK / 32;
+  static constexpr int DOWN = BLOCK == 96 ? 6 : 2, ACROSS = BLOCK == 128 ? 4 : 2;  // waves of 64 x 32, 16 x 48 and 32 x 32
+  static constexpr int STAGES = 4;
+  static constexpr int WAVES = DOWN * ACROSS, THREADS = 64 * WAVES, MT = BLOCK / 16 / DOWN, NT = BLOCK / 16 / ACROSS;
+  static constexpr int BYTES = BLOCK * 128, STAGE = 2 * BYTES, PIECES = BYTES / 1024 / WAVES;
   static constexpr int ROWB = BLOCK * 4, CPR = ROWB / 16;  // of an operand whose terms lie apart: a term's row
 };
 // chunks of 16 bytes of a row, and units of 32 bytes of a term's row, are exchanged so that what is read together lies in different banks
@@ -192,54 +193,79 @@ __device__ inline f16x8 fragment(const char *lds, int rb, int pl, int lane) {
   }
 }
 
-// Finished sums, 4 neighbours of a row, to where they go.
-template <int KIND, typename OUT, bool MUON>
-__device__ inline void finish4(const Args &a, const Tensors &t, const Item &it, int k, int r, int c, bool mirror, float (&v)[4]) {
+// Finished sums, 8 neighbours of a row.  A and P are written here; what is written across as well, or as the caller's matrix, stays in v.
+template <int KIND>
+__device__ inline void finish8(const Args &a, const Item &it, int r, int c, float (&v)[8]) {
   if constexpr (KIND == GRAM) {
     const float s = a.down_x * a.down_x * a.up_a;
-    char *const A = a.ws + it.A;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] *= s;
-    store4(piece(A, 4ll * it.np, r, c), v);
-    if (mirror) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) store1(piece(A, 4ll * it.np, c + e, r), v[e]);
-    }
+    for (int e = 0; e < 8; ++e) v[e] *= s;
+    put8(piece(a.ws + it.A, 4ll * it.np, r, c), v);
   } else if constexpr (KIND == POLY) {
-    float A[4];
-    load4(piece(a.ws + it.A, 4ll * it.np, r, c), A);
+    float A[8];
+    get8(piece(a.ws + it.A, 4ll * it.np, r, c), A);
     const float sa = a.b * a.down_a * a.up_p, ss = a.c * a.down_a * a.down_a * a.up_p;
-    char *const P = a.ws + it.P;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaf(A[e], sa, v[e] * ss);
-    store4(piece(P, 4ll * it.np, r, c), v);
-    if (mirror) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) store1(piece(P, 4ll * it.np, c + e, r), v[e]);
-    }
+    for (int e = 0; e < 8; ++e) v[e] = fmaf(A[e], sa, v[e] * ss);
+    put8(piece(a.ws + it.P, 4ll * it.np, r, c), v);
   } else {
-    float X[4];
-    load4(piece(a.ws + it.x[a.cur], 4ll * it.mp, r, c), X);
+    float X[8];
+    get8(piece(a.ws + it.x[a.cur], 4ll * it.mp, r, c), X);
     const float up = KIND == LAST ? 1.f : a.up_next, sx = a.a * a.down_x * up, ss = a.down_p * a.down_x * up;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaf(X[e], sx, v[e] * ss);
-    if constexpr (KIND == APPLY) {
-      store4(piece(a.ws + it.x[a.cur ^ 1], 4ll * it.mp, r, c), v);
-    } else {
-      const bool tall = it.rows > it.cols;
-      const float shape = tall ? sqrtf((float)it.rows / (float)it.cols) : 1.f;
-      if (r >= it.n) return;
-      OUT *const y = (OUT *)t.y[k];
+    for (int e = 0; e < 8; ++e) v[e] = fmaf(X[e], sx, v[e] * ss);
+    if constexpr (KIND == APPLY) put8(piece(a.ws + it.x[a.cur ^ 1], 4ll * it.mp, r, c), v);
+  }
+}
+// 8 neighbours of a row of the caller's matrix, n of which lie inside
+template <typename OUT, bool MUON>
+__device__ inline void give8(const Tensors &t, const Item &it, int k, int row, int col, int n, float (&v)[8]) {
+  OUT *const y = (OUT *)t.y[k] + (long long)row * it.cols + col;
+  if constexpr (MUON) {
+    const float rate = t.lr * (it.rows > it.cols ? sqrtf((float)it.rows / (float)it.cols) : 1.f);
+    float w[8];
+    load8(y, w, n);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (c + e >= it.m) continue;
-        const long long at = tall ? (long long)(c + e) * it.cols + r : (long long)r * it.cols + c + e;
-        if constexpr (MUON)
-          y[at] = fmaf(-t.lr * shape, v[e], t.keep * (float)y[at]);
-        else
-          y[at] = (OUT)v[e];
-      }
+    for (int e = 0; e < 8; ++e) v[e] = fmaf(-rate, v[e], t.keep * w[e]);
+  }
+  store8(y, v, n);
+}
+
+// A tile of sums in LDS (rows of LDW words) to memory.  Symmetric results of a tile off the diagonal are written across, too.
+template <int BLOCK, int THREADS, int KIND, typename OUT, bool MUON>
+__device__ inline void tile_out(const Args &a, const Tensors &t, const Item &it, int k, int tr, int tc, float *W) {
+  constexpr int LDW = BLOCK + 4, ITEMS = BLOCK * BLOCK / 8;
+  const int rows = it.np - tr * BLOCK, cols = (KIND <= POLY ? it.np : it.mp) - tc * BLOCK;  // inside, whole 32s
+  const bool tall = it.rows > it.cols, across = KIND <= POLY ? tr != tc : KIND == LAST && tall;
+  __syncthreads();
+  for (int i = threadIdx.x; i < ITEMS; i += THREADS) {
+    const int r = i / (BLOCK / 8), c = i % (BLOCK / 8) * 8;
+    if (r >= rows || c >= cols) continue;
+    float v[8];
+    floatx4 *const at = reinterpret_cast<floatx4 *>(W + r * LDW + c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = at[0][e], v[e + 4] = at[1][e];
+    finish8<KIND>(a, it, tr * BLOCK + r, tc * BLOCK + c, v);
+    if (across) {
+      at[0] = floatx4{v[0], v[1], v[2], v[3]}, at[1] = floatx4{v[4], v[5], v[6], v[7]};
+    } else if constexpr (KIND == LAST) {
+      const int row = tr * BLOCK + r, col = tc * BLOCK + c;
+      if (row < it.n && col < it.m) give8<OUT, MUON>(t, it, k, row, col, it.m - col, v);
     }
+  }
+  if (!across) return;
+  __syncthreads();
+  for (int i = threadIdx.x; i < ITEMS; i += THREADS) {  // 8 neighbours of a column
+    const int c = i / (BLOCK / 8), r = i % (BLOCK / 8) * 8;
+    if (r >= rows || c >= cols) continue;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = W[(r + e) * LDW + c];
+    const int row = tc * BLOCK + c, col = tr * BLOCK + r;
+    if constexpr (KIND <= POLY)
+      put8(piece(a.ws + (KIND == GRAM ? it.A : it.P), 4ll * it.np, row, col), v);
+    else if (row < it.m && col < it.n)
+      give8<OUT, MUON>(t, it, k, row, col, it.n - col, v);
   }
 }
 
@@ -251,155 +277,202 @@ __device__ inline void triangle(int t, int &tr, int &tc) {
   tr = t - tc * (tc + 1) / 2;
 }
 
-// BLOCK x BLOCK results by four waves of BLOCK/2 x BLOCK/2; a step is 32 terms.  STAGES of them are in flight: one barrier a step, behind which its
-// stage is whole and the one before it free.  Steps beyond the last are copies of nothing, so that the waits count the same.
-template <int BLOCK, int STAGES, int KIND, typename OUT, bool MUON>
-__global__ __launch_bounds__(LT) void orth_product_kernel(Args a, Tensors t) {
+// BLOCK x BLOCK results by four waves of BLOCK/2 x BLOCK/2; a step is 32 terms.  While a step's products run, the next one's fragments are read and the
+// copies of the STAGES-th next are on their way: one barrier a step, behind which the next stage is whole and this one free.  Steps go in pairs
+// (two sets of fragments); those beyond the last are copies of nothing, so that the waits count the same.
+template <int BLOCK, int KIND, typename OUT, bool MUON>
+__global__ __launch_bounds__(Tile<BLOCK>::THREADS) void orth_product_kernel(Args a, Tensors t) {
   using S = Tile<BLOCK>;
   constexpr bool APART = KIND >= APPLY;
-  constexpr int MT = BLOCK / 32, PIECES = S::PIECES;
-  __shared__ __align__(1024) char lds[STAGES * S::STAGE];
+  constexpr int MT = S::MT, NT = S::NT, STAGES = S::STAGES, WAVES = S::WAVES, PIECES = S::PIECES;
+  constexpr int OUT_BYTES = BLOCK * (BLOCK + 4) * 4, RING = STAGES * S::STAGE;
+  __shared__ __align__(1024) char lds[RING > OUT_BYTES ? RING : OUT_BYTES];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, q = lane >> 4;
-  const int k = __builtin_amdgcn_readfirstlane(item_of(a, blockIdx.x));
+  const int block = xcd_run(blockIdx.x, gridDim.x), k = __builtin_amdgcn_readfirstlane(item_of(a, block));
   const Item &it = a.it[k];
-  int id = blockIdx.x - a.first[k], split = 0, tr, tc;
+  int id = block - a.first[k], split = 0, tr, tc;
   if constexpr (KIND <= POLY) {
-    const int T = it.np / BLOCK, tiles = T * (T + 1) / 2;
+    const int T = (it.np + BLOCK - 1) / BLOCK, tiles = T * (T + 1) / 2;
     if (KIND == GRAM) split = id / tiles, id -= split * tiles;
     triangle(id, tr, tc);
   } else {
-    const int down = it.np / BLOCK;
-    tc = id / down, tr = id - tc * down;
+    // four rows of tiles at a time, column by column: workgroups of an XCD share few rows and columns
+    const int down = (it.np + BLOCK - 1) / BLOCK, across = (it.mp + BLOCK - 1) / BLOCK, band = id / (4 * across), deep = min(4, down - 4 * band);
+    id -= band * 4 * across, tc = id / deep, tr = 4 * band + id - tc * deep;
   }
   const long long ld_a = 4ll * (KIND == GRAM ? it.mp : it.np), ld_b = 4ll * (KIND == POLY ? it.np : it.mp);
   const char *const A = a.ws + (KIND == GRAM ? it.x[a.cur] : KIND == POLY ? it.A : it.P) + (long long)tr * BLOCK * ld_a;
   const char *const B = a.ws + (KIND == POLY ? it.A : it.x[a.cur]) + (APART ? (long long)tc * BLOCK * 4 : (long long)tc * BLOCK * ld_b);
   const int all = (KIND == GRAM ? it.mp : it.np) / 32, s0 = KIND == GRAM ? split * it.per : 0, steps = KIND == GRAM ? min(it.per, all - s0) : all;
+  const int rows = it.np - tr * BLOCK, cols = (KIND <= POLY ? it.np : it.mp) - tc * BLOCK;  // inside
   uint32_t av[PIECES], bv[PIECES];
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
-    const int at = (p * 4 + wave) * 64 + lane, row = at >> 3;
-    av[p] = (uint32_t)(row * ld_a) + (((at & 7) ^ chunk_swizzle(row)) << 4);
+    const int at = (p * WAVES + wave) * 64 + lane, row = at >> 3;
+    av[p] = row < rows ? (uint32_t)(row * ld_a) + (((at & 7) ^ chunk_swizzle(row)) << 4) : OUTSIDE;
     if (APART) {
-      const int term = at / S::CPR, c = at % S::CPR;
-      bv[p] = (uint32_t)(term * ld_b) + ((c ^ (unit_swizzle(term) << 1)) << 4);
+      const int term = at / S::CPR, c = (at % S::CPR) ^ (unit_swizzle(term) << 1);
+      bv[p] = c * 4 < cols ? (uint32_t)(term * ld_b) + (c << 4) : OUTSIDE;
     } else {
-      bv[p] = (uint32_t)(row * ld_b) + (((at & 7) ^ chunk_swizzle(row)) << 4);
+      bv[p] = row < cols ? (uint32_t)(row * ld_b) + (((at & 7) ^ chunk_swizzle(row)) << 4) : OUTSIDE;
     }
   }
-  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-  auto fetch = [&](int s, int stage) {
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
+  auto fetch = [&](int s, int stage, int from, int until) {
     const uintx4 ba = buffer_of(A + (s0 + s) * 128ll), bb = buffer_of(B + (APART ? (long long)s * 32 * ld_b : (s0 + s) * 128ll));
-    const uint32_t to = base + stage * S::STAGE + wave * 1024;
-    const bool live = s < steps;
+    const uint32_t to = base + stage * S::STAGE, none = s < steps ? 0u : OUTSIDE;  // an offset with OUTSIDE's bits lies outside, whatever the others
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) copy16(ba, live ? av[p] : OUTSIDE, to + p * 4096);
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) copy16(bb, live ? bv[p] : OUTSIDE, to + S::BYTES + p * 4096);
+    for (int p = 0; p < 2 * PIECES; ++p)
+      if (p >= from && p < until)
+        p < PIECES ? copy16(ba, av[p % PIECES] | none, to + p * (1024 * WAVES)) : copy16(bb, bv[p % PIECES] | none, to + S::BYTES + (p - PIECES) * (1024 * WAVES));
   };
-  const int wm = (wave >> 1) * (BLOCK / 2), wn = (wave & 1) * (BLOCK / 2);
-  floatx4 acc[MT][MT];
+  const int wm = wave / S::ACROSS * (16 * MT), wn = wave % S::ACROSS * (16 * NT);
+  floatx4 acc[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < MT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  struct Set {
+    f16x8 a[MT][2], b[NT][2];
+  };
+  auto read = [&](Set &f, int stage) {
+    const char *const la = lds + stage * S::STAGE, *const lb = la + S::BYTES;
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s) fetch(s, s);
+    for (int pl = 0; pl < 2; ++pl)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) f.a[i][pl] = fragment<BLOCK, false>(la, wm + 16 * i, pl, lane);
+#pragma unroll
+    for (int pl = 0; pl < 2; ++pl)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) f.b[j][pl] = fragment<BLOCK, APART>(lb, wn + 16 * j, pl, lane);
+  };
   int stage = 0;
-  for (int s = 0; s < steps; ++s) {
+  auto step = [&](int s, Set &now, Set &next) {
     wait_copies<(STAGES - 2) * 2 * PIECES>();
     wait_lds();
     barrier();
-    fetch(s + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
-    const char *const la = lds + stage * S::STAGE, *const lb = la + S::BYTES;
-    f16x8 fa[MT][2], fb[MT][2];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int pl = 0; pl < 2; ++pl) fa[i][pl] = fragment<BLOCK, false>(la, wm + 16 * i, pl, lane), fb[i][pl] = fragment<BLOCK, APART>(lb, wn + 16 * i, pl, lane);
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[j][0], fa[i][1], acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[j][1], fa[i][0], acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[j][0], fa[i][0], acc[i][j], 0, 0, 0);
-      }
+    const int free = stage;
     stage = stage + 1 == STAGES ? 0 : stage + 1;
+    read(next, stage);
+    constexpr int EACH = (2 * PIECES + MT - 1) / MT;  // copies between a row of fragments and the next
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.b[j][0], now.a[i][1], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.b[j][1], now.a[i][0], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.b[j][0], now.a[i][0], acc[i][j], 0, 0, 0);
+      }
+      fetch(s + STAGES, free, i * EACH, (i + 1) * EACH);
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < STAGES; ++s) fetch(s, s, 0, 2 * PIECES);
+  wait_copies<(STAGES - 1) * 2 * PIECES>();
+  barrier();
+  Set even, odd;
+  read(even, 0);
+  for (int s = 0; s < steps; s += 2) {
+    step(s, even, odd);
+    step(s + 1, odd, even);
   }
   wait_copies<0>();
+  wait_lds();
   // a lane has 4 neighbouring columns of a row
-  float *const part = KIND == GRAM && it.splits > 1 ? reinterpret_cast<float *>(a.ws + it.part) + (long long)(blockIdx.x - a.first[k]) * BLOCK * BLOCK : nullptr;
+  if (KIND == GRAM && it.splits > 1) {
+    float *const part = reinterpret_cast<float *>(a.ws + it.part) + (long long)(block - a.first[k]) * BLOCK * BLOCK;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) *reinterpret_cast<floatx4 *>(part + (wm + 16 * i + i16) * BLOCK + wn + 16 * j + 4 * q) = acc[i][j];
+    return;
+  }
+  barrier();
+  float *const W = reinterpret_cast<float *>(lds);
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-      const int r = wm + 16 * i + i16, c = wn + 16 * j + 4 * q;
-      if (KIND == GRAM && part) {
-        *reinterpret_cast<floatx4 *>(part + r * BLOCK + c) = acc[i][j];
-      } else {
-        float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-        finish4<KIND, OUT, MUON>(a, t, it, k, tr * BLOCK + r, tc * BLOCK + c, tr != tc, v);
-      }
-    }
+    for (int j = 0; j < NT; ++j) *reinterpret_cast<floatx4 *>(W + (wm + 16 * i + i16) * (BLOCK + 4) + wn + 16 * j + 4 * q) = acc[i][j];
+  tile_out<BLOCK, S::THREADS, KIND, OUT, MUON>(a, t, it, k, tr, tc, W);
 }
 
-// the parts of A's sums, in order; 4 neighbours of a row to a thread
-template <int BLOCK>
+// the parts of A's sums, in order, a tile to a workgroup
 __global__ __launch_bounds__(LT) void orth_parts_kernel(Args a) {
-  constexpr int WGS = BLOCK * BLOCK / 4 / LT;  // workgroups of a tile
+  constexpr int BLOCK = 64;
+  __shared__ __align__(16) float W[BLOCK * (BLOCK + 4)];
   const int k = __builtin_amdgcn_readfirstlane(item_of(a, blockIdx.x));
   const Item &it = a.it[k];
-  const int id = blockIdx.x - a.first[k], tile = id / WGS, i = (id - tile * WGS) * LT + threadIdx.x, r = i / (BLOCK / 4), c = i % (BLOCK / 4) * 4;
-  const int T = it.np / BLOCK, tiles = T * (T + 1) / 2;
+  const int tile = blockIdx.x - a.first[k], T = (it.np + BLOCK - 1) / BLOCK, tiles = T * (T + 1) / 2;
   int tr, tc;
   triangle(tile, tr, tc);
-  const float *const part = reinterpret_cast<const float *>(a.ws + it.part) + (long long)tile * BLOCK * BLOCK + r * BLOCK + c;
-  floatx4 s = *reinterpret_cast<const floatx4 *>(part);
+  const float *const part = reinterpret_cast<const float *>(a.ws + it.part) + (long long)tile * BLOCK * BLOCK;
+  for (int i = threadIdx.x; i < BLOCK * BLOCK / 4; i += LT) {
+    floatx4 s = reinterpret_cast<const floatx4 *>(part)[i];
 #pragma unroll 4
-  for (int z = 1; z < it.splits; ++z) s += *reinterpret_cast<const floatx4 *>(part + (long long)z * tiles * BLOCK * BLOCK);
-  float v[4] = {s[0], s[1], s[2], s[3]};
+    for (int z = 1; z < it.splits; ++z) s += reinterpret_cast<const floatx4 *>(part + (long long)z * tiles * BLOCK * BLOCK)[i];
+    *reinterpret_cast<floatx4 *>(W + i / (BLOCK / 4) * (BLOCK + 4) + i % (BLOCK / 4) * 4) = s;
+  }
   const Tensors none = {};
-  finish4<GRAM, float, false>(a, none, it, k, tr * BLOCK + r, tc * BLOCK + c, tr != tc, v);
+  tile_out<BLOCK, LT, GRAM, float, false>(a, none, it, k, tr, tc, W);
 }
 
 // ---- plans ----
 struct Plan {
   Args a;
-  int block;
+  int sym, app;  // tiles of the symmetric products, and of the others
   bool parts;
   size_t bytes;
 };
 
+inline long long tiles_of(int side, int block) { return (side + block - 1) / block; }
 inline long long triangle_tiles(const Item &it, int block) {
-  const long long T = it.np / block;
+  const long long T = tiles_of(it.np, block);
   return T * (T + 1) / 2;
+}
+
+// Tiles of the symmetric products: rounds over the workgroups that run together (two of 64 to a CU, one of 96 or 128) by a round's time.  2048x2048: 253
+// tiles of 96 36 us, 528 of 64 44, 136 of 128 46.  The 17 matrices of 64x27 to 512x4608, whose tiles differ in length: 64 and parts 31, 96 42, 128 60.
+int symmetric_tile(const Args &a) {
+  constexpr int sides[3] = {64, 96, 128}, slots[3] = {512, 256, 256};
+  constexpr double time[3] = {0.60, 0.60, 0.72};  // us a step
+  double best = 1e300;
+  int side = 64;
+  for (int i = 0; i < 3; ++i) {
+    double tiles = 0, work = 0, longest = 0;
+    for (int k = 0; k < a.count; ++k) {
+      const double t = (double)triangle_tiles(a.it[k], sides[i]), steps = a.it[k].mp / 32;
+      tiles += t, work += t * steps, longest = std::max(longest, steps);
+    }
+    const double rounds = tiles <= slots[i] ? 1.0 : a.count == 1 ? std::ceil(tiles / slots[i]) : tiles / slots[i];
+    // few tiles of 64 are cut into parts of their sums
+    const double t = i == 0 && tiles < slots[i] ? std::min(time[i] * longest, time[i] * std::max(16.0, work / slots[i]) + 7) : time[i] * rounds * work / tiles;
+    if (t < best) best = t, side = sides[i];
+  }
+  return side;
 }
 
 Plan plan_of(const nf_orth_desc &d, int count, const int32_t *rows, const int32_t *cols) {
   Plan p = {};
   Args &a = p.a;
   a.count = count, a.eps = d.eps;
-  long long tiles = 0;
-  for (int k = 0; k < count; ++k) {
-    const long long n = std::min(rows[k], cols[k]), T = (n + 127) / 128;
-    tiles += T * (T + 1) / 2;
-  }
-  p.block = tiles >= 128 ? 128 : 64;
-  const int B = p.block;
-  long long work = 0;
   for (int k = 0; k < count; ++k) {
     Item &it = a.it[k];
     it.rows = rows[k], it.cols = cols[k], it.n = std::min(rows[k], cols[k]), it.m = std::max(rows[k], cols[k]);
-    it.np = (it.n + B - 1) / B * B, it.mp = (it.m + B - 1) / B * B;
+    it.np = (it.n + 31) / 32 * 32, it.mp = (it.m + 31) / 32 * 32;
     const long long all = (long long)it.rows * it.cols;
     it.chunk = 8192;
     while ((all + it.chunk - 1) / it.chunk > 1024) it.chunk *= 2;
     it.square_parts = (int)((all + it.chunk - 1) / it.chunk);
-    work += triangle_tiles(it, B) * (it.mp / 32);
   }
-  // parts of A's sums: towards 512 workgroups of the same length, 16 steps each at least
-  const int each = (int)std::max<long long>(16, (work + 511) / 512);
+  long long large = 0;
+  for (int k = 0; k < count; ++k) large += tiles_of(a.it[k].np, 128) * tiles_of(a.it[k].mp, 128);
+  p.sym = symmetric_tile(a);
+  p.app = large >= 192 ? 128 : 64;  // the same 17 matrices, 683 tiles of 128: 49 us, of 64 53; 2048x2048, 256 tiles: 48 and 62
+  const int B = p.sym;
+  long long work = 0;
+  for (int k = 0; k < count; ++k) work += triangle_tiles(a.it[k], B) * (a.it[k].mp / 32);
+  // parts of A's sums in tiles of 64: towards 512 workgroups of the same length, 16 steps each at least
+  const int each = (int)std::max<long long>(16, B == 64 ? (work + 511) / 512 : 1ll << 20);
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t was = at;
@@ -431,21 +504,23 @@ unsigned lay(Args &a, F workgroups) {
 }
 
 template <int KIND, typename OUT, bool MUON>
-hipError_t product(Plan &p, const Tensors &t, const char *name128, const char *name64, hipStream_t st) {
-  const int B = p.block;
+hipError_t product(Plan &p, const Tensors &t, const char *const (&names)[3], hipStream_t st) {
+  const int B = KIND <= POLY ? p.sym : p.app;
   double flops = 0;
   const unsigned grid = lay(p.a, [&](const Item &it) -> long long {
     const double side = KIND == POLY ? it.n : it.m;
     flops += (KIND <= POLY ? 1.0 : 2.0) * it.n * it.n * side;
     if (KIND == GRAM) return triangle_tiles(it, B) * it.splits;
     if (KIND == POLY) return triangle_tiles(it, B);
-    return (long long)(it.np / B) * (it.mp / B);
+    return tiles_of(it.np, B) * tiles_of(it.mp, B);
   });
-  return recorded(st, B == 128 ? name128 : name64, flops, 0.0, [&] {
-    if (B == 128)
-      hipLaunchKernelGGL((orth_product_kernel<128, 2, KIND, OUT, MUON>), dim3(grid), dim3(LT), 0, st, p.a, t);
-    else
-      hipLaunchKernelGGL((orth_product_kernel<64, 4, KIND, OUT, MUON>), dim3(grid), dim3(LT), 0, st, p.a, t);
+  return recorded(st, names[B == 64 ? 0 : B == 96 ? 1 : 2], flops, 0.0, [&] {
+    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, st, p.a, t); };
+    if (B == 64) return go(orth_product_kernel<64, KIND, OUT, MUON>, Tile<64>::THREADS);
+    if constexpr (KIND <= POLY) {
+      if (B == 96) return go(orth_product_kernel<96, KIND, OUT, MUON>, Tile<96>::THREADS);
+    }
+    go(orth_product_kernel<128, KIND, OUT, MUON>, Tile<128>::THREADS);
   });
 }
 
@@ -500,7 +575,7 @@ hipError_t run(const nf_orth_desc &d, Plan &p, const Tensors &t, hipStream_t st)
   hipError_t e = recorded(st, "orth_squares", 0.0, sizeof(T) * (MUON ? 3.0 : 1.0) * elements,
                           [&] { hipLaunchKernelGGL((orth_squares_kernel<T, MUON>), dim3(grid), dim3(NT), 0, st, a, t); });
   if (e != hipSuccess) return e;
-  grid = lay(a, [](const Item &it) { return (long long)(it.np / 64) * (it.mp / 64); });
+  grid = lay(a, [](const Item &it) { return tiles_of(it.np, 64) * tiles_of(it.mp, 64); });
   e = recorded(st, "orth_start", 0.0, (sizeof(T) * (MUON ? 2.0 : 1.0) + 4.0) * elements,
                [&] { hipLaunchKernelGGL((orth_start_kernel<T, MUON>), dim3(grid), dim3(NT), 0, st, a, t); });
   for (int k = 0; k < d.steps && e == hipSuccess; ++k) {
@@ -508,20 +583,14 @@ hipError_t run(const nf_orth_desc &d, Plan &p, const Tensors &t, hipStream_t st)
     a.cur = k & 1, a.a = d.a[k], a.b = d.b[k], a.c = d.c[k];
     a.up_x = two(s[k].x), a.down_x = two(-s[k].x), a.up_a = two(s[k].a), a.down_a = two(-s[k].a), a.up_p = two(s[k].p), a.down_p = two(-s[k].p);
     a.up_next = two(end ? last : s[k + 1].x);
-    e = product<GRAM, float, false>(p, t, "orth_gram_128x128", "orth_gram_64x64", st);
+    e = product<GRAM, float, false>(p, t, {"orth_gram_64x64", "orth_gram_96x96", "orth_gram_128x128"}, st);
     if (e == hipSuccess && p.parts) {
-      const int B = p.block;
-      grid = lay(a, [&](const Item &it) { return it.splits > 1 ? triangle_tiles(it, B) * (B * B / 4 / LT) : 0ll; });
-      e = recorded(st, "orth_parts", 0.0, 0.0, [&] {
-        if (B == 128)
-          hipLaunchKernelGGL(orth_parts_kernel<128>, dim3(grid), dim3(LT), 0, st, a);
-        else
-          hipLaunchKernelGGL(orth_parts_kernel<64>, dim3(grid), dim3(LT), 0, st, a);
-      });
+      grid = lay(a, [&](const Item &it) { return it.splits > 1 ? triangle_tiles(it, 64) : 0ll; });
+      e = recorded(st, "orth_parts", 0.0, 0.0, [&] { hipLaunchKernelGGL(orth_parts_kernel, dim3(grid), dim3(LT), 0, st, a); });
     }
-    if (e == hipSuccess) e = product<POLY, float, false>(p, t, "orth_poly_128x128", "orth_poly_64x64", st);
+    if (e == hipSuccess) e = product<POLY, float, false>(p, t, {"orth_poly_64x64", "orth_poly_96x96", "orth_poly_128x128"}, st);
     if (e != hipSuccess) break;
-    e = end ? product<LAST, T, MUON>(p, t, "orth_last_128x128", "orth_last_64x64", st) : product<APPLY, float, false>(p, t, "orth_apply_128x128", "orth_apply_64x64", st);
+    e = end ? product<LAST, T, MUON>(p, t, {"orth_last_64x64", "", "orth_last_128x128"}, st) : product<APPLY, float, false>(p, t, {"orth_apply_64x64", "", "orth_apply_128x128"}, st);
   }
   return e;
 }
