@@ -198,7 +198,7 @@ typedef struct {
 } nf_orth_desc;
 int32_t nf_orthogonalise_workspace_bytes(const nf_orth_desc *d, int32_t n_matrices, const int32_t *rows,
                                          const int32_t *cols, size_t *out);
-/* y = the last X, in G's type (NF_F32, NF_BF16, NF_F16).  y may be g; no two y may be the same. */
+/* y = the last X, in G's type (NF_F32, NF_BF16, NF_F16).  A matrix's y may be its g, not another one's; no two y may be the same. */
 int32_t nf_orthogonalise(const nf_orth_desc *d, int32_t dtype, int32_t n_matrices, const void *const *g, void *const *y,
                          const int32_t *rows, const int32_t *cols, void *ws, size_t ws_bytes, void *stream);
 /* nf_sgd_update for weight matrices, the update made orthogonal (filters [C_out][R][S][C_in] are matrices of C_out rows):

@@ -57,6 +57,9 @@ int32_t nf_orthogonalise(const nf_orth_desc *d, int32_t dtype, int32_t n_matrice
   if (rc) return rc;
   if (dtype != NF_F32 && dtype != NF_BF16 && dtype != NF_F16) return NF_ERR_BAD_DESC;
   if ((rc = check_pointers(n_matrices, g, false)) || (rc = check_pointers(n_matrices, y, true))) return rc;
+  for (int i = 0; i < n_matrices; ++i)  // a matrix may be done before another one is read
+    for (int k = 0; k < n_matrices; ++k)
+      if (i != k && y[i] == g[k]) return NF_ERR_BAD_DESC;
   if ((rc = check_ws(ws, ws_bytes, orth_workspace_bytes(*d, n_matrices, rows, cols)))) return rc;
   NF_HIP(launch_orth(*d, dtype, n_matrices, g, y, rows, cols, ws, static_cast<hipStream_t>(stream)));
   return NF_OK;

@@ -416,10 +416,158 @@ __global__ __launch_bounds__(LT) void orth_parts_kernel(Args a) {
   tile_out<BLOCK, LT, GRAM, float, false>(a, none, it, k, tr, tc, W);
 }
 
+// ---- small matrices ----
+// A matrix to a workgroup, all steps in LDS: nothing but barriers between the products of 16 x 16 results, which are shared out among the waves.  16x27 10 us,
+// in the launches above 70 (17 of 4 us each).  Rows are 16 bytes longer than their elements: the 16 that a fragment takes lie in different banks.
+struct Small {
+  float a[NF_ORTH_STEPS], b[NF_ORTH_STEPS], c[NF_ORTH_STEPS];
+  float up_x[NF_ORTH_STEPS + 1], up_a[NF_ORTH_STEPS], up_p[NF_ORTH_STEPS];  // 2^s, as Args has them
+  int steps;
+};
+constexpr int FEW_LDS = 32 << 10, MANY_LDS = (160 << 10) - 256;
+__host__ __device__ inline int small_row(int columns) { return columns * 4 + 16; }
+inline int small_bytes(const Item &it) { return it.np * (small_row(it.mp) + 2 * small_row(it.np)); }
+
+template <typename T, bool MUON, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void orth_small_kernel(Args a, Tensors t, Small m) {
+  constexpr int THREADS = 64 * WAVES;
+  __shared__ __align__(16) char lds[WAVES == 4 ? FEW_LDS : MANY_LDS];
+  __shared__ double sums[WAVES];
+  const int k = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, q = lane >> 4;
+  const Item &it = a.it[k];
+  const int ldx = small_row(it.mp), lda = small_row(it.np), down = it.np / 16;
+  char *const X = lds, *const A = X + it.np * ldx, *const P = A + it.np * lda;
+  const T *const g = (const T *)t.g[k];
+  float *const v = MUON ? t.v[k] : nullptr;
+  const bool tall = it.rows > it.cols;
+  const int all = it.rows * it.cols;
+  double s = 0;
+  for (int i = tid; i < all; i += THREADS) {
+    float x = (float)g[i];
+    if (MUON && v) {
+      const float n = fmaf(t.momentum, v[i], x);
+      v[i] = n;
+      x = t.nesterov ? fmaf(t.momentum, n, x) : n;
+    }
+    s += (double)x * x;
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+  if (lane == 0) sums[wave] = s;
+  for (int i = tid; i < it.np * ldx / 16; i += THREADS) reinterpret_cast<uintx4 *>(X)[i] = uintx4{0, 0, 0, 0};
+  __syncthreads();
+  s = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) s += sums[w];
+  const float norm = (float)sqrt(s) + a.eps;
+  for (int i = tid; i < all; i += THREADS) {  // the elements that this thread has read and written above
+    const int row = i / it.cols, col = i - row * it.cols, r = tall ? col : row, c = tall ? row : col;
+    _Float16 h, l;
+    split(direction<T, MUON>(t, g, v, i) / norm * m.up_x[0], h, l);
+    char *const p = piece(X, ldx, r, c);
+    *reinterpret_cast<_Float16 *>(p) = h, *reinterpret_cast<_Float16 *>(p + 64) = l;
+  }
+  __syncthreads();
+  auto rows16 = [&](const char *p, int ld, int rb, int kk, int pl) { return *reinterpret_cast<const f16x8 *>(p + (rb + i16) * ld + kk * 128 + pl * 64 + q * 16); };
+  auto terms16 = [&](const char *p, int ld, int cb, int kk, int pl) {  // columns cb .. of an operand whose rows are terms
+    uintx4 f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const char *at = p + (kk * 32 + q * 8 + h * 4 + (i16 >> 2)) * ld + (cb >> 5) * 128 + pl * 64 + (cb & 31) * 2 + (i16 & 3) * 8;
+      const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4 *)at));
+      f[2 * h] = w.x, f[2 * h + 1] = w.y;
+    }
+    return __builtin_bit_cast(f16x8, f);
+  };
+  auto three = [&](const f16x8 &ah, const f16x8 &al, const f16x8 &bh, const f16x8 &bl, floatx4 acc) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(bh, al, acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(bl, ah, acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(bh, ah, acc, 0, 0, 0);
+  };
+  auto get4 = [&](const char *p, float (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (float)reinterpret_cast<const _Float16 *>(p)[e] + (float)reinterpret_cast<const _Float16 *>(p + 64)[e];
+  };
+  auto put4 = [&](char *p, const float (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      _Float16 h, l;
+      split(x[e], h, l);
+      reinterpret_cast<_Float16 *>(p)[e] = h, reinterpret_cast<_Float16 *>(p + 64)[e] = l;
+    }
+  };
+  for (int step = 0; step < m.steps; ++step) {
+    const bool last = step + 1 == m.steps;
+    const float up_x = m.up_x[step], up_a = m.up_a[step], up_p = m.up_p[step], up_next = last ? 1.f : m.up_x[step + 1];
+    for (int z = wave; z < down * down; z += WAVES) {  // A = X X^T
+      const int rb = z / down * 16, cb = z % down * 16;
+      floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+      for (int kk = 0; kk < it.mp / 32; ++kk)
+        acc = three(rows16(X, ldx, rb, kk, 0), rows16(X, ldx, rb, kk, 1), rows16(X, ldx, cb, kk, 0), rows16(X, ldx, cb, kk, 1), acc);
+      const float scale = up_a / (up_x * up_x), w[4] = {acc[0] * scale, acc[1] * scale, acc[2] * scale, acc[3] * scale};
+      put4(piece(A, lda, rb + i16, cb + 4 * q), w);
+    }
+    __syncthreads();
+    for (int z = wave; z < down * down; z += WAVES) {  // P = b A + c A^2
+      const int rb = z / down * 16, cb = z % down * 16;
+      floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+      for (int kk = 0; kk < it.np / 32; ++kk)
+        acc = three(rows16(A, lda, rb, kk, 0), rows16(A, lda, rb, kk, 1), rows16(A, lda, cb, kk, 0), rows16(A, lda, cb, kk, 1), acc);
+      float w[4];
+      get4(piece(A, lda, rb + i16, cb + 4 * q), w);
+      const float sa = m.b[step] * (up_p / up_a), ss = m.c[step] * (up_p / up_a / up_a);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = fmaf(w[e], sa, acc[e] * ss);
+      put4(piece(P, lda, rb + i16, cb + 4 * q), w);
+    }
+    __syncthreads();
+    const float sx = m.a[step] * (up_next / up_x), ss = up_next / up_p / up_x;
+    for (int cb = wave * 16; cb < it.mp; cb += WAVES * 16) {  // X' = a X + P X, in place: 16 columns need no others
+      f16x8 bh[2], bl[2];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+        if (kk * 32 < it.np) bh[kk] = terms16(X, ldx, cb, kk, 0), bl[kk] = terms16(X, ldx, cb, kk, 1);
+      float w[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i * 16 >= it.np) break;
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+          if (kk * 32 < it.np) acc = three(rows16(P, lda, i * 16, kk, 0), rows16(P, lda, i * 16, kk, 1), bh[kk], bl[kk], acc);
+        get4(piece(X, ldx, i * 16 + i16, cb + 4 * q), w[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[i][e] = fmaf(w[i][e], sx, acc[e] * ss);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i * 16 >= it.np) break;
+        const int r = i * 16 + i16, c = cb + 4 * q;
+        if (!last) {
+          put4(piece(X, ldx, r, c), w[i]);
+        } else if (r < it.n) {
+          T *const y = (T *)t.y[k];
+          const float rate = t.lr * (tall ? sqrtf((float)it.rows / (float)it.cols) : 1.f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (c + e >= it.m) continue;
+            const int at = tall ? (c + e) * it.cols + r : r * it.cols + c + e;
+            y[at] = MUON ? (T)fmaf(-rate, w[i][e], t.keep * (float)y[at]) : (T)w[i][e];
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
 // ---- plans ----
 struct Plan {
   Args a;
   int sym, app;  // tiles of the symmetric products, and of the others
+  int small;     // waves to a matrix where all fit a workgroup each, or 0
   bool parts;
   size_t bytes;
 };
@@ -468,6 +616,9 @@ Plan plan_of(const nf_orth_desc &d, int count, const int32_t *rows, const int32_
   for (int k = 0; k < count; ++k) large += tiles_of(a.it[k].np, 128) * tiles_of(a.it[k].mp, 128);
   p.sym = symmetric_tile(a);
   p.app = large >= 192 ? 128 : 64;  // the same 17 matrices, 683 tiles of 128: 49 us, of 64 53; 2048x2048, 256 tiles: 48 and 62
+  int most = 0, tiles = 0;
+  for (int k = 0; k < count; ++k) most = std::max(most, a.it[k].np <= 64 ? small_bytes(a.it[k]) : MANY_LDS + 1), tiles = std::max(tiles, a.it[k].np / 16 * (a.it[k].mp / 16));
+  p.small = most <= FEW_LDS && tiles <= 16 ? 4 : most <= MANY_LDS ? 16 : 0;
   const int B = p.sym;
   long long work = 0;
   for (int k = 0; k < count; ++k) work += triangle_tiles(a.it[k], B) * (a.it[k].mp / 32);
@@ -570,6 +721,22 @@ hipError_t run(const nf_orth_desc &d, Plan &p, const Tensors &t, hipStream_t st)
   auto two = [](int e) { return (float)std::ldexp(1.0, e); };
   double elements = 0;
   for (int k = 0; k < a.count; ++k) elements += (double)a.it[k].rows * a.it[k].cols;
+  if (p.small) {
+    Small m = {};
+    m.steps = d.steps;
+    double flops = 0;
+    for (int k = 0; k < d.steps; ++k) {
+      m.a[k] = d.a[k], m.b[k] = d.b[k], m.c[k] = d.c[k];
+      m.up_x[k] = two(s[k].x), m.up_a[k] = two(s[k].a), m.up_p[k] = two(s[k].p);
+    }
+    for (int k = 0; k < a.count; ++k) flops += d.steps * (2.0 * a.it[k].n * a.it[k].n * (2.0 * a.it[k].m + a.it[k].n));
+    return recorded(st, p.small == 4 ? "orth_small_4_waves" : "orth_small_16_waves", flops, sizeof(T) * (MUON ? 5.0 : 2.0) * elements, [&] {
+      if (p.small == 4)
+        hipLaunchKernelGGL((orth_small_kernel<T, MUON, 4>), dim3(a.count), dim3(256), 0, st, a, t, m);
+      else
+        hipLaunchKernelGGL((orth_small_kernel<T, MUON, 16>), dim3(a.count), dim3(1024), 0, st, a, t, m);
+    });
+  }
   a.up_x = two(s[0].x);
   unsigned grid = lay(a, [](const Item &it) { return (long long)it.square_parts; });
   hipError_t e = recorded(st, "orth_squares", 0.0, sizeof(T) * (MUON ? 3.0 : 1.0) * elements,

@@ -64,12 +64,13 @@ def test_pointers(L):
     need = nf.nf_orthogonalise_workspace_bytes(d, [(16, 27), (64, 64)])
     r, c = _dims(16, 64), _dims(27, 64)
     two = _arr(GOOD, OTHER)
-    def orth(g=two, y=two, rows=r, cols=c, ws=GOOD, n=need, dt=0, desc=C.byref(d)):
+    swapped, apart = _arr(OTHER, GOOD), _arr(GOOD + 0x100000, OTHER + 0x100000)
+    def orth(g=two, y=apart, rows=r, cols=c, ws=GOOD, n=need, dt=0, desc=C.byref(d)):
         return L.nf_orthogonalise(desc, dt, 2, g, y, rows, cols, ws, n, None)
     for k in ("g", "y", "rows", "cols", "desc"):
         assert orth(**{k: None}) == nf.NF_ERR_NULL
     assert orth(g=_arr(GOOD, None)) == orth(y=_arr(None, GOOD)) == nf.NF_ERR_NULL
-    assert orth(g=_arr(GOOD, ODD)) == orth(y=_arr(ODD, GOOD)) == orth(y=_arr(GOOD, GOOD)) == orth(dt=3) == orth(dt=-1) == nf.NF_ERR_BAD_DESC
+    assert orth(g=_arr(GOOD, ODD)) == orth(y=_arr(ODD, GOOD)) == orth(y=_arr(0x900000, 0x900000)) == orth(y=swapped) == orth(dt=3) == orth(dt=-1) == nf.NF_ERR_BAD_DESC
     assert orth(ws=None) == orth(ws=0x10010) == orth(n=need - 1) == nf.NF_ERR_WORKSPACE
     m = nf.MuonDesc(lr=0.1, momentum=0.9, weight_decay=0.0, nesterov=1, orth=d)
     def muon(w=two, g=two, v=two, rows=r, cols=c, ws=GOOD, n=need, desc=C.byref(m)):
