@@ -1,6 +1,7 @@
 // Matrices in 4 bits an element with an exponent to every 32 (rows as those of the e2m1 cache): quantisation by rows and by columns, and
 // products of two such matrices, y = r + D(act(a b^T + bias)), on the scaled matrix instructions.
 #include <algorithm>
+#include <type_traits>
 
 #include "linear.h"
 #include "nf_enqueue.h"
@@ -95,6 +96,21 @@ __device__ inline floatx4 mx_mfma(const uintx4 &a, uint32_t sa, const uintx4 &b,
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, (int)sa, 0, (int)sb);  // 4: e2m1; exponents in the low byte
 }
 
+// The same in place: left to itself the compiler gives sums new registers where paths meet, and beside 128 of them it has none left.  What it does not see: an
+// operand that a vector instruction wrote is read two cycles later at the earliest (these come from LDS), a result 18
+// cycles after its instruction by another one than an MFMA that adds to it (settle_results).
+__device__ inline void mx_mfma_in_place(floatx4 &c, const uintx4 &a, uint32_t sa, const uintx4 &b, uint32_t sb) {
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+v"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+}
+template <int M, int N>
+__device__ inline void settle_results(floatx4 (&c)[M][N]) {
+#pragma unroll
+  for (int i = 0; i < M * N; ++i) asm volatile("" : "+v"(c[i / N][i % N]));
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < M * N; ++i) asm volatile("" : "+v"(c[i / N][i % N]));
+}
+
 struct MxArgs {
   GemmArgs g;  // strides of codes; L = groups, per = groups of a split
   const uint8_t *sa, *sb;
@@ -117,113 +133,213 @@ __device__ inline void copy4(const uintx4 &buf, uint32_t voff, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(buf) : "memory");
 }
 
-// A tile of BLOCK x BLOCK by four waves of BLOCK/2 x BLOCK/2; a step is 8 groups of the sum: 128 bytes of codes and 8 of exponents to a row.  A row's chunks
-// of 16 bytes (groups) are exchanged in LDS so that the 16 rows of a fragment's read lie in different banks.
+// A wave's parts of sums; their rows are whole pieces of 8.
+template <int MT, int NT>
+__device__ inline void write_parts(const GemmArgs &g, int split, long long r0, int c0, int lane, floatx4 (&acc)[MT][NT]) {
+  const int i16 = lane & 15, q = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const long long row = r0 + 16 * i + i16;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int col = c0 + 16 * j + 4 * q;
+      if (row < g.R && col < g.part_ld) *reinterpret_cast<floatx4 *>(g.part + (split * g.R + row) * g.part_ld + col) = acc[i][j];
+    }
+  }
+}
+
+// The steps of a tile of 256: a wave's 128 x 64 results leave registers for the fragments of B and four of A.  A row of fragments of A is read two rows
+// ahead of its products, B's half a step ahead; the barrier that makes the next step's stage whole stands two rows before the end of a step,
+// when all of its own have been read.
+template <typename S, typename F>
+struct WideSteps {
+  static constexpr int MT = S::MT, NT = S::NT;
+  const char *lds;
+  int oa, ob, ea, eb, at[2];  // this lane's place in a stage: codes of A and B without the chunk, exponents, and the chunks of both halves
+  F next;  // behind the barrier that ends step s
+  uintx4 fa[4], fb[2][NT];
+  uint32_t xa[4], xb[2][NT];
+  __device__ inline void read_a(int to, int s, int kk, int i) {
+    const char *const from = lds + (s & 1) * S::STAGE;
+    fa[to] = *reinterpret_cast<const uintx4 *>(from + oa + i * 2048 + at[kk]);
+    xa[to] = *reinterpret_cast<const uint8_t *>(from + ea + i * 16 * 8 + kk * 4);
+  }
+  __device__ inline void read_b(int s, int kk, int j) {
+    const char *const from = lds + (s & 1) * S::STAGE;
+    fb[kk][j] = *reinterpret_cast<const uintx4 *>(from + ob + j * 2048 + at[kk]);
+    xb[kk][j] = *reinterpret_cast<const uint8_t *>(from + eb + j * 16 * 8 + kk * 4);
+  }
+  __device__ inline void begin() {  // the first stage is whole
+#pragma unroll
+    for (int j = 0; j < NT; ++j) read_b(0, 0, j);
+    read_a(0, 0, 0, 0), read_a(1, 0, 0, 1);
+  }
+  template <bool LAST, int KK>
+  __device__ inline void half(floatx4 (&acc)[MT][NT], int s) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      constexpr int first = KK * MT;
+      if (KK == 1 && i == MT - 2 && !LAST) {
+        wait_copies<0>();
+        wait_lds();
+        barrier();
+        next(s);
+      }
+      const int ahead = first + i + 2, to = ahead % 4;
+      if (ahead < 2 * MT)
+        read_a(to, s, ahead / MT, ahead % MT);
+      else if (!LAST)
+        read_a(to, s + 1, 0, ahead - 2 * MT);
+      if (KK == 0 && i >= MT - NT) read_b(s, 1, i - (MT - NT));
+      if (KK == 1 && i >= MT - 2 && !LAST) {
+#pragma unroll
+        for (int j = 0; j < NT / 2; ++j) read_b(s + 1, 0, (i - (MT - 2)) * (NT / 2) + j);
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j) mx_mfma_in_place(acc[i][j], fb[KK][j], xb[KK][j], fa[(first + i) % 4], xa[(first + i) % 4]);
+    }
+  }
+};
+
+// A tile of BLOCK x BLOCK by 2 x ACROSS waves; a step is 8 groups of the sum: 128 bytes of codes and 8 of exponents to a row, copied while the step before
+// it is carried out.  A row's chunks of 16 bytes (groups) are exchanged in LDS so that the 16 rows of a fragment's read lie in different banks.
 constexpr int STEP = 8;  // groups
-template <int BLOCK>
+template <int BLOCK, int ACROSS>
 struct MxTile {
-  static constexpr int CODES = BLOCK * 128, SCALES = BLOCK * STEP, STAGE = 2 * (CODES + SCALES), PIECES = BLOCK / 32;
+  static constexpr int WAVES = 2 * ACROSS, THREADS = 64 * WAVES, MT = BLOCK / 32, NT = BLOCK / 16 / ACROSS;
+  static constexpr int CODES = BLOCK * 128, SCALES = BLOCK * STEP, STAGE = 2 * (CODES + SCALES), PIECES = CODES / 1024 / WAVES, WORDS = SCALES / 4 / (THREADS / 2);
+  static constexpr int HALF = BLOCK == 256 ? MT / 2 : MT, PER_SIMD = BLOCK == 64 || (BLOCK == 128 && ACROSS == 4) ? 4 : 2;  // waves to a SIMD
 };
 __device__ inline int mx_swizzle(int row) { return (row >> 1) & 7; }
 
-template <typename T, int BLOCK>
-__global__ __launch_bounds__(LT) void mx_gemm_kernel(MxArgs m) {
-  using S = MxTile<BLOCK>;
-  constexpr int MT = BLOCK / 32, PIECES = S::PIECES;
+template <typename T, int BLOCK, int ACROSS, bool PARTS>
+__global__ __launch_bounds__((MxTile<BLOCK, ACROSS>::THREADS), (MxTile<BLOCK, ACROSS>::PER_SIMD)) void mx_gemm_kernel(MxArgs m) {
+  using S = MxTile<BLOCK, ACROSS>;
+  constexpr int MT = S::MT, NT = S::NT, PIECES = S::PIECES, WAVES = S::WAVES;
   __shared__ __align__(1024) char lds[2 * S::STAGE];
   const GemmArgs &g = m.g;
   const int id = xcd_run(blockIdx.x, gridDim.x);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, q = lane >> 4;
-  const int split = id / g.tiles, tile = id - split * g.tiles, tr = tile / g.tiles_c;
+  const int split = PARTS ? id / g.tiles : 0, tile = id - split * g.tiles, tr = tile / g.tiles_c;
   const long long r0 = (long long)tr * BLOCK, l0 = split * g.per, l1 = min(g.L, l0 + g.per);
   const int c0 = (tile - tr * g.tiles_c) * BLOCK;
   const int steps = (int)((l1 - l0 + STEP - 1) / STEP);
-  const long long rows_left = g.R - r0;
-  const int cols_left = g.C - c0;
-  // what this lane brings: chunks of codes, and a word of exponents of each operand (tiles of 64: waves 0 and 1 of A's, 2 and 3 of B's)
-  uint32_t av[PIECES], bv[PIECES];
-  int chunk[PIECES];
+  const int rows_left = (int)min(g.R - r0, (long long)BLOCK), cols_left = g.C - c0;
+  // what this lane brings: chunks of codes, and words of exponents: half of the waves those of A, the others those of B
+  uint32_t av[PIECES], bv[PIECES], sv[S::WORDS];
+  const int chunk = (lane & 7) ^ mx_swizzle((wave * 64 + lane) >> 3);  // the same for all pieces: they are WAVES * 8 rows apart
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
-    const int at = (p * 4 + wave) * 64 + lane, row = at >> 3;
-    chunk[p] = (at & 7) ^ mx_swizzle(row);
-    av[p] = row < rows_left ? (uint32_t)(row * g.lda + chunk[p] * 16) : OUTSIDE;
-    bv[p] = row < cols_left ? (uint32_t)(row * g.ldb + chunk[p] * 16) : OUTSIDE;
+    const int row = ((p * WAVES + wave) * 64 + lane) >> 3;
+    av[p] = row < rows_left ? row * (uint32_t)g.lda + chunk * 16 : OUTSIDE;
+    bv[p] = row < cols_left ? row * (uint32_t)g.ldb + chunk * 16 : OUTSIDE;
   }
-  const int srow = BLOCK == 128 ? tid >> 1 : (tid & 127) >> 1;
-  const uint32_t half = (tid & 1) * 4;
-  const uint32_t sav = srow < rows_left ? (uint32_t)(srow * m.lsa) + half : OUTSIDE, sbv = srow < cols_left ? (uint32_t)(srow * m.lsb) + half : OUTSIDE;
+  const bool of_b = wave >= WAVES / 2;
+#pragma unroll
+  for (int w = 0; w < S::WORDS; ++w) {
+    const int row = ((tid & (S::THREADS / 2 - 1)) + w * (S::THREADS / 2)) >> 1;
+    sv[w] = row < (of_b ? cols_left : rows_left) ? row * (uint32_t)(of_b ? m.lsb : m.lsa) + (tid & 1) * 4 : OUTSIDE;
+  }
   const char *const pa = g.a + r0 * g.lda + l0 * 16, *const pb = g.b + c0 * g.ldb + l0 * 16;
-  const char *const psa = (const char *)m.sa + r0 * m.lsa + l0, *const psb = (const char *)m.sb + c0 * m.lsb + l0;
+  const char *const ps = of_b ? (const char *)m.sb + c0 * m.lsb + l0 : (const char *)m.sa + r0 * m.lsa + l0;
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-  auto fetch = [&](int s, int stage) {
-    const int inside = (int)(l1 - l0) - s * STEP;  // groups of this step
-    const uintx4 ba = buffer_of(pa + s * 128ll), bb = buffer_of(pb + s * 128ll);
-    const uint32_t to = base + stage * S::STAGE;
+  auto fetch = [&](int s) {
+    const uint32_t none = chunk < (int)(l1 - l0) - s * STEP ? 0u : OUTSIDE;  // groups behind the last; an offset with OUTSIDE's bits lies outside
+    const uintx4 ba = buffer_of(pa + s * 128ll), bb = buffer_of(pb + s * 128ll), bs = buffer_of(ps + s * STEP);
+    const uint32_t to = base + (s & 1) * S::STAGE;
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) copy16(ba, chunk[p] < inside ? av[p] : OUTSIDE, to + (p * 4 + wave) * 1024);
+    for (int p = 0; p < PIECES; ++p) copy16(ba, av[p] | none, to + (p * WAVES + wave) * 1024);
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) copy16(bb, chunk[p] < inside ? bv[p] : OUTSIDE, to + S::CODES + (p * 4 + wave) * 1024);
-    if constexpr (BLOCK == 128) {
-      copy4(buffer_of(psa + s * STEP), sav, to + 2 * S::CODES + wave * 256);
-      copy4(buffer_of(psb + s * STEP), sbv, to + 2 * S::CODES + S::SCALES + wave * 256);
-    } else {
-      copy4(buffer_of((wave < 2 ? psa : psb) + s * STEP), wave < 2 ? sav : sbv, to + 2 * S::CODES + wave * 256);
-    }
+    for (int p = 0; p < PIECES; ++p) copy16(bb, bv[p] | none, to + S::CODES + (p * WAVES + wave) * 1024);
+#pragma unroll
+    for (int w = 0; w < S::WORDS; ++w)
+      copy4(bs, sv[w], to + 2 * S::CODES + (of_b ? S::SCALES : 0) + (w * (WAVES / 2) + (wave & (WAVES / 2 - 1))) * 256);
   };
-  const int wm = (wave >> 1) * (BLOCK / 2), wn = (wave & 1) * (BLOCK / 2);
-  floatx4 acc[MT][MT];
+  const int wm = wave / ACROSS * (16 * MT), wn = wave % ACROSS * (16 * NT);
+  floatx4 acc[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < MT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-
-  fetch(0, 0);
-  for (int s = 0; s < steps; ++s) {
-    if (s + 1 < steps) {
-      fetch(s + 1, (s + 1) & 1);
-      wait_copies<2 * PIECES + (BLOCK == 128 ? 2 : 1)>();
-    } else {
-      wait_copies<0>();
-    }
-    wait_lds();
-    barrier();
-    const char *const la = lds + (s & 1) * S::STAGE, *const lb = la + S::CODES;
-    const char *const ea = la + 2 * S::CODES, *const eb = ea + S::SCALES;
-    const bool last = l0 + (s + 1) * STEP >= g.L;
+    for (int j = 0; j < NT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int swz = mx_swizzle(i16);  // rows of a wave's fragments are multiples of 16 apart
+  auto step = [&](int s) {
+    const char *const from = lds + (s & 1) * S::STAGE, *const la = from + (wm + i16) * 128, *const lb = from + S::CODES + (wn + i16) * 128;
+    const char *const ea = from + 2 * S::CODES + (wm + i16) * STEP + q, *const eb = from + 2 * S::CODES + S::SCALES + (wn + i16) * STEP + q;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
-      uintx4 fa[MT], fb[MT];
-      uint32_t xa[MT], xb[MT];
+      uintx4 fa[MT], fb[NT];
+      uint32_t xa[MT], xb[NT];
+      const int at = ((kk * 4 + q) ^ swz) << 4;
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        const int ra = wm + 16 * i + i16, rb = wn + 16 * i + i16;
-        fa[i] = *reinterpret_cast<const uintx4 *>(la + ra * 128 + (((kk * 4 + q) ^ mx_swizzle(ra)) << 4));
-        fb[i] = *reinterpret_cast<const uintx4 *>(lb + rb * 128 + (((kk * 4 + q) ^ mx_swizzle(rb)) << 4));
-        xa[i] = *reinterpret_cast<const uint32_t *>(ea + ra * STEP + kk * 4) >> (8 * q);
-        xb[i] = *reinterpret_cast<const uint32_t *>(eb + rb * STEP + kk * 4) >> (8 * q);
-      }
-      if (last) {  // what lies behind a row's last element may be anything
-        const long long group = l0 + s * STEP + kk * 4 + q;
-        const int n = (int)min(max(m.K - group * GROUP, 0ll), (long long)GROUP);
+      for (int j = 0; j < NT; ++j) fb[j] = *reinterpret_cast<const uintx4 *>(lb + j * 2048 + at), xb[j] = *reinterpret_cast<const uint8_t *>(eb + j * 16 * STEP + kk * 4);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          fa[i] = first_codes(fa[i], n);
-          xa[i] = n ? xa[i] : 0u, xb[i] = n ? xb[i] : 0u;
-        }
-      }
+      for (int i = 0; i < MT; ++i) fa[i] = *reinterpret_cast<const uintx4 *>(la + i * 2048 + at), xa[i] = *reinterpret_cast<const uint8_t *>(ea + i * 16 * STEP + kk * 4);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < MT; ++j) acc[i][j] = mx_mfma(fb[j], xb[j], fa[i], xa[i], acc[i][j]);
+        for (int j = 0; j < NT; ++j) mx_mfma_in_place(acc[i][j], fb[j], xb[j], fa[i], xa[i]);
+    }
+  };
+  // What lies behind a row's last element may be anything: zeros take its place in the last step's stage, where that is not a step's end, too.
+  const bool ragged = l1 == g.L && m.K % (STEP * GROUP) != 0;
+  auto end_rows = [&] {
+    char *const stage = lds + ((steps - 1) & 1) * S::STAGE;
+    const int inside = (int)(l1 - l0) - (steps - 1) * STEP, n = m.K % GROUP;  // groups of the step, elements of its last one (0: all)
+    const unsigned long long keep = inside >= 8 ? ~0ull : (1ull << 8 * inside) - 1;
+    for (int r = tid; r < 2 * BLOCK; r += S::THREADS) *reinterpret_cast<unsigned long long *>(stage + 2 * S::CODES + r * STEP) &= keep;
+    if (n) {
+      for (int r = tid; r < BLOCK; r += S::THREADS) {
+        uintx4 *const p = reinterpret_cast<uintx4 *>(stage + r * 128 + (((inside - 1) ^ mx_swizzle(r)) << 4));
+        *p = first_codes(*p, n);
+      }
     }
     wait_lds();
     barrier();
+  };
+  fetch(0);
+  if (steps > 1) {
+    fetch(1);
+    wait_copies<2 * PIECES + S::WORDS>();
+  } else {
+    wait_copies<0>();
   }
-  if (!g.part)
-    write_fwd<T, false, MT>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * MT * MT * 64);
-  else
-    write_sums<T, EPI_FWD, false>(g, split, r0 + wm, c0 + wn, lane, acc);
+  barrier();
+  auto next = [&](int s) {  // step s + 1 is whole, s read by all
+    if (s + 2 < steps)
+      fetch(s + 2);
+    else if (ragged)
+      end_rows();
+  };
+  if constexpr (BLOCK == 256) {
+    WideSteps<S, decltype(next)> w = {lds, (wm + i16) * 128, S::CODES + (wn + i16) * 128, 2 * S::CODES + (wm + i16) * STEP + q, 2 * S::CODES + S::SCALES + (wn + i16) * STEP + q,
+                                      {(q ^ swz) << 4, ((4 + q) ^ swz) << 4}, next};
+    if (ragged && steps == 1) end_rows();
+    w.begin();
+    for (int s = 0; s + 1 < steps; ++s) {
+      w.template half<false, 0>(acc, s);
+      w.template half<false, 1>(acc, s);
+    }
+    w.template half<true, 0>(acc, steps - 1);
+    w.template half<true, 1>(acc, steps - 1);
+  } else {
+    for (int s = 0; s + 1 < steps; ++s) {
+      step(s);
+      wait_copies<0>();
+      wait_lds();
+      barrier();  // the next step's stage is whole, this one's read
+      if (s + 2 < steps) fetch(s + 2);
+    }
+    if (ragged) end_rows();
+    step(steps - 1);
+  }
+  settle_results(acc);
+  if constexpr (PARTS) {
+    write_parts(g, split, r0 + wm, c0 + wn, lane, acc);
+  } else {
+    wait_lds();
+    barrier();
+    write_fwd<T, false, S::HALF>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * S::HALF * NT * 64);
+  }
 }
 
 // Few rows: 16 columns and up to 32 rows to a workgroup, whose waves share the sum's axis; fragments come from memory without LDS.  x is quantised on the
@@ -317,16 +433,21 @@ struct MxPlan {
   long long per;  // groups of a split
   size_t bytes;   // of the splits' sums
 };
-MxPlan mx_plan(long long M, int N, long long K) {
+// Tiles of 256 or 128 by rounds over the workgroups that run together (one to a CU and two) and a round's time: steps, then what ends a tile (us,
+// in tiles of 256 and of 128: 8192x8192x8192 bf16 294 and 389, 16384x2048x2048 48 and 57, 65536x512x2048 131 and 133, with GELU 167 and 148, fp32 results
+// 147 and 184).  Few tiles of 128 become tiles of 64 or parts of sums: towards 512 workgroups, four steps each at least.
+MxPlan mx_plan(int dtype, long long M, int N, long long K) {
   MxPlan p = {0, 1, 0, 0};
   if (M <= FEW) return p;
   const long long steps = ((K + GROUP - 1) / GROUP + STEP - 1) / STEP;
   auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
-  p.tile = tiles(128) >= 256 ? 128 : 64;
+  const bool wide = dtype == NF_F32;
+  const double large = (double)((tiles(256) + 255) / 256) * (2.3 * steps + (wide ? 14 : 12)), medium = std::max(1.0, tiles(128) / 512.0) * (1.5 * steps + (wide ? 8 : 4));
+  p.tile = tiles(128) < 256 ? 64 : tiles(128) >= 512 && large < medium ? 256 : 128;
   const long long t = tiles(p.tile);
-  long long splits = std::max<long long>(1, std::min<long long>(512 / t, steps / 4));
+  const long long splits = std::max<long long>(1, std::min<long long>(512 / t, steps / 4));
   const long long each = (steps + splits - 1) / splits;
-  p.splits = (int)((steps + each - 1) / each), p.per = each * STEP;
+  p.splits = p.tile == 256 ? 1 : (int)((steps + each - 1) / each), p.per = p.splits == 1 ? steps * STEP : each * STEP;
   p.bytes = p.splits > 1 ? (size_t)p.splits * M * ((N + 7) / 8 * 8) * 4 : 0;
   return p;
 }
@@ -334,7 +455,7 @@ inline size_t whole256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <typename T>
 hipError_t product_as(const MxCall &c, const void *raw, const MxRows &a, const MxRows &b, const Epilogue &e, void *ws, hipStream_t st) {
-  const MxPlan p = mx_plan(c.M, c.N, c.K);
+  const MxPlan p = mx_plan(c.dtype, c.M, c.N, c.K);
   MxArgs m = {};
   GemmArgs &g = m.g;
   g.a = raw ? (const char *)raw : (const char *)a.codes, g.b = (const char *)b.codes, g.lda = raw ? (long long)c.K * sizeof(T) : a.cb, g.ldb = b.cb;
@@ -356,12 +477,26 @@ hipError_t product_as(const MxCall &c, const void *raw, const MxRows &a, const M
   g.tiles_c = (c.N + p.tile - 1) / p.tile, g.tiles = (int)((c.M + p.tile - 1) / p.tile) * g.tiles_c;
   g.splits = p.splits, g.per = p.per;
   if (p.splits > 1) g.part = (float *)ws, g.part_ld = (c.N + 7) / 8 * 8;
-  const hipError_t err = recorded(st, p.tile == 128 ? "mx_product_128x128" : "mx_product_64x64", flops, bytes + (p.splits > 1 ? 4.0 * p.splits * c.M * c.N : ends), [&] {
+  const hipError_t err = recorded(st, p.tile == 256 ? "mx_product_256x256" : p.tile == 128 ? "mx_product_128x128" : "mx_product_64x64", flops, bytes + (p.splits > 1 ? 4.0 * p.splits * c.M * c.N : ends), [&] {
     const dim3 grid((unsigned)(g.tiles * g.splits));
-    if (p.tile == 128)
-      hipLaunchKernelGGL((mx_gemm_kernel<T, 128>), grid, dim3(LT), 0, st, m);
+    auto go = [&](auto tile, auto across) {
+      constexpr int B = decltype(tile)::value, A = decltype(across)::value;
+      if (g.part)
+        hipLaunchKernelGGL((mx_gemm_kernel<T, B, A, true>), grid, dim3((MxTile<B, A>::THREADS)), 0, st, m);
+      else
+        hipLaunchKernelGGL((mx_gemm_kernel<T, B, A, false>), grid, dim3((MxTile<B, A>::THREADS)), 0, st, m);
+    };
+    using std::integral_constant;
+    using I2 = integral_constant<int, 2>;
+    using I4 = integral_constant<int, 4>;
+    if (p.tile == 256)
+      go(integral_constant<int, 256>(), I4());
+    else if (p.tile == 64)
+      go(integral_constant<int, 64>(), I2());
+    else if (g.L >= 8 * STEP)
+      go(integral_constant<int, 128>(), I2());
     else
-      hipLaunchKernelGGL((mx_gemm_kernel<T, 64>), grid, dim3(LT), 0, st, m);
+      go(integral_constant<int, 128>(), I4());
   });
   if (err != hipSuccess || p.splits == 1) return err;
   const FinishArgs f = finish_args(p.splits, g);
@@ -395,9 +530,9 @@ bool mx_quantise_fits(long long rows, long long cols) {
   return (double)((rows + TR - 1) / TR) * (double)((cols + TC - 1) / TC) < 2147483648.0;
 }
 
-size_t mx_product_workspace_bytes(const MxCall &c) { return mx_plan(c.M, c.N, c.K).bytes; }
+size_t mx_product_workspace_bytes(const MxCall &c) { return mx_plan(c.dtype, c.M, c.N, c.K).bytes; }
 size_t mx_linear_workspace_bytes(const MxCall &c) {
-  const MxPlan p = mx_plan(c.M, c.N, c.K);
+  const MxPlan p = mx_plan(c.dtype, c.M, c.N, c.K);
   if (!p.tile) return 0;
   const MxRows r = rows_at(nullptr, nullptr, c.K);
   return whole256(p.bytes) + whole256((size_t)c.M * r.cb) + (size_t)c.M * r.sb;
@@ -423,7 +558,7 @@ hipError_t launch_mx_product(const MxCall &c, const void *a, const void *as, con
 // The workspace holds the splits' sums, then x's codes and exponents.
 hipError_t launch_mx_linear(const MxCall &c, const void *x, const void *W, const void *Ws, const float *bias, const void *r, const DropArgs &drop, void *y, void *z,
                             void *ws, hipStream_t st) {
-  const MxPlan p = mx_plan(c.M, c.N, c.K);
+  const MxPlan p = mx_plan(c.dtype, c.M, c.N, c.K);
   if (p.tile) {
     const MxRows sizes = rows_at(nullptr, nullptr, c.K);
     char *const codes = (char *)ws + whole256(p.bytes), *const scales = codes + whole256((size_t)c.M * sizes.cb);
