@@ -13,21 +13,108 @@ namespace {
 constexpr int QT = 256;
 
 // ---- quantisation ----
-// A tile of 128 rows x 64 columns to a workgroup: a thread reads pieces of 8 elements, 4 neighbours of a row share an exponent and write their
-// codes; for the columns the tile goes through LDS as it lies, and a thread takes 32 rows of a column.  Memory-bound: sizeof(T) and 1/2 + 1/32
-// bytes an element, twice the latter where both forms are wanted.
-constexpr int TR = 128, TC = 64;
+// The largest magnitude of a group is found on the elements' bits, whose order is that of the magnitudes (an infinity and a NaN behind all numbers): two
+// 16-bit elements to an instruction.  The conversion divides by 2^E, rounds to nearest, ties to even, and takes elements as they lie; of its scale
+// it reads the exponent bits, which are the group's exponent byte.
+template <typename T>
+__device__ inline uint32_t most(uint32_t m, const Raw8<T> &r) {
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 2) * 4; ++i) {
+    const uint32_t w = r.w[i / 4][i % 4];
+    if constexpr (sizeof(T) == 4) {
+      m = max(m, w & 0x7FFFFFFFu);
+    } else {
+      using ushort2v = __attribute__((ext_vector_type(2))) unsigned short;
+      m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, m), __builtin_bit_cast(ushort2v, w & 0x7FFF7FFFu)));
+    }
+  }
+  return m;
+}
+// E + 127 of a group from most()'s bits, or 255 where the group holds no number: with the magnitude m 2^e, 1 <= m < 2, E = e - 2, or e - 1 where m > 1.5
+template <typename T>
+__device__ inline int group_exponent(uint32_t m) {
+  uint32_t bits = m;
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t h = max(m & 0xFFFFu, m >> 16);
+    bits = __is_same(T, __bf16) ? h << 16 : __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (unsigned short)h));
+  }
+  if (bits >= 0x7F800000u) return 255;
+  return max((int)(bits >> 23) - 2 + ((bits & 0x7FFFFFu) > 0x400000u), 0);
+}
+template <typename T>
+__device__ inline uint32_t codes8(const Raw8<T> &r, int eb) {
+  const float scale = __builtin_bit_cast(float, (uint32_t)eb << 23);
+  uint32_t w = 0;
+  if constexpr (sizeof(T) == 4) {
+    const floatx4 a = __builtin_bit_cast(floatx4, r.w[0]), b = __builtin_bit_cast(floatx4, r.w[1]);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a[0], a[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a[2], a[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, b[0], b[1], scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, b[2], b[3], scale, 3);
+  } else {
+    using V = __attribute__((ext_vector_type(2))) T;
+    const uint32_t p0 = r.w[0][0], p1 = r.w[0][1], p2 = r.w[0][2], p3 = r.w[0][3];  // a bit_cast of a vector's element would take its first
+    auto two = [](uint32_t p) { return __builtin_bit_cast(V, p); };
+    if constexpr (__is_same(T, __bf16)) {
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two(p0), scale, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two(p1), scale, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two(p2), scale, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two(p3), scale, 3);
+    } else {
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, two(p0), scale, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, two(p1), scale, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, two(p2), scale, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, two(p3), scale, 3);
+    }
+  }
+  return w;
+}
+// a group of 32 elements that a thread holds
+template <typename T>
+__device__ inline int group32(const Raw8<T> (&r)[4], uintx4 &codes) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) m = most(m, r[h]);
+  const int eb = group_exponent<T>(m);
+#pragma unroll
+  for (int h = 0; h < 4; ++h) codes[h] = eb < 255 ? codes8(r[h], eb) : 0u;
+  return eb;
+}
 
 struct QuantArgs {
-  long long rows, cols, tiles_c;
+  long long rows, cols, tiles_c, groups;         // groups of a row
   uint8_t *codes, *scales, *codes_t, *scales_t;  // one pair may be null
   long long cb, sb, cbt, sbt;                    // row strides
 };
 
-template <typename T, bool BY_ROWS, bool BY_COLS>
-__global__ __launch_bounds__(QT) void mx_quantise_kernel(QuantArgs a, const T *__restrict__ x) {
+// By rows: a group to a thread, whose reads are in flight together.  Memory-bound: sizeof(T) + 1/2 + 1/32 bytes an element.
+template <typename T>
+__global__ __launch_bounds__(QT) void mx_rows_kernel(QuantArgs a, const T *__restrict__ x) {
+  const long long first = (long long)blockIdx.x * QT, row0 = first / a.groups;
+  const unsigned at = (unsigned)(first - row0 * a.groups) + threadIdx.x, groups = (unsigned)a.groups;  // at most 2^31 groups to a row
+  const long long row = row0 + at / groups;
+  const unsigned group = at % groups;
+  if (row >= a.rows) return;
+  const long long col = (long long)group * GROUP;
+  const int n = (int)min(a.cols - col, (long long)GROUP);
+  Raw8<T> r[4] = {};
+#pragma unroll
+  for (int h = 0; h < 4; ++h)
+    if (n > 8 * h) r[h] = raw8(x + row * a.cols + col + 8 * h, n - 8 * h);
+  uintx4 codes;
+  const int eb = group32(r, codes);
+  *reinterpret_cast<uintx4 *>(a.codes + row * a.cb + col / 2) = codes;
+  a.scales[row * a.sb + group] = (uint8_t)eb;
+}
+
+// By columns, or both: a tile of 128 rows x 64 columns to a workgroup.  A thread reads pieces of 8 elements of a row, of which 4 neighbours share an
+// exponent and write their codes; for the columns the tile goes through LDS as it lies, and a thread takes 32 rows of a column, four neighbours
+// the 128 (64 bytes of codes; a column to 64 lanes, 16 bytes here and there, took 21.8 us for 65536x512 bf16 instead of 16.2).
+constexpr int TR = 128, TC = 64;
+template <typename T, bool BY_ROWS>
+__global__ __launch_bounds__(QT) void mx_columns_kernel(QuantArgs a, const T *__restrict__ x) {
   constexpr int LD = TC + 4 / sizeof(T);
-  __shared__ T lds[BY_COLS ? TR * LD : 1];
+  __shared__ T lds[TR * LD];
   const long long tr = blockIdx.x / a.tiles_c, r0 = tr * TR, c0 = (blockIdx.x - tr * a.tiles_c) * TC;
   const int j = threadIdx.x & 7, down = threadIdx.x >> 3;
   const long long col = c0 + 8 * j;
@@ -40,49 +127,36 @@ __global__ __launch_bounds__(QT) void mx_quantise_kernel(QuantArgs a, const T *_
   }
 #pragma unroll
   for (int k = 0; k < TR / 32; ++k) {
-    const long long row = r0 + k * 32 + down;
-    if constexpr (BY_COLS) __builtin_memcpy(&lds[(k * 32 + down) * LD + 8 * j], &raw[k], sizeof(raw[k]));
+    __builtin_memcpy(&lds[(k * 32 + down) * LD + 8 * j], &raw[k], sizeof(raw[k]));
     if constexpr (BY_ROWS) {
-      float v[8], top = 0.f;
-      unpack8(raw[k], v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fabsf(v[e]) <= INFINITY ? fmaxf(top, fabsf(v[e])) : INFINITY;  // a NaN counts as infinite
-      top = fmaxf(top, __shfl_xor(top, 1));
-      top = fmaxf(top, __shfl_xor(top, 2));
-      const int eb = exponent_byte<NF_Q_E2M1>(top);
-      uint32_t w[2] = {0, 0};
-      if (eb < 255) encode8<NF_Q_E2M1>(v, eb - 127, w);
+      const long long row = r0 + k * 32 + down;
+      uint32_t m = most(0u, raw[k]);
+      if constexpr (sizeof(T) == 2) m = max(m & 0xFFFFu, m >> 16);
+      m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, true));  // the other of two, the other two of four
+      m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, true));
+      const int eb = group_exponent<T>(m);
       if (row < a.rows && (col & ~31ll) < a.cols) {  // whole groups: zeros behind the last element
-        *reinterpret_cast<uint32_t *>(a.codes + row * a.cb + col / 2) = w[0];
+        *reinterpret_cast<uint32_t *>(a.codes + row * a.cb + col / 2) = eb < 255 ? codes8(raw[k], eb) : 0u;
         if ((j & 3) == 0) a.scales[row * a.sb + col / GROUP] = (uint8_t)eb;
       }
     }
   }
-  if constexpr (BY_COLS) {
-    __syncthreads();
-    const int c = threadIdx.x & 63, k = threadIdx.x >> 6;
-    const long long first = r0 + k * 32;
-    if (c0 + c >= a.cols || first >= a.rows) return;
-    float v[4][8], top = 0.f;
+  __syncthreads();
+  const int c = threadIdx.x >> 2, k = threadIdx.x & 3;
+  const long long first = r0 + k * 32;
+  if (c0 + c >= a.cols || first >= a.rows) return;
+  Raw8<T> r[4];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float t = (float)lds[(k * 32 + i) * LD + c];
-      v[i >> 3][i & 7] = t;
-      top = fabsf(t) <= INFINITY ? fmaxf(top, fabsf(t)) : INFINITY;
-    }
-    const int eb = exponent_byte<NF_Q_E2M1>(top);
-    uintx4 out = {0, 0, 0, 0};
-    if (eb < 255) {
+  for (int h = 0; h < 4; ++h) {
+    T t[8];
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        uint32_t w[2];
-        encode8<NF_Q_E2M1>(v[h], eb - 127, w);
-        out[h] = w[0];
-      }
-    }
-    *reinterpret_cast<uintx4 *>(a.codes_t + (c0 + c) * a.cbt + first / 2) = out;
-    a.scales_t[(c0 + c) * a.sbt + first / GROUP] = (uint8_t)eb;
+    for (int e = 0; e < 8; ++e) t[e] = lds[(k * 32 + 8 * h + e) * LD + c];
+    __builtin_memcpy(&r[h], t, sizeof(t));
   }
+  uintx4 codes;
+  const int eb = group32(r, codes);
+  *reinterpret_cast<uintx4 *>(a.codes_t + (c0 + c) * a.cbt + first / 2) = codes;
+  a.scales_t[(c0 + c) * a.sbt + first / GROUP] = (uint8_t)eb;
 }
 
 // ---- products ----
@@ -372,24 +446,11 @@ __global__ __launch_bounds__(64 * NW) void mx_few_rows_kernel(MxArgs m) {
       fx[k] = uintx4{0, 0, 0, 0}, ex[k] = 0;
       if (n <= 0) continue;
       if constexpr (RAW) {
-        float v[4][8], top = 0.f;
         const T *const p = (const T *)(g.a + row * g.lda) + (long long)group * GROUP;
+        Raw8<T> r[4];
 #pragma unroll
-        for (int h = 0; h < 4; ++h) load8(p + 8 * h, v[h], n - 8 * h);
-#pragma unroll
-        for (int h = 0; h < 4; ++h)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) top = fabsf(v[h][e]) <= INFINITY ? fmaxf(top, fabsf(v[h][e])) : INFINITY;
-        const int eb = exponent_byte<NF_Q_E2M1>(top);
-        ex[k] = eb;
-        if (eb < 255) {
-#pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            uint32_t c[2];
-            encode8<NF_Q_E2M1>(v[h], eb - 127, c);
-            fx[k][h] = c[0];
-          }
-        }
+        for (int h = 0; h < 4; ++h) r[h] = raw8(p + 8 * h, n - 8 * h);
+        ex[k] = group32(r, fx[k]);
       } else {
         fx[k] = first_codes(*reinterpret_cast<const uintx4 *>(g.a + row * g.lda + group * 16ll), n);
         ex[k] = m.sa[row * m.lsa + group];
@@ -506,15 +567,15 @@ hipError_t product_as(const MxCall &c, const void *raw, const MxRows &a, const M
 
 template <typename T>
 hipError_t quantise_as(const QuantArgs &a, const T *x, hipStream_t st) {
-  const dim3 grid((unsigned)(a.tiles_c * ((a.rows + TR - 1) / TR)));
   const double n = (double)a.rows * a.cols;
-  return recorded(st, "mx_quantise", 0.0, n * (sizeof(T) + (a.codes ? 0.53 : 0.0) + (a.codes_t ? 0.53 : 0.0)), [&] {
-    if (a.codes && a.codes_t)
-      hipLaunchKernelGGL((mx_quantise_kernel<T, true, true>), grid, dim3(QT), 0, st, a, x);
+  return recorded(st, a.codes_t ? a.codes ? "mx_quantise_both" : "mx_quantise_columns" : "mx_quantise_rows", 0.0, n * (sizeof(T) + (a.codes ? 0.53 : 0.0) + (a.codes_t ? 0.53 : 0.0)), [&] {
+    const dim3 tiles((unsigned)(a.tiles_c * ((a.rows + TR - 1) / TR)));
+    if (!a.codes_t)
+      hipLaunchKernelGGL(mx_rows_kernel<T>, dim3((unsigned)((a.rows * a.groups + QT - 1) / QT)), dim3(QT), 0, st, a, x);
     else if (a.codes)
-      hipLaunchKernelGGL((mx_quantise_kernel<T, true, false>), grid, dim3(QT), 0, st, a, x);
+      hipLaunchKernelGGL((mx_columns_kernel<T, true>), tiles, dim3(QT), 0, st, a, x);
     else
-      hipLaunchKernelGGL((mx_quantise_kernel<T, false, true>), grid, dim3(QT), 0, st, a, x);
+      hipLaunchKernelGGL((mx_columns_kernel<T, false>), tiles, dim3(QT), 0, st, a, x);
   });
 }
 
@@ -540,7 +601,7 @@ size_t mx_linear_workspace_bytes(const MxCall &c) {
 
 hipError_t launch_mx_quantise(int dtype, long long rows, long long cols, const void *x, void *codes, void *scales, void *codes_t, void *scales_t, hipStream_t st) {
   const MxRows r = rows_at(codes, scales, cols), t = rows_at(codes_t, scales_t, rows);
-  const QuantArgs a = {rows, cols, (cols + TC - 1) / TC, r.codes, r.scales, t.codes, t.scales, r.cb, r.sb, t.cb, t.sb};
+  const QuantArgs a = {rows, cols, (cols + TC - 1) / TC, (cols + GROUP - 1) / GROUP, r.codes, r.scales, t.codes, t.scales, r.cb, r.sb, t.cb, t.sb};
   if (dtype == NF_BF16) return quantise_as(a, (const __bf16 *)x, st);
   if (dtype == NF_F16) return quantise_as(a, (const _Float16 *)x, st);
   return quantise_as(a, (const float *)x, st);
