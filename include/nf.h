@@ -203,7 +203,8 @@ int32_t nf_orthogonalise(const nf_orth_desc *d, int32_t dtype, int32_t n_matrice
                          const int32_t *rows, const int32_t *cols, void *ws, size_t ws_bytes, void *stream);
 /* nf_sgd_update for weight matrices, the update made orthogonal (filters [C_out][R][S][C_in] are matrices of C_out rows):
  *   v = momentum v + g;  u = g + momentum v (nesterov != 0) or v;  w = (1 - lr weight_decay) w - lr sqrt(max(1, rows / cols)) X(u)
- * v == NULL or momentum == 0: u = g.  All fp32.  The workspace is nf_orthogonalise's.  No two w, and no two v, may be the same. */
+ * v == NULL or momentum == 0: u = g.  All fp32.  The workspace is nf_orthogonalise's.  No w or v may be
+ * another one's, nor a g. */
 typedef struct {
   float lr, momentum, weight_decay;
   int32_t nesterov;

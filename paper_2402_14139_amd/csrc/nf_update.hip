@@ -73,7 +73,11 @@ int32_t nf_muon_update(const nf_muon_desc *d, int32_t n_matrices, float *const *
   if (rc) return rc;
   auto plain = [](auto p) { return reinterpret_cast<const void *const *>(p); };
   if ((rc = check_pointers(n_matrices, plain(w), true)) || (rc = check_pointers(n_matrices, plain(g), false))) return rc;
-  if (d->momentum != 0.f && v && (rc = check_pointers(n_matrices, plain(v), true))) return rc;
+  if (d->momentum == 0.f) v = nullptr;
+  if (v && (rc = check_pointers(n_matrices, plain(v), true))) return rc;
+  for (int i = 0; i < n_matrices; ++i)  // what is written is nothing else's
+    for (int k = 0; k < n_matrices; ++k)
+      if (w[i] == g[k] || (v && (v[i] == g[k] || v[i] == w[k]))) return NF_ERR_BAD_DESC;
   if ((rc = check_ws(ws, ws_bytes, orth_workspace_bytes(d->orth, n_matrices, rows, cols)))) return rc;
   NF_HIP(launch_muon(*d, n_matrices, w, g, v, rows, cols, ws, static_cast<hipStream_t>(stream)));
   return NF_OK;

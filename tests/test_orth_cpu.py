@@ -73,11 +73,14 @@ def test_pointers(L):
     assert orth(g=_arr(GOOD, ODD)) == orth(y=_arr(ODD, GOOD)) == orth(y=_arr(0x900000, 0x900000)) == orth(y=swapped) == orth(dt=3) == orth(dt=-1) == nf.NF_ERR_BAD_DESC
     assert orth(ws=None) == orth(ws=0x10010) == orth(n=need - 1) == nf.NF_ERR_WORKSPACE
     m = nf.MuonDesc(lr=0.1, momentum=0.9, weight_decay=0.0, nesterov=1, orth=d)
-    def muon(w=two, g=two, v=two, rows=r, cols=c, ws=GOOD, n=need, desc=C.byref(m)):
+    others, third = _arr(GOOD + 0x200000, OTHER + 0x200000), _arr(GOOD + 0x300000, OTHER + 0x300000)
+    def muon(w=two, g=others, v=third, rows=r, cols=c, ws=GOOD, n=need, desc=C.byref(m)):
         return L.nf_muon_update(desc, 2, w, g, v, rows, cols, ws, n, None)
     for k in ("w", "g", "rows", "cols", "desc"):
         assert muon(**{k: None}) == nf.NF_ERR_NULL
     assert muon(w=_arr(GOOD, GOOD)) == muon(v=_arr(GOOD, GOOD)) == muon(v=_arr(GOOD, ODD)) == muon(w=_arr(ODD, GOOD)) == muon(g=_arr(ODD, GOOD)) == nf.NF_ERR_BAD_DESC
+    for k in (dict(g=two), dict(v=two), dict(v=_arr(GOOD + 0x300000, GOOD)), dict(g=_arr(GOOD + 0x100000, GOOD)), dict(v=others), dict(v=_arr(OTHER + 0x200000, GOOD + 0x300000))):
+        assert muon(**k) == nf.NF_ERR_BAD_DESC   # what is written is nothing else's
     assert muon(v=_arr(GOOD, None)) == nf.NF_ERR_NULL
     assert muon(ws=None) == muon(n=need - 1) == nf.NF_ERR_WORKSPACE
     assert nf.nf_orthogonalise_workspace_bytes(d, [(16, 27)]) <= need
