@@ -1,10 +1,13 @@
 """A pointwise residual block over channels-last activations, trained from a quantised activation cache: group norm with its
-activation, a widening linear layer (activation, dropout), a linear layer back with dropout and the residual sum.  Host
-bookkeeping only: every arithmetic step but the example's squared-error loss is a call of include/nf.h.
+activation (or layer norm over a pixel's channels), a widening linear layer (activation, dropout), a linear layer back with dropout and
+the residual sum.  Host bookkeeping only: every arithmetic step but the example's squared-error loss is a call of include/nf.h.
 
-    h = act(GN(x));  a = D1(act(h W1^T + b1));  y = x + D2(a W2^T + b2)
+    h = act(GN(x)) or LN(x);  a = D1(act(h W1^T + b1));  y = x + D2(a W2^T + b2)
 
-``python -m paper_2402_14139_amd.pointwise`` fits such a block to a map that another one computes, from an int8 cache.
+The products run in the activations' type or on 4-bit operands (``mx``), forward and backward; weights are updated by SGD or, made orthogonal, by
+``muon``; ``predict`` serves rows of any number from weights in 4 bits.
+
+``python -m paper_2402_14139_amd.pointwise`` fits such blocks to a map that another one computes, from quantised caches.
 """
 from __future__ import annotations
 
@@ -54,14 +57,43 @@ def workspace_bytes(norm, up, down, B: int) -> int:
                for b in range(1, B + 1))
 
 
+class Rows4:
+    """Room for matrices in 4 bits of up to ``rows`` x ``n`` elements: (codes, exponents) as the calls take them."""
+
+    def __init__(self, rows: int, n: int, device="cuda"):
+        code, scale = nf.nf_qcache_row_bytes(nf.NF_Q_E2M1, n)
+        self.pair = tuple(torch.empty(rows * b, dtype=torch.uint8, device=device) for b in (code, scale))
+
+
+def mx_workspace_bytes(up, down, B: int, HW: int) -> int:
+    """Bytes for the 4-bit products of 1 to ``B`` * ``HW`` rows forward and of 1 to ``B`` maps backward.  How sums are cut into parts changes with the
+    tiles of rows, 64 at least, and wants most at a tile's last row."""
+    most = 0
+    for_dx = [nf.LinearDesc(dtype=d.dtype, K=d.N, N=d.K, act=nf.NF_ACT_NONE) for d in (up, down)]
+    for M in range(64, B * HW + 64, 64):
+        most = max(most, *(nf.nf_mx_linear_workspace_bytes(d, M) for d in (up, down)), *(nf.nf_mx_product_workspace_bytes(d, M) for d in for_dx))
+    for M in range(HW, B * HW + 1, HW):
+        for d in (up, down):
+            most = max(most, nf.nf_mx_product_workspace_bytes(nf.LinearDesc(dtype=nf.NF_F32, K=M, N=d.K, act=nf.NF_ACT_NONE), d.N))
+    return most
+
+
+MUON_STEPS = [(3.4445, -4.7750, 2.0315)] * 5   # drives singular values to between 0.7 and 1.2
+
+
 class PointwiseBlock:
     """Parameters (fp32; the weights also in the activations' type), gradients and buffers of one block for batches of up to
-    ``B`` maps of ``HW`` pixels and ``C`` channels, ``H`` hidden ones."""
+    ``B`` maps of ``HW`` pixels and ``C`` channels, ``H`` hidden ones.  ``norm``: "group" (of ``groups`` groups, with the activation
+    behind it) or "layer"; ``mx``: products on 4-bit operands."""
 
     def __init__(self, dtype, B: int, HW: int, C: int, H: int, groups: int, act=nf.NF_ACT_GELU, p: float = 0.0, seed: int = 0,
-                 device="cuda"):
+                 device="cuda", norm: str = "group", mx: bool = False):
+        if norm not in ("group", "layer"):
+            raise ValueError(f"norm: {norm!r}; want 'group' or 'layer'")
         if not torch.cuda.is_available():
             raise RuntimeError("PointwiseBlock needs a GPU: the library has no CPU path")
+        self.kind, self.mx = norm, mx
+        groups = groups if norm == "group" else 1
         self.dtype, self.B, self.HW, self.C, self.H, self.p, self.seed = dtype, B, HW, C, H, p, seed
         T = TYPES[dtype]
         self.norm = nf.GroupNormDesc(dtype=dtype, C=C, G=groups, act=act, HW=HW, eps=1e-5)
@@ -77,8 +109,25 @@ class PointwiseBlock:
         new = lambda *s, d=T: torch.empty(s, dtype=d, device=device)  # noqa: E731
         self.h, self.z1, self.a, self.y = new(M, C), new(M, H), new(M, H), new(M, C)
         self.dz2, self.da, self.dh, self.dx = new(M, C), new(M, H), new(M, C), new(M, C)
-        self.mean, self.rstd = new(B, groups, d=torch.float32), new(B, groups, d=torch.float32)
-        self.ws = torch.empty(max(workspace_bytes(self.norm, self.up, self.down, B), 1), dtype=torch.uint8, device=device)
+        stats = (B, groups) if norm == "group" else (M,)
+        self.mean, self.rstd = new(*stats, d=torch.float32), new(*stats, d=torch.float32)
+        room = workspace_bytes(self.norm, self.up, self.down, B)
+        if norm == "layer":
+            self.ln = nf.LayerNormDesc(dtype=dtype, C=C, eps=1e-5)
+            room = max(room, *(nf.nf_layernorm_workspace_bytes(self.ln, b * HW) for b in range(1, B + 1)))
+        self.orth = nf.orth_desc(MUON_STEPS)
+        self.v = [torch.zeros_like(self.p32[k]) for k in ("W1", "W2")]   # muon()'s momentum
+        room = max(room, nf.nf_orthogonalise_workspace_bytes(self.orth, [(H, C), (C, H)]))
+        if mx:
+            room = max(room, mx_workspace_bytes(self.up, self.down, B, HW))
+            # gradients by rows and by columns, a layer's input by columns: the wider layer's size
+            wide = max(C, H)
+            self.dz_rows, self.dz_cols, self.in_cols = Rows4(M, wide, device), Rows4(wide, M, device), Rows4(wide, M, device)
+            # the weights by rows (forward) and by columns (gradients)
+            self.q = {k: (Rows4(*self.p32[k].shape, device), Rows4(*self.p32[k].t().shape, device)) for k in ("W1", "W2")}
+        self.ws = torch.empty(max(room, 1), dtype=torch.uint8, device=device)
+        if mx:
+            self.pack()
 
     def _maps(self, name: str, t, B: int):
         if not 1 <= B <= self.B:
@@ -88,15 +137,46 @@ class PointwiseBlock:
     def _drop(self, which: int, step: int):
         return nf.DropoutDesc(p=self.p, seed=self.seed * 2 + which, step=step) if self.p else None
 
+    def pack(self):
+        """The weights in 4 bits, from their fp32 values; sgd() and muon() do it by themselves."""
+        for k, (rows, cols) in self.q.items():
+            nf.nf_mx_quantise(nf.NF_F32, *self.p32[k].shape, self.p32[k], *rows.pair, *cols.pair)
+
+    def _normalise(self, x, M, h, keep: bool):
+        P = self.p32
+        if self.kind == "group":
+            nf.nf_groupnorm_fwd(self.norm, M // self.HW, x, P["gamma"], P["beta"], h, self.mean, self.rstd, self.ws)
+        else:
+            nf.nf_layernorm_fwd(self.ln, M, x, P["gamma"], P["beta"], h, self.mean if keep else None, self.rstd if keep else None)
+
+    def _linear(self, d, M, x, name, r, drop, y, z):
+        b = self.p32["b" + name[1]]
+        if self.mx:
+            nf.nf_mx_linear_fwd(d, M, x, *self.q[name][0].pair, b, r, drop, y, z, self.ws)
+        else:
+            nf.nf_linear_fwd(d, M, x, self.w[name], b, r, drop, y, z, self.ws)
+
+    def _linear_back(self, d, M, dz, x, name, dx):
+        dW = self.grad[name]
+        if not self.mx:
+            nf.nf_linear_bwd(d, M, dz, x, self.w[name], dx, dW, self.ws)
+            return
+        nf.nf_mx_quantise(self.dtype, M, d.N, dz, *self.dz_rows.pair, *self.dz_cols.pair)
+        nf.nf_mx_quantise(self.dtype, M, d.K, x, None, None, *self.in_cols.pair)
+        for_dx = nf.LinearDesc(dtype=self.dtype, K=d.N, N=d.K, act=nf.NF_ACT_NONE)
+        for_dW = nf.LinearDesc(dtype=nf.NF_F32, K=M, N=d.K, act=nf.NF_ACT_NONE)
+        nf.nf_mx_product(for_dx, M, *self.dz_rows.pair, *self.q[name][1].pair, None, None, dx, self.ws)
+        nf.nf_mx_product(for_dW, d.N, *self.dz_cols.pair, *self.in_cols.pair, None, None, dW, self.ws)
+
     def forward(self, x, step: int = 0, train: bool = True):
         """y [B, HW, C] of x [B, HW, C]; ``step`` chooses the dropout masks."""
         B = x.shape[0]
         self._maps("x", x, B)
-        M, P = B * self.HW, self.p32
+        M = B * self.HW
         d1, d2 = (self._drop(0, step), self._drop(1, step)) if train else (None, None)
-        nf.nf_groupnorm_fwd(self.norm, B, x, P["gamma"], P["beta"], self.h, self.mean, self.rstd, self.ws)
-        nf.nf_linear_fwd(self.up, M, self.h, self.w["W1"], P["b1"], None, d1, self.a, self.z1, self.ws)
-        nf.nf_linear_fwd(self.down, M, self.a, self.w["W2"], P["b2"], x, d2, self.y, None, self.ws)
+        self._normalise(x, M, self.h, True)
+        self._linear(self.up, M, self.h, "W1", None, d1, self.a, self.z1)
+        self._linear(self.down, M, self.a, "W2", x, d2, self.y, None)
         return self.y[:M].view(B, self.HW, self.C)
 
     def backward(self, x, dy, step: int = 0):
@@ -106,24 +186,56 @@ class PointwiseBlock:
         self._maps("dy", dy, B)
         M, P, g = B * self.HW, self.p32, self.grad
         nf.nf_linear_bwd_epilogue(self.down, M, dy, None, self._drop(1, step), self.dz2, g["b2"], self.ws)
-        nf.nf_linear_bwd(self.down, M, self.dz2, self.a, self.w["W2"], self.da, g["W2"], self.ws)
+        self._linear_back(self.down, M, self.dz2, self.a, "W2", self.da)
         nf.nf_linear_bwd_epilogue(self.up, M, self.da, self.z1, self._drop(0, step), self.a, g["b1"], self.ws)  # a is not needed again
-        nf.nf_linear_bwd(self.up, M, self.a, self.h, self.w["W1"], self.dh, g["W1"], self.ws)
-        nf.nf_groupnorm_bwd(self.norm, B, self.dh, x, P["gamma"], P["beta"], self.mean, self.rstd, self.dx, g["gamma"], g["beta"],
-                            self.ws)
+        self._linear_back(self.up, M, self.a, self.h, "W1", self.dh)
+        if self.kind == "group":
+            nf.nf_groupnorm_bwd(self.norm, B, self.dh, x, P["gamma"], P["beta"], self.mean, self.rstd, self.dx, g["gamma"], g["beta"],
+                                self.ws)
+        else:
+            nf.nf_layernorm_bwd(self.ln, M, self.dh, x, P["gamma"], self.mean, self.rstd, None, self.dx, g["gamma"], g["beta"], self.ws)
         return self.dx[:M].view(B, self.HW, self.C)
+
+    def predict(self, x):
+        """y of rows x [rows, C], up to the block's pixels and down to a single one, from weights in 4 bits; nothing is kept for a backward pass."""
+        if self.kind != "layer" or not self.mx:
+            raise ValueError("predict: rows by themselves, from weights in 4 bits: the block wants norm='layer' and mx=True")
+        rows = x.shape[0]
+        if not 1 <= rows <= self.B * self.HW:
+            raise ValueError(f"x: {rows} rows; this block's buffers hold 1 to {self.B * self.HW}")
+        _check("x", x, TYPES[self.dtype], self.ws.device, rows, self.C)
+        self._normalise(x, rows, self.h, False)
+        self._linear(self.up, rows, self.h, "W1", None, None, self.a, None)
+        self._linear(self.down, rows, self.a, "W2", x, None, self.y, None)
+        return self.y[:rows]
+
+    def _renew(self):
+        for k, v in self.w.items():
+            v.copy_(self.p32[k])
+        if self.mx:
+            self.pack()
 
     def sgd(self, lr: float):
         names = list(self.p32)
         nf.nf_sgd_update(lr, 0.0, [self.p32[k] for k in names], [self.grad[k] for k in names], None)
-        for k, v in self.w.items():
-            v.copy_(self.p32[k])
+        self._renew()
+
+    def muon(self, lr: float, sgd_lr: float, momentum: float = 0.95, weight_decay: float = 0.0):
+        """The weights' update made orthogonal, with its momentum; the other parameters' by SGD at ``sgd_lr``."""
+        names, others = ("W1", "W2"), [k for k in self.p32 if k not in ("W1", "W2")]
+        d = nf.MuonDesc(lr=lr, momentum=momentum, weight_decay=weight_decay, nesterov=1, orth=self.orth)
+        nf.nf_muon_update(d, [self.p32[k] for k in names], [self.grad[k] for k in names], self.v, self.ws)
+        nf.nf_sgd_update(sgd_lr, 0.0, [self.p32[k] for k in others], [self.grad[k] for k in others], None)
+        self._renew()
 
 
-def fit(dtype=nf.NF_BF16, fmt=nf.NF_Q_INT8, items=256, B=64, HW=64, C=64, H=128, groups=8, epochs=6, lr=0.5, p=0.0, seed=3):
-    """Trains a block towards another one's outputs on rows of a quantised cache; the mean loss of every epoch."""
+def fit(dtype=nf.NF_BF16, fmt=nf.NF_Q_INT8, items=256, B=64, HW=64, C=64, H=128, groups=8, epochs=6, lr=0.5, p=0.0, seed=3,
+        norm="group", mx=False, muon_lr=0.0):
+    """Trains a block towards another one's outputs on rows of a quantised cache; the mean loss of every epoch.  ``muon_lr``: the weights' updates are
+    made orthogonal, at this rate."""
     T = TYPES[dtype]
-    teacher, block = (PointwiseBlock(dtype, B, HW, C, H, groups, p=q, seed=s) for s, q in ((seed, 0.0), (seed + 1, p)))
+    teacher = PointwiseBlock(dtype, B, HW, C, H, groups, seed=seed, norm=norm)
+    block = PointwiseBlock(dtype, B, HW, C, H, groups, p=p, seed=seed + 1, norm=norm, mx=mx)
     g = torch.Generator(device="cuda").manual_seed(seed)
     cache = QuantisedCache(fmt, items, HW * C)
     labels = torch.arange(items, dtype=torch.int32, device="cuda")
@@ -141,7 +253,7 @@ def fit(dtype=nf.NF_BF16, fmt=nf.NF_Q_INT8, items=256, B=64, HW=64, C=64, H=128,
             got = block.forward(x, step)
             off = got.float() - want.float()
             block.backward(x, (off * (2.0 / off.numel() * C)).to(T), step)
-            block.sgd(lr / C)
+            block.muon(muon_lr, lr / C) if muon_lr else block.sgd(lr / C)
             total += off.square().mean().item()
             step += 1
         losses.append(total / (items // B))
@@ -151,3 +263,5 @@ def fit(dtype=nf.NF_BF16, fmt=nf.NF_Q_INT8, items=256, B=64, HW=64, C=64, H=128,
 if __name__ == "__main__":
     for name, fmt in (("int8", nf.NF_Q_INT8), ("e4m3", nf.NF_Q_E4M3), ("e2m1", nf.NF_Q_E2M1)):
         print(name, " ".join(f"{v:.4f}" for v in fit(fmt=fmt)))
+    for name, more in (("layer norm", dict()), ("orthogonal updates", dict(muon_lr=0.02)), ("and 4-bit products", dict(muon_lr=0.02, mx=True))):
+        print(name, " ".join(f"{v:.4f}" for v in fit(norm="layer", **more)))
