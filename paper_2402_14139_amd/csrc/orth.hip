@@ -24,18 +24,10 @@ using shortx4 = __attribute__((ext_vector_type(4))) short;
 constexpr int MOST = NF_ORTH_MATRICES;
 
 struct Item {
-  long long x[2], A, P, part, squares;  // bytes from the workspace's start
-  int rows, cols, n, m, np, mp;         // n <= m, padded; rows > cols: held transposed
-  int splits, per;                      // of A's sums: parts, and their steps of 32 terms
-  int square_parts, chunk;              // of |G|^2
-};
-struct Args {
-  char *ws;
-  int count, cur;
-  int first[MOST + 1];  // first workgroup of each matrix
-  Item it[MOST];
-  float a, b, c, eps;
-  float up_x, down_x, up_a, down_a, up_p, down_p, up_next;  // 2^s and 2^-s of X, A, P and X'
+  unsigned x[2], A, P, part, squares;  // where they begin in the workspace, in units of 256 bytes
+  int rows, cols, n, m, np, mp;        // n <= m, padded; rows > cols: held transposed
+  int splits, per;                     // of A's sums: parts, and their steps of 32 terms
+  int square_parts, chunk;             // of |G|^2
 };
 struct Tensors {
   const void *g[MOST];
@@ -44,12 +36,28 @@ struct Tensors {
   float momentum, keep, lr;  // y = keep y - lr sqrt(max(1, rows / cols)) X
   int nesterov;
 };
+// What all launches of a call read.  The first one gets it as an argument and leaves it at the workspace's start: an argument is read from the host's
+// memory, and a workgroup goes there once for the place of its matrix and again for the matrix (17 launches for 64x576: 104 us, 84 from the workspace).
+enum { SQUARES, START, A_TILES, A_PARTS, P_TILES, X_TILES, LAUNCHES };
+struct Table {
+  int first[LAUNCHES][MOST + 1];  // first workgroup of each matrix; of X' = a X + P X, an XCD's first
+  Item it[MOST];
+  Tensors t;
+};
+constexpr unsigned TABLE = (sizeof(Table) + 255) / 256;  // units of the workspace
+struct Args {
+  char *ws;
+  int count, cur;
+  float a, b, c, eps;
+  float up_x, down_x, up_a, down_a, up_p, down_p, up_next;  // 2^s and 2^-s of X, A, P and X'
+  __host__ __device__ char *at(unsigned unit) const { return ws + 256ull * unit; }
+};
 
 // the matrix that a workgroup works on: the last whose first workgroup is not behind it
-__device__ inline int item_of(const Args &a, int id) {
+__device__ inline int item_of(const int *first, int count, int id) {
   const int lane = threadIdx.x & 63;
-  const bool at = lane < a.count && a.first[lane < MOST ? lane : MOST] <= id;
-  return __popcll(__ballot(at)) - 1;
+  const bool at = lane < count && first[lane < MOST ? lane : MOST] <= id;
+  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(at)) - 1);
 }
 
 // element (r, c) of a matrix in pieces: its h, and its l 64 bytes further
@@ -95,11 +103,14 @@ __device__ inline float direction(const Tensors &t, const T *g, const float *v, 
   return t.nesterov ? fmaf(t.momentum, v[at], gv) : v[at];
 }
 template <typename T, bool MUON>
-__global__ __launch_bounds__(NT) void orth_squares_kernel(Args a, Tensors t) {
+__global__ __launch_bounds__(NT) void orth_squares_kernel(Args a, Table table) {
   __shared__ double lds[4];
-  const int k = item_of(a, blockIdx.x);
-  const Item &it = a.it[k];
-  const int part = blockIdx.x - a.first[k];
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < (int)(sizeof(Table) / 4); i += NT) reinterpret_cast<int *>(a.ws)[i] = reinterpret_cast<const int *>(&table)[i];
+  const int k = item_of(table.first[SQUARES], a.count, blockIdx.x);
+  const Item &it = table.it[k];
+  const Tensors &t = table.t;
+  const int part = blockIdx.x - table.first[SQUARES][k];
   const T *const g = (const T *)t.g[k];
   float *const v = MUON ? t.v[k] : nullptr;
   const long long all = (long long)it.rows * it.cols, from = (long long)part * it.chunk, to = min(all, from + it.chunk);
@@ -121,32 +132,49 @@ __global__ __launch_bounds__(NT) void orth_squares_kernel(Args a, Tensors t) {
     for (int e = 0; e < 8; ++e) s += e < n ? (double)x[e] * x[e] : 0.0;
   }
   s = all_sum(s, lds);
-  if (threadIdx.x == 0) reinterpret_cast<double *>(a.ws + it.squares)[part] = s;
+  if (threadIdx.x == 0) reinterpret_cast<double *>(a.at(it.squares))[part] = s;
 }
 
 // X0 in pieces, a tile of 64 x 64 to a workgroup
 template <typename T, bool MUON>
-__global__ __launch_bounds__(NT) void orth_start_kernel(Args a, Tensors t) {
+__global__ __launch_bounds__(NT) void orth_start_kernel(Args a, const Table *__restrict__ table) {
   __shared__ double lds[4];
   __shared__ float tile[64][65];
-  const int k = item_of(a, blockIdx.x);
-  const Item &it = a.it[k];
-  const int id = blockIdx.x - a.first[k], across = (it.mp + 63) / 64, tr = id / across, r0 = tr * 64, c0 = (id - tr * across) * 64;
-  double s = 0;
-  const double *const squares = reinterpret_cast<const double *>(a.ws + it.squares);
-  for (int i = threadIdx.x; i < it.square_parts; i += NT) s += squares[i];
-  const float norm = (float)sqrt(all_sum(s, lds)) + a.eps;
+  const int k = item_of(table->first[START], a.count, blockIdx.x);
+  const Item it = table->it[k];
+  const Tensors &t = table->t;
+  const int id = blockIdx.x - table->first[START][k], across = (it.mp + 63) / 64, tr = id / across, r0 = tr * 64, c0 = (id - tr * across) * 64;
   const T *const g = (const T *)t.g[k];
   const float *const v = MUON ? t.v[k] : nullptr;
-  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
   const bool tall = it.rows > it.cols;
-  for (int i = y; i < 64; i += 4) {  // along G's rows
-    const int row = (tall ? c0 : r0) + i, col = (tall ? r0 : c0) + x;
-    const float w = row < it.rows && col < it.cols ? direction<T, MUON>(t, g, v, (long long)row * it.cols + col) / norm * a.up_x : 0.f;
-    (tall ? tile[x][i] : tile[i][x]) = w;
+  const int x = (threadIdx.x & 7) * 8, y = threadIdx.x >> 3;  // along G's rows
+  float u[2][8];  // on their way before the sum's barrier
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = (tall ? c0 : r0) + y + 32 * i, col = (tall ? r0 : c0) + x, n = row < it.rows ? it.cols - col : 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[i][e] = 0.f;
+    if (n <= 0) continue;
+    const long long at = (long long)row * it.cols + col;
+    load8(g + at, u[i], n);
+    if constexpr (MUON) {
+      if (!v) continue;
+      float m[8];
+      load8(v + at, m, n);  // the new momentum
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[i][e] = t.nesterov ? fmaf(t.momentum, m[e], u[i][e]) : m[e];
+    }
   }
+  double s = 0;
+  const double *const squares = reinterpret_cast<const double *>(a.at(it.squares));
+  for (int i = threadIdx.x; i < it.square_parts; i += NT) s += squares[i];
+  const float norm = (float)sqrt(all_sum(s, lds)) + a.eps;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) (tall ? tile[x + e][y + 32 * i] : tile[y + 32 * i][x + e]) = u[i][e] / norm * a.up_x;
   __syncthreads();
-  char *const X = a.ws + it.x[0];
+  char *const X = a.at(it.x[0]);
   for (int i = threadIdx.x; i < 512; i += NT) {
     const int r = i >> 3, c = (i & 7) * 8;
     if (r0 + r >= it.np || c0 + c >= it.mp) continue;
@@ -200,21 +228,21 @@ __device__ inline void finish8(const Args &a, const Item &it, int r, int c, floa
     const float s = a.down_x * a.down_x * a.up_a;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= s;
-    put8(piece(a.ws + it.A, 4ll * it.np, r, c), v);
+    put8(piece(a.at(it.A), 4ll * it.np, r, c), v);
   } else if constexpr (KIND == POLY) {
     float A[8];
-    get8(piece(a.ws + it.A, 4ll * it.np, r, c), A);
+    get8(piece(a.at(it.A), 4ll * it.np, r, c), A);
     const float sa = a.b * a.down_a * a.up_p, ss = a.c * a.down_a * a.down_a * a.up_p;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = fmaf(A[e], sa, v[e] * ss);
-    put8(piece(a.ws + it.P, 4ll * it.np, r, c), v);
+    put8(piece(a.at(it.P), 4ll * it.np, r, c), v);
   } else {
     float X[8];
-    get8(piece(a.ws + it.x[a.cur], 4ll * it.mp, r, c), X);
+    get8(piece(a.at(a.cur ? it.x[1] : it.x[0]), 4ll * it.mp, r, c), X);
     const float up = KIND == LAST ? 1.f : a.up_next, sx = a.a * a.down_x * up, ss = a.down_p * a.down_x * up;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = fmaf(X[e], sx, v[e] * ss);
-    if constexpr (KIND == APPLY) put8(piece(a.ws + it.x[a.cur ^ 1], 4ll * it.mp, r, c), v);
+    if constexpr (KIND == APPLY) put8(piece(a.at(a.cur ? it.x[0] : it.x[1]), 4ll * it.mp, r, c), v);
   }
 }
 // 8 neighbours of a row of the caller's matrix, n of which lie inside
@@ -263,7 +291,7 @@ __device__ inline void tile_out(const Args &a, const Tensors &t, const Item &it,
     for (int e = 0; e < 8; ++e) v[e] = W[(r + e) * LDW + c];
     const int row = tc * BLOCK + c, col = tr * BLOCK + r;
     if constexpr (KIND <= POLY)
-      put8(piece(a.ws + (KIND == GRAM ? it.A : it.P), 4ll * it.np, row, col), v);
+      put8(piece(a.at(KIND == GRAM ? it.A : it.P), 4ll * it.np, row, col), v);
     else if (row < it.m && col < it.n)
       give8<OUT, MUON>(t, it, k, row, col, it.n - col, v);
   }
@@ -281,28 +309,35 @@ __device__ inline void triangle(int t, int &tr, int &tc) {
 // copies of the STAGES-th next are on their way: one barrier a step, behind which the next stage is whole and this one free.  Steps go in pairs
 // (two sets of fragments); those beyond the last are copies of nothing, so that the waits count the same.
 template <int BLOCK, int KIND, typename OUT, bool MUON>
-__global__ __launch_bounds__(Tile<BLOCK>::THREADS) void orth_product_kernel(Args a, Tensors t) {
+__global__ __launch_bounds__(Tile<BLOCK>::THREADS) void orth_product_kernel(Args a, const Table *__restrict__ table) {
   using S = Tile<BLOCK>;
   constexpr bool APART = KIND >= APPLY;
   constexpr int MT = S::MT, NT = S::NT, STAGES = S::STAGES, WAVES = S::WAVES, PIECES = S::PIECES;
   constexpr int OUT_BYTES = BLOCK * (BLOCK + 4) * 4, RING = STAGES * S::STAGE;
   __shared__ __align__(1024) char lds[RING > OUT_BYTES ? RING : OUT_BYTES];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, q = lane >> 4;
-  const int block = xcd_run(blockIdx.x, gridDim.x), k = __builtin_amdgcn_readfirstlane(item_of(a, block));
-  const Item &it = a.it[k];
-  int id = block - a.first[k], split = 0, tr, tc;
+  // A's and P's tiles: an XCD has few matrices, whose operands its L2 holds (17 matrices of 64x27 to 512x4608: A 26 us, 32 by eighths); X's: an eighth of each, so
+  // that all XCDs have as much to do (46, 49)
+  constexpr int LAUNCH = KIND == GRAM ? A_TILES : KIND == POLY ? P_TILES : X_TILES;
+  const int block = APART ? blockIdx.x >> 3 : xcd_run(blockIdx.x, gridDim.x), k = item_of(table->first[LAUNCH], a.count, block), first = table->first[LAUNCH][k];
+  const Item it = table->it[k];
+  const Tensors &t = table->t;
+  const int place = block - first + (APART ? (blockIdx.x & 7) * (table->first[LAUNCH][k + 1] - first) : 0);
+  int id = place, split = 0, tr, tc;
   if constexpr (KIND <= POLY) {
     const int T = (it.np + BLOCK - 1) / BLOCK, tiles = T * (T + 1) / 2;
     if (KIND == GRAM) split = id / tiles, id -= split * tiles;
     triangle(id, tr, tc);
   } else {
     // four rows of tiles at a time, column by column: workgroups of an XCD share few rows and columns
-    const int down = (it.np + BLOCK - 1) / BLOCK, across = (it.mp + BLOCK - 1) / BLOCK, band = id / (4 * across), deep = min(4, down - 4 * band);
+    const int down = (it.np + BLOCK - 1) / BLOCK, across = (it.mp + BLOCK - 1) / BLOCK;
+    if (id >= down * across) return;
+    const int band = id / (4 * across), deep = min(4, down - 4 * band);
     id -= band * 4 * across, tc = id / deep, tr = 4 * band + id - tc * deep;
   }
   const long long ld_a = 4ll * (KIND == GRAM ? it.mp : it.np), ld_b = 4ll * (KIND == POLY ? it.np : it.mp);
-  const char *const A = a.ws + (KIND == GRAM ? it.x[a.cur] : KIND == POLY ? it.A : it.P) + (long long)tr * BLOCK * ld_a;
-  const char *const B = a.ws + (KIND == POLY ? it.A : it.x[a.cur]) + (APART ? (long long)tc * BLOCK * 4 : (long long)tc * BLOCK * ld_b);
+  const char *const A = a.at(KIND == GRAM ? (a.cur ? it.x[1] : it.x[0]) : KIND == POLY ? it.A : it.P) + (long long)tr * BLOCK * ld_a;
+  const char *const B = a.at(KIND == POLY ? it.A : (a.cur ? it.x[1] : it.x[0])) + (APART ? (long long)tc * BLOCK * 4 : (long long)tc * BLOCK * ld_b);
   const int all = (KIND == GRAM ? it.mp : it.np) / 32, s0 = KIND == GRAM ? split * it.per : 0, steps = KIND == GRAM ? min(it.per, all - s0) : all;
   const int rows = it.np - tr * BLOCK, cols = (KIND <= POLY ? it.np : it.mp) - tc * BLOCK;  // inside
   uint32_t av[PIECES], bv[PIECES];
@@ -380,7 +415,7 @@ __global__ __launch_bounds__(Tile<BLOCK>::THREADS) void orth_product_kernel(Args
   wait_lds();
   // a lane has 4 neighbouring columns of a row
   if (KIND == GRAM && it.splits > 1) {
-    float *const part = reinterpret_cast<float *>(a.ws + it.part) + (long long)(block - a.first[k]) * BLOCK * BLOCK;
+    float *const part = reinterpret_cast<float *>(a.at(it.part)) + (long long)place * BLOCK * BLOCK;
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -397,23 +432,27 @@ __global__ __launch_bounds__(Tile<BLOCK>::THREADS) void orth_product_kernel(Args
 }
 
 // the parts of A's sums, in order, a tile to a workgroup
-__global__ __launch_bounds__(LT) void orth_parts_kernel(Args a) {
+__global__ __launch_bounds__(LT) void orth_parts_kernel(Args a, const Table *__restrict__ table) {
   constexpr int BLOCK = 64;
   __shared__ __align__(16) float W[BLOCK * (BLOCK + 4)];
-  const int k = __builtin_amdgcn_readfirstlane(item_of(a, blockIdx.x));
-  const Item &it = a.it[k];
-  const int tile = blockIdx.x - a.first[k], T = (it.np + BLOCK - 1) / BLOCK, tiles = T * (T + 1) / 2;
+  const int k = item_of(table->first[A_PARTS], a.count, blockIdx.x);
+  const Item it = table->it[k];
+  const int tile = blockIdx.x - table->first[A_PARTS][k], T = (it.np + BLOCK - 1) / BLOCK, tiles = T * (T + 1) / 2;
   int tr, tc;
   triangle(tile, tr, tc);
-  const float *const part = reinterpret_cast<const float *>(a.ws + it.part) + (long long)tile * BLOCK * BLOCK;
-  for (int i = threadIdx.x; i < BLOCK * BLOCK / 4; i += LT) {
-    floatx4 s = reinterpret_cast<const floatx4 *>(part)[i];
+  const float *const part = reinterpret_cast<const float *>(a.at(it.part)) + (long long)tile * BLOCK * BLOCK;
+  constexpr int EACH = BLOCK * BLOCK / 4 / LT;
+  floatx4 s[EACH] = {};
 #pragma unroll 4
-    for (int z = 1; z < it.splits; ++z) s += reinterpret_cast<const floatx4 *>(part + (long long)z * tiles * BLOCK * BLOCK)[i];
-    *reinterpret_cast<floatx4 *>(W + i / (BLOCK / 4) * (BLOCK + 4) + i % (BLOCK / 4) * 4) = s;
+  for (int z = 0; z < it.splits; ++z)
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) s[e] += reinterpret_cast<const floatx4 *>(part + (long long)z * tiles * BLOCK * BLOCK)[threadIdx.x + e * LT];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const int i = threadIdx.x + e * LT;
+    *reinterpret_cast<floatx4 *>(W + i / (BLOCK / 4) * (BLOCK + 4) + i % (BLOCK / 4) * 4) = s[e];
   }
-  const Tensors none = {};
-  tile_out<BLOCK, LT, GRAM, float, false>(a, none, it, k, tr, tc, W);
+  tile_out<BLOCK, LT, GRAM, float, false>(a, table->t, it, k, tr, tc, W);
 }
 
 // ---- small matrices ----
@@ -429,12 +468,13 @@ __host__ __device__ inline int small_row(int columns) { return columns * 4 + 16;
 inline int small_bytes(const Item &it) { return it.np * (small_row(it.mp) + 2 * small_row(it.np)); }
 
 template <typename T, bool MUON, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void orth_small_kernel(Args a, Tensors t, Small m) {
+__global__ __launch_bounds__(64 * WAVES) void orth_small_kernel(float eps, Table table, Small m) {
   constexpr int THREADS = 64 * WAVES;
   __shared__ __align__(16) char lds[WAVES == 4 ? FEW_LDS : MANY_LDS];
   __shared__ double sums[WAVES];
   const int k = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, q = lane >> 4;
-  const Item &it = a.it[k];
+  const Item &it = table.it[k];
+  const Tensors &t = table.t;
   const int ldx = small_row(it.mp), lda = small_row(it.np), down = it.np / 16;
   char *const X = lds, *const A = X + it.np * ldx, *const P = A + it.np * lda;
   const T *const g = (const T *)t.g[k];
@@ -459,7 +499,7 @@ __global__ __launch_bounds__(64 * WAVES) void orth_small_kernel(Args a, Tensors 
   s = 0;
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) s += sums[w];
-  const float norm = (float)sqrt(s) + a.eps;
+  const float norm = (float)sqrt(s) + eps;
   for (int i = tid; i < all; i += THREADS) {  // the elements that this thread has read and written above
     const int row = i / it.cols, col = i - row * it.cols, r = tall ? col : row, c = tall ? row : col;
     _Float16 h, l;
@@ -566,6 +606,8 @@ __global__ __launch_bounds__(64 * WAVES) void orth_small_kernel(Args a, Tensors 
 // ---- plans ----
 struct Plan {
   Args a;
+  Table table;
+  unsigned grid[LAUNCHES];
   int sym, app;  // tiles of the symmetric products, and of the others
   int small;     // waves to a matrix where all fit a workgroup each, or 0
   bool parts;
@@ -580,18 +622,18 @@ inline long long triangle_tiles(const Item &it, int block) {
 
 // Tiles of the symmetric products: rounds over the workgroups that run together (two of 64 to a CU, one of 96 or 128) by a round's time.  2048x2048: 253
 // tiles of 96 36 us, 528 of 64 44, 136 of 128 46.  The 17 matrices of 64x27 to 512x4608, whose tiles differ in length: 64 and parts 31, 96 42, 128 60.
-int symmetric_tile(const Args &a) {
+int symmetric_tile(const Item *it, int count) {
   constexpr int sides[3] = {64, 96, 128}, slots[3] = {512, 256, 256};
   constexpr double time[3] = {0.60, 0.60, 0.72};  // us a step
   double best = 1e300;
   int side = 64;
   for (int i = 0; i < 3; ++i) {
     double tiles = 0, work = 0, longest = 0;
-    for (int k = 0; k < a.count; ++k) {
-      const double t = (double)triangle_tiles(a.it[k], sides[i]), steps = a.it[k].mp / 32;
+    for (int k = 0; k < count; ++k) {
+      const double t = (double)triangle_tiles(it[k], sides[i]), steps = it[k].mp / 32;
       tiles += t, work += t * steps, longest = std::max(longest, steps);
     }
-    const double rounds = tiles <= slots[i] ? 1.0 : a.count == 1 ? std::ceil(tiles / slots[i]) : tiles / slots[i];
+    const double rounds = tiles <= slots[i] ? 1.0 : count == 1 ? std::ceil(tiles / slots[i]) : tiles / slots[i];
     // few tiles of 64 are cut into parts of their sums
     const double t = i == 0 && tiles < slots[i] ? std::min(time[i] * longest, time[i] * std::max(16.0, work / slots[i]) + 7) : time[i] * rounds * work / tiles;
     if (t < best) best = t, side = sides[i];
@@ -604,7 +646,7 @@ Plan plan_of(const nf_orth_desc &d, int count, const int32_t *rows, const int32_
   Args &a = p.a;
   a.count = count, a.eps = d.eps;
   for (int k = 0; k < count; ++k) {
-    Item &it = a.it[k];
+    Item &it = p.table.it[k];
     it.rows = rows[k], it.cols = cols[k], it.n = std::min(rows[k], cols[k]), it.m = std::max(rows[k], cols[k]);
     it.np = (it.n + 31) / 32 * 32, it.mp = (it.m + 31) / 32 * 32;
     const long long all = (long long)it.rows * it.cols;
@@ -613,60 +655,59 @@ Plan plan_of(const nf_orth_desc &d, int count, const int32_t *rows, const int32_
     it.square_parts = (int)((all + it.chunk - 1) / it.chunk);
   }
   long long large = 0;
-  for (int k = 0; k < count; ++k) large += tiles_of(a.it[k].np, 128) * tiles_of(a.it[k].mp, 128);
-  p.sym = symmetric_tile(a);
+  for (int k = 0; k < count; ++k) large += tiles_of(p.table.it[k].np, 128) * tiles_of(p.table.it[k].mp, 128);
+  p.sym = symmetric_tile(p.table.it, count);
   p.app = large >= 192 ? 128 : 64;  // the same 17 matrices, 683 tiles of 128: 49 us, of 64 53; 2048x2048, 256 tiles: 48 and 62
   int most = 0, tiles = 0;
-  for (int k = 0; k < count; ++k) most = std::max(most, a.it[k].np <= 64 ? small_bytes(a.it[k]) : MANY_LDS + 1), tiles = std::max(tiles, a.it[k].np / 16 * (a.it[k].mp / 16));
+  for (int k = 0; k < count; ++k) most = std::max(most, p.table.it[k].np <= 64 ? small_bytes(p.table.it[k]) : MANY_LDS + 1), tiles = std::max(tiles, p.table.it[k].np / 16 * (p.table.it[k].mp / 16));
   p.small = most <= FEW_LDS && tiles <= 16 ? 4 : most <= MANY_LDS ? 16 : 0;
   const int B = p.sym;
   long long work = 0;
-  for (int k = 0; k < count; ++k) work += triangle_tiles(a.it[k], B) * (a.it[k].mp / 32);
+  for (int k = 0; k < count; ++k) work += triangle_tiles(p.table.it[k], B) * (p.table.it[k].mp / 32);
   // parts of A's sums in tiles of 64: towards 512 workgroups of the same length, 16 steps each at least
   const int each = (int)std::max<long long>(16, B == 64 ? (work + 511) / 512 : 1ll << 20);
-  size_t at = 0;
+  size_t at = 256ull * TABLE;
   auto take = [&](size_t n) {
     const size_t was = at;
     at = (at + n + 255) / 256 * 256;
-    return (long long)was;
+    return (unsigned)(was / 256);
   };
   for (int k = 0; k < count; ++k) {
-    Item &it = a.it[k];
+    Item &it = p.table.it[k];
     const int steps = it.mp / 32;
     it.splits = std::max(1, (steps + each / 2) / each);
     it.per = (steps + it.splits - 1) / it.splits, it.splits = (steps + it.per - 1) / it.per;
     it.x[0] = take(4ull * it.np * it.mp), it.x[1] = take(4ull * it.np * it.mp);
     it.A = take(4ull * it.np * it.np), it.P = take(4ull * it.np * it.np);
     it.squares = take(8ull * it.square_parts);
-    it.part = it.splits > 1 ? take(4ull * it.splits * triangle_tiles(it, B) * B * B) : 0;
+    it.part = it.splits > 1 ? take(4ull * it.splits * triangle_tiles(it, B) * B * B) : 0u;
     p.parts |= it.splits > 1;
   }
   p.bytes = at;
   return p;
 }
 
-// fills the first workgroups; returns their number
+// Fills the first workgroups of a launch, or those of each share of its matrices.
 template <typename F>
-unsigned lay(Args &a, F workgroups) {
+void lay(Plan &p, int launch, F workgroups, int shares = 1) {
   long long at = 0;
-  for (int k = 0; k < a.count; ++k) a.first[k] = (int)at, at += workgroups(a.it[k]);
-  a.first[a.count] = (int)at;
-  return (unsigned)at;
+  int *const first = p.table.first[launch];
+  for (int k = 0; k < p.a.count; ++k) first[k] = (int)at, at += (workgroups(p.table.it[k]) + shares - 1) / shares;
+  first[p.a.count] = (int)at;
+  p.grid[launch] = (unsigned)(at * shares);
 }
 
 template <int KIND, typename OUT, bool MUON>
-hipError_t product(Plan &p, const Tensors &t, const char *const (&names)[3], hipStream_t st) {
+hipError_t product(const Plan &p, const char *const (&names)[3], hipStream_t st) {
   const int B = KIND <= POLY ? p.sym : p.app;
+  const unsigned grid = p.grid[KIND == GRAM ? A_TILES : KIND == POLY ? P_TILES : X_TILES];
   double flops = 0;
-  const unsigned grid = lay(p.a, [&](const Item &it) -> long long {
-    const double side = KIND == POLY ? it.n : it.m;
-    flops += (KIND <= POLY ? 1.0 : 2.0) * it.n * it.n * side;
-    if (KIND == GRAM) return triangle_tiles(it, B) * it.splits;
-    if (KIND == POLY) return triangle_tiles(it, B);
-    return tiles_of(it.np, B) * tiles_of(it.mp, B);
-  });
+  for (int k = 0; k < p.a.count; ++k) {
+    const Item &it = p.table.it[k];
+    flops += (KIND <= POLY ? 1.0 : 2.0) * it.n * it.n * (KIND == POLY ? it.n : it.m);
+  }
   return recorded(st, names[B == 64 ? 0 : B == 96 ? 1 : 2], flops, 0.0, [&] {
-    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, st, p.a, t); };
+    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, st, p.a, (const Table *)p.a.ws); };
     if (B == 64) return go(orth_product_kernel<64, KIND, OUT, MUON>, Tile<64>::THREADS);
     if constexpr (KIND <= POLY) {
       if (B == 96) return go(orth_product_kernel<96, KIND, OUT, MUON>, Tile<96>::THREADS);
@@ -713,14 +754,14 @@ bool orth_scales(const nf_orth_desc &d, Scales *s, int *last) {
 }
 
 template <typename T, bool MUON>
-hipError_t run(const nf_orth_desc &d, Plan &p, const Tensors &t, hipStream_t st) {
+hipError_t run(const nf_orth_desc &d, Plan &p, hipStream_t st) {
   Scales s[NF_ORTH_STEPS];
   int last;
   if (!orth_scales(d, s, &last)) return hipErrorInvalidValue;
   Args &a = p.a;
   auto two = [](int e) { return (float)std::ldexp(1.0, e); };
   double elements = 0;
-  for (int k = 0; k < a.count; ++k) elements += (double)a.it[k].rows * a.it[k].cols;
+  for (int k = 0; k < a.count; ++k) elements += (double)p.table.it[k].rows * p.table.it[k].cols;
   if (p.small) {
     Small m = {};
     m.steps = d.steps;
@@ -729,35 +770,38 @@ hipError_t run(const nf_orth_desc &d, Plan &p, const Tensors &t, hipStream_t st)
       m.a[k] = d.a[k], m.b[k] = d.b[k], m.c[k] = d.c[k];
       m.up_x[k] = two(s[k].x), m.up_a[k] = two(s[k].a), m.up_p[k] = two(s[k].p);
     }
-    for (int k = 0; k < a.count; ++k) flops += d.steps * (2.0 * a.it[k].n * a.it[k].n * (2.0 * a.it[k].m + a.it[k].n));
+    for (int k = 0; k < a.count; ++k) flops += d.steps * (2.0 * p.table.it[k].n * p.table.it[k].n * (2.0 * p.table.it[k].m + p.table.it[k].n));
     return recorded(st, p.small == 4 ? "orth_small_4_waves" : "orth_small_16_waves", flops, sizeof(T) * (MUON ? 5.0 : 2.0) * elements, [&] {
       if (p.small == 4)
-        hipLaunchKernelGGL((orth_small_kernel<T, MUON, 4>), dim3(a.count), dim3(256), 0, st, a, t, m);
+        hipLaunchKernelGGL((orth_small_kernel<T, MUON, 4>), dim3(a.count), dim3(256), 0, st, a.eps, p.table, m);
       else
-        hipLaunchKernelGGL((orth_small_kernel<T, MUON, 16>), dim3(a.count), dim3(1024), 0, st, a, t, m);
+        hipLaunchKernelGGL((orth_small_kernel<T, MUON, 16>), dim3(a.count), dim3(1024), 0, st, a.eps, p.table, m);
     });
   }
   a.up_x = two(s[0].x);
-  unsigned grid = lay(a, [](const Item &it) { return (long long)it.square_parts; });
+  lay(p, SQUARES, [](const Item &it) { return (long long)it.square_parts; });
+  lay(p, START, [](const Item &it) { return tiles_of(it.np, 64) * tiles_of(it.mp, 64); });
+  lay(p, A_TILES, [&](const Item &it) { return triangle_tiles(it, p.sym) * it.splits; });
+  lay(p, A_PARTS, [&](const Item &it) { return it.splits > 1 ? triangle_tiles(it, 64) : 0ll; });
+  lay(p, P_TILES, [&](const Item &it) { return triangle_tiles(it, p.sym); });
+  lay(p, X_TILES, [&](const Item &it) { return tiles_of(it.np, p.app) * tiles_of(it.mp, p.app); }, 8);
   hipError_t e = recorded(st, "orth_squares", 0.0, sizeof(T) * (MUON ? 3.0 : 1.0) * elements,
-                          [&] { hipLaunchKernelGGL((orth_squares_kernel<T, MUON>), dim3(grid), dim3(NT), 0, st, a, t); });
+                          [&] { hipLaunchKernelGGL((orth_squares_kernel<T, MUON>), dim3(p.grid[SQUARES]), dim3(NT), 0, st, a, p.table); });
   if (e != hipSuccess) return e;
-  grid = lay(a, [](const Item &it) { return tiles_of(it.np, 64) * tiles_of(it.mp, 64); });
+  const Table *const table = (const Table *)a.ws;
   e = recorded(st, "orth_start", 0.0, (sizeof(T) * (MUON ? 2.0 : 1.0) + 4.0) * elements,
-               [&] { hipLaunchKernelGGL((orth_start_kernel<T, MUON>), dim3(grid), dim3(NT), 0, st, a, t); });
+               [&] { hipLaunchKernelGGL((orth_start_kernel<T, MUON>), dim3(p.grid[START]), dim3(NT), 0, st, a, table); });
   for (int k = 0; k < d.steps && e == hipSuccess; ++k) {
     const bool end = k + 1 == d.steps;
     a.cur = k & 1, a.a = d.a[k], a.b = d.b[k], a.c = d.c[k];
     a.up_x = two(s[k].x), a.down_x = two(-s[k].x), a.up_a = two(s[k].a), a.down_a = two(-s[k].a), a.up_p = two(s[k].p), a.down_p = two(-s[k].p);
     a.up_next = two(end ? last : s[k + 1].x);
-    e = product<GRAM, float, false>(p, t, {"orth_gram_64x64", "orth_gram_96x96", "orth_gram_128x128"}, st);
-    if (e == hipSuccess && p.parts) {
-      grid = lay(a, [&](const Item &it) { return it.splits > 1 ? triangle_tiles(it, 64) : 0ll; });
-      e = recorded(st, "orth_parts", 0.0, 0.0, [&] { hipLaunchKernelGGL(orth_parts_kernel, dim3(grid), dim3(LT), 0, st, a); });
-    }
-    if (e == hipSuccess) e = product<POLY, float, false>(p, t, {"orth_poly_64x64", "orth_poly_96x96", "orth_poly_128x128"}, st);
+    e = product<GRAM, float, false>(p, {"orth_gram_64x64", "orth_gram_96x96", "orth_gram_128x128"}, st);
+    if (e == hipSuccess && p.parts)
+      e = recorded(st, "orth_parts", 0.0, 0.0, [&] { hipLaunchKernelGGL(orth_parts_kernel, dim3(p.grid[A_PARTS]), dim3(LT), 0, st, a, table); });
+    if (e == hipSuccess) e = product<POLY, float, false>(p, {"orth_poly_64x64", "orth_poly_96x96", "orth_poly_128x128"}, st);
     if (e != hipSuccess) break;
-    e = end ? product<LAST, T, MUON>(p, t, {"orth_last_64x64", "", "orth_last_128x128"}, st) : product<APPLY, float, false>(p, t, {"orth_apply_64x64", "", "orth_apply_128x128"}, st);
+    e = end ? product<LAST, T, MUON>(p, {"orth_last_64x64", "", "orth_last_128x128"}, st) : product<APPLY, float, false>(p, {"orth_apply_64x64", "", "orth_apply_128x128"}, st);
   }
   return e;
 }
@@ -776,21 +820,21 @@ hipError_t launch_orth(const nf_orth_desc &d, int dtype, int count, const void *
                        hipStream_t st) {
   Plan p = plan_of(d, count, rows, cols);
   p.a.ws = (char *)ws;
-  Tensors t = {};
+  Tensors &t = p.table.t;
   for (int k = 0; k < count; ++k) t.g[k] = g[k], t.y[k] = y[k];
-  if (dtype == NF_BF16) return run<__bf16, false>(d, p, t, st);
-  if (dtype == NF_F16) return run<_Float16, false>(d, p, t, st);
-  return run<float, false>(d, p, t, st);
+  if (dtype == NF_BF16) return run<__bf16, false>(d, p, st);
+  if (dtype == NF_F16) return run<_Float16, false>(d, p, st);
+  return run<float, false>(d, p, st);
 }
 
 hipError_t launch_muon(const nf_muon_desc &d, int count, float *const *w, const float *const *g, float *const *v, const int32_t *rows, const int32_t *cols, void *ws,
                        hipStream_t st) {
   Plan p = plan_of(d.orth, count, rows, cols);
   p.a.ws = (char *)ws;
-  Tensors t = {};
+  Tensors &t = p.table.t;
   for (int k = 0; k < count; ++k) t.g[k] = g[k], t.y[k] = w[k], t.v[k] = v && d.momentum != 0 ? v[k] : nullptr;
   t.momentum = d.momentum, t.lr = d.lr, t.keep = (float)(1.0 - (double)d.lr * d.weight_decay), t.nesterov = d.nesterov;
-  return run<float, true>(d.orth, p, t, st);
+  return run<float, true>(d.orth, p, st);
 }
 
 }  // namespace nf
