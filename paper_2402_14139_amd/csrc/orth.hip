@@ -190,7 +190,7 @@ enum { GRAM, POLY, APPLY, LAST };
 
 template <int BLOCK>
 struct Tile {
-  static constexpr int DOWN = BLOCK == 96 ? 6 : 2, ACROSS = BLOCK == 128 ? 4 : 2;  // waves of 64 x 32, 16 x 48 and 32 x 32
+  static constexpr int DOWN = BLOCK == 96 ? 3 : 2, ACROSS = BLOCK == 128 ? 4 : 2;  // waves of 64 x 32, 32 x 48 (12 of 16 x 48 1.5 us slower at 2048x2048) and 32 x 32
   static constexpr int STAGES = 4;
   static constexpr int WAVES = DOWN * ACROSS, THREADS = 64 * WAVES, MT = BLOCK / 16 / DOWN, NT = BLOCK / 16 / ACROSS;
   static constexpr int BYTES = BLOCK * 128, STAGE = 2 * BYTES, PIECES = BYTES / 1024 / WAVES;
@@ -305,7 +305,7 @@ __device__ inline void triangle(int t, int &tr, int &tc) {
   tr = t - tc * (tc + 1) / 2;
 }
 
-// BLOCK x BLOCK results by four waves of BLOCK/2 x BLOCK/2; a step is 32 terms.  While a step's products run, the next one's fragments are read and the
+// BLOCK x BLOCK results; a step is 32 terms.  While a step's products run, the next one's fragments are read and the
 // copies of the STAGES-th next are on their way: one barrier a step, behind which the next stage is whole and this one free.  Steps go in pairs
 // (two sets of fragments); those beyond the last are copies of nothing, so that the waits count the same.
 template <int BLOCK, int KIND, typename OUT, bool MUON>
@@ -621,10 +621,10 @@ inline long long triangle_tiles(const Item &it, int block) {
 }
 
 // Tiles of the symmetric products: rounds over the workgroups that run together (two of 64 to a CU, one of 96 or 128) by a round's time.  2048x2048: 253
-// tiles of 96 36 us, 528 of 64 44, 136 of 128 46.  The 17 matrices of 64x27 to 512x4608, whose tiles differ in length: 64 and parts 31, 96 42, 128 60.
+// tiles of 96 35 us, 528 of 64 44, 136 of 128 46.  The 17 matrices of 64x27 to 512x4608, whose tiles differ in length: 64 and parts 31, 96 42, 128 60.
 int symmetric_tile(const Item *it, int count) {
   constexpr int sides[3] = {64, 96, 128}, slots[3] = {512, 256, 256};
-  constexpr double time[3] = {0.60, 0.60, 0.72};  // us a step
+  constexpr double time[3] = {0.60, 0.56, 0.72};  // us a step
   double best = 1e300;
   int side = 64;
   for (int i = 0; i < 3; ++i) {
