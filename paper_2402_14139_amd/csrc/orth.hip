@@ -620,25 +620,33 @@ inline long long triangle_tiles(const Item &it, int block) {
   return T * (T + 1) / 2;
 }
 
-// Tiles of the symmetric products: rounds over the workgroups that run together (two of 64 to a CU, one of 96 or 128) by a round's time.  2048x2048: 253
-// tiles of 96 35 us, 528 of 64 44, 136 of 128 46.  The 17 matrices of 64x27 to 512x4608, whose tiles differ in length: 64 and parts 31, 96 42, 128 60.
-int symmetric_tile(const Item *it, int count) {
+// Tiles of the symmetric products, by rounds over the workgroups that run together (two of 64 to a CU, one of 96 or 128) and a step's time, and whether A's
+// sums are cut into parts, towards 512 workgroups of tiles of 64, 16 steps each at least, and added in a launch of their own.  2048x2048: 253 tiles of
+// 96 35 us, 528 of 64 44, 136 of 128 46.  17 matrices of 64x27 to 512x4608, whose tiles differ in length: 64 and parts 34, 96 42, 128 60.  1000x1000,
+// 136 tiles of 64, one to a CU: 14, and with parts 19.
+struct Symmetric {
+  int side;
+  bool parts;
+};
+Symmetric symmetric_tile(const Item *it, int count) {
   constexpr int sides[3] = {64, 96, 128}, slots[3] = {512, 256, 256};
-  constexpr double time[3] = {0.60, 0.56, 0.72};  // us a step
+  constexpr double time[3] = {0.60, 0.56, 0.72}, alone = 0.33;  // us a step; of a tile of 64 on a CU of its own
   double best = 1e300;
-  int side = 64;
+  Symmetric s = {64, false};
+  auto see = [&](double t, int side, bool parts) {
+    if (t < best) best = t, s = Symmetric{side, parts};
+  };
   for (int i = 0; i < 3; ++i) {
     double tiles = 0, work = 0, longest = 0;
     for (int k = 0; k < count; ++k) {
       const double t = (double)triangle_tiles(it[k], sides[i]), steps = it[k].mp / 32;
       tiles += t, work += t * steps, longest = std::max(longest, steps);
     }
-    const double rounds = tiles <= slots[i] ? 1.0 : count == 1 ? std::ceil(tiles / slots[i]) : tiles / slots[i];
-    // few tiles of 64 are cut into parts of their sums
-    const double t = i == 0 && tiles < slots[i] ? std::min(time[i] * longest, time[i] * std::max(16.0, work / slots[i]) + 7) : time[i] * rounds * work / tiles;
-    if (t < best) best = t, side = sides[i];
+    const double rounds = count == 1 ? std::ceil(tiles / slots[i]) : std::max(1.0, tiles / slots[i]);
+    see(i == 0 && tiles <= 256 ? alone * longest : tiles <= slots[i] ? time[i] * longest : time[i] * rounds * work / tiles, sides[i], false);
+    if (i == 0) see(time[0] * std::max(16.0, work / 512) + 8, 64, true);
   }
-  return side;
+  return s;
 }
 
 Plan plan_of(const nf_orth_desc &d, int count, const int32_t *rows, const int32_t *cols) {
@@ -656,7 +664,8 @@ Plan plan_of(const nf_orth_desc &d, int count, const int32_t *rows, const int32_
   }
   long long large = 0;
   for (int k = 0; k < count; ++k) large += tiles_of(p.table.it[k].np, 128) * tiles_of(p.table.it[k].mp, 128);
-  p.sym = symmetric_tile(p.table.it, count);
+  const Symmetric sym = symmetric_tile(p.table.it, count);
+  p.sym = sym.side;
   p.app = large >= 192 ? 128 : 64;  // the same 17 matrices, 683 tiles of 128: 49 us, of 64 53; 2048x2048, 256 tiles: 48 and 62
   int most = 0, tiles = 0;
   for (int k = 0; k < count; ++k) most = std::max(most, p.table.it[k].np <= 64 ? small_bytes(p.table.it[k]) : MANY_LDS + 1), tiles = std::max(tiles, p.table.it[k].np / 16 * (p.table.it[k].mp / 16));
@@ -664,8 +673,7 @@ Plan plan_of(const nf_orth_desc &d, int count, const int32_t *rows, const int32_
   const int B = p.sym;
   long long work = 0;
   for (int k = 0; k < count; ++k) work += triangle_tiles(p.table.it[k], B) * (p.table.it[k].mp / 32);
-  // parts of A's sums in tiles of 64: towards 512 workgroups of the same length, 16 steps each at least
-  const int each = (int)std::max<long long>(16, B == 64 ? (work + 511) / 512 : 1ll << 20);
+  const int each = (int)std::max<long long>(16, sym.parts ? (work + 511) / 512 : 1ll << 20);
   size_t at = 256ull * TABLE;
   auto take = [&](size_t n) {
     const size_t was = at;

@@ -97,8 +97,8 @@ def on_gpu(g, steps, eps):
 
 
 ORTH = [([(16, 27)], {"orth_small_4_waves": 1}), ([(64, 64)], {"orth_small_16_waves": 1}), ([(64, 200), (512, 10)], {"orth_small_16_waves": 1}), ([(64, 576)], orth_kernels(64, 64)),
-        ([(1000, 1000)], orth_kernels(64, 64, True)), ([(1700, 1690)], orth_kernels(96, 128)), ([(2040, 2048)], orth_kernels(96, 128)), ([(2300, 2301)], orth_kernels(128, 128)),
-        ([(9000, 700)], orth_kernels(64, 128, True)), ([(1000, 1500), (1400, 1300), (700, 4000)], orth_kernels(96, 128))]
+        ([(1000, 1000)], orth_kernels(64, 64)), ([(500, 2050)], orth_kernels(64, 64, True)), ([(1700, 1690)], orth_kernels(96, 128)), ([(2040, 2048)], orth_kernels(96, 128)), ([(2300, 2301)], orth_kernels(128, 128)),
+        ([(9000, 700)], orth_kernels(64, 128, True)), ([(1000, 1500), (1400, 1300), (700, 4000)], orth_kernels(64, 128, True))]
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16"])
