@@ -277,20 +277,22 @@ struct WideSteps {
 
 // A tile of BLOCK x BLOCK by 2 x ACROSS waves; a step is 8 groups of the sum: 128 bytes of codes and 8 of exponents to a row, copied while the step before
 // it is carried out.  A row's chunks of 16 bytes (groups) are exchanged in LDS so that the 16 rows of a fragment's read lie in different banks.
-constexpr int STEP = 8;  // groups
-template <int BLOCK, int ACROSS>
+template <int BLOCK, int ACROSS, int STEP>
 struct MxTile {
   static constexpr int WAVES = 2 * ACROSS, THREADS = 64 * WAVES, MT = BLOCK / 32, NT = BLOCK / 16 / ACROSS;
-  static constexpr int CODES = BLOCK * 128, SCALES = BLOCK * STEP, STAGE = 2 * (CODES + SCALES), PIECES = CODES / 1024 / WAVES, WORDS = SCALES / 4 / (THREADS / 2);
-  static constexpr int HALF = BLOCK == 256 ? MT / 2 : MT, PER_SIMD = BLOCK == 64 || (BLOCK == 128 && ACROSS == 4) ? 4 : 2;  // waves to a SIMD
+  static constexpr int ROW = STEP * 16, CODES = BLOCK * ROW, SCALES = BLOCK * STEP, STAGE = 2 * (CODES + SCALES), PIECES = CODES / 1024 / WAVES;
+  static constexpr int LOADERS = THREADS < SCALES / 2 ? THREADS : SCALES / 2, WORDS = SCALES / 2 / LOADERS;  // of exponents: threads (others bring the same again), and 4 bytes of a row each
+  static constexpr int STAGES = STEP == 4 ? 3 : 2, SUMS = STEP == 4 ? MT / 2 : BLOCK == 256 ? MT / 2 : MT;
+  static constexpr int PER_SIMD = STEP == 4 ? WAVES * 3 / 4 : BLOCK == 64 || (BLOCK == 128 && ACROSS == 4) ? 4 : 2;  // waves to a SIMD
 };
-__device__ inline int mx_swizzle(int row) { return (row >> 1) & 7; }
+template <int STEP>
+__device__ inline int mx_swizzle(int row) { return (row >> 1) & (STEP - 1); }
 
-template <typename T, int BLOCK, int ACROSS, bool PARTS>
-__global__ __launch_bounds__((MxTile<BLOCK, ACROSS>::THREADS), (MxTile<BLOCK, ACROSS>::PER_SIMD)) void mx_gemm_kernel(MxArgs m) {
-  using S = MxTile<BLOCK, ACROSS>;
-  constexpr int MT = S::MT, NT = S::NT, PIECES = S::PIECES, WAVES = S::WAVES;
-  __shared__ __align__(1024) char lds[2 * S::STAGE];
+template <typename T, int BLOCK, int ACROSS, int STEP, bool PARTS>
+__global__ __launch_bounds__((MxTile<BLOCK, ACROSS, STEP>::THREADS), (MxTile<BLOCK, ACROSS, STEP>::PER_SIMD)) void mx_gemm_kernel(MxArgs m) {
+  using S = MxTile<BLOCK, ACROSS, STEP>;
+  constexpr int MT = S::MT, NT = S::NT, PIECES = S::PIECES, WAVES = S::WAVES, STAGES = S::STAGES;
+  __shared__ __align__(1024) char lds[STAGES * S::STAGE];
   const GemmArgs &g = m.g;
   const int id = xcd_run(blockIdx.x, gridDim.x);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, q = lane >> 4;
@@ -301,33 +303,34 @@ __global__ __launch_bounds__((MxTile<BLOCK, ACROSS>::THREADS), (MxTile<BLOCK, AC
   const int rows_left = (int)min(g.R - r0, (long long)BLOCK), cols_left = g.C - c0;
   // what this lane brings: chunks of codes, and words of exponents: half of the waves those of A, the others those of B
   uint32_t av[PIECES], bv[PIECES], sv[S::WORDS];
-  const int chunk = (lane & 7) ^ mx_swizzle((wave * 64 + lane) >> 3);  // the same for all pieces: they are WAVES * 8 rows apart
+  const int chunk = (lane & (STEP - 1)) ^ mx_swizzle<STEP>((wave * 64 + lane) / STEP);  // the same for all pieces: they are whole eights of rows apart
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
-    const int row = ((p * WAVES + wave) * 64 + lane) >> 3;
+    const int row = ((p * WAVES + wave) * 64 + lane) / STEP;
     av[p] = row < rows_left ? row * (uint32_t)g.lda + chunk * 16 : OUTSIDE;
     bv[p] = row < cols_left ? row * (uint32_t)g.ldb + chunk * 16 : OUTSIDE;
   }
-  const bool of_b = wave >= WAVES / 2;
+  constexpr int LOADERS = S::LOADERS;
+  const bool of_b = (wave & (LOADERS / 64 - 1)) >= LOADERS / 128;
 #pragma unroll
   for (int w = 0; w < S::WORDS; ++w) {
-    const int row = ((tid & (S::THREADS / 2 - 1)) + w * (S::THREADS / 2)) >> 1;
-    sv[w] = row < (of_b ? cols_left : rows_left) ? row * (uint32_t)(of_b ? m.lsb : m.lsa) + (tid & 1) * 4 : OUTSIDE;
+    const int at = (tid & (LOADERS / 2 - 1)) + w * (LOADERS / 2), row = at / (STEP / 4);
+    sv[w] = row < (of_b ? cols_left : rows_left) ? row * (uint32_t)(of_b ? m.lsb : m.lsa) + at % (STEP / 4) * 4 : OUTSIDE;
   }
   const char *const pa = g.a + r0 * g.lda + l0 * 16, *const pb = g.b + c0 * g.ldb + l0 * 16;
   const char *const ps = of_b ? (const char *)m.sb + c0 * m.lsb + l0 : (const char *)m.sa + r0 * m.lsa + l0;
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
   auto fetch = [&](int s) {
     const uint32_t none = chunk < (int)(l1 - l0) - s * STEP ? 0u : OUTSIDE;  // groups behind the last; an offset with OUTSIDE's bits lies outside
-    const uintx4 ba = buffer_of(pa + s * 128ll), bb = buffer_of(pb + s * 128ll), bs = buffer_of(ps + s * STEP);
-    const uint32_t to = base + (s & 1) * S::STAGE;
+    const uintx4 ba = buffer_of(pa + s * (long long)S::ROW), bb = buffer_of(pb + s * (long long)S::ROW), bs = buffer_of(ps + s * STEP);
+    const uint32_t to = base + s % STAGES * S::STAGE;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) copy16(ba, av[p] | none, to + (p * WAVES + wave) * 1024);
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) copy16(bb, bv[p] | none, to + S::CODES + (p * WAVES + wave) * 1024);
 #pragma unroll
     for (int w = 0; w < S::WORDS; ++w)
-      copy4(bs, sv[w], to + 2 * S::CODES + (of_b ? S::SCALES : 0) + (w * (WAVES / 2) + (wave & (WAVES / 2 - 1))) * 256);
+      copy4(bs, sv[w], to + 2 * S::CODES + (of_b ? S::SCALES : 0) + (w * (LOADERS / 128) + (wave & (LOADERS / 128 - 1))) * 256);
   };
   const int wm = wave / ACROSS * (16 * MT), wn = wave % ACROSS * (16 * NT);
   floatx4 acc[MT][NT];
@@ -335,19 +338,19 @@ __global__ __launch_bounds__((MxTile<BLOCK, ACROSS>::THREADS), (MxTile<BLOCK, AC
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const int swz = mx_swizzle(i16);  // rows of a wave's fragments are multiples of 16 apart
+  const int swz = mx_swizzle<STEP>(i16);  // rows of a wave's fragments are multiples of 16 apart
   auto step = [&](int s) {
-    const char *const from = lds + (s & 1) * S::STAGE, *const la = from + (wm + i16) * 128, *const lb = from + S::CODES + (wn + i16) * 128;
+    const char *const from = lds + s % STAGES * S::STAGE, *const la = from + (wm + i16) * S::ROW, *const lb = from + S::CODES + (wn + i16) * S::ROW;
     const char *const ea = from + 2 * S::CODES + (wm + i16) * STEP + q, *const eb = from + 2 * S::CODES + S::SCALES + (wn + i16) * STEP + q;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
+    for (int kk = 0; kk < STEP / 4; ++kk) {
       uintx4 fa[MT], fb[NT];
       uint32_t xa[MT], xb[NT];
       const int at = ((kk * 4 + q) ^ swz) << 4;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) fb[j] = *reinterpret_cast<const uintx4 *>(lb + j * 2048 + at), xb[j] = *reinterpret_cast<const uint8_t *>(eb + j * 16 * STEP + kk * 4);
+      for (int j = 0; j < NT; ++j) fb[j] = *reinterpret_cast<const uintx4 *>(lb + j * 16 * S::ROW + at), xb[j] = *reinterpret_cast<const uint8_t *>(eb + j * 16 * STEP + kk * 4);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) fa[i] = *reinterpret_cast<const uintx4 *>(la + i * 2048 + at), xa[i] = *reinterpret_cast<const uint8_t *>(ea + i * 16 * STEP + kk * 4);
+      for (int i = 0; i < MT; ++i) fa[i] = *reinterpret_cast<const uintx4 *>(la + i * 16 * S::ROW + at), xa[i] = *reinterpret_cast<const uint8_t *>(ea + i * 16 * STEP + kk * 4);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -357,13 +360,14 @@ __global__ __launch_bounds__((MxTile<BLOCK, ACROSS>::THREADS), (MxTile<BLOCK, AC
   // What lies behind a row's last element may be anything: zeros take its place in the last step's stage, where that is not a step's end, too.
   const bool ragged = l1 == g.L && m.K % (STEP * GROUP) != 0;
   auto end_rows = [&] {
-    char *const stage = lds + ((steps - 1) & 1) * S::STAGE;
+    char *const stage = lds + (steps - 1) % STAGES * S::STAGE;
     const int inside = (int)(l1 - l0) - (steps - 1) * STEP, n = m.K % GROUP;  // groups of the step, elements of its last one (0: all)
-    const unsigned long long keep = inside >= 8 ? ~0ull : (1ull << 8 * inside) - 1;
-    for (int r = tid; r < 2 * BLOCK; r += S::THREADS) *reinterpret_cast<unsigned long long *>(stage + 2 * S::CODES + r * STEP) &= keep;
+    using Exponents = std::conditional_t<STEP == 8, unsigned long long, uint32_t>;
+    const Exponents keep = inside >= STEP ? ~(Exponents)0 : ((Exponents)1 << 8 * inside) - 1;
+    for (int r = tid; r < 2 * BLOCK; r += S::THREADS) *reinterpret_cast<Exponents *>(stage + 2 * S::CODES + r * STEP) &= keep;
     if (n) {
       for (int r = tid; r < BLOCK; r += S::THREADS) {
-        uintx4 *const p = reinterpret_cast<uintx4 *>(stage + r * 128 + (((inside - 1) ^ mx_swizzle(r)) << 4));
+        uintx4 *const p = reinterpret_cast<uintx4 *>(stage + r * S::ROW + (((inside - 1) ^ mx_swizzle<STEP>(r)) << 4));
         *p = first_codes(*p, n);
       }
     }
@@ -371,20 +375,35 @@ __global__ __launch_bounds__((MxTile<BLOCK, ACROSS>::THREADS), (MxTile<BLOCK, AC
     barrier();
   };
   fetch(0);
-  if (steps > 1) {
-    fetch(1);
-    wait_copies<2 * PIECES + S::WORDS>();
-  } else {
-    wait_copies<0>();
-  }
-  barrier();
+  if (steps > 1) fetch(1);
+  auto first = [&] {
+    if (steps > 1)
+      wait_copies<2 * PIECES + S::WORDS>();
+    else
+      wait_copies<0>();
+    barrier();
+  };
   auto next = [&](int s) {  // step s + 1 is whole, s read by all
     if (s + 2 < steps)
       fetch(s + 2);
     else if (ragged)
       end_rows();
   };
-  if constexpr (BLOCK == 256) {
+  if constexpr (STEP == 4) {
+    for (int s = 0; s + 1 < steps; ++s) {
+      wait_copies<2 * PIECES + S::WORDS>();  // all but the next step's
+      wait_lds();
+      barrier();
+      if (s + 2 < steps) fetch(s + 2);
+      step(s);
+    }
+    wait_copies<0>();
+    wait_lds();
+    barrier();
+    if (ragged) end_rows();
+    step(steps - 1);
+  } else if constexpr (BLOCK == 256) {
+    first();
     WideSteps<S, decltype(next)> w = {lds, (wm + i16) * 128, S::CODES + (wn + i16) * 128, 2 * S::CODES + (wm + i16) * STEP + q, 2 * S::CODES + S::SCALES + (wn + i16) * STEP + q,
                                       {(q ^ swz) << 4, ((4 + q) ^ swz) << 4}, next};
     if (ragged && steps == 1) end_rows();
@@ -396,6 +415,7 @@ __global__ __launch_bounds__((MxTile<BLOCK, ACROSS>::THREADS), (MxTile<BLOCK, AC
     w.template half<true, 0>(acc, steps - 1);
     w.template half<true, 1>(acc, steps - 1);
   } else {
+    first();
     for (int s = 0; s + 1 < steps; ++s) {
       step(s);
       wait_copies<0>();
@@ -412,7 +432,7 @@ __global__ __launch_bounds__((MxTile<BLOCK, ACROSS>::THREADS), (MxTile<BLOCK, AC
   } else {
     wait_lds();
     barrier();
-    write_fwd<T, false, S::HALF>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * S::HALF * NT * 64);
+    write_fwd<T, false, S::SUMS>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * S::SUMS * NT * 64);
   }
 }
 
@@ -489,21 +509,24 @@ __global__ __launch_bounds__(64 * NW) void mx_few_rows_kernel(MxArgs m) {
 
 // ---- plans ----
 constexpr int FEW = 32;  // rows
+constexpr int STEP = 8;  // groups
 struct MxPlan {
   int tile, splits;
   long long per;  // groups of a split
   size_t bytes;   // of the splits' sums
 };
-// Tiles of 256 or 128 by rounds over the workgroups that run together (one to a CU and two) and a round's time: steps, then what ends a tile (us,
-// in tiles of 256 and of 128: 8192x8192x8192 bf16 294 and 389, 16384x2048x2048 48 and 57, 65536x512x2048 131 and 133, with GELU 167 and 148, fp32 results
-// 147 and 184).  Few tiles of 128 become tiles of 64 or parts of sums: towards 512 workgroups, four steps each at least.
-MxPlan mx_plan(int dtype, long long M, int N, long long K) {
+// Tiles of 256 or 128 by rounds over the workgroups that run together (one to a CU and two, three where sums are short) and a round's time: steps, then
+// what ends a tile, with no other workgroup's steps beside it in a CU that holds one (us, in tiles of 256 and of 128: 8192x8192x8192 bf16 276 and 389,
+// 16384x2048x2048 48 and 57, 16384x1500x2048 with GELU 60 and 55, 65536x512x2048 131 and 110, with GELU 167 and 132, fp32 results
+// 147 and 215).  Few tiles of 128 become tiles of 64 or parts of sums: towards 512 workgroups, four steps each at least.
+MxPlan mx_plan(int dtype, int act, long long M, int N, long long K) {
   MxPlan p = {0, 1, 0, 0};
   if (M <= FEW) return p;
   const long long steps = ((K + GROUP - 1) / GROUP + STEP - 1) / STEP;
   auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
-  const bool wide = dtype == NF_F32;
-  const double large = (double)((tiles(256) + 255) / 256) * (2.3 * steps + (wide ? 14 : 12)), medium = std::max(1.0, tiles(128) / 512.0) * (1.5 * steps + (wide ? 8 : 4));
+  const bool wide = dtype == NF_F32, exps = act != NF_ACT_NONE && act != NF_ACT_RELU;
+  const double large = (double)((tiles(256) + 255) / 256) * (2.3 * steps + (wide ? 14 : 12) + (exps ? 4.5 : 0));
+  const double medium = std::max(1.0, tiles(128) / 512.0) * (1.5 * steps + (wide ? 8 : 4) + (exps ? 1.4 : 0));
   p.tile = tiles(128) < 256 ? 64 : tiles(128) >= 512 && large < medium ? 256 : 128;
   const long long t = tiles(p.tile);
   const long long splits = std::max<long long>(1, std::min<long long>(512 / t, steps / 4));
@@ -516,7 +539,7 @@ inline size_t whole256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <typename T>
 hipError_t product_as(const MxCall &c, const void *raw, const MxRows &a, const MxRows &b, const Epilogue &e, void *ws, hipStream_t st) {
-  const MxPlan p = mx_plan(c.dtype, c.M, c.N, c.K);
+  const MxPlan p = mx_plan(c.dtype, c.act, c.M, c.N, c.K);
   MxArgs m = {};
   GemmArgs &g = m.g;
   g.a = raw ? (const char *)raw : (const char *)a.codes, g.b = (const char *)b.codes, g.lda = raw ? (long long)c.K * sizeof(T) : a.cb, g.ldb = b.cb;
@@ -540,24 +563,27 @@ hipError_t product_as(const MxCall &c, const void *raw, const MxRows &a, const M
   if (p.splits > 1) g.part = (float *)ws, g.part_ld = (c.N + 7) / 8 * 8;
   const hipError_t err = recorded(st, p.tile == 256 ? "mx_product_256x256" : p.tile == 128 ? "mx_product_128x128" : "mx_product_64x64", flops, bytes + (p.splits > 1 ? 4.0 * p.splits * c.M * c.N : ends), [&] {
     const dim3 grid((unsigned)(g.tiles * g.splits));
-    auto go = [&](auto tile, auto across) {
-      constexpr int B = decltype(tile)::value, A = decltype(across)::value;
-      if (g.part)
-        hipLaunchKernelGGL((mx_gemm_kernel<T, B, A, true>), grid, dim3((MxTile<B, A>::THREADS)), 0, st, m);
+    auto go = [&](auto tile, auto across, auto step) {
+      constexpr int B = decltype(tile)::value, A = decltype(across)::value, G = decltype(step)::value;
+      if (G == 8 && g.part)  // sums of at most 16 groups have no parts
+        hipLaunchKernelGGL((mx_gemm_kernel<T, B, A, 8, true>), grid, dim3((MxTile<B, A, 8>::THREADS)), 0, st, m);
       else
-        hipLaunchKernelGGL((mx_gemm_kernel<T, B, A, false>), grid, dim3((MxTile<B, A>::THREADS)), 0, st, m);
+        hipLaunchKernelGGL((mx_gemm_kernel<T, B, A, G, false>), grid, dim3((MxTile<B, A, G>::THREADS)), 0, st, m);
     };
     using std::integral_constant;
     using I2 = integral_constant<int, 2>;
     using I4 = integral_constant<int, 4>;
+    using I8 = integral_constant<int, 8>;
     if (p.tile == 256)
-      go(integral_constant<int, 256>(), I4());
+      go(integral_constant<int, 256>(), I4(), I8());
     else if (p.tile == 64)
-      go(integral_constant<int, 64>(), I2());
+      go(integral_constant<int, 64>(), I2(), I8());
+    else if (g.L <= 2 * STEP)
+      go(integral_constant<int, 128>(), I2(), I4());
     else if (g.L >= 8 * STEP)
-      go(integral_constant<int, 128>(), I2());
+      go(integral_constant<int, 128>(), I2(), I8());
     else
-      go(integral_constant<int, 128>(), I4());
+      go(integral_constant<int, 128>(), I4(), I8());
   });
   if (err != hipSuccess || p.splits == 1) return err;
   const FinishArgs f = finish_args(p.splits, g);
@@ -591,9 +617,9 @@ bool mx_quantise_fits(long long rows, long long cols) {
   return (double)((rows + TR - 1) / TR) * (double)((cols + TC - 1) / TC) < 2147483648.0;
 }
 
-size_t mx_product_workspace_bytes(const MxCall &c) { return mx_plan(c.dtype, c.M, c.N, c.K).bytes; }
+size_t mx_product_workspace_bytes(const MxCall &c) { return mx_plan(c.dtype, c.act, c.M, c.N, c.K).bytes; }
 size_t mx_linear_workspace_bytes(const MxCall &c) {
-  const MxPlan p = mx_plan(c.dtype, c.M, c.N, c.K);
+  const MxPlan p = mx_plan(c.dtype, c.act, c.M, c.N, c.K);
   if (!p.tile) return 0;
   const MxRows r = rows_at(nullptr, nullptr, c.K);
   return whole256(p.bytes) + whole256((size_t)c.M * r.cb) + (size_t)c.M * r.sb;
@@ -619,7 +645,7 @@ hipError_t launch_mx_product(const MxCall &c, const void *a, const void *as, con
 // The workspace holds the splits' sums, then x's codes and exponents.
 hipError_t launch_mx_linear(const MxCall &c, const void *x, const void *W, const void *Ws, const float *bias, const void *r, const DropArgs &drop, void *y, void *z,
                             void *ws, hipStream_t st) {
-  const MxPlan p = mx_plan(c.dtype, c.M, c.N, c.K);
+  const MxPlan p = mx_plan(c.dtype, c.act, c.M, c.N, c.K);
   if (p.tile) {
     const MxRows sizes = rows_at(nullptr, nullptr, c.K);
     char *const codes = (char *)ws + whole256(p.bytes), *const scales = codes + whole256((size_t)c.M * sizes.cb);
