@@ -471,7 +471,8 @@ int32_t nf_qcache_read(int32_t format, int32_t dtype, const uint8_t *codes, cons
  * row strides: nf_qcache_row_bytes; nf_qcache_write fills and nf_qcache_read reads one, too).  nf_mx_quantise writes x [rows][cols], of
  * type dtype, by rows into codes and scales, and by columns, that is as the matrix [cols][rows], into codes_t and scales_t; either pair may be
  * NULL.  Codes behind a row's last element, up to a whole group, are 0; other bytes between a row's end and its stride are left as they
- * are, and products read none of them as numbers.  Rows and columns beyond 2^44 elements in all: NF_ERR_UNSUPPORTED. */
+ * are, and products read none of them as numbers.  Beyond 2^32 groups by rows, 2^24 tiles of 128 x 64 by columns or
+ * 2^44 elements: NF_ERR_UNSUPPORTED. */
 int32_t nf_mx_quantise(int32_t dtype, int64_t rows, int64_t cols, const void *x, uint8_t *codes, uint8_t *scales,
                        uint8_t *codes_t, uint8_t *scales_t, void *stream);
 /* y = r + act(a b^T + bias) [M][N]: a holds M rows of K, b N rows of K, both in 4 bits; d->dtype is that of y and r; bias and r may be

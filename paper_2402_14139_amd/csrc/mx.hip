@@ -613,8 +613,9 @@ MxRows rows_at(void *codes, void *scales, long long n) {
 
 }  // namespace
 
-bool mx_quantise_fits(long long rows, long long cols) {
-  return (double)((rows + TR - 1) / TR) * (double)((cols + TC - 1) / TC) < 2147483648.0;
+bool mx_quantise_fits(long long rows, long long cols, bool by_columns) {
+  const double blocks = by_columns ? (double)((rows + TR - 1) / TR) * (double)((cols + TC - 1) / TC) : (double)rows * (double)((cols + GROUP - 1) / GROUP) / QT;
+  return blocks < (1 << 24) - 1;  // a launch has less than 2^32 threads
 }
 
 size_t mx_product_workspace_bytes(const MxCall &c) { return mx_plan(c.dtype, c.act, c.M, c.N, c.K).bytes; }

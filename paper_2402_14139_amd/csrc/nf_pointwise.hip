@@ -296,7 +296,7 @@ int32_t nf_mx_quantise(int32_t dtype, int64_t rows, int64_t cols, const void *x,
                        uint8_t *codes_t, uint8_t *scales_t, void *stream) {
   if (!x || (codes == nullptr) != (scales == nullptr) || (codes_t == nullptr) != (scales_t == nullptr) || (!codes && !codes_t)) return NF_ERR_NULL;
   if (!dtype_ok(dtype) || rows <= 0 || cols <= 0) return NF_ERR_BAD_DESC;
-  if (rows > (1ll << 44) / cols || !mx_quantise_fits(rows, cols)) return NF_ERR_UNSUPPORTED;
+  if (rows > (1ll << 44) / cols || (codes && !codes_t && !mx_quantise_fits(rows, cols, false)) || (codes_t && !mx_quantise_fits(rows, cols, true))) return NF_ERR_UNSUPPORTED;
   if (!all_aligned16(x, codes, scales, codes_t, scales_t)) return NF_ERR_BAD_DESC;
   NF_HIP(launch_mx_quantise(dtype, rows, cols, x, codes, scales, codes_t, scales_t, static_cast<hipStream_t>(stream)));
   return NF_OK;
@@ -341,7 +341,7 @@ int32_t nf_mx_linear_fwd(const nf_linear_desc *d, int64_t M, const void *x, cons
   if (rc) return rc;
   if (!x || !W || !W_scales || !y) return NF_ERR_NULL;
   if (drop && (rc = check_drop(drop))) return rc;
-  if (!mx_quantise_fits(M, d->K)) return NF_ERR_UNSUPPORTED;
+  if (!mx_quantise_fits(M, d->K, false)) return NF_ERR_UNSUPPORTED;
   if (!all_aligned16(x, W, W_scales, b, r, y, z)) return NF_ERR_BAD_DESC;
   if ((rc = check_ws(ws, ws_bytes, mx_linear_workspace_bytes(c)))) return rc;
   NF_HIP(launch_mx_linear(c, x, W, W_scales, b, r, drop_args(drop), y, z, ws, static_cast<hipStream_t>(stream)));

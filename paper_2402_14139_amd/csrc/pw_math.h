@@ -265,7 +265,7 @@ struct MxCall {
   int N;
   long long K;
 };
-bool mx_quantise_fits(long long rows, long long cols);
+bool mx_quantise_fits(long long rows, long long cols, bool by_columns);
 hipError_t launch_mx_quantise(int dtype, long long rows, long long cols, const void *x, void *codes, void *scales, void *codes_t, void *scales_t, hipStream_t st);
 size_t mx_product_workspace_bytes(const MxCall &c);
 size_t mx_linear_workspace_bytes(const MxCall &c);

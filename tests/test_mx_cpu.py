@@ -76,6 +76,8 @@ def test_quantise_refusals(L):
     assert call(dt=3) == call(dt=-1) == call(rows=0) == call(cols=0) == call(rows=-1) == call(cols=-7) == nf.NF_ERR_BAD_DESC
     assert call(rows=1 << 43, cols=3) == call(rows=1, cols=1 << 45) == call(rows=1 << 62, cols=1 << 62) == nf.NF_ERR_UNSUPPORTED
     assert call(rows=1, cols=1 << 40) == nf.NF_ERR_UNSUPPORTED   # more tiles than a grid has
+    # 2^32 groups by rows, 2^24 tiles by columns: more threads than a launch has
+    assert call(rows=1 << 32, cols=1, codes_t=None, scales_t=None) == call(rows=1 << 31, cols=1) == call(rows=1 << 12, cols=1 << 25) == nf.NF_ERR_UNSUPPORTED
 
 
 def test_reference_against_the_caches():
