@@ -86,6 +86,8 @@ class PointwiseBlock:
     ``B`` maps of ``HW`` pixels and ``C`` channels, ``H`` hidden ones.  ``norm``: "group" (of ``groups`` groups, with the activation
     behind it) or "layer"; ``mx``: products on 4-bit operands."""
 
+    kept = True   # no predict() since the last forward()
+
     def __init__(self, dtype, B: int, HW: int, C: int, H: int, groups: int, act=nf.NF_ACT_GELU, p: float = 0.0, seed: int = 0,
                  device="cuda", norm: str = "group", mx: bool = False):
         if norm not in ("group", "layer"):
@@ -177,6 +179,7 @@ class PointwiseBlock:
         self._normalise(x, M, self.h, True)
         self._linear(self.up, M, self.h, "W1", None, d1, self.a, self.z1)
         self._linear(self.down, M, self.a, "W2", x, d2, self.y, None)
+        self.kept = True
         return self.y[:M].view(B, self.HW, self.C)
 
     def backward(self, x, dy, step: int = 0):
@@ -184,6 +187,8 @@ class PointwiseBlock:
         B = x.shape[0]
         self._maps("x", x, B)
         self._maps("dy", dy, B)
+        if not self.kept:
+            raise RuntimeError("backward: predict() has taken the buffers of forward()")
         M, P, g = B * self.HW, self.p32, self.grad
         nf.nf_linear_bwd_epilogue(self.down, M, dy, None, self._drop(1, step), self.dz2, g["b2"], self.ws)
         self._linear_back(self.down, M, self.dz2, self.a, "W2", self.da)
@@ -197,13 +202,15 @@ class PointwiseBlock:
         return self.dx[:M].view(B, self.HW, self.C)
 
     def predict(self, x):
-        """y of rows x [rows, C], up to the block's pixels and down to a single one, from weights in 4 bits; nothing is kept for a backward pass."""
+        """y of rows x [rows, C], up to the block's pixels and down to a single one, from weights in 4 bits; nothing is kept for a backward pass,
+        nor what a forward() before it kept."""
         if self.kind != "layer" or not self.mx:
             raise ValueError("predict: rows by themselves, from weights in 4 bits: the block wants norm='layer' and mx=True")
         rows = x.shape[0]
         if not 1 <= rows <= self.B * self.HW:
             raise ValueError(f"x: {rows} rows; this block's buffers hold 1 to {self.B * self.HW}")
         _check("x", x, TYPES[self.dtype], self.ws.device, rows, self.C)
+        self.kept = False
         self._normalise(x, rows, self.h, False)
         self._linear(self.up, rows, self.h, "W1", None, None, self.a, None)
         self._linear(self.down, rows, self.a, "W2", x, None, self.y, None)

@@ -191,3 +191,13 @@ def test_another_stream_and_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(w + v + y, want)), turn
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 50), (70, 200)])
+@pytest.mark.parametrize("power", [126, -120])
+def test_norms_beyond_fp32(rows, cols, power):
+    """|G| leaves fp32's range where no element does: without eps a power of two changes nothing."""
+    g = torch.randn(rows, cols, generator=torch.Generator().manual_seed(rows)).clamp(-1.9, 1.9)
+    g = torch.where(g.abs() < 2.0 ** -5, 2.0 ** -5, g).bfloat16().float()   # 8 bits each: nothing is lost at 2^-120
+    want, got = (run("f32", [m], ref.MUON, eps=0.0)[0] for m in (g, g * 2.0 ** power))
+    assert torch.isfinite(g * 2.0 ** power).all() and torch.equal(want, got)

@@ -167,6 +167,10 @@ def test_a_row_served_is_a_row_trained():
     blk, x, _ = prepared("f16", 2, 40, 64, 96, mx=True)
     want = blk.forward(x.cuda(), train=False).clone()
     assert torch.equal(blk.predict(x.cuda().view(80, 64)), want.view(80, 64))
+    with pytest.raises(RuntimeError):
+        blk.backward(x.cuda(), x.cuda())
+    blk.forward(x.cuda())
+    blk.backward(x.cuda(), x.cuda())
 
 
 @pytest.mark.parametrize("more", [dict(norm="layer"), dict(norm="layer", muon_lr=0.02), dict(norm="layer", muon_lr=0.02, mx=True, fmt=nf.NF_Q_E2M1),

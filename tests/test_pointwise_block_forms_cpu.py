@@ -40,6 +40,15 @@ def test_training_refuses(no_kernels, why):  # noqa: F811
         serving().backward(torch.zeros(4, 6, 8, dtype=BF16), MAPS[why])
 
 
+def test_no_backward_pass_behind_predict(no_kernels):  # noqa: F811
+    x, b = torch.zeros(4, 6, 8, dtype=BF16), serving(kept=False)
+    with pytest.raises(RuntimeError):
+        b.backward(x, x)
+    b.kept = True
+    with pytest.raises(AttributeError):   # on its way to the kernels, which this block has no buffers for
+        b.backward(x, x)
+
+
 def test_unknown_norm():
     with pytest.raises(ValueError):
         pw.PointwiseBlock(nf.NF_BF16, 1, 1, 8, 8, 1, norm="batch")
