@@ -87,7 +87,8 @@ struct QuantArgs {
   long long cb, sb, cbt, sbt;                    // row strides
 };
 
-// By rows: a group to a thread, whose reads are in flight together.  Memory-bound: sizeof(T) + 1/2 + 1/32 bytes an element.
+// By rows: a group to a thread, whose reads are in flight together.  Memory-bound: sizeof(T) + 1/2 + 1/32 bytes an element.  16384x2048 bf16 19 us from HBM
+// (4.4 TB/s), 14.5 from the last-level cache; by columns 21.6 and 15, both ways 32.5 and 21.8, whose codes are lines of 32 and 64 bytes.
 template <typename T>
 __global__ __launch_bounds__(QT) void mx_rows_kernel(QuantArgs a, const T *__restrict__ x) {
   const long long first = (long long)blockIdx.x * QT, row0 = first / a.groups;
@@ -277,6 +278,9 @@ struct WideSteps {
 
 // A tile of BLOCK x BLOCK by 2 x ACROSS waves; a step is 8 groups of the sum: 128 bytes of codes and 8 of exponents to a row, copied while the step before
 // it is carried out.  A row's chunks of 16 bytes (groups) are exchanged in LDS so that the 16 rows of a fragment's read lie in different banks.
+// Sums of at most 16 groups take steps of 4 in three stages of 17 KB: three workgroups to a CU, which hide each other's first copies and epilogues.
+// 8192x8192x8192 bf16 276 us, 4 PFLOP/s: copies from L2, reads of LDS and matrix instructions take 1.0, 0.8 and 0.9 us of a step's 2.3 in a tile of 256 and
+// overlap in part.  65536x512x2048 110 us, with GELU 133: 3.4 us a tile of 128, of which the results' 32 KB need 1.2 at a fill's 6.9 TB/s.
 template <int BLOCK, int ACROSS, int STEP>
 struct MxTile {
   static constexpr int WAVES = 2 * ACROSS, THREADS = 64 * WAVES, MT = BLOCK / 32, NT = BLOCK / 16 / ACROSS;
@@ -439,7 +443,7 @@ __global__ __launch_bounds__((MxTile<BLOCK, ACROSS, STEP>::THREADS), (MxTile<BLO
 // Few rows: 16 columns and up to 32 rows to a workgroup, whose waves share the sum's axis; fragments come from memory without LDS.  x is quantised on the
 // way where it is not held in 4 bits yet (RAW): a lane's fragment is a group, whose 32 elements it reads and codes by itself.  Up to 8 rows
 // (HALVES) the instruction's 16 x 16 results hold 8 columns of W's first half of groups by x's, and 8 of the second by the second, so
-// that twice as many workgroups share W.
+// that twice as many workgroups share W.  1 row, 2048x2048 bf16 4.1 us: the launch's 2.5, and the time of one chain of reads.
 template <typename T, int MT, int NW, bool HALVES, bool RAW>
 __global__ __launch_bounds__(64 * NW) void mx_few_rows_kernel(MxArgs m) {
   constexpr int ROWS = HALVES ? 8 : 16 * MT, COLS = HALVES ? 8 : 16;

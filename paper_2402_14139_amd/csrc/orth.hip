@@ -308,6 +308,8 @@ __device__ inline void triangle(int t, int &tr, int &tc) {
 // BLOCK x BLOCK results; a step is 32 terms.  While a step's products run, the next one's fragments are read and the
 // copies of the STAGES-th next are on their way: one barrier a step, behind which the next stage is whole and this one free.  Steps go in pairs
 // (two sets of fragments); those beyond the last are copies of nothing, so that the waits count the same.
+// 2048x2048: X' in 256 tiles of 128 48 us, 1070 TFLOP/s of fp16 products (the matrix instructions by themselves 38, copies and reads by themselves 32: they
+// overlap but for a third); A and A^2 in 253 tiles of 96 35 each.  17 matrices of 64x27 to 512x4608: X' 45, which reads and writes 132 MB besides.
 template <int BLOCK, int KIND, typename OUT, bool MUON>
 __global__ __launch_bounds__(Tile<BLOCK>::THREADS) void orth_product_kernel(Args a, const Table *__restrict__ table) {
   using S = Tile<BLOCK>;
@@ -456,8 +458,8 @@ __global__ __launch_bounds__(LT) void orth_parts_kernel(Args a, const Table *__r
 }
 
 // ---- small matrices ----
-// A matrix to a workgroup, all steps in LDS: nothing but barriers between the products of 16 x 16 results, which are shared out among the waves.  16x27 10 us,
-// in the launches above 70 (17 of 4 us each).  Rows are 16 bytes longer than their elements: the 16 that a fragment takes lie in different banks.
+// A matrix to a workgroup, all steps in LDS: nothing but barriers between the products of 16 x 16 results, which are shared out among the waves.  16x27 12 us,
+// in the launches above 70 (17 of 4 us each); 64x200 42, of which each step's barriers and short chains of products take most.  Rows are 16 bytes longer than their elements: the 16 that a fragment takes lie in different banks.
 struct Small {
   float a[NF_ORTH_STEPS], b[NF_ORTH_STEPS], c[NF_ORTH_STEPS];
   float up_x[NF_ORTH_STEPS + 1], up_a[NF_ORTH_STEPS], up_p[NF_ORTH_STEPS];  // 2^s, as Args has them
@@ -677,7 +679,7 @@ Plan plan_of(const nf_orth_desc &d, int count, const int32_t *rows, const int32_
   for (int k = 0; k < count; ++k) large += tiles_of(p.table.it[k].np, 128) * tiles_of(p.table.it[k].mp, 128);
   const Symmetric sym = symmetric_tile(p.table.it, count);
   p.sym = sym.side;
-  p.app = large >= 192 ? 128 : 64;  // the same 17 matrices, 683 tiles of 128: 49 us, of 64 53; 2048x2048, 256 tiles: 48 and 62
+  p.app = large >= 192 ? 128 : 64;  // the same 17 matrices, 683 tiles of 128: 45 us, of 64 51; 2048x2048, 256 tiles: 48 and 62
   int most = 0, tiles = 0;
   for (int k = 0; k < count; ++k) most = std::max(most, p.table.it[k].np <= 64 ? small_bytes(p.table.it[k]) : MANY_LDS + 1), tiles = std::max(tiles, p.table.it[k].np / 16 * (p.table.it[k].mp / 16));
   p.small = most <= FEW_LDS && tiles <= 16 ? 4 : most <= MANY_LDS ? 16 : 0;
