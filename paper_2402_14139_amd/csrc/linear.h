@@ -31,9 +31,10 @@ struct GemmArgs {
   Epilogue e;
 };
 
-// 8 neighbouring results of a row through the forward's epilogue; s holds the residual
+// 8 neighbouring results of a row through the forward's epilogue; s holds the residual as it lies.  What a launch does not ask for is branched over:
+// left to itself the compiler carries out both sides and chooses, 4 instructions an element, where GELU and all else take 27.
 template <typename T>
-__device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int C, const float (&bias)[8], const float (&s)[8], float (&v)[8]) {
+__device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int C, const float (&bias)[8], const Raw8<T> &s, float (&v)[8]) {
   const int n = C - col;
   const long long at = row * C + col;
 #pragma unroll
@@ -41,16 +42,26 @@ __device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int
   if (e.z) store8((T *)e.z + at, v, n);
   act_of<T>(e.act, v);
   drop8(e.drop, (unsigned long long)row * (unsigned)((C + 7) >> 3) + (unsigned)(col >> 3), v);
+  if (e.res) {
+    asm volatile("");
+    float r[8];
+    unpack8(s, r);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = e.res ? fmaf(v[i], e.drop.scale, s[i]) : v[i] * e.drop.scale;
+    for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], e.drop.scale, r[i]);
+  } else if (e.drop.T) {  // else the scale is 1
+    asm volatile("");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= e.drop.scale;
+  }
   store8((T *)e.out + at, v, n);
 }
 template <typename T>
 __device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int C, float (&v)[8]) {
-  float s[8], bias[8];
+  float bias[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) bias[i] = s[i] = 0.f;
-  if (e.res) load8((const T *)e.res + row * C + col, s, C - col);
+  for (int i = 0; i < 8; ++i) bias[i] = 0.f;
+  Raw8<T> s = {};
+  if (e.res) s = raw8((const T *)e.res + row * C + col, C - col);
   if (e.bias) load8(e.bias + col, bias, C - col);
   finish_fwd<T>(e, row, col, C, bias, s, v);
 }
@@ -150,10 +161,13 @@ __device__ inline void write_fwd(const GemmArgs &g, long long r0, int c0, int la
           lds[r * CH + (c ^ (r & (CH - 1) & 15))] = acc[from + i][j];
         }
     };
-    if (h == 0)
+    if (h == 0) {
       put(0);
-    else
+      asm volatile("; the first rows" ::: "memory");  // else both halves' writes become one, with a choice of every sum
+    } else {
       put(MT - HALF);
+      asm volatile("; the others" ::: "memory");
+    }
 #pragma unroll 1
     for (int k0 = 0; k0 < TURNS; k0 += AHEAD) {
       Raw8<T> now[AHEAD];
@@ -170,11 +184,10 @@ __device__ inline void write_fwd(const GemmArgs &g, long long r0, int c0, int la
         const floatx4 lo = lds[r * CH + ((2 * c8) ^ (r & (CH - 1) & 15))], hi = lds[r * CH + ((2 * c8 + 1) ^ (r & (CH - 1) & 15))];
         const long long row = first + u * DOWN;
         if (row >= g.R || n <= 0) continue;
-        float v[8], s[8];
-        unpack8(now[u], s);
+        float v[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = lo[e], v[e + 4] = hi[e];
-        finish_fwd<T>(g.e, row, col, g.C, bias, s, v);
+        finish_fwd<T>(g.e, row, col, g.C, bias, now[u], v);
       }
     }
   }

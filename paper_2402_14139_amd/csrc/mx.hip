@@ -582,8 +582,8 @@ hipError_t product_as(const MxCall &c, const void *raw, const MxRows &a, const M
       go(integral_constant<int, 256>(), I4(), I8());
     else if (p.tile == 64)
       go(integral_constant<int, 64>(), I2(), I8());
-    else if (g.L <= 2 * STEP)
-      go(integral_constant<int, 128>(), I2(), I4());
+    else if (sizeof(T) == 2 && g.L <= 2 * STEP)  // fp32 results' epilogue wants more registers than three workgroups leave
+      go(integral_constant<int, 128>(), I2(), integral_constant<int, sizeof(T) == 2 ? 4 : 8>());
     else if (g.L >= 8 * STEP)
       go(integral_constant<int, 128>(), I2(), I8());
     else
