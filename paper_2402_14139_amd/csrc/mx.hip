@@ -280,7 +280,8 @@ struct WideSteps {
 // it is carried out.  A row's chunks of 16 bytes (groups) are exchanged in LDS so that the 16 rows of a fragment's read lie in different banks.
 // Sums of at most 16 groups take steps of 4 in three stages of 17 KB: three workgroups to a CU, which hide each other's first copies and epilogues.
 // 8192x8192x8192 bf16 276 us, 4 PFLOP/s: copies from L2, reads of LDS and matrix instructions take 1.0, 0.8 and 0.9 us of a step's 2.3 in a tile of 256 and
-// overlap in part.  65536x512x2048 110 us, with GELU 133: 3.4 us a tile of 128, of which the results' 32 KB need 1.2 at a fill's 6.9 TB/s.
+// overlap in part.  65536x512x2048 108 us, with GELU 123: 3.4 us a tile of 128, of which the results' 32 KB need 1.2 at a fill's 6.9 TB/s;
+// its vector instructions, 24 an element with GELU, 2.8.
 template <int BLOCK, int ACROSS, int STEP>
 struct MxTile {
   static constexpr int WAVES = 2 * ACROSS, THREADS = 64 * WAVES, MT = BLOCK / 32, NT = BLOCK / 16 / ACROSS;
@@ -436,7 +437,7 @@ __global__ __launch_bounds__((MxTile<BLOCK, ACROSS, STEP>::THREADS), (MxTile<BLO
   } else {
     wait_lds();
     barrier();
-    write_fwd<T, false, S::SUMS>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * S::SUMS * NT * 64);
+    write_fwd<T, false, S::SUMS, true>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * S::SUMS * NT * 64);
   }
 }
 
@@ -507,7 +508,7 @@ __global__ __launch_bounds__(64 * NW) void mx_few_rows_kernel(MxArgs m) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += lo2[e], v[e + 4] += hi2[e];
     }
-    finish_fwd<T>(g.e, r, col, g.C, v);
+    finish_fwd<T, true>(g.e, r, col, g.C, v);
   }
 }
 
@@ -521,7 +522,7 @@ struct MxPlan {
 };
 // Tiles of 256 or 128 by rounds over the workgroups that run together (one to a CU and two, three where sums are short) and a round's time: steps, then
 // what ends a tile, with no other workgroup's steps beside it in a CU that holds one (us, in tiles of 256 and of 128: 8192x8192x8192 bf16 276 and 389,
-// 16384x2048x2048 48 and 57, 16384x1500x2048 with GELU 60 and 55, 65536x512x2048 131 and 110, with GELU 167 and 132, fp32 results
+// 16384x2048x2048 48 and 57, 16384x1500x2048 with GELU 60 and 55, 65536x512x2048 131 and 108, with GELU 167 and 123, fp32 results
 // 147 and 215).  Few tiles of 128 become tiles of 64 or parts of sums: towards 512 workgroups, four steps each at least.
 MxPlan mx_plan(int dtype, int act, long long M, int N, long long K) {
   MxPlan p = {0, 1, 0, 0};
@@ -592,7 +593,7 @@ hipError_t product_as(const MxCall &c, const void *raw, const MxRows &a, const M
   if (err != hipSuccess || p.splits == 1) return err;
   const FinishArgs f = finish_args(p.splits, g);
   return recorded(st, "mx_product_finish", 0.0, 4.0 * p.splits * c.M * c.N + ends,
-                  [&] { hipLaunchKernelGGL(fwd_finish_kernel<T>, dim3(finish_blocks(f)), dim3(LT), 0, st, f); });
+                  [&] { hipLaunchKernelGGL((fwd_finish_kernel<T, true>), dim3(finish_blocks(f)), dim3(LT), 0, st, f); });
 }
 
 template <typename T>

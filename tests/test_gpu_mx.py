@@ -276,3 +276,27 @@ def test_another_stream_and_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), turn
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("M,K", [(1, 32), (40, 32), (40, 2100)])
+def test_activations_along_the_line(t, act, M, K):
+    """Sums of nothing but a bias: every size of number, and the limits, in each kernel that has an epilogue."""
+    line = torch.cat([torch.linspace(-12, 12, 3001), torch.linspace(-0.01, 0.01, 500), torch.logspace(-30, 30, 121), -torch.logspace(-30, 30, 121),
+                      torch.tensor([float("inf"), -float("inf"), float("nan"), 0.0, -0.0, 4.5, -4.5, 4.4999, -4.4999])])
+    N = line.numel()
+    a, b = (tuple(torch.zeros(r, s, dtype=torch.uint8, device="cuda") for s in strides(K)) for r in (M, N))
+    d = nf.LinearDesc(dtype=DT[t], K=K, N=N, act=ACTS.index(act))
+    y = Out(M, N, dtype=TYPES[t])
+    nf.nf_mx_product(d, M, *a, *b, line.cuda(), None, y.t, workspace(nf.nf_mx_product_workspace_bytes(d, M)))
+    got, z = y.cpu(), line.double()
+    assert torch.equal(got.isnan(), z.isnan().expand(M, N))
+    want = {"none": z, "relu": z.clamp(min=0), "silu": z * torch.sigmoid(z), "gelu": 0.5 * z * torch.special.erfc(-z * 0.5 ** 0.5)}[act]
+    want = torch.where(z == -float("inf"), -float("inf") if act == "none" else 0.0, want)
+    big = torch.finfo(TYPES[t]).max
+    fits = z.isfinite() & (want.abs() < big * (1 - HALF[t]))
+    assert torch.equal(got[:, ~z.isnan() & ~fits].abs() >= big, (want[~z.isnan() & ~fits].abs() >= big).expand(M, -1))
+    want, z = want[fits], z[fits]
+    tol = (FUNC if act in ("silu", "gelu") else 0.0) * z.abs() + (HALF[t] + 2 * SUM) * want.abs() + TINY[t]
+    assert ((got[:, fits] - want).abs() <= tol).all(), (got[:, fits] - want).abs().max()
