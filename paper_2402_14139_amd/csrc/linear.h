@@ -147,8 +147,11 @@ __device__ inline void write_fwd(const GemmArgs &g, long long r0, int c0, int la
   };
   constexpr int AHEAD = TURNS < 4 ? TURNS : 4;  // turns whose residuals are in flight while as many are finished
   Raw8<T> next[AHEAD];
+  constexpr bool ALWAYS = sizeof(T) == 4;  // a branch over both costs fp32 results of a tile of 256 registers that they do not have
+  if (ALWAYS || g.e.res) {
 #pragma unroll
-  for (int u = 0; u < AHEAD; ++u) next[u] = fetch(r0 + rr + u * DOWN);
+    for (int u = 0; u < AHEAD; ++u) next[u] = fetch(r0 + rr + u * DOWN);
+  }
 #pragma unroll 1
   for (int h = 0; h < MT / HALF; ++h) {
     auto put = [&](int from) {
@@ -171,12 +174,15 @@ __device__ inline void write_fwd(const GemmArgs &g, long long r0, int c0, int la
 #pragma unroll 1
     for (int k0 = 0; k0 < TURNS; k0 += AHEAD) {
       Raw8<T> now[AHEAD];
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) now[u] = next[u];
       const long long first = r0 + rr + (h * TURNS + k0) * DOWN;  // turns run on through both halves
-      if (h * TURNS + k0 + AHEAD < MT / HALF * TURNS) {
+      if (ALWAYS || g.e.res) {
+        if (!ALWAYS) asm volatile("");
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) next[u] = fetch(first + (AHEAD + u) * DOWN);
+        for (int u = 0; u < AHEAD; ++u) now[u] = next[u];
+        if (h * TURNS + k0 + AHEAD < MT / HALF * TURNS) {
+#pragma unroll
+          for (int u = 0; u < AHEAD; ++u) next[u] = fetch(first + (AHEAD + u) * DOWN);
+        }
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
