@@ -210,6 +210,8 @@ class PointwiseBlock:
         if not 1 <= rows <= self.B * self.HW:
             raise ValueError(f"x: {rows} rows; this block's buffers hold 1 to {self.B * self.HW}")
         _check("x", x, TYPES[self.dtype], self.ws.device, rows, self.C)
+        if x.untyped_storage().data_ptr() == self.y.untyped_storage().data_ptr():
+            raise ValueError("x: this block's own results, whose place the new ones take; clone them")
         self.kept = False
         self._normalise(x, rows, self.h, False)
         self._linear(self.up, rows, self.h, "W1", None, None, self.a, None)

@@ -162,6 +162,14 @@ def test_serving(t, rows):
     check_product("y", t, y, four(blk.a[:rows]), four(blk.p32["W2"]), P["b2"], x.double().cpu())
 
 
+def test_serving_its_own_results():
+    blk, x, _ = prepared("bf16", 1, 40, 64, 96, mx=True)
+    y = blk.predict(x.cuda().view(40, 64))
+    with pytest.raises(ValueError):
+        blk.predict(y[:3])
+    assert torch.isfinite(blk.predict(y[:3].clone())).all()
+
+
 def test_a_row_served_is_a_row_trained():
     """What is kept for the gradients changes no bit."""
     blk, x, _ = prepared("f16", 2, 40, 64, 96, mx=True)
