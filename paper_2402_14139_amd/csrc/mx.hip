@@ -114,8 +114,8 @@ __global__ __launch_bounds__(QT) void mx_rows_kernel(QuantArgs a, const T *__res
 constexpr int TR = 128, TC = 64;
 template <typename T, bool BY_ROWS>
 __global__ __launch_bounds__(QT) void mx_columns_kernel(QuantArgs a, const T *__restrict__ x) {
-  constexpr int LD = TC + 4 / sizeof(T);
-  __shared__ T lds[TR * LD];
+  constexpr int LD = TC + 4 / sizeof(T), BAND = 32 * LD + 16;  // 32 rows; the four that a wave reads from lie in different banks
+  __shared__ T lds[TR / 32 * BAND];
   const long long tr = blockIdx.x / a.tiles_c, r0 = tr * TR, c0 = (blockIdx.x - tr * a.tiles_c) * TC;
   const int j = threadIdx.x & 7, down = threadIdx.x >> 3;
   const long long col = c0 + 8 * j;
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(QT) void mx_columns_kernel(QuantArgs a, const T *__
   }
 #pragma unroll
   for (int k = 0; k < TR / 32; ++k) {
-    __builtin_memcpy(&lds[(k * 32 + down) * LD + 8 * j], &raw[k], sizeof(raw[k]));
+    __builtin_memcpy(&lds[k * BAND + down * LD + 8 * j], &raw[k], sizeof(raw[k]));
     if constexpr (BY_ROWS) {
       const long long row = r0 + k * 32 + down;
       uint32_t m = most(0u, raw[k]);
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(QT) void mx_columns_kernel(QuantArgs a, const T *__
   for (int h = 0; h < 4; ++h) {
     T t[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = lds[(k * 32 + 8 * h + e) * LD + c];
+    for (int e = 0; e < 8; ++e) t[e] = lds[k * BAND + (8 * h + e) * LD + c];
     __builtin_memcpy(&r[h], t, sizeof(t));
   }
   uintx4 codes;
