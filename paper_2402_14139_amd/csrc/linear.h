@@ -33,14 +33,14 @@ struct GemmArgs {
 
 // 8 neighbouring results of a row through the forward's epilogue; s holds the residual as it lies.  What a launch does not ask for is branched over:
 // left to itself the compiler carries out both sides and chooses, 4 instructions an element, where GELU and all else take 27.
-template <typename T, bool SHORT>
+template <typename T>
 __device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int C, const float (&bias)[8], const Raw8<T> &s, float (&v)[8]) {
   const int n = C - col;
   const long long at = row * C + col;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] += bias[i];
   if (e.z) store8((T *)e.z + at, v, n);
-  act_of<T, SHORT>(e.act, v);
+  act_of<T>(e.act, v);
   drop8(e.drop, (unsigned long long)row * (unsigned)((C + 7) >> 3) + (unsigned)(col >> 3), v);
   if (e.res) {
     asm volatile("");
@@ -55,7 +55,7 @@ __device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int
   }
   store8((T *)e.out + at, v, n);
 }
-template <typename T, bool SHORT = false>
+template <typename T>
 __device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int C, float (&v)[8]) {
   float bias[8];
 #pragma unroll
@@ -63,7 +63,7 @@ __device__ inline void finish_fwd(const Epilogue &e, long long row, int col, int
   Raw8<T> s = {};
   if (e.res) s = raw8((const T *)e.res + row * C + col, C - col);
   if (e.bias) load8(e.bias + col, bias, C - col);
-  finish_fwd<T, SHORT>(e, row, col, C, bias, s, v);
+  finish_fwd<T>(e, row, col, C, bias, s, v);
 }
 
 constexpr uint32_t OUTSIDE = 0xF0000000u;  // beyond every buffer's end: reads as zeros
@@ -132,7 +132,7 @@ __device__ inline void write_sums(const GemmArgs &g, int split, long long r0, in
 // The forward's go through LDS that only this wave uses, all rows or half of them at a time (HALF fragments): its epilogue is a loop, not a copy of its code to every
 // fragment (80 KB of instructions, more than their cache holds), and a lane has 8 neighbours of a row: 16-byte accesses of 16 bits,
 // whole lines, and one Philox call.  lds: 16 rows x NT fragments x 1 KB per 16 rows; chunk c of row r at c ^ (r & 15).
-template <typename T, bool KEPT, int HALF, bool SHORT = false, int MT, int NT>
+template <typename T, bool KEPT, int HALF, int MT, int NT>
 __device__ inline void write_fwd(const GemmArgs &g, long long r0, int c0, int lane, floatx4 (&acc)[MT][NT], floatx4 *lds) {
   constexpr int CH = 4 * NT, ACROSS = 2 * NT, DOWN = 64 / ACROSS, TURNS = 16 * HALF / DOWN;
   const int c8 = lane % ACROSS, rr = lane / ACROSS, col = c0 + 8 * c8, n = g.C - col;
@@ -193,7 +193,7 @@ __device__ inline void write_fwd(const GemmArgs &g, long long r0, int c0, int la
         float v[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = lo[e], v[e + 4] = hi[e];
-        finish_fwd<T, SHORT>(g.e, row, col, g.C, bias, now[u], v);
+        finish_fwd<T>(g.e, row, col, g.C, bias, now[u], v);
       }
     }
   }
@@ -207,7 +207,7 @@ struct FinishArgs {
   long long R;
   Epilogue e;
 };
-template <typename T, typename OUT, bool FWD, bool SHORT = false>
+template <typename T, typename OUT, bool FWD>
 __device__ inline void gemm_finish(const FinishArgs &f, long long block, float *lds) {
   const int items = f.lanes == 1 ? LT : f.lanes == 4 ? LT / 4 : LT / 16;
   const int groups = (f.C + 7) / 8, k = threadIdx.x & (items - 1), zl = f.lanes == 1 ? 0 : threadIdx.x / (f.lanes == 4 ? LT / 4 : LT / 16);
@@ -238,15 +238,15 @@ __device__ inline void gemm_finish(const FinishArgs &f, long long block, float *
   }
   if (!live) return;
   if constexpr (FWD) {
-    finish_fwd<T, SHORT>(f.e, row, col, f.C, v);
+    finish_fwd<T>(f.e, row, col, f.C, v);
   } else {
     store8((OUT *)f.e.out + row * f.C + col, v, f.C - col);
   }
 }
-template <typename T, bool SHORT = false>
+template <typename T>
 __global__ __launch_bounds__(LT) void fwd_finish_kernel(FinishArgs f) {
   __shared__ float lds[LT * 9];
-  gemm_finish<T, T, true, SHORT>(f, blockIdx.x, lds);
+  gemm_finish<T, T, true>(f, blockIdx.x, lds);
 }
 inline FinishArgs finish_args(int splits, const GemmArgs &g) {
   FinishArgs f = {g.part, splits, g.C, 1, g.R, g.e};

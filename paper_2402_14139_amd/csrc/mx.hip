@@ -437,7 +437,7 @@ __global__ __launch_bounds__((MxTile<BLOCK, ACROSS, STEP>::THREADS), (MxTile<BLO
   } else {
     wait_lds();
     barrier();
-    write_fwd<T, false, S::SUMS, true>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * S::SUMS * NT * 64);
+    write_fwd<T, false, S::SUMS>(g, r0 + wm, c0 + wn, lane, acc, reinterpret_cast<floatx4 *>(lds) + wave * S::SUMS * NT * 64);
   }
 }
 
@@ -508,7 +508,7 @@ __global__ __launch_bounds__(64 * NW) void mx_few_rows_kernel(MxArgs m) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += lo2[e], v[e + 4] += hi2[e];
     }
-    finish_fwd<T, true>(g.e, r, col, g.C, v);
+    finish_fwd<T>(g.e, r, col, g.C, v);
   }
 }
 
@@ -593,7 +593,7 @@ hipError_t product_as(const MxCall &c, const void *raw, const MxRows &a, const M
   if (err != hipSuccess || p.splits == 1) return err;
   const FinishArgs f = finish_args(p.splits, g);
   return recorded(st, "mx_product_finish", 0.0, 4.0 * p.splits * c.M * c.N + ends,
-                  [&] { hipLaunchKernelGGL((fwd_finish_kernel<T, true>), dim3(finish_blocks(f)), dim3(LT), 0, st, f); });
+                  [&] { hipLaunchKernelGGL(fwd_finish_kernel<T>, dim3(finish_blocks(f)), dim3(LT), 0, st, f); });
 }
 
 template <typename T>

@@ -128,31 +128,9 @@ __device__ inline float normal_tail(float z, float &bell, float &t) {
 __device__ float mul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
 __device__ inline float fading(float v, float f) { return mul_legacy(v, f); }
 
-// GELU of 16 bits without exponential and reciprocal, whose time is four instructions' each: 14 instructions for 13 and two of those, 56 cycles for 84.
-// Phi(z) = 1/2 + z R(w), w = 2 z^2 / 4.5^2 - 1, |z| <= 4.5, R of degree 9 a minimax fit that passes 0 and 1 at the ends and is cut off there: off by 4.3e-6 in
-// fp32, which is absolute (normal_tail's 2e-6 are relative: small results at z < -3 keep fewer digits here).  A NaN is clamped to -4.5 as -z, so that its
-// Phi is 1 and it stays one; an infinity gives the limit.
-__device__ inline float gelu_short(float z) {
-  const float m = __builtin_amdgcn_fmed3f(-z, -4.5f, 4.5f), w = fmaf(m * m, 0.098765432098765432f, -1.f);
-  float R = -0.0018062586f;
-  R = fmaf(R, w, 0.0049646627f);
-  R = fmaf(R, w, -0.006323096f);
-  R = fmaf(R, w, 0.009647942f);
-  R = fmaf(R, w, -0.018315192f);
-  R = fmaf(R, w, 0.02886155f);
-  R = fmaf(R, w, -0.040277842f);
-  R = fmaf(R, w, 0.05463665f);
-  R = fmaf(R, w, -0.077183284f);
-  R = fmaf(R, w, 0.15690607f);
-  float phi;
-  asm("v_fma_f32 %0, -%1, %2, 0.5 clamp" : "=v"(phi) : "v"(m), "v"(R));  // clamp: to 0 ... 1
-  return fading(z, phi);
-}
-
 // The activation of N values, and its slope at them (times what s holds).  The activation is the same for a whole launch: one
 // branch to a vector, not to an element.
-// SHORT: GELU as above where results are 16 bits.
-template <typename T, bool SHORT = false, int N>
+template <typename T, int N>
 __device__ inline void act_of(int act, float (&v)[N]) {
   if (act == NF_ACT_RELU) {
 #pragma unroll
@@ -160,9 +138,6 @@ __device__ inline void act_of(int act, float (&v)[N]) {
   } else if (act == NF_ACT_SILU) {
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = fading(v[e], recip<T>(1.f + exp_of<T>(-v[e])));
-  } else if (act == NF_ACT_GELU && SHORT && sizeof(T) == 2) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = gelu_short(v[e]);
   } else if (act == NF_ACT_GELU) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {  // v Phi(v) = max(v, 0) - |v| Q(|v|); a NaN stays one through Q
