@@ -51,10 +51,12 @@ class QuantisedCache:
                           x_out, labels_out)
 
 
-def workspace_bytes(norm, up, down, B: int) -> int:
-    """Bytes for batches of 1 to ``B`` maps: fewer rows are cut into other parts and may want more than many do."""
-    return max(max(nf.nf_groupnorm_workspace_bytes(norm, b), *(nf.nf_linear_workspace_bytes(d, b * norm.HW) for d in (up, down)))
-               for b in range(1, B + 1))
+def workspace_bytes(norm, up, down, B: int, HW: int = 0) -> int:
+    """Bytes for batches of 1 to ``B`` maps of ``HW`` pixels (a group norm's own): fewer rows are cut into other parts and may want more than many do."""
+    group = isinstance(norm, nf.GroupNormDesc)
+    HW = norm.HW if group else HW
+    sums = lambda b: nf.nf_groupnorm_workspace_bytes(norm, b) if group else nf.nf_layernorm_workspace_bytes(norm, b * HW)  # noqa: E731
+    return max(max(sums(b), *(nf.nf_linear_workspace_bytes(d, b * HW) for d in (up, down))) for b in range(1, B + 1))
 
 
 class Rows4:
@@ -95,10 +97,12 @@ class PointwiseBlock:
         if not torch.cuda.is_available():
             raise RuntimeError("PointwiseBlock needs a GPU: the library has no CPU path")
         self.kind, self.mx = norm, mx
-        groups = groups if norm == "group" else 1
         self.dtype, self.B, self.HW, self.C, self.H, self.p, self.seed = dtype, B, HW, C, H, p, seed
         T = TYPES[dtype]
-        self.norm = nf.GroupNormDesc(dtype=dtype, C=C, G=groups, act=act, HW=HW, eps=1e-5)
+        if norm == "group":
+            self.norm = nf.GroupNormDesc(dtype=dtype, C=C, G=groups, act=act, HW=HW, eps=1e-5)
+        else:
+            self.ln = nf.LayerNormDesc(dtype=dtype, C=C, eps=1e-5)
         self.up = nf.LinearDesc(dtype=dtype, K=C, N=H, act=act)
         self.down = nf.LinearDesc(dtype=dtype, K=H, N=C, act=nf.NF_ACT_NONE)
         g = torch.Generator().manual_seed(seed)
@@ -113,10 +117,7 @@ class PointwiseBlock:
         self.dz2, self.da, self.dh, self.dx = new(M, C), new(M, H), new(M, C), new(M, C)
         stats = (B, groups) if norm == "group" else (M,)
         self.mean, self.rstd = new(*stats, d=torch.float32), new(*stats, d=torch.float32)
-        room = workspace_bytes(self.norm, self.up, self.down, B)
-        if norm == "layer":
-            self.ln = nf.LayerNormDesc(dtype=dtype, C=C, eps=1e-5)
-            room = max(room, *(nf.nf_layernorm_workspace_bytes(self.ln, b * HW) for b in range(1, B + 1)))
+        room = workspace_bytes(self.norm if norm == "group" else self.ln, self.up, self.down, B, HW)
         self.orth = nf.orth_desc(MUON_STEPS)
         self.v = [torch.zeros_like(self.p32[k]) for k in ("W1", "W2")]   # muon()'s momentum
         room = max(room, nf.nf_orthogonalise_workspace_bytes(self.orth, [(H, C), (C, H)]))
