@@ -89,6 +89,8 @@ class PointwiseBlock:
     behind it) or "layer"; ``mx``: products on 4-bit operands."""
 
     kept = True   # no predict() since the last forward()
+    v = muon_ws = None   # muon()'s momentum and workspace, from its first call on
+    captured = False   # that call was recorded into a graph
 
     def __init__(self, dtype, B: int, HW: int, C: int, H: int, groups: int, act=nf.NF_ACT_GELU, p: float = 0.0, seed: int = 0,
                  device="cuda", norm: str = "group", mx: bool = False):
@@ -119,8 +121,7 @@ class PointwiseBlock:
         self.mean, self.rstd = new(*stats, d=torch.float32), new(*stats, d=torch.float32)
         room = workspace_bytes(self.norm if norm == "group" else self.ln, self.up, self.down, B, HW)
         self.orth = nf.orth_desc(MUON_STEPS)
-        self.v = [torch.zeros_like(self.p32[k]) for k in ("W1", "W2")]   # muon()'s momentum
-        room = max(room, nf.nf_orthogonalise_workspace_bytes(self.orth, [(H, C), (C, H)]))
+        self.unmoved = torch.ones((), dtype=torch.bool, device=device)   # no update has run on momentum that was made in a capture
         if mx:
             room = max(room, mx_workspace_bytes(self.up, self.down, B, HW))
             # gradients by rows and by columns, a layer's input by columns: the wider layer's size
@@ -230,11 +231,28 @@ class PointwiseBlock:
         nf.nf_sgd_update(lr, 0.0, [self.p32[k] for k in names], [self.grad[k] for k in names], None)
         self._renew()
 
+    def prepare_muon(self):
+        """Momentum and workspace for muon(), whose first call does it by itself; a block that is updated otherwise goes without."""
+        if self.v is not None:
+            return
+        weights = [self.p32[k] for k in ("W1", "W2")]
+        room = nf.nf_orthogonalise_workspace_bytes(self.orth, [w.shape for w in weights])
+        self.captured = self.ws.is_cuda and torch.cuda.is_current_stream_capturing()
+        self.muon_ws = torch.empty(room, dtype=torch.uint8, device=self.ws.device)
+        # zeros written in a capture would be written by every replay
+        self.v = [torch.empty_like(w) if self.captured else torch.zeros_like(w) for w in weights]
+
     def muon(self, lr: float, sgd_lr: float, momentum: float = 0.95, weight_decay: float = 0.0):
-        """The weights' update made orthogonal, with its momentum; the other parameters' by SGD at ``sgd_lr``."""
+        """The weights' update made orthogonal, with its momentum; the other parameters' by SGD at ``sgd_lr``.  Where the first call is recorded into a
+        graph, updates clear the momentum unless one has run, a pass over it more: prepare_muon() before the capture spares that."""
+        self.prepare_muon()
         names, others = ("W1", "W2"), [k for k in self.p32 if k not in ("W1", "W2")]
         d = nf.MuonDesc(lr=lr, momentum=momentum, weight_decay=weight_decay, nesterov=1, orth=self.orth)
-        nf.nf_muon_update(d, [self.p32[k] for k in names], [self.grad[k] for k in names], self.v, self.ws)
+        if self.captured:
+            for v in self.v:
+                v.masked_fill_(self.unmoved, 0.0)
+            self.unmoved.fill_(False)
+        nf.nf_muon_update(d, [self.p32[k] for k in names], [self.grad[k] for k in names], self.v, self.muon_ws)
         nf.nf_sgd_update(sgd_lr, 0.0, [self.p32[k] for k in others], [self.grad[k] for k in others], None)
         self._renew()
 

@@ -22,3 +22,32 @@ def test_layer_norms_own_limits(on_host, B, HW, C, H):
     assert block.ws.numel() >= need
     with pytest.raises(nf.NfError):
         on_host(nf.NF_BF16, B, HW, C, H, 1)
+
+
+@pytest.mark.parametrize("more", [dict(), dict(norm="layer")])
+def test_a_block_without_orthogonal_updates_has_no_room_for_them(on_host, monkeypatch, more):
+    """Neither their workspace nor the momentum, nor their limits: only muon() asks."""
+    C, H, B, HW = 256, 1024, 2, 8
+    orth = nf.nf_orthogonalise_workspace_bytes(nf.orth_desc(pw.MUON_STEPS), [(H, C), (C, H)])
+
+    def refuses(*a):
+        raise nf.NfError(nf.NF_ERR_UNSUPPORTED, "nf_orthogonalise_workspace_bytes")
+
+    monkeypatch.setattr(nf, "nf_orthogonalise_workspace_bytes", refuses)
+    block = on_host(nf.NF_BF16, B, HW, C, H, 8, **more)
+    need = pw.workspace_bytes(block.ln if more else block.norm, block.up, block.down, B, HW)
+    assert block.ws.numel() == max(need, 1) < orth and block.v is None
+    with pytest.raises(nf.NfError):
+        block.muon(0.1, 0.1)
+    assert block.v is None   # a second call asks again
+
+
+def test_momentum_is_made_once(on_host):
+    block = on_host(nf.NF_BF16, 2, 8, 64, 128, 8)
+    block.prepare_muon()
+    v, ws = block.v, block.muon_ws
+    assert [t.shape for t in v] == [(128, 64), (64, 128)] and not any(t.any() for t in v)
+    assert ws.numel() == nf.nf_orthogonalise_workspace_bytes(block.orth, [(128, 64), (64, 128)])
+    with pytest.raises(AssertionError):   # on its way to the kernels
+        block.muon(0.1, 0.1)
+    assert block.v is v and block.muon_ws is ws
