@@ -88,7 +88,7 @@ class PointwiseBlock:
     ``B`` maps of ``HW`` pixels and ``C`` channels, ``H`` hidden ones.  ``norm``: "group" (of ``groups`` groups, with the activation
     behind it) or "layer"; ``mx``: products on 4-bit operands."""
 
-    kept = True   # no predict() since the last forward()
+    kept = False   # the buffers hold what backward() reads: from forward() to the next predict() or backward()
     v = muon_ws = None   # muon()'s momentum and workspace, from its first call on
     captured = False   # that call was recorded into a graph
 
@@ -185,15 +185,16 @@ class PointwiseBlock:
         return self.y[:M].view(B, self.HW, self.C)
 
     def backward(self, x, dy, step: int = 0):
-        """Gradients of the parameters (``grad``) and of x but for the residual's part, which is dy itself."""
+        """Gradients of the parameters (``grad``) and of x but for the residual's part, which is dy itself; once for every forward()."""
         B = x.shape[0]
         self._maps("x", x, B)
         self._maps("dy", dy, B)
         if not self.kept:
-            raise RuntimeError("backward: predict() has taken the buffers of forward()")
+            raise RuntimeError("backward: no forward() before it, or its buffers taken since by predict() or another backward()")
         M, P, g = B * self.HW, self.p32, self.grad
         nf.nf_linear_bwd_epilogue(self.down, M, dy, None, self._drop(1, step), self.dz2, g["b2"], self.ws)
         self._linear_back(self.down, M, self.dz2, self.a, "W2", self.da)
+        self.kept = False
         nf.nf_linear_bwd_epilogue(self.up, M, self.da, self.z1, self._drop(0, step), self.a, g["b1"], self.ws)  # a is not needed again
         self._linear_back(self.up, M, self.a, self.h, "W1", self.dh)
         if self.kind == "group":

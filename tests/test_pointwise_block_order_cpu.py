@@ -1,0 +1,34 @@
+"""In which order a pointwise block's calls may come, and on what, without a GPU: its bookkeeping on host memory, with kernels that do nothing."""
+import pytest
+import torch
+
+from paper_2402_14139_amd import binding as nf
+from paper_2402_14139_amd import pointwise as pw
+
+FORMS = [dict(), dict(norm="layer"), dict(norm="layer", mx=True), dict(mx=True)]
+B, HW, C, H = 3, 4, 16, 24
+
+
+@pytest.fixture
+def idle(monkeypatch):
+    for name in nf.EXPORTS:
+        if not name.endswith("_bytes"):
+            monkeypatch.setattr(nf, name, lambda *a, **k: None, raising=False)
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    return lambda **k: pw.PointwiseBlock(nf.NF_BF16, B, HW, C, H, 2, device="cpu", **k)
+
+
+def maps():
+    return torch.zeros(B, HW, C, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("more", FORMS)
+def test_one_backward_pass_for_a_forward_pass(idle, more):
+    block = idle(**more)
+    with pytest.raises(RuntimeError):   # uninitialised buffers
+        block.backward(maps(), maps())
+    for _ in range(2):
+        block.forward(maps())
+        block.backward(maps(), maps())
+        with pytest.raises(RuntimeError):   # the second layer's input is gone: dW2 would be wrong
+            block.backward(maps(), maps())
