@@ -138,6 +138,10 @@ class PointwiseBlock:
             raise ValueError(f"{name}: a batch of {B}; this block's buffers hold 1 to {self.B}")
         _check(name, t, TYPES[self.dtype], self.ws.device, B, self.HW * self.C)
 
+    def _not_own(self, x):
+        if x.untyped_storage().data_ptr() == self.y.untyped_storage().data_ptr():
+            raise ValueError("x: this block's own results, whose place the new ones take; clone them")
+
     def _drop(self, which: int, step: int):
         return nf.DropoutDesc(p=self.p, seed=self.seed * 2 + which, step=step) if self.p else None
 
@@ -176,6 +180,7 @@ class PointwiseBlock:
         """y [B, HW, C] of x [B, HW, C]; ``step`` chooses the dropout masks."""
         B = x.shape[0]
         self._maps("x", x, B)
+        self._not_own(x)
         M = B * self.HW
         d1, d2 = (self._drop(0, step), self._drop(1, step)) if train else (None, None)
         self._normalise(x, M, self.h, True)
@@ -213,8 +218,7 @@ class PointwiseBlock:
         if not 1 <= rows <= self.B * self.HW:
             raise ValueError(f"x: {rows} rows; this block's buffers hold 1 to {self.B * self.HW}")
         _check("x", x, TYPES[self.dtype], self.ws.device, rows, self.C)
-        if x.untyped_storage().data_ptr() == self.y.untyped_storage().data_ptr():
-            raise ValueError("x: this block's own results, whose place the new ones take; clone them")
+        self._not_own(x)
         self.kept = False
         self._normalise(x, rows, self.h, False)
         self._linear(self.up, rows, self.h, "W1", None, None, self.a, None)

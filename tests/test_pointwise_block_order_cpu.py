@@ -32,3 +32,15 @@ def test_one_backward_pass_for_a_forward_pass(idle, more):
         block.backward(maps(), maps())
         with pytest.raises(RuntimeError):   # the second layer's input is gone: dW2 would be wrong
             block.backward(maps(), maps())
+
+
+@pytest.mark.parametrize("more", FORMS)
+def test_forward_refuses_its_own_results(idle, more):
+    """They would be written over while the residual is read, and backward() would normalise the new ones."""
+    block = idle(**more)
+    y = block.forward(maps())
+    for train in (True, False):
+        for own in (y, y[1:], block.y.view(B, HW, C)[:2]):
+            with pytest.raises(ValueError):
+                block.forward(own, train=train)
+    block.forward(y.clone())
