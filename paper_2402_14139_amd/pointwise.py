@@ -177,7 +177,7 @@ class PointwiseBlock:
         nf.nf_mx_product(for_dW, d.N, *self.dz_cols.pair, *self.in_cols.pair, None, None, dW, self.ws)
 
     def forward(self, x, step: int = 0, train: bool = True):
-        """y [B, HW, C] of x [B, HW, C]; ``step`` chooses the dropout masks."""
+        """y [B, HW, C] of x [B, HW, C]; ``step`` chooses the dropout masks, which ``train=False`` leaves out."""
         B = x.shape[0]
         self._maps("x", x, B)
         self._not_own(x)
@@ -186,7 +186,7 @@ class PointwiseBlock:
         self._normalise(x, M, self.h, True)
         self._linear(self.up, M, self.h, "W1", None, d1, self.a, self.z1)
         self._linear(self.down, M, self.a, "W2", x, d2, self.y, None)
-        self.kept = True
+        self.kept = train or not self.p   # backward() applies the masks
         return self.y[:M].view(B, self.HW, self.C)
 
     def backward(self, x, dy, step: int = 0):
@@ -195,7 +195,7 @@ class PointwiseBlock:
         self._maps("x", x, B)
         self._maps("dy", dy, B)
         if not self.kept:
-            raise RuntimeError("backward: no forward() before it, or its buffers taken since by predict() or another backward()")
+            raise RuntimeError("backward: no forward() before it, one without its dropout, or its buffers taken since by predict() or another backward()")
         M, P, g = B * self.HW, self.p32, self.grad
         nf.nf_linear_bwd_epilogue(self.down, M, dy, None, self._drop(1, step), self.dz2, g["b2"], self.ws)
         self._linear_back(self.down, M, self.dz2, self.a, "W2", self.da)

@@ -44,3 +44,17 @@ def test_forward_refuses_its_own_results(idle, more):
             with pytest.raises(ValueError):
                 block.forward(own, train=train)
     block.forward(y.clone())
+
+
+@pytest.mark.parametrize("more", FORMS)
+def test_no_backward_pass_behind_a_forward_pass_without_its_dropout(idle, more):
+    """Masks would be applied to the gradients that no result had."""
+    block = idle(p=0.2, **more)
+    block.forward(maps(), train=False)
+    with pytest.raises(RuntimeError):
+        block.backward(maps(), maps())
+    block.forward(maps())
+    block.backward(maps(), maps())
+    block = idle(**more)   # no dropout: the same function either way
+    block.forward(maps(), train=False)
+    block.backward(maps(), maps())
