@@ -570,10 +570,13 @@ hipError_t product_as(const MxCall &c, const void *raw, const MxRows &a, const M
     const dim3 grid((unsigned)(g.tiles * g.splits));
     auto go = [&](auto tile, auto across, auto step) {
       constexpr int B = decltype(tile)::value, A = decltype(across)::value, G = decltype(step)::value;
-      if (G == 8 && g.part)  // sums of at most 16 groups have no parts
-        hipLaunchKernelGGL((mx_gemm_kernel<T, B, A, 8, true>), grid, dim3((MxTile<B, A, 8>::THREADS)), 0, st, m);
-      else
-        hipLaunchKernelGGL((mx_gemm_kernel<T, B, A, G, false>), grid, dim3((MxTile<B, A, G>::THREADS)), 0, st, m);
+      if constexpr (G == 8 && B != 256) {  // tiles of 256 and sums of at most 16 groups have no parts
+        if (g.part) {
+          hipLaunchKernelGGL((mx_gemm_kernel<T, B, A, 8, true>), grid, dim3((MxTile<B, A, 8>::THREADS)), 0, st, m);
+          return;
+        }
+      }
+      hipLaunchKernelGGL((mx_gemm_kernel<T, B, A, G, false>), grid, dim3((MxTile<B, A, G>::THREADS)), 0, st, m);
     };
     using std::integral_constant;
     using I2 = integral_constant<int, 2>;
