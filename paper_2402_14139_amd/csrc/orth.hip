@@ -570,7 +570,7 @@ __global__ __launch_bounds__(64 * WAVES) void orth_small_kernel(float eps, Table
         acc = four(rows16(A, lda, rb, kk, 0), rows16(A, lda, rb, kk, 1), rows16(A, lda, cb, kk, 0), rows16(A, lda, cb, kk, 1), acc);
       float w[4];
       get4(piece(A, lda, rb + i16, cb + 4 * q), w);
-      const float sa = m.b[step] * (up_p / up_a), ss = m.c[step] * (up_p / up_a / up_a);
+      const float sa = m.b[step] / up_a * up_p, ss = m.c[step] / up_a / up_a * up_p;  // b and c first: up_p / up_a^2 may leave fp32's range
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] = fmaf(w[e], sa, acc[e] * ss);
       put4(piece(P, lda, rb + i16, cb + 4 * q), w);
