@@ -186,8 +186,8 @@ int32_t nf_sgd_update(const nf_sgd_desc *s, int32_t n_tensors, float *const *w, 
 /* Updates made orthogonal.  A matrix G [rows][cols], dense, goes through `steps` Newton-Schulz steps,
  *   X = G / (|G| + eps), |G| the root of the sum of squares;  X <- a X + (b A + c A^2) X with A = X X^T (rows <= cols; else X^T X),
  * step k with a[k], b[k], c[k].  They drive the singular values towards those that the polynomial x (a + b x^2 + c x^4) repeats.  Products keep 22 bits of their
- * operands and sums are fp32, as errors of small singular values grow by the a's product.  Every step's results have to stay bounded (by 1e9) where the
- * singular values begin at most at 1: else NF_ERR_UNSUPPORTED.  1 <= steps <= NF_ORTH_STEPS, eps >= 0.
+ * operands and sums are fp32, as errors of small singular values grow by the a's product.  The bound of every step's results, where the singular values
+ * begin at most at 1, has to lie between 1e-6 and 1e9 (or to be 0: a = b = c = 0): else NF_ERR_UNSUPPORTED.  1 <= steps <= NF_ORTH_STEPS, eps >= 0.
  * n_matrices (<= NF_ORTH_MATRICES) share the launches; rows, cols, and the arrays of device pointers are HOST arrays.  rows, cols <= 2^20, the lesser of them
  * <= 2^14.  A matrix with an infinity or a NaN gives NaN throughout, and so does one of zeros where eps is 0. */
 #define NF_ORTH_STEPS 12

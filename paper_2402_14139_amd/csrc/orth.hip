@@ -739,12 +739,13 @@ hipError_t product(const Plan &p, const char *const (&names)[3], hipStream_t st)
 
 // The exponents s of X, A, P and X' at every step, from a bound u of the singular values: |x| <= u, elements of A are at most u^2, of P = b A + c A^2
 // the largest |b y + c y^2| over y <= u^2, and the next u is the largest |f(x)| over x <= u.  Extremes lie at the ends or where the slope is 0.
+// Bounds from 1e-6 to 1e9 (or 0) keep all scales, and what the kernels form of them, in fp32's range.
 struct Scales {
   int x, a, p;
 };
 bool orth_scales(const nf_orth_desc &d, Scales *s, int *last) {
   double u = 1;
-  auto exponent = [](double bound) { return 15 - (int)std::ceil(std::log2(std::max(bound * 1.01, 1e-12))); };
+  auto exponent = [](double bound) { return 15 - (int)std::ceil(std::log2(bound * 1.01)); };
   for (int k = 0; k <= d.steps; ++k) {
     if (!(u < 1e9)) return false;
     if (k == d.steps) {
@@ -767,9 +768,10 @@ bool orth_scales(const nf_orth_desc &d, Scales *s, int *last) {
     } else if (b != 0) {
       see(-a / (3 * b));
     }
-    if (!(p < 1e9) || !(f < 1e9)) return false;
-    s[k] = Scales{exponent(u), exponent(u * u), exponent(p)};
-    u = std::max(f, 1e-9);
+    if (!(p < 1e9) || !(f < 1e9) || (f > 0 && f < 1e-6)) return false;
+    // beside a X, P's digits count from 2^-10 of f / u on; where f is 0, all results are
+    s[k] = Scales{exponent(u), exponent(u * u), exponent(f > 0 ? std::max(p, f / u / 1024) : 1.0)};
+    u = f > 0 ? f : 1.0;
   }
   return true;
 }
