@@ -645,8 +645,9 @@ def orth_desc(steps, eps: float = 1e-7) -> OrthDesc:
 
 
 def _dims(shapes):
-    n = len(shapes)
-    return (C.c_int32 * n)(*[int(s[0]) for s in shapes]), (C.c_int32 * n)(*[int(s[1]) for s in shapes])
+    """Sizes beyond 32 bits become the largest (or least) there is, which the library refuses; ctypes would cut them off."""
+    n, fit = len(shapes), lambda v: min(max(int(v), -2 ** 31), 2 ** 31 - 1)
+    return (C.c_int32 * n)(*[fit(s[0]) for s in shapes]), (C.c_int32 * n)(*[fit(s[1]) for s in shapes])
 
 
 def _as_matrices(ts):

@@ -1,5 +1,7 @@
-"""Steps of orthogonal updates whose results leave the range that products of fp16 pieces keep their digits in are refused."""
+"""Steps of orthogonal updates whose results leave the range that products of fp16 pieces keep their digits in are refused, and so are sizes
+beyond 32 bits."""
 import pytest
+import torch
 
 from paper_2402_14139_amd import binding as nf
 
@@ -22,3 +24,17 @@ def test_refused(which):
     with pytest.raises(nf.NfError) as e:
         nf.nf_orthogonalise_workspace_bytes(nf.orth_desc(BAD[which]), [(8, 8)])
     assert e.value.status == nf.NF_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 2 ** 32 + 64), (2 ** 32 + 64, 1), (2 ** 33 + 8, 2 ** 33 + 8), (8, 2 ** 31)])
+def test_sizes_beyond_32_bits(rows, cols):
+    with pytest.raises(nf.NfError) as e:
+        nf.nf_orthogonalise_workspace_bytes(nf.orth_desc([ONE]), [(rows, cols)])
+    assert e.value.status == nf.NF_ERR_UNSUPPORTED
+
+
+def test_a_tensor_beyond_32_bits():
+    """The sizes that the calls take from their tensors."""
+    t = torch.empty(1, 2 ** 32 + 64, dtype=torch.bfloat16, device="meta")
+    rows, cols = nf._as_matrices([t, torch.empty(64, 3, 3, 3, device="meta")])
+    assert list(rows) == [1, 64] and list(cols) == [2 ** 31 - 1, 27]
