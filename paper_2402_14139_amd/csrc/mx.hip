@@ -280,8 +280,8 @@ struct WideSteps {
 // it is carried out.  A row's chunks of 16 bytes (groups) are exchanged in LDS so that the 16 rows of a fragment's read lie in different banks.
 // Sums of at most 16 groups take steps of 4 in three stages of 17 KB: three workgroups to a CU, which hide each other's first copies and epilogues.
 // 8192x8192x8192 bf16 276 us, 4 PFLOP/s: copies from L2, reads of LDS and matrix instructions take 1.0, 0.8 and 0.9 us of a step's 2.3 in a tile of 256 and
-// overlap in part.  65536x512x2048 105 us, with GELU 120: 3.3 us a tile of 128, of which the results' 32 KB need 1.2 at a fill's 6.9 TB/s;
-// its vector instructions, 23 an element with GELU, 2.7.
+// overlap in part.  65536x512x2048 106 us, with GELU 125: 3.9 us a tile of 128, of which the results' 32 KB need 1.2 at a fill's 6.9 TB/s;
+// its vector instructions, 25 an element with GELU, two of them an exponential and a reciprocal, 3.4.
 template <int BLOCK, int ACROSS, int STEP>
 struct MxTile {
   static constexpr int WAVES = 2 * ACROSS, THREADS = 64 * WAVES, MT = BLOCK / 32, NT = BLOCK / 16 / ACROSS;
@@ -522,7 +522,7 @@ struct MxPlan {
 };
 // Tiles of 256 or 128 by rounds over the workgroups that run together (one to a CU and two, three where sums are short) and a round's time: steps, then
 // what ends a tile, with no other workgroup's steps beside it in a CU that holds one (us, in tiles of 256 and of 128: 8192x8192x8192 bf16 276 and 389,
-// 16384x2048x2048 48 and 57, 16384x1500x2048 with GELU 60 and 55, 65536x512x2048 131 and 105, with GELU 167 and 120, fp32 results
+// 16384x2048x2048 48 and 57, 16384x1500x2048 with GELU 60 and 55, 65536x512x2048 131 and 106, with GELU 167 and 125, fp32 results
 // 147 and 215).  Few tiles of 128 become tiles of 64 or parts of sums: towards 512 workgroups, four steps each at least.
 MxPlan mx_plan(int dtype, int act, long long M, int N, long long K) {
   MxPlan p = {0, 1, 0, 0};
