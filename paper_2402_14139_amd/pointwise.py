@@ -89,6 +89,7 @@ class PointwiseBlock:
     behind it) or "layer"; ``mx``: products on 4-bit operands."""
 
     kept = False   # the buffers hold what backward() reads: from forward() to the next predict() or backward()
+    of = None   # its batch, and its step where that chooses masks
     v = muon_ws = None   # muon()'s momentum and workspace, from its first call on
     captured = False   # that call was recorded into a graph
 
@@ -187,6 +188,7 @@ class PointwiseBlock:
         self._linear(self.up, M, self.h, "W1", None, d1, self.a, self.z1)
         self._linear(self.down, M, self.a, "W2", x, d2, self.y, None)
         self.kept = train or not self.p   # backward() applies the masks
+        self.of = (B, step if self.p else None)
         return self.y[:M].view(B, self.HW, self.C)
 
     def backward(self, x, dy, step: int = 0):
@@ -196,6 +198,8 @@ class PointwiseBlock:
         self._maps("dy", dy, B)
         if not self.kept:
             raise RuntimeError("backward: no forward() before it, one without its dropout, or its buffers taken since by predict() or another backward()")
+        if self.of not in (None, (B, step if self.p else None)):
+            raise RuntimeError(f"backward: a batch of {B} in step {step}; forward() before it had (batch, step) {self.of}")
         M, P, g = B * self.HW, self.p32, self.grad
         nf.nf_linear_bwd_epilogue(self.down, M, dy, None, self._drop(1, step), self.dz2, g["b2"], self.ws)
         self._linear_back(self.down, M, self.dz2, self.a, "W2", self.da)

@@ -58,3 +58,18 @@ def test_no_backward_pass_behind_a_forward_pass_without_its_dropout(idle, more):
     block = idle(**more)   # no dropout: the same function either way
     block.forward(maps(), train=False)
     block.backward(maps(), maps())
+
+
+@pytest.mark.parametrize("more", FORMS)
+def test_backward_is_of_the_same_batch_and_masks(idle, more):
+    block = idle(p=0.2, **more)
+    block.forward(maps(), 5)
+    for x, step in ((maps()[:2], 5), (maps(), 4)):
+        with pytest.raises(RuntimeError):
+            block.backward(x, x, step)
+    block.backward(maps(), maps(), 5)
+    block = idle(**more)
+    block.forward(maps()[:2], 5)
+    with pytest.raises(RuntimeError):
+        block.backward(maps(), maps(), 5)
+    block.backward(maps()[:2], maps()[:2], 4)   # no masks to choose
